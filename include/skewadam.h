@@ -372,6 +372,68 @@ int32_t skew_num_tensors(const skew_handle_t *h);
 /* One-line reason for the last failure on `h` (or of skew_create when h is NULL). */
 const char *skew_last_error(const skew_handle_t *h);
 
+/* ==========================================================================
+ * Around the step: what a trainer computes with the tiers' tensors before it.
+ *
+ * Conventions as above. The entry points below report the reason of a failed
+ * call through skew_ops_last_error (per host thread). They neither synchronise
+ * nor allocate device memory (skew_clip_bind alone synchronises), and can be
+ * captured into a CUDA graph after one call outside of it.
+ * ======================================================================== */
+
+/* One-line reason for the last failure of a skew_clip_*, skew_embed_* or skew_gate_* call on this host thread. */
+const char *skew_ops_last_error(void);
+
+/* ---- global gradient norm and clipping -------------------------------------
+ *   norm  = sqrt(sum over all tensors and elements of g^2)
+ *   gamma = min(1, max_norm / (norm + 1e-6))
+ *   out   = gamma * g
+ * gamma is what skew_step_scaled takes as grad_scale, so that a trainer whose
+ * gradients go to the step only needs skew_clip_norm (one read of them). Squares
+ * are summed in fp32 (two-term sums) and joined in fp64, in an order that depends on the
+ * tensors' sizes alone; elements whose squares leave fp32's range are summed scaled,
+ * so the norm is right for any finite gradient (and Inf only where it exceeds fp32
+ * itself). A NaN in a gradient makes norm and gamma NaN; an Inf makes norm Inf and
+ * gamma 0 (0 * Inf is then NaN in the clipped tensor).
+ */
+#define SKEW_CLIP_GRAD_FP32 1u /* g is fp32 (else bf16)                          */
+#define SKEW_CLIP_OUT_FP32 2u  /* out is fp32 (else bf16); needs an fp32 g       */
+
+typedef struct skew_clip skew_clip_t; /* opaque */
+
+/*
+ * One gradient tensor.
+ *   grad  : device pointer to `numel` contiguous elements, aligned to their type
+ *           (16-byte alignment enables vector accesses). Borrowed while bound.
+ *   out   : where skew_clip_apply writes; `grad` itself to clip in place (same
+ *           type), else memory that overlaps no gradient and no other `out`. NULL
+ *           in every descriptor of a handle that only computes norms.
+ *   numel : 0 to 2^40.
+ */
+typedef struct {
+    const void *grad;
+    void *out;
+    int64_t numel;
+    uint32_t flags; /* SKEW_CLIP_* */
+    uint32_t zero;  /* 0 */
+} skew_clip_desc_t;
+
+/* Plans for `n` tensors (0 allowed: the norm is then 0). Host only. Errors: SKEW_EINVAL, SKEW_ENOMEM. */
+int skew_clip_create(const skew_clip_desc_t *tensors, int32_t n, skew_clip_t **out);
+int skew_clip_destroy(skew_clip_t *h); /* NULL is a no-op */
+/* Bytes of device workspace (tile table and partial sums); 0 for NULL. */
+size_t skew_clip_workspace_bytes(const skew_clip_t *h);
+/* Binds a 256-byte aligned workspace and uploads the table on `stream` (synchronises it). */
+int skew_clip_bind(skew_clip_t *h, void *workspace, size_t workspace_bytes, void *stream);
+/*
+ * result[0] = norm, result[1] = gamma (device, fp32, 4-byte aligned). max_norm: finite, >= 0.
+ * Calls on one handle must not overlap on the GPU. Errors: SKEW_ESTATE, SKEW_EINVAL, SKEW_ECUDA.
+ */
+int skew_clip_norm(skew_clip_t *h, float max_norm, float *result, void *stream);
+/* skew_clip_norm, then out = gamma * g for every tensor (nothing is read or written for one that is clipped in
+ * place by gamma = 1). Errors: also SKEW_ESTATE for a handle planned without `out`. */
+int skew_clip_apply(skew_clip_t *h, float max_norm, float *result, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,332 @@
+// Global gradient norm and clipping over many tensors (skew_clip_* in include/skewadam.h).
+//
+//   norm = sqrt(sum g^2), gamma = min(1, max_norm / (norm + 1e-6)), out = gamma g.
+//
+// The tensors are cut into tiles at create time, one table entry each that holds all a CTA needs to know
+// (one trip to L2 ahead of the data). Both kernels are bound by memory: the sum of squares reads every
+// gradient once, 2 flops an element; the factor depends on all of them, so clipping reads them again,
+// the last tiles first, which are the ones that L2 still holds.
+#include "skew_ops.h"
+
+#include <cmath>
+#include <cstring>
+#include <new>
+#include <vector>
+
+namespace skew {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr uint32_t kMaxCtas = 8192;   // partial sums that the workspace has room for
+constexpr int kBatch = 4;             // 8-element units a thread loads before it uses them
+// Bytes of gradient in a tile. Small ones spread a small set over the SMs.
+constexpr int64_t kTileBytes = 65536, kSmallTileBytes = 16384;
+constexpr int64_t kSmallSet = int64_t(152) * 4 * kTileBytes;
+
+enum : uint32_t { kGradF32 = SKEW_CLIP_GRAD_FP32, kOutF32 = SKEW_CLIP_OUT_FP32, kVectors = 4u, kNoVectors = 8u };
+
+// A run of elements of one tensor. kVectors: g and out start on 16-byte boundaries; kNoVectors: g does not.
+struct alignas(16) ClipTile {
+    const void *g;
+    void *out;
+    uint32_t n, flags, zero[2];
+};
+
+struct ClipArgs {
+    const ClipTile *tiles;
+    double *part;
+    uint32_t *ticket;
+    float *result;
+    uint32_t n_tiles;
+    float max_norm;
+};
+
+// Sums of squares outside [2^-100, 2^100] may have lost elements to overflow or underflow: with at most
+// 2^17 elements and inside that range, no square has overflowed, and what squares below 2^-126 lose (2^-150
+// each) is below 2^-32 of the sum. Outside, the elements are summed again, scaled into the range.
+constexpr float kSumLow = 0x1p-100f, kSumHigh = 0x1p100f;
+constexpr float kScaleUp = 0x1p100f, kScaleDown = 0x1p-80f;
+
+template <bool F32, class F>
+__device__ __forceinline__ void each_unit(const ClipTile &t, F &&f) {  // f(8 elements) for the thread's units
+    const uint32_t units = t.n >> 3;
+    uint32_t u = threadIdx.x;
+    for (; u + (kBatch - 1) * kThreads < units; u += kBatch * kThreads) {
+        Vec8<F32> v[kBatch];
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) v[b] = load8<F32>(t.g, int64_t(u + b * kThreads) * 8);
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) f(v[b]);
+    }
+    for (; u < units; u += kThreads) f(load8<F32>(t.g, int64_t(u) * 8));
+}
+
+// Sum of (scale x)^2 over the thread's elements of a tile; `any`: the OR of their magnitudes' bits.
+template <bool F32, bool SCALED>
+__device__ __forceinline__ float tile_squares(const ClipTile &t, float scale, uint32_t &any) {
+    float s0 = 0.f, s1 = 0.f;
+    any = 0;
+    uint32_t left = threadIdx.x;  // elements one at a time: what 8 does not divide, or all
+    if (!(t.flags & kNoVectors)) {
+        each_unit<F32>(t, [&](const Vec8<F32> &v) {
+#pragma unroll
+            for (int q = 0; q < (F32 ? 2 : 1); ++q) any |= v.u[q].x | v.u[q].y | v.u[q].z | v.u[q].w;
+#pragma unroll
+            for (int k = 0; k < 8; k += 2) {
+                const float a = SCALED ? v.at(k) * scale : v.at(k), b = SCALED ? v.at(k + 1) * scale : v.at(k + 1);
+                s0 = fmaf(a, a, s0);
+                s1 = fmaf(b, b, s1);
+            }
+        });
+        any &= F32 ? 0x7FFFFFFFu : 0x7FFF7FFFu;
+        left += t.n & ~7u;
+    }
+    for (uint32_t i = left; i < t.n; i += kThreads) {
+        const float a = load1<F32>(t.g, i);
+        any |= __float_as_uint(a) & 0x7FFFFFFFu;
+        s0 = fmaf(SCALED ? a * scale : a, SCALED ? a * scale : a, s0);
+    }
+    return s0 + s1;
+}
+
+// The thread's sum of squares: a two-term fp32 sum, and in fp64 what fp32 does not hold.
+struct Squares {
+    float hi = 0.f, lo = 0.f;
+    double rest = 0.0;
+    template <bool F32>
+    __device__ __forceinline__ void add(const ClipTile &t) {
+        uint32_t any, unused;
+        const float s = tile_squares<F32, false>(t, 1.f, any);
+        if (s >= kSumLow && s <= kSumHigh) {
+            const float sum = hi + s, back = sum - hi;
+            lo += (hi - (sum - back)) + (s - back);
+            hi = sum;
+        } else if (any) {
+            const float scale = s < kSumLow ? kScaleUp : kScaleDown;  // a NaN stays one either way
+            const double r = 1.0 / double(scale);
+            rest += double(tile_squares<F32, true>(t, scale, unused)) * r * r;
+        }
+    }
+};
+
+__device__ __forceinline__ double cta_sum(double x) {  // the sum, in thread 0
+    __shared__ double warp[kThreads / 32];
+    for (int d = 16; d; d >>= 1) x += __shfl_down_sync(kFullMask, x, d);
+    if ((threadIdx.x & 31) == 0) warp[threadIdx.x >> 5] = x;
+    __syncthreads();
+    x = 0.0;
+    if (threadIdx.x == 0)
+        for (int w = 0; w < kThreads / 32; ++w) x += warp[w];
+    __syncthreads();
+    return x;
+}
+
+// Norm and factor. The CTAs' sums are joined by whichever ends last, in the order of the CTAs.
+__global__ void __launch_bounds__(kThreads) k_clip_norm(const __grid_constant__ ClipArgs A) {
+    Squares sq;
+    for (uint32_t k = blockIdx.x; k < A.n_tiles; k += gridDim.x) {
+        const ClipTile t = A.tiles[k];
+        if (t.flags & kGradF32)
+            sq.add<true>(t);
+        else
+            sq.add<false>(t);
+    }
+    const double mine = cta_sum(double(sq.hi) + double(sq.lo) + sq.rest);
+    __shared__ bool last;
+    if (threadIdx.x == 0) {
+        A.part[blockIdx.x] = mine;
+        __threadfence();
+        last = atomicInc(A.ticket, gridDim.x - 1) == gridDim.x - 1;  // back at 0 for the next call
+        __threadfence();
+    }
+    __syncthreads();
+    if (!last) return;
+    double x = 0.0;
+    for (uint32_t k = threadIdx.x; k < gridDim.x; k += kThreads) x += __ldcg(A.part + k);
+    x = cta_sum(x);
+    if (threadIdx.x == 0) {
+        const float norm = float(sqrt(x)), gamma = A.max_norm / (norm + 1e-6f);
+        A.result[0] = norm;
+        A.result[1] = gamma > 1.f ? 1.f : gamma;  // a NaN stays one
+    }
+}
+
+template <bool GF32, bool OF32>
+__device__ __forceinline__ void scale_tile(const ClipTile &t, float gamma) {
+    uint32_t left = threadIdx.x;
+    if (t.flags & kVectors) {
+        const uint32_t units = t.n >> 3;
+        for (uint32_t u = threadIdx.x; u < units; u += kBatch * kThreads) {
+            Vec8<GF32> v[kBatch];
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b)
+                if (u + b * kThreads < units) v[b] = load8<GF32>(t.g, int64_t(u + b * kThreads) * 8);
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b)
+                if (u + b * kThreads < units) {
+                    float x[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) x[k] = v[b].at(k) * gamma;
+                    store8<OF32>(t.out, int64_t(u + b * kThreads) * 8, x);
+                }
+        }
+        left += t.n & ~7u;
+    }
+    for (uint32_t i = left; i < t.n; i += kThreads) store1<OF32>(t.out, i, load1<GF32>(t.g, i) * gamma);
+}
+
+__global__ void __launch_bounds__(kThreads, 4) k_clip_apply(const __grid_constant__ ClipArgs A) {
+    wait_launch_before();
+    const float gamma = __ldcg(A.result + 1);
+    for (uint32_t k = blockIdx.x; k < A.n_tiles; k += gridDim.x) {
+        const ClipTile t = A.tiles[A.n_tiles - 1 - k];
+        if (t.g == t.out && gamma == 1.f) continue;
+        if (!(t.flags & kGradF32))
+            scale_tile<false, false>(t, gamma);
+        else if (t.flags & kOutF32)
+            scale_tile<true, true>(t, gamma);
+        else
+            scale_tile<true, false>(t, gamma);
+    }
+}
+
+}  // namespace
+}  // namespace skew
+
+using namespace skew;
+
+struct skew_clip {
+    std::vector<ClipTile> tiles;
+    bool writes = true;  // every tensor has an `out`
+    size_t ws_ticket = 0, ws_tiles = 0, ws_bytes = 0;
+    char *ws = nullptr;
+    bool bound = false;
+    uint32_t norm_ctas = 1, apply_ctas = 1;
+};
+
+extern "C" {
+
+int skew_clip_create(const skew_clip_desc_t *tensors, int32_t n, skew_clip_t **out) {
+    if (!out) return ops_fail(SKEW_EINVAL, "out is NULL");
+    *out = nullptr;
+    if (n < 0 || (n > 0 && !tensors)) return ops_fail(SKEW_EINVAL, "bad tensor list");
+    int64_t total = 0;
+    bool writes = true, reads_only = true;
+    for (int32_t k = 0; k < n; ++k) {
+        const skew_clip_desc_t &d = tensors[k];
+        if (d.flags & ~(SKEW_CLIP_GRAD_FP32 | SKEW_CLIP_OUT_FP32) || d.zero) return ops_fail(SKEW_EINVAL, "tensor %d: unknown flags", k);
+        const int64_t ge = d.flags & SKEW_CLIP_GRAD_FP32 ? 4 : 2, oe = d.flags & SKEW_CLIP_OUT_FP32 ? 4 : 2;
+        if (oe > ge) return ops_fail(SKEW_EINVAL, "tensor %d: a bf16 gradient is clipped to bf16", k);
+        if (d.numel < 0 || d.numel > (int64_t(1) << 40)) return ops_fail(SKEW_EINVAL, "tensor %d: numel must be in [0, 2^40]", k);
+        if (d.numel && !d.grad) return ops_fail(SKEW_EINVAL, "tensor %d: null grad", k);
+        if ((uintptr_t)d.grad & (ge - 1) || (uintptr_t)d.out & (oe - 1)) return ops_fail(SKEW_EINVAL, "tensor %d: pointers must be aligned to their type", k);
+        if (d.out == d.grad && d.grad && oe != ge) return ops_fail(SKEW_EINVAL, "tensor %d: in place needs one type", k);
+        if (d.numel) (d.out ? reads_only : writes) = false;
+        total += d.numel * ge;
+    }
+    if (!writes && !reads_only) return ops_fail(SKEW_EINVAL, "`out` is given for some tensors and not for others");
+    if (total > int64_t(1) << 46) return ops_fail(SKEW_EINVAL, "too many elements");
+    skew_clip *h = new (std::nothrow) skew_clip();
+    if (!h) return ops_fail(SKEW_ENOMEM, "out of host memory");
+    h->writes = writes;
+    const int64_t tile_bytes = total < kSmallSet ? kSmallTileBytes : kTileBytes;
+    try {
+        for (int32_t k = 0; k < n; ++k) {
+            const skew_clip_desc_t &d = tensors[k];
+            const int64_t ge = d.flags & SKEW_CLIP_GRAD_FP32 ? 4 : 2, oe = d.flags & SKEW_CLIP_OUT_FP32 ? 4 : 2;
+            // The first elements, up to where vectors may start: of both if there is such a place, else of g.
+            const char *g = (const char *)d.grad;
+            char *o = (char *)d.out;
+            int64_t head = -1, head_g = 0;
+            for (int64_t e = 7; e >= 0; --e) {
+                const bool ga = ((uintptr_t)(g + e * ge) & 15) == 0, oa = ((uintptr_t)(o + e * oe) & 15) == 0;
+                if (ga) head_g = e;
+                if (ga && oa) head = e;
+            }
+            const bool both = head >= 0;
+            if (!both) head = head_g;
+            if (head > d.numel) head = d.numel;
+            auto cut = [&](int64_t at, int64_t count, uint32_t flags) {
+                h->tiles.push_back(ClipTile{g + at * ge, o ? o + at * oe : nullptr, (uint32_t)count, d.flags | flags, {0, 0}});
+            };
+            if (head) cut(0, head, kNoVectors);
+            const int64_t step = tile_bytes / ge;
+            for (int64_t at = head; at < d.numel; at += step) cut(at, d.numel - at < step ? d.numel - at : step, both ? kVectors : 0u);
+        }
+    } catch (...) {
+        delete h;
+        return ops_fail(SKEW_ENOMEM, "out of host memory");
+    }
+    h->ws_ticket = kMaxCtas * sizeof(double);
+    h->ws_tiles = h->ws_ticket + 256;
+    h->ws_bytes = (h->ws_tiles + h->tiles.size() * sizeof(ClipTile) + 255) / 256 * 256;
+    *out = h;
+    return SKEW_OK;
+}
+
+int skew_clip_destroy(skew_clip_t *h) {
+    delete h;
+    return SKEW_OK;
+}
+
+size_t skew_clip_workspace_bytes(const skew_clip_t *h) { return h ? h->ws_bytes : 0; }
+
+int skew_clip_bind(skew_clip_t *h, void *workspace, size_t workspace_bytes, void *stream) {
+    if (!h) return ops_fail(SKEW_EINVAL, "handle is NULL");
+    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes != h->ws_bytes)
+        return ops_fail(SKEW_EINVAL, "workspace must be 256-byte aligned and exactly %zu bytes", h->ws_bytes);
+    cudaStream_t s = (cudaStream_t)stream;
+    const int sms = ops_sm_count();
+    int norm_occ = 0, apply_occ = 0, rc;
+    if ((rc = ops_cuda(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&norm_occ, k_clip_norm, kThreads, 0), "occupancy")) ||
+        (rc = ops_cuda(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&apply_occ, k_clip_apply, kThreads, 0), "occupancy")))
+        return rc;
+    h->bound = false;
+    char *ws = (char *)workspace;
+    if ((rc = ops_cuda(cudaMemsetAsync(ws, 0, h->ws_tiles, s), "zero-fill of the workspace"))) return rc;
+    if (!h->tiles.empty() &&
+        (rc = ops_cuda(cudaMemcpyAsync(ws + h->ws_tiles, h->tiles.data(), h->tiles.size() * sizeof(ClipTile), cudaMemcpyHostToDevice, s), "upload of the tile table")))
+        return rc;
+    if ((rc = ops_cuda(cudaStreamSynchronize(s), "bind"))) return rc;
+    auto ctas = [&](int occ) {
+        const uint64_t most = uint64_t(sms > 0 ? sms : 1) * (occ > 0 ? occ : 1), n = h->tiles.size();
+        const uint64_t c = n < most ? n : most;
+        return (uint32_t)(c < 1 ? 1 : c < kMaxCtas ? c : kMaxCtas);
+    };
+    h->norm_ctas = ctas(norm_occ);
+    h->apply_ctas = ctas(apply_occ);
+    h->ws = ws;
+    h->bound = true;
+    return SKEW_OK;
+}
+
+static int clip_args(skew_clip_t *h, float max_norm, float *result, ClipArgs &A) {
+    if (!h) return ops_fail(SKEW_EINVAL, "handle is NULL");
+    if (!h->bound) return ops_fail(SKEW_ESTATE, "call before skew_clip_bind");
+    if (!std::isfinite(max_norm) || max_norm < 0.f) return ops_fail(SKEW_EINVAL, "max_norm must be finite and >= 0");
+    if (!result || ((uintptr_t)result & 3)) return ops_fail(SKEW_EINVAL, "result must be a 4-byte aligned device pointer");
+    A.tiles = reinterpret_cast<const ClipTile *>(h->ws + h->ws_tiles);
+    A.part = reinterpret_cast<double *>(h->ws);
+    A.ticket = reinterpret_cast<uint32_t *>(h->ws + h->ws_ticket);
+    A.result = result;
+    A.n_tiles = (uint32_t)h->tiles.size();
+    A.max_norm = max_norm;
+    return SKEW_OK;
+}
+
+int skew_clip_norm(skew_clip_t *h, float max_norm, float *result, void *stream) {
+    ClipArgs A{};
+    if (const int rc = clip_args(h, max_norm, result, A)) return rc;
+    return ops_cuda(ops_launch(false, k_clip_norm, h->norm_ctas, kThreads, 0, (cudaStream_t)stream, A), "k_clip_norm");
+}
+
+int skew_clip_apply(skew_clip_t *h, float max_norm, float *result, void *stream) {
+    ClipArgs A{};
+    if (const int rc = clip_args(h, max_norm, result, A)) return rc;
+    if (!h->writes) return ops_fail(SKEW_ESTATE, "the handle was planned without `out`");
+    int rc = ops_cuda(ops_launch(false, k_clip_norm, h->norm_ctas, kThreads, 0, (cudaStream_t)stream, A), "k_clip_norm");
+    if (rc || !A.n_tiles) return rc;
+    return ops_cuda(ops_launch(true, k_clip_apply, h->apply_ctas, kThreads, 0, (cudaStream_t)stream, A), "k_clip_apply");
+}
+
+}  // extern "C"

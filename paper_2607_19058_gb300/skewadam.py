@@ -26,12 +26,15 @@ F_NO_DECAY = 1
 F_FP32 = 2
 KIND_FULL, KIND_FACTORED = 0, 1
 ROUTE_OWN, ROUTE_RIDING, ROUTE_ROWS, ROUTE_SMALL = 0, 1, 2, 3
+CLIP_GRAD_FP32, CLIP_OUT_FP32 = 1, 2
 
 EXPORTS = ["skew_create", "skew_destroy", "skew_state_bytes", "skew_workspace_bytes", "skew_bind", "skew_step",
            "skew_sync_status", "skew_tensor_scalars", "skew_matrix_scalars", "skew_tensor_info", "skew_num_tensors", "skew_last_error",
            "skew_profile_begin", "skew_profile_end", "skew_kernel_name", "skew_step_tensor_noalloc",
            "skew_launches_per_step", "skew_selftest_wait_timeout", "skew_noalloc_sync_status", "skew_step_scaled",
-           "skew_noalloc_selftest_wait_timeout", "skew_tensor_route"]
+           "skew_noalloc_selftest_wait_timeout", "skew_tensor_route", "skew_ops_last_error",
+           "skew_clip_create", "skew_clip_destroy", "skew_clip_workspace_bytes", "skew_clip_bind", "skew_clip_norm",
+           "skew_clip_apply"]
 
 
 class SkewError(RuntimeError):
@@ -55,6 +58,11 @@ class TensorInfo(C.Structure):
                 ("rows", C.c_int64), ("cols", C.c_int64), ("numel", C.c_int64), ("m_offset", C.c_int64),
                 ("v_offset", C.c_int64), ("r_offset", C.c_int64), ("c_offset", C.c_int64), ("rowpath", C.c_int32),
                 ("stack", C.c_int32)]
+
+
+class ClipDesc(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("numel", C.c_int64), ("flags", C.c_uint32),
+                ("zero", C.c_uint32)]
 
 
 _lock = threading.Lock()
@@ -118,6 +126,19 @@ def load(path: Optional[str] = None) -> C.CDLL:
         L.skew_noalloc_sync_status.restype = C.c_int
         L.skew_noalloc_selftest_wait_timeout.argtypes = [vp]
         L.skew_noalloc_selftest_wait_timeout.restype = C.c_int
+        L.skew_ops_last_error.argtypes = []
+        L.skew_ops_last_error.restype = C.c_char_p
+        L.skew_clip_create.argtypes = [C.POINTER(ClipDesc), i32, C.POINTER(vp)]
+        L.skew_clip_create.restype = C.c_int
+        L.skew_clip_destroy.argtypes = [vp]
+        L.skew_clip_destroy.restype = C.c_int
+        L.skew_clip_workspace_bytes.argtypes = [vp]
+        L.skew_clip_workspace_bytes.restype = sz
+        L.skew_clip_bind.argtypes = [vp, vp, sz, vp]
+        L.skew_clip_bind.restype = C.c_int
+        for f in (L.skew_clip_norm, L.skew_clip_apply):
+            f.argtypes = [vp, C.c_float, vp, vp]
+            f.restype = C.c_int
         if path is None:
             _lib = L
         return L
@@ -127,6 +148,11 @@ def _check(rc: int, h=None):
     if rc != SKEW_OK:
         msg = load().skew_last_error(h)
         raise SkewError(rc, msg.decode() if msg else "")
+
+
+def _check_op(rc: int):
+    if rc != SKEW_OK:
+        raise SkewError(rc, skew_ops_last_error())
 
 
 # --------------------------------------------------------------------------
@@ -258,13 +284,115 @@ def skew_noalloc_selftest_wait_timeout(stream: int) -> None:
         raise SkewError(rc, "CUDA error")
 
 
+def skew_ops_last_error() -> str:
+    m = load().skew_ops_last_error()
+    return m.decode() if m else ""
+
+
+def skew_clip_create(tensors: Sequence[ClipDesc]) -> C.c_void_p:
+    arr = (ClipDesc * max(1, len(tensors)))(*tensors)
+    h = C.c_void_p()
+    _check_op(load().skew_clip_create(arr, len(tensors), C.byref(h)))
+    return h
+
+
+def skew_clip_destroy(h) -> None:
+    load().skew_clip_destroy(h)
+
+
+def skew_clip_workspace_bytes(h) -> int:
+    return int(load().skew_clip_workspace_bytes(h))
+
+
+def skew_clip_bind(h, ws_ptr: int, ws_bytes: int, stream: int) -> None:
+    _check_op(load().skew_clip_bind(h, ws_ptr, ws_bytes, stream))
+
+
+def skew_clip_norm(h, max_norm: float, result_ptr: int, stream: int) -> None:
+    _check_op(load().skew_clip_norm(h, max_norm, result_ptr, stream))
+
+
+def skew_clip_apply(h, max_norm: float, result_ptr: int, stream: int) -> None:
+    _check_op(load().skew_clip_apply(h, max_norm, result_ptr, stream))
+
+
 def hparams(beta1=0.9, beta2=0.999, eps=1e-8, clip_d=1.0, weight_decay=0.05, policy=POLICY_TIERED) -> HParams:
     return HParams(beta1, beta2, eps, clip_d, weight_decay, policy)
 
 
 # --------------------------------------------------------------------------
-# torch convenience wrapper
+# torch convenience wrappers
 # --------------------------------------------------------------------------
+def _stream_of(stream) -> int:
+    if stream is None:
+        import torch
+        return torch.cuda.current_stream().cuda_stream
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+class GradClip:
+    """The global norm of many gradients, its clip factor, and clipping.
+
+    ``grads``: contiguous bf16 or fp32 CUDA tensors of any shapes. ``out``: where ``clip`` writes
+    the clipped gradients, one tensor for each: of the gradient's type, or bf16 for an fp32 one
+    (microbatches accumulated in fp32, handed to the step in bf16). ``None``: in place.
+
+    ``norm`` and ``clip`` return ``result``, a device tensor [norm, gamma] that the next call
+    overwrites; ``gamma`` is the view of its second element that ``SkewAdam.step`` takes as
+    ``grad_scale``. The tensors are borrowed: they must live, and stay where they are, as long as this object.
+    """
+
+    def __init__(self, grads: Iterable, out: Optional[Iterable] = None, stream=None):
+        import torch
+        grads = list(grads)
+        outs = grads if out is None else list(out)
+        if len(outs) != len(grads):
+            raise ValueError("out must have one tensor for each gradient")
+        descs: List[ClipDesc] = []
+        for g, o in zip(grads, outs):
+            if g.dtype not in (torch.bfloat16, torch.float32) or o.dtype not in (torch.bfloat16, torch.float32):
+                raise TypeError("gradients must be bf16 or fp32")
+            if o.dtype == torch.float32 and g.dtype != torch.float32:
+                raise TypeError("a bf16 gradient is clipped to bf16")
+            if not (g.is_cuda and o.is_cuda and g.is_contiguous() and o.is_contiguous()):
+                raise ValueError("gradients must be contiguous CUDA tensors")
+            if g.shape != o.shape or g.device != o.device or g.device != grads[0].device:
+                raise ValueError("gradient and out must have one shape, and all tensors one device")
+            descs.append(ClipDesc(g.data_ptr(), o.data_ptr(), g.numel(),
+                                  (CLIP_GRAD_FP32 if g.dtype == torch.float32 else 0) |
+                                  (CLIP_OUT_FP32 if o.dtype == torch.float32 else 0), 0))
+        self.grads, self.out = grads, outs
+        self.h = skew_clip_create(descs)
+        dev = grads[0].device if grads else torch.device("cuda")
+        n = skew_clip_workspace_bytes(self.h)
+        self.workspace = torch.empty(n, dtype=torch.uint8, device=dev)
+        self.result = torch.zeros(2, dtype=torch.float32, device=dev)
+        self.gamma = self.result[1:]
+        self._result = self.result.data_ptr()
+        skew_clip_bind(self.h, self.workspace.data_ptr(), n, _stream_of(stream))
+
+    def norm(self, max_norm: float, stream=None):
+        """[norm, gamma] with gamma = min(1, max_norm / (norm + 1e-6)); the gradients are only read."""
+        skew_clip_norm(self.h, max_norm, self._result, _stream_of(stream))
+        return self.result
+
+    def clip(self, max_norm: float, stream=None):
+        """``norm``, then out = gamma * g for every tensor."""
+        skew_clip_apply(self.h, max_norm, self._result, _stream_of(stream))
+        return self.result
+
+    def close(self):
+        if getattr(self, "h", None):
+            skew_clip_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
 class SkewAdam:
     """SkewAdam over a list of (weight, grad, tier[, flags]) CUDA tensors, bf16 or fp32
     (an fp32 pair, as the paper keeps the norms and the router, is stepped in fp32

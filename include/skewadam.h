@@ -434,6 +434,56 @@ int skew_clip_norm(skew_clip_t *h, float max_norm, float *result, void *stream);
  * place by gamma = 1). Errors: also SKEW_ESTATE for a handle planned without `out`. */
 int skew_clip_apply(skew_clip_t *h, float max_norm, float *result, void *stream);
 
+/* ---- routing of tokens to experts --------------------------------------------
+ * Per token, with logits x over the experts:
+ *   score   s = softmax(x) or sigmoid(x)
+ *   choice  c = s + bias (bias != NULL), else x, which orders as s does
+ *   groups  (groups > 1) experts are `groups` consecutive runs; a run counts by its largest
+ *           c (group_top 1) or the sum of its two largest s + bias (group_top 2); the
+ *           top_groups best keep their experts
+ *   chosen  the top_k largest c of what is left, largest first, the lowest index first among equals
+ *   weight  w = scale * s, divided by the sum of the chosen s with SKEW_GATE_RENORM
+ * A bias steers which experts are chosen and never enters a weight (it balances
+ * loads without a loss term). Experts with a logit of -Inf or NaN, or a choice that is
+ * -Inf or NaN, are never chosen: a slot that finds no expert is -1 with weight 0. A sum of
+ * zero gives weights of zero. A NaN logit makes the weights of its token NaN. Scores are fp32.
+ */
+#define SKEW_GATE_SOFTMAX 0
+#define SKEW_GATE_SIGMOID 1
+#define SKEW_GATE_RENORM 1u /* weights divided by their sum                     */
+#define SKEW_GATE_FP32 2u   /* logits and their gradient are fp32 (else bf16)   */
+
+/*
+ * experts 1 to 512; groups 1 to 32, a divisor of experts; top_groups 1 to groups; group_top
+ * 1 or 2; top_k 1 to 32 and at most the experts of top_groups groups; score
+ * SKEW_GATE_SOFTMAX or _SIGMOID; scale finite.
+ */
+typedef struct {
+    int32_t experts, top_k, groups, top_groups, group_top, score;
+    float scale;
+    uint32_t flags; /* SKEW_GATE_* */
+} skew_gate_config_t;
+
+/* Bytes of device workspace that `counts` need (0 for an invalid config). */
+size_t skew_gate_workspace_bytes(const skew_gate_config_t *c);
+/*
+ * logits: `tokens` rows of `experts` elements, `ld` >= experts elements apart, aligned to their type
+ * (16-byte aligned rows enable vector loads). bias: fp32 per expert, or NULL. chosen, weights:
+ * (tokens, top_k), contiguous. counts: how many tokens chose each expert (int32 per expert), or
+ * NULL. workspace: zero-filled once by the caller; every call leaves it zeroed; calls that
+ * share one must not overlap on the GPU. tokens: 0 to 2^31 - 1.
+ * Errors: SKEW_EINVAL, SKEW_ECUDA.
+ */
+int skew_gate_forward(const skew_gate_config_t *c, const void *logits, int64_t ld, const float *bias, int64_t tokens,
+                      int32_t *chosen, float *weights, int32_t *counts, void *workspace, size_t workspace_bytes, void *stream);
+/*
+ * The logits' gradient from the weights' (tokens, top_k), for the experts in `chosen` (distinct within a
+ * token; entries outside [0, experts) have none). Every element of the `tokens` rows of dlogits, `ld_out`
+ * elements apart, is written (zeros included). dlogits has the logits' type and may not overlap any input.
+ */
+int skew_gate_grad(const skew_gate_config_t *c, const void *logits, int64_t ld, const int32_t *chosen, const float *dweights,
+                   int64_t tokens, void *dlogits, int64_t ld_out, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -359,7 +359,7 @@ __global__ void __launch_bounds__(kThreads) k_gate_grad_chosen(const __grid_cons
             q = sum == 0.f ? 0.f : q / sum;
             g -= slots_sum(e >= 0 ? g * q : 0.f, A.kp_log2);
         }
-        if (e >= 0) rows[tt * A.E + e] = q == 0.f && g == g ? 0.f : A.scale * q * g * rest;
+        if (e >= 0) rows[tt * A.E + e] = A.scale * q * g * rest;
         __syncwarp();
         if (A.flat) {  // whole 8-element units, rows one after another
             const int units = n * A.E >> 3;

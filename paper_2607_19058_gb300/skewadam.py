@@ -27,6 +27,8 @@ F_FP32 = 2
 KIND_FULL, KIND_FACTORED = 0, 1
 ROUTE_OWN, ROUTE_RIDING, ROUTE_ROWS, ROUTE_SMALL = 0, 1, 2, 3
 CLIP_GRAD_FP32, CLIP_OUT_FP32 = 1, 2
+GATE_SOFTMAX, GATE_SIGMOID = 0, 1
+GATE_RENORM, GATE_FP32 = 1, 2
 
 EXPORTS = ["skew_create", "skew_destroy", "skew_state_bytes", "skew_workspace_bytes", "skew_bind", "skew_step",
            "skew_sync_status", "skew_tensor_scalars", "skew_matrix_scalars", "skew_tensor_info", "skew_num_tensors", "skew_last_error",
@@ -34,7 +36,7 @@ EXPORTS = ["skew_create", "skew_destroy", "skew_state_bytes", "skew_workspace_by
            "skew_launches_per_step", "skew_selftest_wait_timeout", "skew_noalloc_sync_status", "skew_step_scaled",
            "skew_noalloc_selftest_wait_timeout", "skew_tensor_route", "skew_ops_last_error",
            "skew_clip_create", "skew_clip_destroy", "skew_clip_workspace_bytes", "skew_clip_bind", "skew_clip_norm",
-           "skew_clip_apply"]
+           "skew_clip_apply", "skew_gate_workspace_bytes", "skew_gate_forward", "skew_gate_grad"]
 
 
 class SkewError(RuntimeError):
@@ -63,6 +65,11 @@ class TensorInfo(C.Structure):
 class ClipDesc(C.Structure):
     _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("numel", C.c_int64), ("flags", C.c_uint32),
                 ("zero", C.c_uint32)]
+
+
+class GateConfig(C.Structure):
+    _fields_ = [("experts", C.c_int32), ("top_k", C.c_int32), ("groups", C.c_int32), ("top_groups", C.c_int32),
+                ("group_top", C.c_int32), ("score", C.c_int32), ("scale", C.c_float), ("flags", C.c_uint32)]
 
 
 _lock = threading.Lock()
@@ -139,6 +146,12 @@ def load(path: Optional[str] = None) -> C.CDLL:
         for f in (L.skew_clip_norm, L.skew_clip_apply):
             f.argtypes = [vp, C.c_float, vp, vp]
             f.restype = C.c_int
+        L.skew_gate_workspace_bytes.argtypes = [C.POINTER(GateConfig)]
+        L.skew_gate_workspace_bytes.restype = sz
+        L.skew_gate_forward.argtypes = [C.POINTER(GateConfig), vp, i64, vp, i64, vp, vp, vp, vp, sz, vp]
+        L.skew_gate_forward.restype = C.c_int
+        L.skew_gate_grad.argtypes = [C.POINTER(GateConfig), vp, i64, vp, vp, i64, vp, i64, vp]
+        L.skew_gate_grad.restype = C.c_int
         if path is None:
             _lib = L
         return L
@@ -316,6 +329,23 @@ def skew_clip_apply(h, max_norm: float, result_ptr: int, stream: int) -> None:
     _check_op(load().skew_clip_apply(h, max_norm, result_ptr, stream))
 
 
+def skew_gate_workspace_bytes(c: GateConfig) -> int:
+    return int(load().skew_gate_workspace_bytes(C.byref(c)))
+
+
+def skew_gate_forward(c: GateConfig, logits_ptr: int, ld: int, bias_ptr: int, tokens: int, chosen_ptr: int,
+                      weights_ptr: int, counts_ptr: int, ws_ptr: int, ws_bytes: int, stream: int) -> None:
+    """`bias_ptr`, `counts_ptr`: 0 for none."""
+    _check_op(load().skew_gate_forward(C.byref(c), logits_ptr, ld, bias_ptr or None, tokens, chosen_ptr, weights_ptr,
+                                       counts_ptr or None, ws_ptr, ws_bytes, stream))
+
+
+def skew_gate_grad(c: GateConfig, logits_ptr: int, ld: int, chosen_ptr: int, dweights_ptr: int, tokens: int,
+                   dlogits_ptr: int, ld_out: int, stream: int) -> None:
+    _check_op(load().skew_gate_grad(C.byref(c), logits_ptr, ld, chosen_ptr, dweights_ptr, tokens, dlogits_ptr, ld_out,
+                                    stream))
+
+
 def hparams(beta1=0.9, beta2=0.999, eps=1e-8, clip_d=1.0, weight_decay=0.05, policy=POLICY_TIERED) -> HParams:
     return HParams(beta1, beta2, eps, clip_d, weight_decay, policy)
 
@@ -391,6 +421,75 @@ class GradClip:
             self.close()
         except Exception:
             pass
+
+
+def _rows(t, width: int, what: str) -> int:
+    """The row stride of a 2-D CUDA tensor whose rows are contiguous."""
+    if not t.is_cuda or t.dim() != 2 or t.shape[1] != width or (width > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what} must be a 2-D CUDA tensor of {width} columns, contiguous within a row")
+    return t.stride(0) if t.shape[0] > 1 else max(width, t.stride(0))
+
+
+class Router:
+    """Routing of tokens to experts (the gate of an MoE layer) and its gradient.
+
+    ``score``: "softmax" or "sigmoid"; ``renorm``: weights divided by their sum over the chosen;
+    ``groups``, ``top_groups``, ``group_top``: experts are first narrowed to the best groups, each by its
+    best one or the sum of its best two choices; ``scale``: a factor on the weights. See
+    ``skew_gate_forward`` in the header for the definition, masked experts and ties.
+    """
+
+    def __init__(self, experts: int, top_k: int, score: str = "softmax", renorm: bool = True, groups: int = 1,
+                 top_groups: int = 1, group_top: int = 1, scale: float = 1.0):
+        kinds = {"softmax": GATE_SOFTMAX, "sigmoid": GATE_SIGMOID}
+        if score not in kinds:
+            raise ValueError("score must be 'softmax' or 'sigmoid'")
+        self.experts, self.top_k = experts, top_k
+        flags = GATE_RENORM if renorm else 0
+        make = lambda f: GateConfig(experts, top_k, groups, top_groups, group_top, kinds[score], scale, f)  # noqa: E731
+        self.config = {False: make(flags), True: make(flags | GATE_FP32)}
+        self._ws_bytes = skew_gate_workspace_bytes(self.config[True])
+        if not self._ws_bytes:
+            raise SkewError(SKEW_EINVAL, skew_ops_last_error())
+        self.workspace = None
+
+    def _config(self, logits):
+        import torch
+        if logits.dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError("logits must be bf16 or fp32")
+        return self.config[logits.dtype == torch.float32]
+
+    def route(self, logits, bias=None, stream=None):
+        """(chosen int32 (T, k), weights fp32 (T, k), counts int32 (experts,)) of (T, experts) logits, whose rows
+        may lie apart. ``bias``: fp32 (experts,), added to the scores for the choice alone. Calls on one
+        object share a workspace: they must not overlap on the GPU."""
+        import torch
+        ld, T, dev = _rows(logits, self.experts, "logits"), logits.shape[0], logits.device
+        c = self._config(logits)
+        if bias is not None and not (bias.device == dev and bias.dtype == torch.float32 and bias.is_contiguous()
+                                     and bias.shape == (self.experts,)):
+            raise ValueError("bias must be a contiguous fp32 tensor of one value for each expert, on the logits' device")
+        if self.workspace is None or self.workspace.device != dev:
+            self.workspace = torch.zeros(self._ws_bytes, dtype=torch.uint8, device=dev)
+        chosen = torch.empty((T, self.top_k), dtype=torch.int32, device=dev)
+        weights = torch.empty((T, self.top_k), dtype=torch.float32, device=dev)
+        counts = torch.empty(self.experts, dtype=torch.int32, device=dev)
+        skew_gate_forward(c, logits.data_ptr(), ld, 0 if bias is None else bias.data_ptr(), T, chosen.data_ptr(),
+                          weights.data_ptr(), counts.data_ptr(), self.workspace.data_ptr(), self._ws_bytes,
+                          _stream_of(stream))
+        return chosen, weights, counts
+
+    def grad(self, logits, chosen, dweights, stream=None):
+        """The logits' gradient, (T, experts) of their type, from the weights' gradient (T, k) fp32."""
+        import torch
+        ld, T, dev = _rows(logits, self.experts, "logits"), logits.shape[0], logits.device
+        for t, dt, what in ((chosen, torch.int32, "chosen"), (dweights, torch.float32, "dweights")):
+            if not (t.device == dev and t.dtype == dt and t.is_contiguous() and t.shape == (T, self.top_k)):
+                raise ValueError(f"{what} must be a contiguous ({T}, {self.top_k}) {dt} tensor on the logits' device")
+        dlogits = torch.empty((T, self.experts), dtype=logits.dtype, device=dev)
+        skew_gate_grad(self._config(logits), logits.data_ptr(), ld, chosen.data_ptr(), dweights.data_ptr(), T,
+                       dlogits.data_ptr(), self.experts, _stream_of(stream))
+        return dlogits
 
 
 class SkewAdam:

@@ -80,3 +80,53 @@ def test_clip_wrapper_refuses_host_tensors_and_types():
         S.GradClip([torch.zeros(4)], out=[])
     with pytest.raises(TypeError):
         S.GradClip([torch.zeros(4, dtype=torch.bfloat16)], out=[torch.zeros(4)])
+
+
+def _gate(experts=8, top_k=2, groups=1, top_groups=1, group_top=1, score=0, scale=1.0, flags=S.GATE_FP32):
+    return S.GateConfig(experts, top_k, groups, top_groups, group_top, score, scale, flags)
+
+
+def test_gate_struct_layout():
+    assert _sizes(["sizeof(skew_gate_config_t)", "offsetof(skew_gate_config_t, scale)", "offsetof(skew_gate_config_t, flags)"]) == \
+        [C.sizeof(S.GateConfig), S.GateConfig.scale.offset, S.GateConfig.flags.offset]
+
+
+@pytest.mark.parametrize("kw,what", [
+    (dict(experts=0), "experts"), (dict(experts=513), "experts"), (dict(experts=8, groups=3), "groups"), (dict(experts=66, groups=33), "groups"),
+    (dict(groups=0), "groups"), (dict(groups=2, top_groups=3), "top_groups"), (dict(top_groups=0), "top_groups"),
+    (dict(group_top=3), "group_top"), (dict(group_top=0), "group_top"), (dict(top_k=0), "top_k"), (dict(top_k=9), "top_k"),
+    (dict(experts=64, top_k=33), "top_k"), (dict(groups=4, top_groups=1, top_k=3), "top_k"), (dict(score=2), "score"),
+    (dict(flags=4), "flags"), (dict(scale=float("nan")), "scale"), (dict(scale=float("inf")), "scale")])
+def test_gate_refuses_configs(kw, what):
+    c = _gate(**kw)
+    assert S.skew_gate_workspace_bytes(c) == 0 and what in S.skew_ops_last_error()
+    _refused(S.SKEW_EINVAL, what, S.skew_gate_forward, c, 0x1000, 8, 0, 4, 0x1000, 0x1000, 0x1000, 0x1000, 4096, 0)
+    _refused(S.SKEW_EINVAL, what, S.skew_gate_grad, c, 0x1000, 8, 0x1000, 0x1000, 4, 0x1000, 8, 0)
+
+
+@pytest.mark.parametrize("at,value,what", [
+    (0, 0, "logits"), (0, 0x1002, "logits"), (1, 7, "stride"), (1, (1 << 31) + 1, "stride"), (2, 0x1002, "bias"), (3, -1, "tokens"), (3, 1 << 31, "tokens"),
+    (4, 0, "chosen"), (5, 0x1001, "chosen"), (6, 0x1002, "workspace"), (7, 0, "workspace"), (8, 35, "workspace")])
+def test_gate_forward_refuses(at, value, what):
+    a = [0x1000, 8, 0, 4, 0x1000, 0x1000, 0x1000, 0x1000, 36]
+    a[at] = value
+    _refused(S.SKEW_EINVAL, what, S.skew_gate_forward, _gate(), *a, 0)
+
+
+@pytest.mark.parametrize("at,value,what", [
+    (0, 0, "logits"), (1, 7, "logits"), (2, 0, "chosen"), (3, 0x1002, "chosen"), (4, -1, "tokens"), (5, 0, "dlogits"), (5, 0x1002, "dlogits"), (6, 7, "dlogits")])
+def test_gate_grad_refuses(at, value, what):
+    a = [0x1000, 8, 0x1000, 0x1000, 4, 0x1000, 8]
+    a[at] = value
+    _refused(S.SKEW_EINVAL, what, S.skew_gate_grad, _gate(), *a, 0)
+
+
+def test_router_refuses():
+    import torch
+    with pytest.raises(ValueError):
+        S.Router(8, 2, score="relu")
+    with pytest.raises(S.SkewError):
+        S.Router(8, 9)
+    with pytest.raises(ValueError):
+        S.Router(8, 2).route(torch.zeros((4, 8)))
+    assert S.skew_gate_forward(_gate(), 0, 8, 0, 0, 0, 0, 0, 0, 0, 0) is None  # no tokens, no counts: nothing to do

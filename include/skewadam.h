@@ -484,6 +484,44 @@ int skew_gate_forward(const skew_gate_config_t *c, const void *logits, int64_t l
 int skew_gate_grad(const skew_gate_config_t *c, const void *logits, int64_t ld, const int32_t *chosen, const float *dweights,
                    int64_t tokens, void *dlogits, int64_t ld_out, void *stream);
 
+/* ---- embedding lookup and its gradient -----------------------------------------
+ *   lookup    y[t] = scale * W[id_t]
+ *   gradient  dW[v] = base[v] + scale * (sum over the t with id_t = v of dy[t])
+ * W is (rows, width), contiguous. An id outside [0, rows) is padding: its y is zero and it has no
+ * gradient. Terms are added in fp32 in the tokens' order (a row with more than 32 terms: in runs of at
+ * most 32, whose sums are then added in order), so results do not depend on timing; each element is
+ * rounded once.
+ */
+#define SKEW_EMBED_TABLE_FP32 1u /* W, base and dW are fp32 (else bf16) */
+#define SKEW_EMBED_ACT_FP32 2u   /* y and dy are fp32 (else bf16)       */
+#define SKEW_EMBED_IDS_64 4u     /* ids are int64 (else int32)          */
+
+/* rows 1 to 2^31 - 1, width 1 to 2^20, scale finite. */
+typedef struct {
+    int64_t rows, width;
+    float scale;
+    uint32_t flags; /* SKEW_EMBED_* */
+} skew_embed_config_t;
+
+/*
+ * tokens: 0 to 2^31 - 1 ids, contiguous. out: `tokens` rows of `width` elements, `ld_out` >= width
+ * elements apart. Pointers aligned to their types (rows that start on 16-byte boundaries, of a
+ * width that 8 divides, enable vector accesses). Errors: SKEW_EINVAL, SKEW_ECUDA.
+ */
+int skew_embed_lookup(const skew_embed_config_t *c, const void *table, const void *ids, int64_t tokens, void *out,
+                      int64_t ld_out, void *stream);
+/* Bytes of device workspace that the gradient of `tokens` tokens needs (0 for an invalid config). */
+size_t skew_embed_workspace_bytes(const skew_embed_config_t *c, int64_t tokens);
+/*
+ * dout: the gradient of `out`, rows `ld_dout` apart. Every element of dtable is written, rows without
+ * tokens as base or zero. base: NULL, a tensor like dtable that overlaps nothing else, or dtable itself, to which the
+ * gradient is then added; rows without tokens are not touched (the gradient of a table
+ * that the output head shares). workspace: 256-byte aligned, of any content; calls that share one
+ * must not overlap on the GPU.
+ */
+int skew_embed_grad(const skew_embed_config_t *c, const void *ids, int64_t tokens, const void *dout, int64_t ld_dout,
+                    const void *base, void *dtable, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

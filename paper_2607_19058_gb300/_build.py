@@ -13,7 +13,8 @@ OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libskewadam.so")
 INCLUDE = os.path.join(ROOT, "include")
 
-SOURCES = ["skew_host.cpp", "skew_kernels.cu", "skew_noalloc.cu", "skew_ops.cpp", "skew_clip.cu", "skew_gate.cu"]
+SOURCES = ["skew_host.cpp", "skew_kernels.cu", "skew_noalloc.cu", "skew_ops.cpp", "skew_clip.cu", "skew_gate.cu",
+           "skew_embed.cu"]
 HEADERS = [os.path.join(CSRC, "skew_plan.h"), os.path.join(CSRC, "skew_ops.h"), os.path.join(INCLUDE, "skewadam.h")]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall",

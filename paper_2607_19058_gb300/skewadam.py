@@ -29,6 +29,7 @@ ROUTE_OWN, ROUTE_RIDING, ROUTE_ROWS, ROUTE_SMALL = 0, 1, 2, 3
 CLIP_GRAD_FP32, CLIP_OUT_FP32 = 1, 2
 GATE_SOFTMAX, GATE_SIGMOID = 0, 1
 GATE_RENORM, GATE_FP32 = 1, 2
+EMBED_TABLE_FP32, EMBED_ACT_FP32, EMBED_IDS_64 = 1, 2, 4
 
 EXPORTS = ["skew_create", "skew_destroy", "skew_state_bytes", "skew_workspace_bytes", "skew_bind", "skew_step",
            "skew_sync_status", "skew_tensor_scalars", "skew_matrix_scalars", "skew_tensor_info", "skew_num_tensors", "skew_last_error",
@@ -36,7 +37,8 @@ EXPORTS = ["skew_create", "skew_destroy", "skew_state_bytes", "skew_workspace_by
            "skew_launches_per_step", "skew_selftest_wait_timeout", "skew_noalloc_sync_status", "skew_step_scaled",
            "skew_noalloc_selftest_wait_timeout", "skew_tensor_route", "skew_ops_last_error",
            "skew_clip_create", "skew_clip_destroy", "skew_clip_workspace_bytes", "skew_clip_bind", "skew_clip_norm",
-           "skew_clip_apply", "skew_gate_workspace_bytes", "skew_gate_forward", "skew_gate_grad"]
+           "skew_clip_apply", "skew_gate_workspace_bytes", "skew_gate_forward", "skew_gate_grad",
+           "skew_embed_lookup", "skew_embed_workspace_bytes", "skew_embed_grad"]
 
 
 class SkewError(RuntimeError):
@@ -70,6 +72,10 @@ class ClipDesc(C.Structure):
 class GateConfig(C.Structure):
     _fields_ = [("experts", C.c_int32), ("top_k", C.c_int32), ("groups", C.c_int32), ("top_groups", C.c_int32),
                 ("group_top", C.c_int32), ("score", C.c_int32), ("scale", C.c_float), ("flags", C.c_uint32)]
+
+
+class EmbedConfig(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("width", C.c_int64), ("scale", C.c_float), ("flags", C.c_uint32)]
 
 
 _lock = threading.Lock()
@@ -152,6 +158,12 @@ def load(path: Optional[str] = None) -> C.CDLL:
         L.skew_gate_forward.restype = C.c_int
         L.skew_gate_grad.argtypes = [C.POINTER(GateConfig), vp, i64, vp, vp, i64, vp, i64, vp]
         L.skew_gate_grad.restype = C.c_int
+        L.skew_embed_lookup.argtypes = [C.POINTER(EmbedConfig), vp, vp, i64, vp, i64, vp]
+        L.skew_embed_lookup.restype = C.c_int
+        L.skew_embed_workspace_bytes.argtypes = [C.POINTER(EmbedConfig), i64]
+        L.skew_embed_workspace_bytes.restype = sz
+        L.skew_embed_grad.argtypes = [C.POINTER(EmbedConfig), vp, i64, vp, i64, vp, vp, vp, sz, vp]
+        L.skew_embed_grad.restype = C.c_int
         if path is None:
             _lib = L
         return L
@@ -346,6 +358,22 @@ def skew_gate_grad(c: GateConfig, logits_ptr: int, ld: int, chosen_ptr: int, dwe
                                     stream))
 
 
+def skew_embed_lookup(c: EmbedConfig, table_ptr: int, ids_ptr: int, tokens: int, out_ptr: int, ld_out: int,
+                      stream: int) -> None:
+    _check_op(load().skew_embed_lookup(C.byref(c), table_ptr, ids_ptr, tokens, out_ptr, ld_out, stream))
+
+
+def skew_embed_workspace_bytes(c: EmbedConfig, tokens: int) -> int:
+    return int(load().skew_embed_workspace_bytes(C.byref(c), tokens))
+
+
+def skew_embed_grad(c: EmbedConfig, ids_ptr: int, tokens: int, dout_ptr: int, ld_dout: int, base_ptr: int,
+                    dtable_ptr: int, ws_ptr: int, ws_bytes: int, stream: int) -> None:
+    """`base_ptr`: 0 for none."""
+    _check_op(load().skew_embed_grad(C.byref(c), ids_ptr, tokens, dout_ptr, ld_dout, base_ptr or None, dtable_ptr,
+                                     ws_ptr, ws_bytes, stream))
+
+
 def hparams(beta1=0.9, beta2=0.999, eps=1e-8, clip_d=1.0, weight_decay=0.05, policy=POLICY_TIERED) -> HParams:
     return HParams(beta1, beta2, eps, clip_d, weight_decay, policy)
 
@@ -421,6 +449,77 @@ class GradClip:
             self.close()
         except Exception:
             pass
+
+
+class Embedding:
+    """Lookup of a (rows, width) table by token ids, scaled, and the table's gradient.
+
+    ``table_dtype`` (of the table and its gradient) and ``act_dtype`` (of the looked-up rows and their
+    gradient) are bf16 or fp32. Ids are int32 or int64, of any shape; one outside [0, rows) is padding: its
+    row is zero and it has no gradient.
+    """
+
+    def __init__(self, rows: int, width: int, table_dtype=None, act_dtype=None, scale: float = 1.0):
+        import torch
+        self.table_dtype, self.act_dtype = table_dtype or torch.bfloat16, act_dtype or torch.bfloat16
+        if not {self.table_dtype, self.act_dtype} <= {torch.bfloat16, torch.float32}:
+            raise TypeError("table and activations must be bf16 or fp32")
+        self.rows, self.width = rows, width
+        flags = (EMBED_TABLE_FP32 if self.table_dtype == torch.float32 else 0) | \
+                (EMBED_ACT_FP32 if self.act_dtype == torch.float32 else 0)
+        make = lambda f: EmbedConfig(rows, width, scale, f)  # noqa: E731
+        self.config = {torch.int32: make(flags), torch.int64: make(flags | EMBED_IDS_64)}
+        if not skew_embed_workspace_bytes(self.config[torch.int32], 0):
+            raise SkewError(SKEW_EINVAL, skew_ops_last_error())
+        self.workspace, self._sizes = None, {}
+
+    def _ids(self, ids):
+        c = self.config.get(ids.dtype)
+        if c is None:
+            raise TypeError("ids must be int32 or int64")
+        if not (ids.is_cuda and ids.is_contiguous()):
+            raise ValueError("ids must be a contiguous CUDA tensor")
+        return c
+
+    def _table(self, t, dev, what: str):
+        if not (t.device == dev and t.dtype == self.table_dtype and t.is_contiguous() and t.shape == (self.rows, self.width)):
+            raise ValueError(f"{what} must be a contiguous ({self.rows}, {self.width}) {self.table_dtype} tensor on the ids' device")
+        return t.data_ptr()
+
+    def lookup(self, table, ids, stream=None):
+        """scale * table[ids], of shape ids.shape + (width,)."""
+        import torch
+        c = self._ids(ids)
+        p = self._table(table, ids.device, "table")
+        out = torch.empty((*ids.shape, self.width), dtype=self.act_dtype, device=ids.device)
+        skew_embed_lookup(c, p, ids.data_ptr(), ids.numel(), out.data_ptr(), self.width, _stream_of(stream))
+        return out
+
+    def grad(self, ids, dy, base=None, out=None, stream=None):
+        """The table's gradient, every row of it, from the looked-up rows' (``ids.shape + (width,)``; a 2-D one may
+        have rows apart). ``base``: what it adds to; ``out``: where it goes (``base`` itself: in place, and rows
+        without tokens are not touched; None: a new tensor). Calls on one object share a
+        workspace: they must not overlap on the GPU."""
+        import torch
+        c, dev, n = self._ids(ids), ids.device, ids.numel()
+        if dy.dtype != self.act_dtype or dy.shape != (*ids.shape, self.width) or dy.device != dev:
+            raise ValueError(f"dy must be a {(*ids.shape, self.width)} {self.act_dtype} tensor on the ids' device")
+        if dy.is_contiguous():
+            ld = self.width
+        else:
+            ld = _rows(dy, self.width, "dy that is not contiguous")
+        b = 0 if base is None else self._table(base, dev, "base")
+        if out is None:
+            out = torch.empty((self.rows, self.width), dtype=self.table_dtype, device=dev)
+        p = self._table(out, dev, "out")
+        need = self._sizes.get(n)
+        if need is None:
+            need = self._sizes[n] = skew_embed_workspace_bytes(c, n)
+        if self.workspace is None or self.workspace.numel() < need or self.workspace.device != dev:
+            self.workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        skew_embed_grad(c, ids.data_ptr(), n, dy.data_ptr(), ld, b, p, self.workspace.data_ptr(),
+                        self.workspace.numel(), _stream_of(stream))
+        return out
 
 
 def _rows(t, width: int, what: str) -> int:

@@ -130,3 +130,50 @@ def test_router_refuses():
     with pytest.raises(ValueError):
         S.Router(8, 2).route(torch.zeros((4, 8)))
     assert S.skew_gate_forward(_gate(), 0, 8, 0, 0, 0, 0, 0, 0, 0, 0) is None  # no tokens, no counts: nothing to do
+
+
+def _embed(rows=100, width=16, scale=1.0, flags=0):
+    return S.EmbedConfig(rows, width, scale, flags)
+
+
+def test_embed_struct_layout():
+    assert _sizes(["sizeof(skew_embed_config_t)", "offsetof(skew_embed_config_t, scale)", "offsetof(skew_embed_config_t, flags)"]) == \
+        [C.sizeof(S.EmbedConfig), S.EmbedConfig.scale.offset, S.EmbedConfig.flags.offset]
+
+
+@pytest.mark.parametrize("kw,what", [(dict(rows=0), "rows"), (dict(rows=1 << 31), "rows"), (dict(width=0), "width"), (dict(width=(1 << 20) + 1), "width"),
+                                     (dict(scale=float("nan")), "scale"), (dict(flags=8), "flags")])
+def test_embed_refuses_configs(kw, what):
+    c = _embed(**kw)
+    assert S.skew_embed_workspace_bytes(c, 4) == 0 and what in S.skew_ops_last_error()
+    _refused(S.SKEW_EINVAL, what, S.skew_embed_lookup, c, 0x1000, 0x1000, 4, 0x1000, 16, 0)
+    _refused(S.SKEW_EINVAL, what, S.skew_embed_grad, c, 0x1000, 4, 0x1000, 16, 0, 0x1000, 0x1000, 1 << 30, 0)
+
+
+@pytest.mark.parametrize("at,value,what", [(0, 0, "table"), (0, 0x1001, "table"), (1, 0, "ids"), (1, 0x1002, "ids"), (2, -1, "tokens"), (2, 1 << 31, "tokens"),
+                                           (3, 0, "out"), (3, 0x1001, "out"), (4, 15, "stride"), (4, (1 << 31) + 1, "stride")])
+def test_embed_lookup_refuses(at, value, what):
+    a = [0x1000, 0x1000, 4, 0x1000, 16]
+    a[at] = value
+    _refused(S.SKEW_EINVAL, what, S.skew_embed_lookup, _embed(), *a, 0)
+
+
+@pytest.mark.parametrize("at,value,what", [(0, 0, "ids"), (0, 0x1002, "ids"), (1, -1, "tokens"), (2, 0, "dout"), (2, 0x1001, "dout"), (3, 15, "stride"),
+                                           (4, 0x1001, "base"), (5, 0, "dtable"), (5, 0x1001, "dtable"), (6, 0, "workspace"), (6, 0x1010, "workspace"), (7, 1024, "workspace")])
+def test_embed_grad_refuses(at, value, what):
+    a = [0x1000, 4, 0x1000, 16, 0, 0x1000, 0x1000, 1 << 20]
+    a[at] = value
+    _refused(S.SKEW_EINVAL, what, S.skew_embed_grad, _embed(), *a, 0)
+
+
+def test_embedding_refuses():
+    import torch
+    with pytest.raises(TypeError):
+        S.Embedding(10, 8, torch.float16)
+    with pytest.raises(S.SkewError):
+        S.Embedding(0, 8)
+    e = S.Embedding(10, 8)
+    with pytest.raises(TypeError):
+        e.lookup(torch.zeros((10, 8), dtype=torch.bfloat16), torch.zeros(3))
+    with pytest.raises(ValueError):
+        e.lookup(torch.zeros((10, 8), dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int64))

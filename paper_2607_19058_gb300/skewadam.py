@@ -381,10 +381,14 @@ def hparams(beta1=0.9, beta2=0.999, eps=1e-8, clip_d=1.0, weight_decay=0.05, pol
 # --------------------------------------------------------------------------
 # torch convenience wrappers
 # --------------------------------------------------------------------------
-def _stream_of(stream) -> int:
+def _stream_of(stream, device=None) -> int:
+    """The raw handle of a stream, or of the current one of a tensor's device."""
     if stream is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # 0.1 us; the public call takes 2 to 3
+        if raw is not None and device is not None and device.index is not None:
+            return raw(device.index)
+        return torch.cuda.current_stream(device).cuda_stream
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -426,17 +430,18 @@ class GradClip:
         self.workspace = torch.empty(n, dtype=torch.uint8, device=dev)
         self.result = torch.zeros(2, dtype=torch.float32, device=dev)
         self.gamma = self.result[1:]
-        self._result = self.result.data_ptr()
-        skew_clip_bind(self.h, self.workspace.data_ptr(), n, _stream_of(stream))
+        self._result, self._device = self.result.data_ptr(), self.result.device
+        self._norm, self._apply = load().skew_clip_norm, load().skew_clip_apply
+        skew_clip_bind(self.h, self.workspace.data_ptr(), n, _stream_of(stream, self._device))
 
     def norm(self, max_norm: float, stream=None):
         """[norm, gamma] with gamma = min(1, max_norm / (norm + 1e-6)); the gradients are only read."""
-        skew_clip_norm(self.h, max_norm, self._result, _stream_of(stream))
+        _check_op(self._norm(self.h, max_norm, self._result, _stream_of(stream, self._device)))
         return self.result
 
     def clip(self, max_norm: float, stream=None):
         """``norm``, then out = gamma * g for every tensor."""
-        skew_clip_apply(self.h, max_norm, self._result, _stream_of(stream))
+        _check_op(self._apply(self.h, max_norm, self._result, _stream_of(stream, self._device)))
         return self.result
 
     def close(self):
@@ -467,14 +472,17 @@ class Embedding:
         self.rows, self.width = rows, width
         flags = (EMBED_TABLE_FP32 if self.table_dtype == torch.float32 else 0) | \
                 (EMBED_ACT_FP32 if self.act_dtype == torch.float32 else 0)
-        make = lambda f: EmbedConfig(rows, width, scale, f)  # noqa: E731
-        self.config = {torch.int32: make(flags), torch.int64: make(flags | EMBED_IDS_64)}
+        self.config = {torch.int32: EmbedConfig(rows, width, scale, flags),
+                       torch.int64: EmbedConfig(rows, width, scale, flags | EMBED_IDS_64)}
         if not skew_embed_workspace_bytes(self.config[torch.int32], 0):
             raise SkewError(SKEW_EINVAL, skew_ops_last_error())
+        self._ref = {dt: C.byref(c) for dt, c in self.config.items()}
+        self._shape = (rows, width)
+        self._empty, self._lookup, self._grad = torch.empty, load().skew_embed_lookup, load().skew_embed_grad
         self.workspace, self._sizes = None, {}
 
     def _ids(self, ids):
-        c = self.config.get(ids.dtype)
+        c = self._ref.get(ids.dtype)
         if c is None:
             raise TypeError("ids must be int32 or int64")
         if not (ids.is_cuda and ids.is_contiguous()):
@@ -482,17 +490,16 @@ class Embedding:
         return c
 
     def _table(self, t, dev, what: str):
-        if not (t.device == dev and t.dtype == self.table_dtype and t.is_contiguous() and t.shape == (self.rows, self.width)):
-            raise ValueError(f"{what} must be a contiguous ({self.rows}, {self.width}) {self.table_dtype} tensor on the ids' device")
+        if not (t.dtype == self.table_dtype and t.shape == self._shape and t.is_contiguous() and t.device == dev):
+            raise ValueError(f"{what} must be a contiguous {self._shape} {self.table_dtype} tensor on the ids' device")
         return t.data_ptr()
 
     def lookup(self, table, ids, stream=None):
         """scale * table[ids], of shape ids.shape + (width,)."""
-        import torch
-        c = self._ids(ids)
-        p = self._table(table, ids.device, "table")
-        out = torch.empty((*ids.shape, self.width), dtype=self.act_dtype, device=ids.device)
-        skew_embed_lookup(c, p, ids.data_ptr(), ids.numel(), out.data_ptr(), self.width, _stream_of(stream))
+        c, dev = self._ids(ids), ids.device
+        p = self._table(table, dev, "table")
+        out = self._empty((*ids.shape, self.width), dtype=self.act_dtype, device=dev)
+        _check_op(self._lookup(c, p, ids.data_ptr(), ids.numel(), out.data_ptr(), self.width, _stream_of(stream, dev)))
         return out
 
     def grad(self, ids, dy, base=None, out=None, stream=None):
@@ -500,25 +507,24 @@ class Embedding:
         have rows apart). ``base``: what it adds to; ``out``: where it goes (``base`` itself: in place, and rows
         without tokens are not touched; None: a new tensor). Calls on one object share a
         workspace: they must not overlap on the GPU."""
-        import torch
         c, dev, n = self._ids(ids), ids.device, ids.numel()
         if dy.dtype != self.act_dtype or dy.shape != (*ids.shape, self.width) or dy.device != dev:
             raise ValueError(f"dy must be a {(*ids.shape, self.width)} {self.act_dtype} tensor on the ids' device")
-        if dy.is_contiguous():
-            ld = self.width
-        else:
-            ld = _rows(dy, self.width, "dy that is not contiguous")
-        b = 0 if base is None else self._table(base, dev, "base")
+        ld = self.width if dy.is_contiguous() else _rows(dy, self.width, "dy that is not contiguous")
+        b = None if base is None else self._table(base, dev, "base")
         if out is None:
-            out = torch.empty((self.rows, self.width), dtype=self.table_dtype, device=dev)
-        p = self._table(out, dev, "out")
+            out = self._empty(self._shape, dtype=self.table_dtype, device=dev)
+            p = out.data_ptr()
+        else:
+            p = self._table(out, dev, "out")
+        ws = self.workspace
         need = self._sizes.get(n)
         if need is None:
-            need = self._sizes[n] = skew_embed_workspace_bytes(c, n)
-        if self.workspace is None or self.workspace.numel() < need or self.workspace.device != dev:
-            self.workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-        skew_embed_grad(c, ids.data_ptr(), n, dy.data_ptr(), ld, b, p, self.workspace.data_ptr(),
-                        self.workspace.numel(), _stream_of(stream))
+            need = self._sizes[n] = skew_embed_workspace_bytes(self.config[ids.dtype], n)
+        if ws is None or ws.numel() < need or ws.device != dev:
+            import torch
+            ws = self.workspace = self._empty(need, dtype=torch.uint8, device=dev)
+        _check_op(self._grad(c, ids.data_ptr(), n, dy.data_ptr(), ld, b, p, ws.data_ptr(), need, _stream_of(stream, dev)))
         return out
 
 
@@ -540,54 +546,57 @@ class Router:
 
     def __init__(self, experts: int, top_k: int, score: str = "softmax", renorm: bool = True, groups: int = 1,
                  top_groups: int = 1, group_top: int = 1, scale: float = 1.0):
+        import torch
         kinds = {"softmax": GATE_SOFTMAX, "sigmoid": GATE_SIGMOID}
         if score not in kinds:
             raise ValueError("score must be 'softmax' or 'sigmoid'")
         self.experts, self.top_k = experts, top_k
         flags = GATE_RENORM if renorm else 0
         make = lambda f: GateConfig(experts, top_k, groups, top_groups, group_top, kinds[score], scale, f)  # noqa: E731
-        self.config = {False: make(flags), True: make(flags | GATE_FP32)}
-        self._ws_bytes = skew_gate_workspace_bytes(self.config[True])
+        self.config = {torch.bfloat16: make(flags), torch.float32: make(flags | GATE_FP32)}
+        self._ws_bytes = skew_gate_workspace_bytes(self.config[torch.float32])
         if not self._ws_bytes:
             raise SkewError(SKEW_EINVAL, skew_ops_last_error())
+        self._ref = {dt: C.byref(c) for dt, c in self.config.items()}
+        self._empty, self._i32, self._f32 = torch.empty, torch.int32, torch.float32
+        self._forward, self._grad = load().skew_gate_forward, load().skew_gate_grad
         self.workspace = None
 
-    def _config(self, logits):
-        import torch
-        if logits.dtype not in (torch.float32, torch.bfloat16):
+    def _logits(self, logits):
+        c = self._ref.get(logits.dtype)
+        if c is None:
             raise TypeError("logits must be bf16 or fp32")
-        return self.config[logits.dtype == torch.float32]
+        return c, _rows(logits, self.experts, "logits"), logits.shape[0], logits.device
 
     def route(self, logits, bias=None, stream=None):
         """(chosen int32 (T, k), weights fp32 (T, k), counts int32 (experts,)) of (T, experts) logits, whose rows
         may lie apart. ``bias``: fp32 (experts,), added to the scores for the choice alone. Calls on one
         object share a workspace: they must not overlap on the GPU."""
-        import torch
-        ld, T, dev = _rows(logits, self.experts, "logits"), logits.shape[0], logits.device
-        c = self._config(logits)
-        if bias is not None and not (bias.device == dev and bias.dtype == torch.float32 and bias.is_contiguous()
-                                     and bias.shape == (self.experts,)):
-            raise ValueError("bias must be a contiguous fp32 tensor of one value for each expert, on the logits' device")
-        if self.workspace is None or self.workspace.device != dev:
-            self.workspace = torch.zeros(self._ws_bytes, dtype=torch.uint8, device=dev)
-        chosen = torch.empty((T, self.top_k), dtype=torch.int32, device=dev)
-        weights = torch.empty((T, self.top_k), dtype=torch.float32, device=dev)
-        counts = torch.empty(self.experts, dtype=torch.int32, device=dev)
-        skew_gate_forward(c, logits.data_ptr(), ld, 0 if bias is None else bias.data_ptr(), T, chosen.data_ptr(),
-                          weights.data_ptr(), counts.data_ptr(), self.workspace.data_ptr(), self._ws_bytes,
-                          _stream_of(stream))
+        c, ld, T, dev = self._logits(logits)
+        k, empty, ws = self.top_k, self._empty, self.workspace
+        if bias is not None:
+            if not (bias.dtype == self._f32 and bias.shape == (self.experts,) and bias.is_contiguous() and bias.device == dev):
+                raise ValueError("bias must be a contiguous fp32 tensor of one value for each expert, on the logits' device")
+            bias = bias.data_ptr()
+        if ws is None or ws.device != dev:
+            import torch
+            ws = self.workspace = torch.zeros(self._ws_bytes, dtype=torch.uint8, device=dev)
+        chosen = empty((T, k), dtype=self._i32, device=dev)
+        weights = empty((T, k), dtype=self._f32, device=dev)
+        counts = empty(self.experts, dtype=self._i32, device=dev)
+        _check_op(self._forward(c, logits.data_ptr(), ld, bias, T, chosen.data_ptr(), weights.data_ptr(), counts.data_ptr(),
+                                ws.data_ptr(), self._ws_bytes, _stream_of(stream, dev)))
         return chosen, weights, counts
 
     def grad(self, logits, chosen, dweights, stream=None):
         """The logits' gradient, (T, experts) of their type, from the weights' gradient (T, k) fp32."""
-        import torch
-        ld, T, dev = _rows(logits, self.experts, "logits"), logits.shape[0], logits.device
-        for t, dt, what in ((chosen, torch.int32, "chosen"), (dweights, torch.float32, "dweights")):
-            if not (t.device == dev and t.dtype == dt and t.is_contiguous() and t.shape == (T, self.top_k)):
-                raise ValueError(f"{what} must be a contiguous ({T}, {self.top_k}) {dt} tensor on the logits' device")
-        dlogits = torch.empty((T, self.experts), dtype=logits.dtype, device=dev)
-        skew_gate_grad(self._config(logits), logits.data_ptr(), ld, chosen.data_ptr(), dweights.data_ptr(), T,
-                       dlogits.data_ptr(), self.experts, _stream_of(stream))
+        c, ld, T, dev = self._logits(logits)
+        for t, dt in ((chosen, self._i32), (dweights, self._f32)):
+            if not (t.dtype == dt and t.shape == (T, self.top_k) and t.is_contiguous() and t.device == dev):
+                raise ValueError(f"chosen and dweights must be contiguous ({T}, {self.top_k}) int32 and fp32 tensors on the logits' device")
+        dlogits = self._empty((T, self.experts), dtype=logits.dtype, device=dev)
+        _check_op(self._grad(c, logits.data_ptr(), ld, chosen.data_ptr(), dweights.data_ptr(), T, dlogits.data_ptr(),
+                             self.experts, _stream_of(stream, dev)))
         return dlogits
 
 

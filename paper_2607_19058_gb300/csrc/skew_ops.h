@@ -110,6 +110,15 @@ __device__ __forceinline__ Vec8<F32> load8(const void *p, int64_t i) {
 }
 
 template <bool F32>
+__device__ __forceinline__ Vec8<F32> load8_cached(const void *p, int64_t i) {  // likely read again
+    const uint4 *q = reinterpret_cast<const uint4 *>(elem_ptr<F32>(p, i));
+    Vec8<F32> v;
+    v.u[0] = q[0];
+    if constexpr (F32) v.u[1] = q[1];
+    return v;
+}
+
+template <bool F32>
 __device__ __forceinline__ void store8(void *p, int64_t i, const float (&x)[8]) {
     char *q = const_cast<char *>(elem_ptr<F32>(p, i));
     if constexpr (F32) {

@@ -24,8 +24,10 @@ constexpr int kParts = 4;
 constexpr int kChunk = 32;       // most places of the sorted list to a warp: one to a lane
 constexpr int kCols = 256;       // columns to a warp: 8 to a lane
 constexpr int kFewWarps = 152 * 8;
-constexpr int kFill = 8;         // rows of the table to a warp that writes those without tokens
-constexpr int kJoin = 4;         // pieces that are under way at a time where they are added up
+constexpr uint32_t kFillWarps = 152 * 48;
+constexpr int kGradThreads = 128;
+constexpr int kRing = 16 * (kCols * 2 + 32);  // bytes of shared memory that a warp has rows copied to
+constexpr uint32_t kJoin = 16;   // pieces that one warp adds up
 constexpr int kLookups = 8;      // most tokens to a warp of the lookup
 
 __device__ __forceinline__ int64_t load_id(const void *ids, bool wide, int64_t t) {
@@ -103,14 +105,15 @@ struct EmbedGradArgs {
     int32_t wide;
     uint32_t own_rows, splits;  // rows of the table to an owner; CTAs of k_embed_split
     int32_t chunk;              // places of the list to a warp: at most kChunk, a power of two
-    uint32_t chunks, tiles, fill;  // chunks of the list, tiles of columns, warps' shares of the rows without tokens (0: they stay)
+    uint32_t chunks, tiles, fill;  // chunks of the list, tiles of columns, (32 rows, tile)s to look through for rows without tokens (0: they stay)
     // workspace
     int32_t *first;    // [kOwners * own_rows + 1]: where each row's run starts in the list, by packed()
     uint32_t *start;   // [kOwners + 1][splits]
     uint2 *part;       // [splits][1024]: (id, token)
     int32_t *order;    // [tokens]: the list: tokens by id
     int32_t *key;      // [tokens]: their ids
-    uint32_t *done;    // [chunks * tiles]: pieces done of the run that is cut first at a chunk's end
+    uint32_t *done;    // [chunks][3][tiles]: by the chunk where they start, pieces done of kJoin (of a run that came in, of one
+                       // that starts there), and such sums done of a run that starts there
     float *piece;      // [2 * chunks][width padded]: sums of pieces that start before a chunk, and in it
 };
 
@@ -197,7 +200,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const __grid_con
     uint32_t *mine = hist + warp * window;
     for (uint32_t i = threadIdx.x; i < kSortWarps * window; i += kSortThreads) hist[i] = 0;
     if constexpr (SPLIT) wait_launch_before();
-    for (uint32_t i = me * kSortThreads + threadIdx.x; i < A.chunks * A.tiles; i += kOwners * kSortThreads) A.done[i] = 0;
+    for (uint32_t i = me * kSortThreads + threadIdx.x; i < 3 * A.chunks * A.tiles; i += kOwners * kSortThreads) A.done[i] = 0;
     // a warp's run of tokens: parts [from, to) of k_embed_split, or 32 ids each
     const uint32_t pieces = SPLIT ? A.splits : uint32_t((A.tokens + 31) / 32), share = (pieces + kSortWarps - 1) / kSortWarps;
     const uint32_t from = warp * share < pieces ? warp * share : pieces, to = from + share < pieces ? from + share : pieces;
@@ -308,13 +311,18 @@ struct Cells {
 };
 template <bool F32>
 struct Cells<F32, false> {
-    float v[8];
+    uint32_t v[8];  // as they are in memory, so that no load is waited for before all are under way
     __device__ __forceinline__ void load(const void *p, int64_t row_at, int64_t c0, int64_t width) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (column<false>(c0, k) < width) v[k] = load1<F32>(p, row_at + column<false>(c0, k));
+        for (int k = 0; k < 8; ++k) {
+            const int64_t c = column<false>(c0, k), i = row_at + (c < width ? c : width - 1);  // past the last column: the last again
+            if constexpr (F32)
+                v[k] = static_cast<const uint32_t *>(p)[i];
+            else
+                v[k] = static_cast<const uint16_t *>(p)[i];
+        }
     }
-    __device__ __forceinline__ float at(int k) const { return v[k]; }
+    __device__ __forceinline__ float at(int k) const { return __uint_as_float(F32 ? v[k] : v[k] << 16); }
 };
 
 // Stores a row's 8 columns of a lane.
@@ -329,145 +337,237 @@ __device__ __forceinline__ void put_row(const EmbedGradArgs &A, int64_t row, int
     }
 }
 
-// A piece of a cut run [r0, r1) of `row`; the last piece done adds them all, in order.
-template <bool TF32, bool VEC>
-__device__ __forceinline__ void put_piece(const EmbedGradArgs &A, int row, int r0, int r1, uint32_t chunk, uint32_t tile, const float (&sum)[8]) {
+// A piece of a cut run [r0, r1). Of every kJoin pieces the last one done adds them up in order, and of those sums
+// the last one done again (two short chains of loads instead of a long one): then `sum` is the run's, and the answer true.
+__device__ __forceinline__ bool put_piece(const EmbedGradArgs &A, int r0, int r1, uint32_t chunk, uint32_t tile, float2 (&sum)[4]) {
     const int lane = threadIdx.x & 31;
     const int64_t pitch = int64_t(A.tiles) * kCols;
     const uint32_t first = uint32_t(r0 / A.chunk), last = uint32_t((r1 - 1) / A.chunk);
     auto place = [&](uint32_t c) { return reinterpret_cast<float4 *>(A.piece + (2 * int64_t(c) + (c == first)) * pitch + int64_t(tile) * kCols + 8 * lane); };
-    float4 *p = place(chunk);
-    __stcg(p, make_float4(sum[0], sum[1], sum[2], sum[3]));
-    __stcg(p + 1, make_float4(sum[4], sum[5], sum[6], sum[7]));
-    __threadfence();
-    __syncwarp();
-    uint32_t before = 0;
-    if (lane == 0) before = atomicAdd(A.done + int64_t(first) * A.tiles + tile, 1u);
-    before = __shfl_sync(kFullMask, before, 0);
-    if (before != last - first) return;
-    __threadfence();
-    float all[8] = {};
-    for (uint32_t c = first; c <= last; c += kJoin) {
-        float4 a[kJoin], b[kJoin];
+    uint32_t at = first + (chunk - first) / kJoin * kJoin, mine = chunk, step = 1, to = last + 1 - at < kJoin ? last + 1 : at + kJoin;
+#pragma unroll 1
+    for (int level = 0; level < 2; ++level) {  // pieces at, at + step, ... before `to`
+        float4 *p = place(mine);
+        __stcg(p, make_float4(sum[0].x, sum[0].y, sum[1].x, sum[1].y));
+        __stcg(p + 1, make_float4(sum[2].x, sum[2].y, sum[3].x, sum[3].y));
+        __threadfence();
+        __syncwarp();
+        uint32_t before = 0;
+        if (lane == 0) before = atomicAdd(A.done + (3 * int64_t(at) + (level ? 2 : at == first)) * A.tiles + tile, 1u);
+        before = __shfl_sync(kFullMask, before, 0);
+        __threadfence();
+        if (before + 1 != (to - at + step - 1) / step) return false;
 #pragma unroll
-        for (int j = 0; j < kJoin; ++j)
-            if (c + j <= last) a[j] = __ldcg(place(c + j)), b[j] = __ldcg(place(c + j) + 1);
+        for (int k = 0; k < 4; ++k) sum[k] = make_float2(0.f, 0.f);
+        for (uint32_t c = at; c < to; c += 4 * step) {
+            float4 a[4], b[4];
 #pragma unroll
-        for (int j = 0; j < kJoin; ++j)
-            if (c + j <= last) {
-                all[0] += a[j].x, all[1] += a[j].y, all[2] += a[j].z, all[3] += a[j].w;
-                all[4] += b[j].x, all[5] += b[j].y, all[6] += b[j].z, all[7] += b[j].w;
-            }
+            for (int j = 0; j < 4; ++j)
+                if (c + j * step < to) a[j] = __ldcg(place(c + j * step)), b[j] = __ldcg(place(c + j * step) + 1);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (c + j * step < to) {
+                    sum[0].x += a[j].x, sum[0].y += a[j].y, sum[1].x += a[j].z, sum[1].y += a[j].w;
+                    sum[2].x += b[j].x, sum[2].y += b[j].y, sum[3].x += b[j].z, sum[3].y += b[j].w;
+                }
+        }
+        mine = at;
+        at = first;
+        step = kJoin;
+        to = last + 1;
     }
-    Cells<TF32, VEC> base;
-    if (A.base) base.load(A.base, int64_t(row) * A.width, int64_t(tile) * kCols, A.width);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) all[k] = A.base ? fmaf(all[k], A.scale, base.at(k)) : all[k] * A.scale;
-    put_row<TF32, VEC>(A, row, int64_t(tile) * kCols, all);
+    return true;
 }
 
-// The first chunks x tiles warps add up the runs, the others write the rows without tokens. BASE: A.base is there.
-template <bool TF32, bool YF32, bool VEC, bool BASE>
-__global__ void __launch_bounds__(kThreads, 2) k_embed_grad(const __grid_constant__ EmbedGradArgs A) {
-    constexpr int kBatch = VEC && !YF32 && !BASE ? 8 : 4;  // rows of dy that are under way at a time
-    const int lane = threadIdx.x & 31;
-    const int64_t w = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5);
-    wait_launch_before();
-    if (w < int64_t(A.chunks) * A.tiles) {
-        const uint32_t chunk = uint32_t(w / A.tiles), tile = uint32_t(w - int64_t(chunk) * A.tiles);
-        const int64_t c0 = int64_t(tile) * kCols;
-        const int n = A.first[kOwners * A.own_rows], C = A.chunk;  // places in the list, in a chunk
-        if (int64_t(chunk) * C >= n) return;
-        const int s0 = int(chunk) * C, end = n - s0 < C ? n : s0 + C, s_mine = s0 + lane;
-        // a lane to a place of the chunk: its token and its run; `after`: the token C places on
-        const bool has = s_mine < end;
-        const int row = has ? A.key[s_mine] : 0, token = has ? A.order[s_mine] : 0, after = has && s_mine + C < n ? A.order[s_mine + C] : 0;
-        const uint32_t at = packed(A, uint32_t(row));
-        const int r0 = has ? A.first[at] : 0, r1 = has ? A.first[at + 1] : 0;
-        const bool cut = r1 - r0 > C;
-        const uint32_t whole = __ballot_sync(kFullMask, has && !cut && r0 >= s0);  // runs that start here and are not cut
-        const uint32_t ends = __ballot_sync(kFullMask, s_mine + 1 == r1);
-        auto token_at = [&](int i) { return int64_t(__shfl_sync(kFullMask, i < C ? token : after, i & (C - 1))); };
-        if (whole) {
-            const int tail = 31 - __clz(whole), stop = __shfl_sync(kFullMask, r1, tail);  // the last one is followed to its end
-            float sum[8] = {};
-            for (int s = s0 + __ffs(whole) - 1; s < stop; s += kBatch) {
-                Cells<YF32, VEC> v[kBatch];
-                Cells<TF32, VEC> base[BASE ? kBatch : 1];
+__device__ __forceinline__ void copy16(uint32_t dst, const char *src, uint32_t bytes) {  // the rest of the 16 as zeros
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+
+// One row's kCols columns in shared memory. VEC: as they lie; else from the 16-byte boundary before them on, so that rows
+// of any alignment come by 16-byte copies ([lo, hi) is the whole array: no byte outside of it is read).
+template <bool F32, bool VEC>
+struct Staged {
+    static constexpr int kElem = F32 ? 4 : 2, kBytes = kCols * kElem + (VEC ? 0 : 32);
+    // `bytes` of a row from `from` on
+    static __device__ __forceinline__ void fetch(uint32_t to, const char *from, int bytes, const char *lo, const char *hi) {
+        const int lane = threadIdx.x & 31;
+        if constexpr (VEC) {
 #pragma unroll
-                for (int b = 0; b < kBatch; ++b) {
-                    const int i = s + b - s0;
-                    const int64_t t = token_at(i);
-                    if (s + b < stop) v[b].load(A.dy, t * A.ld_dy, c0, A.width);
-                    if constexpr (BASE) {
-                        const int64_t r = __shfl_sync(kFullMask, row, i < tail ? i : tail);
-                        if (s + b + 1 == stop || (i < tail && (ends >> i & 1))) base[b].load(A.base, r * A.width, c0, A.width);
-                    }
-                }
-#pragma unroll
-                for (int b = 0; b < kBatch; ++b) {
-                    if (s + b < stop) {
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) sum[k] += v[b].at(k);
-                    }
-                    const int i = s + b - s0;
-                    const int r = __shfl_sync(kFullMask, row, i < tail ? i : tail);
-                    if (s + b + 1 == stop || (i < tail && (ends >> i & 1))) {
-                        float y[8];
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            y[k] = BASE ? fmaf(sum[k], A.scale, base[BASE ? b : 0].at(k)) : sum[k] * A.scale;
-                            sum[k] = 0.f;
+            for (int j = 0; j < kElem / 2; ++j)
+                if (16 * lane + 512 * j < bytes) copy16(to + 16 * lane + 512 * j, from + 16 * lane + 512 * j, 16);
+        } else {
+            const int off = int((uintptr_t)from & 15);
+            for (int j = 16 * lane; j < off + bytes; j += 512) {
+                const char *src = from - off + j;
+                if (src < lo) {  // the array's first bytes
+                    for (int i = 0; i < 16; i += kElem)
+                        if (src + i >= lo && src + i < hi) {
+                            if constexpr (F32)
+                                asm volatile("st.shared.u32 [%0], %1;" ::"r"(to + j + i), "r"(*reinterpret_cast<const uint32_t *>(src + i)) : "memory");
+                            else
+                                asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + j + i), "h"(*reinterpret_cast<const uint16_t *>(src + i)) : "memory");
                         }
-                        put_row<TF32, VEC>(A, r, c0, y);
-                    }
+                } else {
+                    copy16(to + j, src, hi - src < 16 ? uint32_t(hi - src) : 16u);
                 }
             }
         }
-        // pieces of cut runs: of one that comes in (or fills the chunk), of one that goes on
-#pragma unroll 1
-        for (int which = 0; which < 2; ++which) {
-            const int at = which ? end - 1 - s0 : 0;
-            const int a0 = __shfl_sync(kFullMask, r0, at), a1 = __shfl_sync(kFullMask, r1, at), r = __shfl_sync(kFullMask, row, at);
-            if (a1 - a0 <= C || (a0 >= s0) != bool(which)) continue;
-            const int from = which ? a0 : s0, to = a1 < end ? a1 : end;
-            float sum[8] = {};
-            for (int s = from; s < to; s += kBatch) {
-                Cells<YF32, VEC> v[kBatch];
+    }
+    // this lane's 8 columns of a row that was fetched to `at`, as they lie; `from`: the low bits of where the row lies
+    uint32_t raw[VEC ? 2 * kElem : 8];
+    __device__ __forceinline__ void read(const char *at, uint32_t from) {
+        const int lane = threadIdx.x & 31;
+        if constexpr (VEC) {
 #pragma unroll
-                for (int b = 0; b < kBatch; ++b) {
-                    const int64_t t = token_at(s + b - s0);
-                    if (s + b < to) v[b].load(A.dy, t * A.ld_dy, c0, A.width);
-                }
-#pragma unroll
-                for (int b = 0; b < kBatch; ++b)
-                    if (s + b < to)
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) sum[k] += v[b].at(k);
+            for (int j = 0; j < kElem / 2; ++j) {
+                const uint4 u = *reinterpret_cast<const uint4 *>(at + 8 * kElem * lane + 16 * j);
+                raw[4 * j] = u.x, raw[4 * j + 1] = u.y, raw[4 * j + 2] = u.z, raw[4 * j + 3] = u.w;
             }
-            put_piece<TF32, VEC>(A, r, a0, a1, chunk, tile, sum);
+        } else {
+            at += from & 15;
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if constexpr (F32)
+                    raw[k] = reinterpret_cast<const uint32_t *>(at)[32 * k + lane];
+                else
+                    raw[k] = reinterpret_cast<const uint16_t *>(at)[32 * k + lane];
         }
-    } else {
-        const int64_t f = w - int64_t(A.chunks) * A.tiles, v0 = f * kFill, left = A.rows - v0;
-        if (f >= A.fill) return;
-        const uint32_t at = lane < kFill && lane < left ? packed(A, uint32_t(v0 + lane)) : 0;
-        const uint32_t empty = __ballot_sync(kFullMask, lane < kFill && lane < left && A.first[at] == A.first[at + 1]);
-        for (uint32_t tile = 0; tile < A.tiles; ++tile) {
-            const int64_t c0 = int64_t(tile) * kCols;
-            Cells<TF32, VEC> base[BASE ? kFill : 1];
+    }
+    __device__ __forceinline__ float2 pair(int k) const {  // columns 2 k and 2 k + 1 of the 8
+        if constexpr (F32)
+            return make_float2(__uint_as_float(raw[2 * k]), __uint_as_float(raw[2 * k + 1]));
+        else if constexpr (VEC)
+            return make_float2(bf16_low(raw[k]), bf16_high(raw[k]));
+        else
+            return make_float2(bf16_low(raw[2 * k]), bf16_low(raw[2 * k + 1]));
+    }
+};
+
+// A warp to (chunk, tile of columns): it has the chunk's rows of dy copied to shared memory, kRound at a time, writes its
+// share of the rows without tokens while they come, and adds up the runs. Warps past the last chunk only do the latter.
+// BASE: A.base is there; the rows of it that the round's runs need come by copies of their own.
+template <bool TF32, bool YF32, bool VEC, bool BASE>
+__global__ void __launch_bounds__(kGradThreads, 5) k_embed_grad(const __grid_constant__ EmbedGradArgs A) {
+    using Y = Staged<YF32, VEC>;
+    using T = Staged<TF32, VEC>;
+    constexpr int kSlot = Y::kBytes + (BASE ? T::kBytes : 0), kRound = kRing / kSlot / 2;  // rows of a round: two rounds at a time are under way or in use
+    static_assert(kRound >= 1, "two rounds fit the warp's shared memory");
+    extern __shared__ __align__(16) char ring_all[];
+    const char *ring = ring_all + (threadIdx.x >> 5) * kRing;
+    const uint32_t ring_at = uint32_t(__cvta_generic_to_shared(ring));
+    const int lane = threadIdx.x & 31;
+    const uint32_t w = blockIdx.x * (kGradThreads / 32) + (threadIdx.x >> 5);
+    wait_launch_before();
+    const uint32_t chunk = w / A.tiles, tile = w - chunk * A.tiles;
+    const int64_t c0 = int64_t(tile) * kCols;
+    const int cols = A.width - c0 < kCols ? int(A.width - c0) : kCols;
+    const int n = chunk < A.chunks ? A.first[kOwners * A.own_rows] : 0, C = A.chunk;  // places in the list, in a chunk
+    const bool some = chunk < A.chunks && int64_t(chunk) * C < n;
+    const int s0 = some ? int(chunk) * C : 0, end = !some ? 0 : n - s0 < C ? n : s0 + C, s_mine = s0 + lane;
+    const char *dy = static_cast<const char *>(A.dy), *dy_end = dy + ((A.tokens - 1) * A.ld_dy + A.width) * Y::kElem;
+    const char *base = static_cast<const char *>(A.base), *base_end = base + A.rows * A.width * T::kElem;
+    // a lane to a place of the chunk: its run, and where its row of dy lies; `after`: the row of C places on
+    const bool has = s_mine < end;
+    const int row = has ? A.key[s_mine] : 0;
+    const uint64_t mine = reinterpret_cast<uint64_t>(dy + ((has ? A.order[s_mine] : 0) * A.ld_dy + c0) * Y::kElem);
+    const uint64_t after = reinterpret_cast<uint64_t>(dy + ((has && s_mine + C < n ? A.order[s_mine + C] : 0) * A.ld_dy + c0) * Y::kElem);
+    const uint32_t run = packed(A, uint32_t(row));
+    const int r0 = has ? A.first[run] : 0, r1 = has ? A.first[run + 1] : 0;
+    const bool cut = r1 - r0 > C;
+    const uint32_t own = __ballot_sync(kFullMask, has && (cut || r0 >= s0));  // others: a run of the chunk before
+    const uint32_t ends = __ballot_sync(kFullMask, has && (s_mine + 1 == r1 || (cut && s_mine + 1 == end)));
+    const int tail = some ? end - 1 - s0 : 0;  // a run that starts here and is not cut is followed to its end
+    const int stop = own ? __shfl_sync(kFullMask, cut ? end : r1, tail) : 0, go = own ? s0 + __ffs(own) - 1 : 0;
+    auto in_round = [&](int s) { return stop - s < kRound ? stop - s : kRound; };
+    auto ends_from = [&](int s) {  // bit i: a run, or a piece of one, ends at place s + i
+        const uint32_t m = s - s0 < 32 ? ends >> (s - s0) : 0;
+        return stop > s && stop - s <= 32 ? m | 1u << (stop - 1 - s) : m;
+    };
+    auto place_row = [&](int i) { return __shfl_sync(kFullMask, row, i < tail ? i : tail); };
+    auto fetch = [&](int s, int half) {  // (nothing past `stop`)
+        const uint32_t to = ring_at + half * (kRound * kSlot);
+        const int count = in_round(s);
+        const uint32_t done = ends_from(s);
+#pragma unroll 4
+        for (int i = 0; i < count; ++i) {
+            const int q = s - s0 + i;
+            Y::fetch(to + i * kSlot, reinterpret_cast<const char *>(__shfl_sync(kFullMask, q < C ? mine : after, q & (C - 1))), cols * Y::kElem, dy, dy_end);
             if constexpr (BASE)
+                if (done >> i & 1)
+                    T::fetch(to + i * kSlot + Y::kBytes, base + (int64_t(place_row(q)) * A.width + c0) * T::kElem, cols * T::kElem, base, base_end);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    fetch(go, 0);
+    fetch(go + kRound, 1);
+    for (uint32_t f = w; f < A.fill; f += gridDim.x * (kGradThreads / 32)) {  // 32 rows, one tile of columns
+        const uint32_t v0 = f / A.tiles * 32;
+        const int64_t fc = int64_t(f - f / A.tiles * A.tiles) * kCols;
+        const uint32_t p = packed(A, v0 + lane < A.rows ? v0 + lane : 0);
+        uint32_t empty = __ballot_sync(kFullMask, v0 + lane < A.rows && A.first[p] == A.first[p + 1]);
+        while (empty) {
+            uint32_t which[4], there[4];
+            Cells<TF32, VEC> b[BASE ? 4 : 1];
 #pragma unroll
-                for (int i = 0; i < kFill; ++i)
-                    if (empty >> i & 1) base[i].load(A.base, (v0 + i) * A.width, c0, A.width);
+            for (int i = 0; i < 4; ++i) {
+                there[i] = empty;
+                which[i] = v0 + __ffs(empty) - 1;
+                empty &= empty - 1;
+                if (BASE && there[i]) b[BASE ? i : 0].load(A.base, which[i] * A.width, fc, A.width);
+            }
 #pragma unroll
-            for (int i = 0; i < kFill; ++i)
-                if (empty >> i & 1) {
+            for (int i = 0; i < 4; ++i)
+                if (there[i]) {
                     float y[8];
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) y[k] = BASE ? base[BASE ? i : 0].at(k) : 0.f;
-                    put_row<TF32, VEC>(A, v0 + i, c0, y);
+                    for (int k = 0; k < 8; ++k) y[k] = BASE ? b[BASE ? i : 0].at(k) : 0.f;
+                    put_row<TF32, VEC>(A, which[i], fc, y);
                 }
         }
+    }
+    if (!own) return;
+    float2 sum[4] = {};
+    int half = 0;
+    for (int s = go; s < stop; s += kRound, half ^= 1) {
+        const char *at = ring + half * (kRound * kSlot);
+        const int count = in_round(s);
+        const uint32_t done = ends_from(s);
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+        __syncwarp();
+        constexpr int kRead = VEC && !YF32 ? 4 : 2;
+        for (int i0 = 0; i0 < count; i0 += kRead) {
+            Y y[kRead];
+#pragma unroll
+            for (int j = 0; j < kRead; ++j) {
+                const int q = s - s0 + i0 + j;
+                const uint32_t from = VEC ? 0u : __shfl_sync(kFullMask, uint32_t(q < C ? mine : after), q & (C - 1));
+                if (i0 + j < kRound) y[j].read(at + (i0 + j) * kSlot, from);
+            }
+#pragma unroll
+            for (int j = 0; j < kRead; ++j) {
+                if (i0 + j >= count) break;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) sum[k] = __fadd2_rn(sum[k], y[j].pair(k));
+                if (!(done >> (i0 + j) & 1)) continue;
+                const int q = s - s0 + i0 + j, from = q < tail ? q : tail;
+                const int r = place_row(q), a0 = __shfl_sync(kFullMask, r0, from), a1 = __shfl_sync(kFullMask, r1, from);
+                if (a1 - a0 <= C || put_piece(A, a0, a1, chunk, tile, sum)) {
+                    float out[8];
+                    T b;
+                    if constexpr (BASE) b.read(at + (i0 + j) * kSlot + Y::kBytes, uint32_t(reinterpret_cast<uint64_t>(base + (int64_t(r) * A.width + c0) * T::kElem)));
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        out[2 * k] = BASE ? fmaf(sum[k].x, A.scale, b.pair(k).x) : sum[k].x * A.scale;
+                        out[2 * k + 1] = BASE ? fmaf(sum[k].y, A.scale, b.pair(k).y) : sum[k].y * A.scale;
+                    }
+                    put_row<TF32, VEC>(A, r, c0, out);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) sum[k] = make_float2(0.f, 0.f);
+            }
+        }
+        __syncwarp();
+        fetch(s + 2 * kRound, half);
     }
 }
 
@@ -516,7 +616,7 @@ Layout layout(const skew_embed_config_t *c, int64_t tokens) {
     L.part = take(size_t(L.splits) * kSortThreads * 8);
     L.order = take(size_t(tokens) * 4);
     L.key = take(size_t(tokens) * 4);
-    L.done = take(size_t(L.chunks) * L.tiles * 4);
+    L.done = take(size_t(L.chunks) * L.tiles * 12);
     L.piece = take(size_t(L.chunks) * 2 * L.tiles * kCols * 4);
     L.bytes = at;
     return L;
@@ -543,10 +643,15 @@ cudaError_t launch_sort(const EmbedGradArgs &A, cudaStream_t s) {
 
 template <bool TF32, bool YF32>
 cudaError_t launch_grad(const EmbedGradArgs &A, bool vec, cudaStream_t s) {
-    const int64_t warps = int64_t(A.chunks) * A.tiles + A.fill;
-    const uint32_t grid = uint32_t((warps + kWarps - 1) / kWarps);
-    if (!grid) return cudaSuccess;
-    auto go = [&](auto k) { return ops_launch(true, k, grid, kThreads, 0, s, A); };
+    // warps of their own for the rows without tokens where there are few chunks
+    uint32_t warps = A.fill < kFillWarps ? A.fill : kFillWarps;
+    if (warps < A.chunks * A.tiles) warps = A.chunks * A.tiles;
+    if (!warps) return cudaSuccess;
+    auto go = [&](auto k) {
+        constexpr int kSmem = kGradThreads / 32 * kRing;
+        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        return e != cudaSuccess ? e : ops_launch(true, k, (warps + kGradThreads / 32 - 1) / (kGradThreads / 32), kGradThreads, kSmem, s, A);
+    };
     return vec ? (A.base ? go(k_embed_grad<TF32, YF32, true, true>) : go(k_embed_grad<TF32, YF32, true, false>))
                : (A.base ? go(k_embed_grad<TF32, YF32, false, true>) : go(k_embed_grad<TF32, YF32, false, false>));
 }
@@ -592,9 +697,8 @@ int skew_embed_grad(const skew_embed_config_t *c, const void *ids, int64_t token
     const Layout L = layout(c, tokens);
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < L.bytes)
         return ops_fail(SKEW_EINVAL, "workspace must be 256-byte aligned and at least %zu bytes", L.bytes);
-    const int64_t fill = base == dtable ? 0 : (c->rows + kFill - 1) / kFill;
-    if (int64_t(L.chunks) * L.tiles + fill > int64_t(INT32_MAX) * kWarps || int64_t(L.chunks) * L.tiles > INT32_MAX)
-        return ops_fail(SKEW_EINVAL, "too many tokens for this width");
+    const int64_t fill = base == dtable ? 0 : (c->rows + 31) / 32 * L.tiles;
+    if (fill > INT32_MAX || int64_t(L.chunks) * L.tiles > INT32_MAX / 3) return ops_fail(SKEW_EINVAL, "too many rows or tokens for this width");
     EmbedGradArgs A{};
     char *ws = (char *)workspace;
     A.ids = ids;

@@ -19,9 +19,10 @@ namespace {
 constexpr int kThreads = 256;
 constexpr uint32_t kMaxCtas = 8192;   // partial sums that the workspace has room for
 constexpr int kBatch = 4;             // 8-element units a thread loads before it uses them
-// Bytes of gradient in a tile. Small ones spread a small set over the SMs.
-constexpr int64_t kTileBytes = 65536, kSmallTileBytes = 16384;
-constexpr int64_t kSmallSet = int64_t(152) * 4 * kTileBytes;
+// Bytes of gradient in a tile: smaller ones where tiles are few for the SMs, larger ones where reading the table tells
+// (16 and 32 KiB, us: norm of 13.6 GB 1854 1810, norm and clipping of 1.07 GB of fp32 399 410).
+constexpr int64_t kTileBytes = 16384, kLargeTileBytes = 32768, kLargeSet = int64_t(2) << 30;
+constexpr int64_t kKeepBytes = 64 << 20;
 
 enum : uint32_t { kGradF32 = SKEW_CLIP_GRAD_FP32, kOutF32 = SKEW_CLIP_OUT_FP32, kVectors = 4u, kNoVectors = 8u };
 
@@ -37,7 +38,7 @@ struct ClipArgs {
     double *part;
     uint32_t *ticket;
     float *result;
-    uint32_t n_tiles;
+    uint32_t n_tiles, keep;  // tiles from `keep` on are to stay in L2
     float max_norm;
 };
 
@@ -47,28 +48,51 @@ struct ClipArgs {
 constexpr float kSumLow = 0x1p-100f, kSumHigh = 0x1p100f;
 constexpr float kScaleUp = 0x1p100f, kScaleDown = 0x1p-80f;
 
+// Eight elements, with an L2 eviction policy.
+template <bool F32>
+__device__ __forceinline__ Vec8<F32> load8_policy(const void *p, int64_t i, uint64_t policy) {
+    Vec8<F32> v;
+#pragma unroll
+    for (int q = 0; q < (F32 ? 2 : 1); ++q)
+        asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v4.u32 {%0,%1,%2,%3}, [%4], %5;"
+                     : "=r"(v.u[q].x), "=r"(v.u[q].y), "=r"(v.u[q].z), "=r"(v.u[q].w)
+                     : "l"(elem_ptr<F32>(p, i) + 16 * q), "l"(policy));
+    return v;
+}
+
+__device__ __forceinline__ uint64_t evict_last() {
+    uint64_t p;
+    asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(p));
+    return p;
+}
+__device__ __forceinline__ uint64_t evict_first() {
+    uint64_t p;
+    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+    return p;
+}
+
 template <bool F32, class F>
-__device__ __forceinline__ void each_unit(const ClipTile &t, F &&f) {  // f(8 elements) for the thread's units
+__device__ __forceinline__ void each_unit(const ClipTile &t, uint64_t policy, F &&f) {  // f(8 elements) for the thread's units
     const uint32_t units = t.n >> 3;
     uint32_t u = threadIdx.x;
     for (; u + (kBatch - 1) * kThreads < units; u += kBatch * kThreads) {
         Vec8<F32> v[kBatch];
 #pragma unroll
-        for (int b = 0; b < kBatch; ++b) v[b] = load8<F32>(t.g, int64_t(u + b * kThreads) * 8);
+        for (int b = 0; b < kBatch; ++b) v[b] = load8_policy<F32>(t.g, int64_t(u + b * kThreads) * 8, policy);
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) f(v[b]);
     }
-    for (; u < units; u += kThreads) f(load8<F32>(t.g, int64_t(u) * 8));
+    for (; u < units; u += kThreads) f(load8_policy<F32>(t.g, int64_t(u) * 8, policy));
 }
 
 // Sum of (scale x)^2 over the thread's elements of a tile; `any`: the OR of their magnitudes' bits.
 template <bool F32, bool SCALED>
-__device__ __forceinline__ float tile_squares(const ClipTile &t, float scale, uint32_t &any) {
+__device__ __forceinline__ float tile_squares(const ClipTile &t, uint64_t policy, float scale, uint32_t &any) {
     float s0 = 0.f, s1 = 0.f;
     any = 0;
     uint32_t left = threadIdx.x;  // elements one at a time: what 8 does not divide, or all
     if (!(t.flags & kNoVectors)) {
-        each_unit<F32>(t, [&](const Vec8<F32> &v) {
+        each_unit<F32>(t, policy, [&](const Vec8<F32> &v) {
 #pragma unroll
             for (int q = 0; q < (F32 ? 2 : 1); ++q) any |= v.u[q].x | v.u[q].y | v.u[q].z | v.u[q].w;
 #pragma unroll
@@ -94,9 +118,9 @@ struct Squares {
     float hi = 0.f, lo = 0.f;
     double rest = 0.0;
     template <bool F32>
-    __device__ __forceinline__ void add(const ClipTile &t) {
+    __device__ __forceinline__ void add(const ClipTile &t, uint64_t policy) {
         uint32_t any, unused;
-        const float s = tile_squares<F32, false>(t, 1.f, any);
+        const float s = tile_squares<F32, false>(t, policy, 1.f, any);
         if (s >= kSumLow && s <= kSumHigh) {
             const float sum = hi + s, back = sum - hi;
             lo += (hi - (sum - back)) + (s - back);
@@ -104,7 +128,7 @@ struct Squares {
         } else if (any) {
             const float scale = s < kSumLow ? kScaleUp : kScaleDown;  // a NaN stays one either way
             const double r = 1.0 / double(scale);
-            rest += double(tile_squares<F32, true>(t, scale, unused)) * r * r;
+            rest += double(tile_squares<F32, true>(t, policy, scale, unused)) * r * r;
         }
     }
 };
@@ -124,12 +148,14 @@ __device__ __forceinline__ double cta_sum(double x) {  // the sum, in thread 0
 // Norm and factor. The CTAs' sums are joined by whichever ends last, in the order of the CTAs.
 __global__ void __launch_bounds__(kThreads) k_clip_norm(const __grid_constant__ ClipArgs A) {
     Squares sq;
+    const uint64_t keep = evict_last(), drop = evict_first();
     for (uint32_t k = blockIdx.x; k < A.n_tiles; k += gridDim.x) {
         const ClipTile t = A.tiles[k];
+        const uint64_t policy = k >= A.keep ? keep : drop;
         if (t.flags & kGradF32)
-            sq.add<true>(t);
+            sq.add<true>(t, policy);
         else
-            sq.add<false>(t);
+            sq.add<false>(t, policy);
     }
     const double mine = cta_sum(double(sq.hi) + double(sq.lo) + sq.rest);
     __shared__ bool last;
@@ -152,24 +178,26 @@ __global__ void __launch_bounds__(kThreads) k_clip_norm(const __grid_constant__ 
 }
 
 template <bool GF32, bool OF32>
-__device__ __forceinline__ void scale_tile(const ClipTile &t, float gamma) {
+__device__ __forceinline__ void scale_tile(const ClipTile &t, uint64_t policy, float gamma) {
+    constexpr int kUnits = GF32 ? kBatch / 2 : kBatch;  // under way at a time
     uint32_t left = threadIdx.x;
     if (t.flags & kVectors) {
+        auto scale = [&](uint32_t u, const Vec8<GF32> &v) {
+            float x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = v.at(k) * gamma;
+            store8<OF32>(t.out, int64_t(u) * 8, x);
+        };
         const uint32_t units = t.n >> 3;
-        for (uint32_t u = threadIdx.x; u < units; u += kBatch * kThreads) {
-            Vec8<GF32> v[kBatch];
+        uint32_t u = threadIdx.x;
+        for (; u + (kUnits - 1) * kThreads < units; u += kUnits * kThreads) {
+            Vec8<GF32> v[kUnits];
 #pragma unroll
-            for (int b = 0; b < kBatch; ++b)
-                if (u + b * kThreads < units) v[b] = load8<GF32>(t.g, int64_t(u + b * kThreads) * 8);
+            for (int b = 0; b < kUnits; ++b) v[b] = load8_policy<GF32>(t.g, int64_t(u + b * kThreads) * 8, policy);
 #pragma unroll
-            for (int b = 0; b < kBatch; ++b)
-                if (u + b * kThreads < units) {
-                    float x[8];
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) x[k] = v[b].at(k) * gamma;
-                    store8<OF32>(t.out, int64_t(u + b * kThreads) * 8, x);
-                }
+            for (int b = 0; b < kUnits; ++b) scale(u + b * kThreads, v[b]);
         }
+        for (; u < units; u += kThreads) scale(u, load8_policy<GF32>(t.g, int64_t(u) * 8, policy));
         left += t.n & ~7u;
     }
     for (uint32_t i = left; i < t.n; i += kThreads) store1<OF32>(t.out, i, load1<GF32>(t.g, i) * gamma);
@@ -178,15 +206,16 @@ __device__ __forceinline__ void scale_tile(const ClipTile &t, float gamma) {
 __global__ void __launch_bounds__(kThreads, 4) k_clip_apply(const __grid_constant__ ClipArgs A) {
     wait_launch_before();
     const float gamma = __ldcg(A.result + 1);
+    const uint64_t drop = evict_first();
     for (uint32_t k = blockIdx.x; k < A.n_tiles; k += gridDim.x) {
         const ClipTile t = A.tiles[A.n_tiles - 1 - k];
         if (t.g == t.out && gamma == 1.f) continue;
         if (!(t.flags & kGradF32))
-            scale_tile<false, false>(t, gamma);
+            scale_tile<false, false>(t, drop, gamma);
         else if (t.flags & kOutF32)
-            scale_tile<true, true>(t, gamma);
+            scale_tile<true, true>(t, drop, gamma);
         else
-            scale_tile<true, false>(t, gamma);
+            scale_tile<true, false>(t, drop, gamma);
     }
 }
 
@@ -198,6 +227,7 @@ using namespace skew;
 struct skew_clip {
     std::vector<ClipTile> tiles;
     bool writes = true;  // every tensor has an `out`
+    uint32_t keep = 0;   // the first of the tiles that skew_clip_apply finds in L2
     size_t ws_ticket = 0, ws_tiles = 0, ws_bytes = 0;
     char *ws = nullptr;
     bool bound = false;
@@ -229,8 +259,9 @@ int skew_clip_create(const skew_clip_desc_t *tensors, int32_t n, skew_clip_t **o
     skew_clip *h = new (std::nothrow) skew_clip();
     if (!h) return ops_fail(SKEW_ENOMEM, "out of host memory");
     h->writes = writes;
-    const int64_t tile_bytes = total < kSmallSet ? kSmallTileBytes : kTileBytes;
+    const int64_t tile_bytes = total < kLargeSet ? kTileBytes : kLargeTileBytes;
     try {
+        h->tiles.reserve(size_t(total / tile_bytes + 2 * int64_t(n)));
         for (int32_t k = 0; k < n; ++k) {
             const skew_clip_desc_t &d = tensors[k];
             const int64_t ge = d.flags & SKEW_CLIP_GRAD_FP32 ? 4 : 2, oe = d.flags & SKEW_CLIP_OUT_FP32 ? 4 : 2;
@@ -256,6 +287,12 @@ int skew_clip_create(const skew_clip_desc_t *tensors, int32_t n, skew_clip_t **o
     } catch (...) {
         delete h;
         return ops_fail(SKEW_ENOMEM, "out of host memory");
+    }
+    h->keep = (uint32_t)h->tiles.size();
+    for (int64_t bytes = 0; h->keep > 0; --h->keep) {
+        const ClipTile &t = h->tiles[h->keep - 1];
+        bytes += int64_t(t.n) * (t.flags & kGradF32 ? 4 : 2);
+        if (bytes > kKeepBytes) break;
     }
     h->ws_ticket = kMaxCtas * sizeof(double);
     h->ws_tiles = h->ws_ticket + 256;
@@ -310,6 +347,7 @@ static int clip_args(skew_clip_t *h, float max_norm, float *result, ClipArgs &A)
     A.ticket = reinterpret_cast<uint32_t *>(h->ws + h->ws_ticket);
     A.result = result;
     A.n_tiles = (uint32_t)h->tiles.size();
+    A.keep = A.n_tiles;
     A.max_norm = max_norm;
     return SKEW_OK;
 }
@@ -324,6 +362,7 @@ int skew_clip_apply(skew_clip_t *h, float max_norm, float *result, void *stream)
     ClipArgs A{};
     if (const int rc = clip_args(h, max_norm, result, A)) return rc;
     if (!h->writes) return ops_fail(SKEW_ESTATE, "the handle was planned without `out`");
+    A.keep = h->keep;
     int rc = ops_cuda(ops_launch(false, k_clip_norm, h->norm_ctas, kThreads, 0, (cudaStream_t)stream, A), "k_clip_norm");
     if (rc || !A.n_tiles) return rc;
     return ops_cuda(ops_launch(true, k_clip_apply, h->apply_ctas, kThreads, 0, (cudaStream_t)stream, A), "k_clip_apply");

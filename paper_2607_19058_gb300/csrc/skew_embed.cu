@@ -28,7 +28,7 @@ constexpr uint32_t kFillWarps = 152 * 48;
 constexpr int kGradThreads = 128;
 constexpr int kRing = 16 * (kCols * 2 + 32);  // bytes of shared memory that a warp has rows copied to
 constexpr uint32_t kJoin = 16;   // pieces that one warp adds up
-constexpr int kLookups = 8;      // most tokens to a warp of the lookup
+constexpr int kLookups = 4;      // most tokens to a warp of the lookup
 
 __device__ __forceinline__ int64_t load_id(const void *ids, bool wide, int64_t t) {
     return wide ? static_cast<const int64_t *>(ids)[t] : static_cast<const int32_t *>(ids)[t];
@@ -50,7 +50,7 @@ struct LookupArgs {
 // A warp to `per` tokens and kCols columns: all rows are under way before the first is stored. VEC: rows of both
 // sides start on 16-byte boundaries.
 template <bool TF32, bool YF32, bool VEC>
-__global__ void __launch_bounds__(kThreads) k_lookup(const __grid_constant__ LookupArgs A) {
+__global__ void __launch_bounds__(kThreads, TF32 ? 5 : 8) k_lookup(const __grid_constant__ LookupArgs A) {
     const int lane = threadIdx.x & 31;
     const int64_t w = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5);
     const int64_t t0 = w / A.tiles * A.per, c0 = (w - w / A.tiles * A.tiles) * kCols;

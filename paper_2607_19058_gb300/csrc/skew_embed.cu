@@ -629,31 +629,37 @@ cudaError_t launch_lookup(const LookupArgs &A, bool vec, cudaStream_t s) {
     return vec ? ops_launch(false, k_lookup<TF32, YF32, true>, grid, kThreads, 0, s, A) : ops_launch(false, k_lookup<TF32, YF32, false>, grid, kThreads, 0, s, A);
 }
 
-template <bool WIDE>
-cudaError_t launch_sort(const EmbedGradArgs &A, cudaStream_t s) {
-    cudaError_t e = cudaSuccess;
-    auto sort = [&](bool after, auto k) {
-        e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortWarps * (int)kSortRows * 4);
-        return e != cudaSuccess ? e : ops_launch(after, k, kOwners, kSortThreads, size_t(kSortWarps) * (A.own_rows < kSortRows ? A.own_rows : kSortRows) * 4, s, A);
-    };
-    if (!A.splits) return sort(false, k_embed_sort<WIDE, false>);
-    e = ops_launch(false, k_embed_split<WIDE>, A.splits, kSortThreads, 0, s, A);
-    return e != cudaSuccess ? e : sort(true, k_embed_sort<false, true>);
+template <bool WIDE, bool SPLIT>
+cudaError_t launch_sort_of(const EmbedGradArgs &A, cudaStream_t s) {
+    constexpr auto k = k_embed_sort<WIDE, SPLIT>;
+    const cudaError_t e = ops_allow_smem<k>(kSortWarps * (int)kSortRows * 4);
+    if (e != cudaSuccess) return e;
+    return ops_launch(SPLIT, k, kOwners, kSortThreads, size_t(kSortWarps) * (A.own_rows < kSortRows ? A.own_rows : kSortRows) * 4, s, A);
 }
 
-template <bool TF32, bool YF32>
-cudaError_t launch_grad(const EmbedGradArgs &A, bool vec, cudaStream_t s) {
+template <bool WIDE>
+cudaError_t launch_sort(const EmbedGradArgs &A, cudaStream_t s) {
+    if (!A.splits) return launch_sort_of<WIDE, false>(A, s);
+    const cudaError_t e = ops_launch(false, k_embed_split<WIDE>, A.splits, kSortThreads, 0, s, A);
+    return e != cudaSuccess ? e : launch_sort_of<false, true>(A, s);
+}
+
+template <bool TF32, bool YF32, bool VEC, bool BASE>
+cudaError_t launch_grad_of(const EmbedGradArgs &A, cudaStream_t s) {
+    constexpr auto k = k_embed_grad<TF32, YF32, VEC, BASE>;
+    constexpr int kSmem = kGradThreads / 32 * kRing;
     // warps of their own for the rows without tokens where there are few chunks
     uint32_t warps = A.fill < kFillWarps ? A.fill : kFillWarps;
     if (warps < A.chunks * A.tiles) warps = A.chunks * A.tiles;
     if (!warps) return cudaSuccess;
-    auto go = [&](auto k) {
-        constexpr int kSmem = kGradThreads / 32 * kRing;
-        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-        return e != cudaSuccess ? e : ops_launch(true, k, (warps + kGradThreads / 32 - 1) / (kGradThreads / 32), kGradThreads, kSmem, s, A);
-    };
-    return vec ? (A.base ? go(k_embed_grad<TF32, YF32, true, true>) : go(k_embed_grad<TF32, YF32, true, false>))
-               : (A.base ? go(k_embed_grad<TF32, YF32, false, true>) : go(k_embed_grad<TF32, YF32, false, false>));
+    const cudaError_t e = ops_allow_smem<k>(kSmem);
+    return e != cudaSuccess ? e : ops_launch(true, k, (warps + kGradThreads / 32 - 1) / (kGradThreads / 32), kGradThreads, kSmem, s, A);
+}
+
+template <bool TF32, bool YF32>
+cudaError_t launch_grad(const EmbedGradArgs &A, bool vec, cudaStream_t s) {
+    return vec ? (A.base ? launch_grad_of<TF32, YF32, true, true>(A, s) : launch_grad_of<TF32, YF32, true, false>(A, s))
+               : (A.base ? launch_grad_of<TF32, YF32, false, true>(A, s) : launch_grad_of<TF32, YF32, false, false>(A, s));
 }
 
 }  // namespace

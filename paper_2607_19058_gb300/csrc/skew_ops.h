@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "skewadam.h"
 
 namespace skew {
@@ -20,6 +22,21 @@ inline int ops_cuda(cudaError_t e, const char *what) {
 }
 
 #ifdef __CUDACC__
+
+// Lets `k` have up to `bytes` of dynamic shared memory on the current device: asked once for a kernel and device
+// (0.5 us a call otherwise).
+template <auto k>
+cudaError_t ops_allow_smem(int bytes) {
+    static std::atomic<uint64_t> allowed{0};  // by device
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+    if (allowed.load(std::memory_order_acquire) & bit) return cudaSuccess;
+    e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) allowed.fetch_or(bit, std::memory_order_release);
+    return e;
+}
 
 // `after`: a programmatic dependent of the launch before it (it starts up while that one ends; the kernel
 // orders itself by wait_launch_before).

@@ -381,15 +381,42 @@ def hparams(beta1=0.9, beta2=0.999, eps=1e-8, clip_d=1.0, weight_decay=0.05, pol
 # --------------------------------------------------------------------------
 # torch convenience wrappers
 # --------------------------------------------------------------------------
-def _stream_of(stream, device=None) -> int:
-    """The raw handle of a stream, or of the current one of a tensor's device."""
+def _stream_of(stream, device) -> int:
+    """The raw handle of a stream; None: of the current one of a tensor's device."""
     if stream is None:
-        import torch
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # 0.1 us; the public call takes 2 to 3
-        if raw is not None and device is not None and device.index is not None:
-            return raw(device.index)
-        return torch.cuda.current_stream(device).cuda_stream
+        return _raw_stream()(device.index)
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+_current = None
+
+
+def _raw_stream():
+    """A function from a device's index to the raw handle of its current stream."""
+    global _current
+    if _current is None:
+        import torch
+        _current = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # 0.1 us; the public call takes 2 to 3
+        if _current is None:
+            _current = lambda index: torch.cuda.current_stream(index).cuda_stream  # noqa: E731
+    return _current
+
+
+_fresh = None
+
+
+def _allocator():
+    """A function (shape, strides, dtype, device) -> a new tensor. Beside a kernel launch torch.empty costs 2.6 us a
+    tensor, most of these operators' time on small inputs; the call behind compiled torch programs costs 1.2, for the current device."""
+    global _fresh
+    if _fresh is None:
+        import torch
+        quick = getattr(getattr(getattr(torch._C, "_dynamo", None), "guards", None), "_empty_strided_cuda", None)
+        if quick is not None and torch.cuda.device_count() == 1:
+            _fresh = lambda shape, strides, dtype, device: quick(shape, strides, dtype)  # noqa: E731
+        else:
+            _fresh = lambda shape, strides, dtype, device: torch.empty_strided(shape, strides, dtype=dtype, device=device)  # noqa: E731
+    return _fresh
 
 
 class GradClip:
@@ -431,17 +458,22 @@ class GradClip:
         self.result = torch.zeros(2, dtype=torch.float32, device=dev)
         self.gamma = self.result[1:]
         self._result, self._device = self.result.data_ptr(), self.result.device
-        self._norm, self._apply = load().skew_clip_norm, load().skew_clip_apply
+        self._norm, self._apply, self._stream = load().skew_clip_norm, load().skew_clip_apply, _raw_stream()
+        self._index = self._device.index
         skew_clip_bind(self.h, self.workspace.data_ptr(), n, _stream_of(stream, self._device))
 
     def norm(self, max_norm: float, stream=None):
         """[norm, gamma] with gamma = min(1, max_norm / (norm + 1e-6)); the gradients are only read."""
-        _check_op(self._norm(self.h, max_norm, self._result, _stream_of(stream, self._device)))
+        rc = self._norm(self.h, max_norm, self._result, self._stream(self._index) if stream is None else _stream_of(stream, None))
+        if rc:
+            _check_op(rc)
         return self.result
 
     def clip(self, max_norm: float, stream=None):
         """``norm``, then out = gamma * g for every tensor."""
-        _check_op(self._apply(self.h, max_norm, self._result, _stream_of(stream, self._device)))
+        rc = self._apply(self.h, max_norm, self._result, self._stream(self._index) if stream is None else _stream_of(stream, None))
+        if rc:
+            _check_op(rc)
         return self.result
 
     def close(self):
@@ -478,7 +510,8 @@ class Embedding:
             raise SkewError(SKEW_EINVAL, skew_ops_last_error())
         self._ref = {dt: C.byref(c) for dt, c in self.config.items()}
         self._shape = (rows, width)
-        self._empty, self._lookup, self._grad = torch.empty, load().skew_embed_lookup, load().skew_embed_grad
+        self._new, self._lookup, self._grad = _allocator(), load().skew_embed_lookup, load().skew_embed_grad
+        self._stream = _raw_stream()
         self.workspace, self._sizes = None, {}
 
     def _ids(self, ids):
@@ -498,9 +531,13 @@ class Embedding:
         """scale * table[ids], of shape ids.shape + (width,)."""
         c, dev = self._ids(ids), ids.device
         p = self._table(table, dev, "table")
-        out = self._empty((*ids.shape, self.width), dtype=self.act_dtype, device=dev)
-        _check_op(self._lookup(c, p, ids.data_ptr(), ids.numel(), out.data_ptr(), self.width, _stream_of(stream, dev)))
-        return out
+        n, d = ids.numel(), self.width
+        out = self._new((n, d), (d, 1), self.act_dtype, dev)
+        rc = self._lookup(c, p, ids.data_ptr(), n, out.data_ptr(), d,
+                          self._stream(dev.index) if stream is None else _stream_of(stream, dev))
+        if rc:
+            _check_op(rc)
+        return out if ids.dim() == 1 else out.view(*ids.shape, d)
 
     def grad(self, ids, dy, base=None, out=None, stream=None):
         """The table's gradient, every row of it, from the looked-up rows' (``ids.shape + (width,)``; a 2-D one may
@@ -513,7 +550,7 @@ class Embedding:
         ld = self.width if dy.is_contiguous() else _rows(dy, self.width, "dy that is not contiguous")
         b = None if base is None else self._table(base, dev, "base")
         if out is None:
-            out = self._empty(self._shape, dtype=self.table_dtype, device=dev)
+            out = self._new(self._shape, (self.width, 1), self.table_dtype, dev)
             p = out.data_ptr()
         else:
             p = self._table(out, dev, "out")
@@ -523,8 +560,11 @@ class Embedding:
             need = self._sizes[n] = skew_embed_workspace_bytes(self.config[ids.dtype], n)
         if ws is None or ws.numel() < need or ws.device != dev:
             import torch
-            ws = self.workspace = self._empty(need, dtype=torch.uint8, device=dev)
-        _check_op(self._grad(c, ids.data_ptr(), n, dy.data_ptr(), ld, b, p, ws.data_ptr(), need, _stream_of(stream, dev)))
+            ws = self.workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        rc = self._grad(c, ids.data_ptr(), n, dy.data_ptr(), ld, b, p, ws.data_ptr(), need,
+                        self._stream(dev.index) if stream is None else _stream_of(stream, dev))
+        if rc:
+            _check_op(rc)
         return out
 
 
@@ -558,22 +598,25 @@ class Router:
         if not self._ws_bytes:
             raise SkewError(SKEW_EINVAL, skew_ops_last_error())
         self._ref = {dt: C.byref(c) for dt, c in self.config.items()}
-        self._empty, self._i32, self._f32 = torch.empty, torch.int32, torch.float32
-        self._forward, self._grad = load().skew_gate_forward, load().skew_gate_grad
+        self._new, self._i32, self._f32 = _allocator(), torch.int32, torch.float32
+        self._forward, self._grad, self._stream = load().skew_gate_forward, load().skew_gate_grad, _raw_stream()
         self.workspace = None
 
     def _logits(self, logits):
         c = self._ref.get(logits.dtype)
         if c is None:
             raise TypeError("logits must be bf16 or fp32")
-        return c, _rows(logits, self.experts, "logits"), logits.shape[0], logits.device
+        T, E = logits.shape if logits.dim() == 2 else (0, 0)
+        if E == self.experts and logits.is_cuda and logits.is_contiguous():
+            return c, E, T, logits.device
+        return c, _rows(logits, self.experts, "logits"), T, logits.device
 
     def route(self, logits, bias=None, stream=None):
         """(chosen int32 (T, k), weights fp32 (T, k), counts int32 (experts,)) of (T, experts) logits, whose rows
         may lie apart. ``bias``: fp32 (experts,), added to the scores for the choice alone. Calls on one
         object share a workspace: they must not overlap on the GPU."""
         c, ld, T, dev = self._logits(logits)
-        k, empty, ws = self.top_k, self._empty, self.workspace
+        k, new, ws = self.top_k, self._new, self.workspace
         if bias is not None:
             if not (bias.dtype == self._f32 and bias.shape == (self.experts,) and bias.is_contiguous() and bias.device == dev):
                 raise ValueError("bias must be a contiguous fp32 tensor of one value for each expert, on the logits' device")
@@ -581,11 +624,13 @@ class Router:
         if ws is None or ws.device != dev:
             import torch
             ws = self.workspace = torch.zeros(self._ws_bytes, dtype=torch.uint8, device=dev)
-        chosen = empty((T, k), dtype=self._i32, device=dev)
-        weights = empty((T, k), dtype=self._f32, device=dev)
-        counts = empty(self.experts, dtype=self._i32, device=dev)
-        _check_op(self._forward(c, logits.data_ptr(), ld, bias, T, chosen.data_ptr(), weights.data_ptr(), counts.data_ptr(),
-                                ws.data_ptr(), self._ws_bytes, _stream_of(stream, dev)))
+        chosen = new((T, k), (k, 1), self._i32, dev)
+        weights = new((T, k), (k, 1), self._f32, dev)
+        counts = new((self.experts,), (1,), self._i32, dev)
+        rc = self._forward(c, logits.data_ptr(), ld, bias, T, chosen.data_ptr(), weights.data_ptr(), counts.data_ptr(),
+                           ws.data_ptr(), self._ws_bytes, self._stream(dev.index) if stream is None else _stream_of(stream, dev))
+        if rc:
+            _check_op(rc)
         return chosen, weights, counts
 
     def grad(self, logits, chosen, dweights, stream=None):
@@ -594,9 +639,11 @@ class Router:
         for t, dt in ((chosen, self._i32), (dweights, self._f32)):
             if not (t.dtype == dt and t.shape == (T, self.top_k) and t.is_contiguous() and t.device == dev):
                 raise ValueError(f"chosen and dweights must be contiguous ({T}, {self.top_k}) int32 and fp32 tensors on the logits' device")
-        dlogits = self._empty((T, self.experts), dtype=logits.dtype, device=dev)
-        _check_op(self._grad(c, logits.data_ptr(), ld, chosen.data_ptr(), dweights.data_ptr(), T, dlogits.data_ptr(),
-                             self.experts, _stream_of(stream, dev)))
+        dlogits = self._new((T, self.experts), (self.experts, 1), logits.dtype, dev)
+        rc = self._grad(c, logits.data_ptr(), ld, chosen.data_ptr(), dweights.data_ptr(), T, dlogits.data_ptr(),
+                        self.experts, self._stream(dev.index) if stream is None else _stream_of(stream, dev))
+        if rc:
+            _check_op(rc)
         return dlogits
 
 

@@ -19,7 +19,7 @@ constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
 constexpr int kOwnerBits = 7;
 constexpr uint32_t kOwners = 1u << kOwnerBits;  // CTAs of the sort: about as many as there are SMs
 constexpr uint32_t kSortRows = 1024;  // rows that a CTA of the sort has counters for at a time
-constexpr int64_t kDirect = 2048;     // most tokens that every CTA of the sort reads itself
+constexpr int64_t kDirect = 4096;     // most tokens that every CTA of the sort reads itself
 constexpr int kParts = 4;
 constexpr int kChunk = 32;       // most places of the sorted list to a warp: one to a lane
 constexpr int kCols = 256;       // columns to a warp: 8 to a lane
@@ -105,7 +105,7 @@ struct EmbedGradArgs {
     int32_t wide;
     uint32_t own_rows, splits;  // rows of the table to an owner; CTAs of k_embed_split
     int32_t chunk;              // places of the list to a warp: at most kChunk, a power of two
-    uint32_t chunks, tiles, fill;  // chunks of the list, tiles of columns, (32 rows, tile)s to look through for rows without tokens (0: they stay)
+    uint32_t chunks, tiles, fill;  // chunks of the list, tiles of columns, shares of 32 rows to look through for rows without tokens (0: they stay)
     // workspace
     int32_t *first;    // [kOwners * own_rows + 1]: where each row's run starts in the list, by packed()
     uint32_t *start;   // [kOwners + 1][splits]
@@ -233,10 +233,15 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const __grid_con
                 }
             }
         } else {
-            for (uint32_t p = from; p < to; ++p) {
-                const uint32_t id = read_id(A, WIDE, int64_t(p) * 32 + lane);
-                const bool in = id != kNobody && (id & (kOwners - 1)) == me;
-                if (__any_sync(kFullMask, in)) f(id / kOwners, p * 32 + lane, in);
+            for (uint32_t p = from; p < to; p += kParts) {
+                uint32_t id[kParts];
+#pragma unroll
+                for (int k = 0; k < kParts; ++k) id[k] = p + k < to ? read_id(A, WIDE, int64_t(p + k) * 32 + lane) : kNobody;
+#pragma unroll
+                for (int k = 0; k < kParts; ++k) {
+                    const bool in = id[k] != kNobody && (id[k] & (kOwners - 1)) == me;
+                    if (__any_sync(kFullMask, in)) f(id[k] / kOwners, (p + k) * 32 + lane, in);
+                }
             }
         }
     };
@@ -300,30 +305,36 @@ __device__ __forceinline__ int64_t column(int64_t c0, int k) {
     return VEC ? c0 + 8 * (threadIdx.x & 31) + k : c0 + 32 * k + (threadIdx.x & 31);
 }
 
-// A lane's 8 elements of a row, as they are loaded.
-template <bool F32, bool VEC>
-struct Cells {
-    Vec8<F32> v;
-    __device__ __forceinline__ void load(const void *p, int64_t row_at, int64_t c0, int64_t width) {
-        if (column<true>(c0, 0) < width) v = load8<F32>(p, row_at + column<true>(c0, 0));
-    }
-    __device__ __forceinline__ float at(int k) const { return v.at(k); }
-};
-template <bool F32>
-struct Cells<F32, false> {
-    uint32_t v[8];  // as they are in memory, so that no load is waited for before all are under way
-    __device__ __forceinline__ void load(const void *p, int64_t row_at, int64_t c0, int64_t width) {
+// dW = base, or zero, over `count` elements from `at` on: whole rows without tokens, one after another, or a part of them.
+template <bool F32, bool BASE>
+__device__ __forceinline__ void fill(const EmbedGradArgs &A, int64_t at, int64_t count) {
+    constexpr int kElem = F32 ? 4 : 2;
+    const int lane = threadIdx.x & 31;
+    char *to = static_cast<char *>(A.dw) + at * kElem;
+    const char *from = BASE ? static_cast<const char *>(A.base) + at * kElem : nullptr;
+    auto one = [&](int64_t i) { store1<F32>(A.dw, at + i, BASE ? load1<F32>(A.base, at + i) : 0.f); };
+    int64_t done = 0;
+    if (!BASE || (((uintptr_t)to ^ (uintptr_t)from) & 15) == 0) {
+        const int64_t head = (-(intptr_t)to & 15) / kElem < count ? (-(intptr_t)to & 15) / kElem : count, units = (count - head) * kElem / 16;
+        if (lane < head) one(lane);
+        to += head * kElem;
+        from += BASE ? head * kElem : 0;
+        constexpr int kUnits = 8;  // under way at a time
+        for (int64_t u = lane; u < units; u += 32 * kUnits) {
+            uint4 v[kUnits];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int64_t c = column<false>(c0, k), i = row_at + (c < width ? c : width - 1);  // past the last column: the last again
-            if constexpr (F32)
-                v[k] = static_cast<const uint32_t *>(p)[i];
-            else
-                v[k] = static_cast<const uint16_t *>(p)[i];
+            for (int k = 0; k < kUnits; ++k) {
+                v[k] = make_uint4(0, 0, 0, 0);
+                if (BASE && u + 32 * k < units) v[k] = ld_stream(from + 16 * (u + 32 * k));
+            }
+#pragma unroll
+            for (int k = 0; k < kUnits; ++k)
+                if (u + 32 * k < units) st_stream(to + 16 * (u + 32 * k), v[k]);
         }
+        done = head + units * 16 / kElem;
     }
-    __device__ __forceinline__ float at(int k) const { return __uint_as_float(F32 ? v[k] : v[k] << 16); }
-};
+    for (int64_t i = done + lane; i < count; i += 32) one(i);
+}
 
 // Stores a row's 8 columns of a lane.
 template <bool TF32, bool VEC>
@@ -371,6 +382,7 @@ __device__ __forceinline__ bool put_piece(const EmbedGradArgs &A, int r0, int r1
                     sum[2].x += b[j].x, sum[2].y += b[j].y, sum[3].x += b[j].z, sum[3].y += b[j].w;
                 }
         }
+        if (last - first < kJoin) break;  // one sum
         mine = at;
         at = first;
         step = kJoin;
@@ -500,29 +512,15 @@ __global__ void __launch_bounds__(kGradThreads, 5) k_embed_grad(const __grid_con
     };
     fetch(go, 0);
     fetch(go + kRound, 1);
-    for (uint32_t f = w; f < A.fill; f += gridDim.x * (kGradThreads / 32)) {  // 32 rows, one tile of columns
-        const uint32_t v0 = f / A.tiles * 32;
-        const int64_t fc = int64_t(f - f / A.tiles * A.tiles) * kCols;
+    for (uint32_t f = w; f < A.fill; f += gridDim.x * (kGradThreads / 32)) {  // a share of 32 rows
+        const uint32_t v0 = f / A.tiles * 32, share = f - f / A.tiles * A.tiles;
         const uint32_t p = packed(A, v0 + lane < A.rows ? v0 + lane : 0);
         uint32_t empty = __ballot_sync(kFullMask, v0 + lane < A.rows && A.first[p] == A.first[p + 1]);
-        while (empty) {
-            uint32_t which[4], there[4];
-            Cells<TF32, VEC> b[BASE ? 4 : 1];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                there[i] = empty;
-                which[i] = v0 + __ffs(empty) - 1;
-                empty &= empty - 1;
-                if (BASE && there[i]) b[BASE ? i : 0].load(A.base, which[i] * A.width, fc, A.width);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (there[i]) {
-                    float y[8];
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) y[k] = BASE ? b[BASE ? i : 0].at(k) : 0.f;
-                    put_row<TF32, VEC>(A, which[i], fc, y);
-                }
+        while (empty) {  // runs of rows without tokens: this share of each
+            const int r = __ffs(empty) - 1, n = __ffs(~(empty >> r)) - 1 < 0 ? 32 - r : __ffs(~(empty >> r)) - 1;
+            empty &= r + n < 32 ? ~0u << (r + n) : 0u;
+            const int64_t all = n * A.width, part = (all / A.tiles + 63) / 64 * 64, at = share * part;
+            if (at < all) fill<TF32, BASE>(A, (int64_t(v0) + r) * A.width + at, share + 1 == A.tiles || at + part > all ? all - at : part);
         }
     }
     if (!own) return;

@@ -391,7 +391,7 @@ const char *skew_ops_last_error(void);
  * gamma is what skew_step_scaled takes as grad_scale, so that a trainer whose
  * gradients go to the step only needs skew_clip_norm (one read of them). Squares
  * are summed in fp32 (two-term sums) and joined in fp64, in an order that depends on the
- * tensors' sizes alone; elements whose squares leave fp32's range are summed scaled,
+ * tensors' sizes, types and alignment alone; elements whose squares leave fp32's range are summed scaled,
  * so the norm is right for any finite gradient (and Inf only where it exceeds fp32
  * itself). A NaN in a gradient makes norm and gamma NaN; an Inf makes norm Inf and
  * gamma 0 (0 * Inf is then NaN in the clipped tensor).
@@ -446,7 +446,8 @@ int skew_clip_apply(skew_clip_t *h, float max_norm, float *result, void *stream)
  * A bias steers which experts are chosen and never enters a weight (it balances
  * loads without a loss term). Experts with a logit of -Inf or NaN, or a choice that is
  * -Inf or NaN, are never chosen: a slot that finds no expert is -1 with weight 0. A sum of
- * zero gives weights of zero. A NaN logit makes the weights of its token NaN. Scores are fp32.
+ * zero gives weights of zero. A NaN logit makes the weights of its token NaN (and, by a softmax, its
+ * scores, so that nothing is chosen where a bias makes experts go by them). Scores are fp32.
  */
 #define SKEW_GATE_SOFTMAX 0
 #define SKEW_GATE_SIGMOID 1
@@ -488,9 +489,9 @@ int skew_gate_grad(const skew_gate_config_t *c, const void *logits, int64_t ld, 
  *   lookup    y[t] = scale * W[id_t]
  *   gradient  dW[v] = base[v] + scale * (sum over the t with id_t = v of dy[t])
  * W is (rows, width), contiguous. An id outside [0, rows) is padding: its y is zero and it has no
- * gradient. Terms are added in fp32 in the tokens' order (a row with more than 32 terms: in runs of at
- * most 32, whose sums are then added in order), so results do not depend on timing; each element is
- * rounded once.
+ * gradient. Terms are added in fp32 in the tokens' order (a row with many terms: in runs of at most
+ * 32, then sixteen of those sums at a time, then the rest, each in order), so results do not depend on
+ * timing; each element is rounded once.
  */
 #define SKEW_EMBED_TABLE_FP32 1u /* W, base and dW are fp32 (else bf16) */
 #define SKEW_EMBED_ACT_FP32 2u   /* y and dy are fp32 (else bf16)       */

@@ -1,9 +1,9 @@
 // Routing of tokens to experts and its gradient (skew_gate_* in include/skewadam.h).
 //
-// Forward: L lanes of a warp own a token, N consecutive logits each. Scores and choices stay in registers;
-// an expert is picked as the maximum over the lanes' own maxima of order-preserving integer keys, the lowest
-// lane first among equals, so ties go to the lowest index. Reads the logits once (bound by memory at few
-// experts a token, by instructions at many).
+// Forward, bound by instructions (the logits are read once): a thread to a token for many tokens of few experts
+// (k_gate_thread), else a warp to a token, N consecutive logits a lane (k_gate_wide), with
+// route_token for what that does not settle. Experts are chosen by the logits themselves, or by fp32
+// scores plus biases, never by quicker ones; the lowest index first among equals.
 //
 // Backward: as many lanes as top_k, rounded up to a power of two, own a token, one chosen expert each. Only the
 // softmax that is not renormalised has a gradient elsewhere, and reads whole rows.
@@ -17,6 +17,11 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxExperts = 512, kMaxK = 32, kMaxGroups = 32;
+// A thread routes a token of up to kThreadExperts experts, where the tokens give the SMs enough threads: kThreadTokens to an
+// expert (thread and warp to a token, us: 2 of 8 experts 4096 tokens 6.3 5.7, 8192 6.4 7.7, 65536 7.7 29; 6 of 64
+// 16384 15 12, 32768 18 19, 65536 22 33; 11 of 56 16384 17 13, 65536 30 38).
+constexpr int kThreadExperts = 64;
+constexpr int64_t kThreadTokens = 600;
 
 struct GateArgs {
     const void *x;
@@ -27,6 +32,8 @@ struct GateArgs {
     uint32_t *ws;  // [0, E): tokens of each expert so far, [E]: CTAs done; zero between calls
     int64_t ld, tokens;
     int32_t E, k, groups, top_groups, group_top, group_size, sigmoid, renorm, vec;
+    int32_t warp_floats;  // shared memory of a warp (k_gate_thread)
+    int32_t per, lane_n;  // lanes to a group, experts to a lane (k_gate_wide)
     float scale;
 };
 
@@ -42,28 +49,17 @@ __device__ __forceinline__ bool choosable(float x) { return x > -INFINITY; }  //
 
 __device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
 
-template <int L>
-__device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
-    if constexpr (L == 32) {
-        return __reduce_max_sync(kFullMask, v);
-    } else {
-#pragma unroll
-        for (int d = L / 2; d; d >>= 1) v = max(v, __shfl_xor_sync(kFullMask, v, d));
-        return v;
-    }
-}
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v) { return __reduce_max_sync(kFullMask, v); }
 
-template <int L>
 __device__ __forceinline__ float lanes_max(float v) {
 #pragma unroll
-    for (int d = L / 2; d; d >>= 1) v = fmaxf(v, __shfl_xor_sync(kFullMask, v, d));
+    for (int d = 16; d; d >>= 1) v = fmaxf(v, __shfl_xor_sync(kFullMask, v, d));
     return v;
 }
 
-template <int L>
 __device__ __forceinline__ float lanes_sum(float v) {
 #pragma unroll
-    for (int d = L / 2; d; d >>= 1) v += __shfl_xor_sync(kFullMask, v, d);
+    for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(kFullMask, v, d);
     return v;
 }
 
@@ -73,10 +69,10 @@ __device__ __forceinline__ void merge_two(float &a1, float &a2, float b1, float 
     a1 = fmaxf(a1, b1);
 }
 
-// A lane's N logits from `e0` on; what lies past E, and rows past the last, as -Inf.
+// A lane's N logits from `e0` on; what lies past E as -Inf.
 template <bool F32, int N>
-__device__ __forceinline__ void load_logits(const GateArgs &A, int64_t t, bool there, int e0, float (&x)[N]) {
-    if (there && A.vec && e0 < A.E) {
+__device__ __forceinline__ void load_logits(const GateArgs &A, int64_t t, int e0, float (&x)[N]) {
+    if (A.vec && e0 < A.E) {
         const char *p = elem_ptr<F32>(A.x, t * A.ld + e0);
         if constexpr (F32) {
 #pragma unroll
@@ -99,29 +95,21 @@ __device__ __forceinline__ void load_logits(const GateArgs &A, int64_t t, bool t
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < N; ++j) x[j] = there && e0 + j < A.E ? load1<F32>(A.x, t * A.ld + e0 + j) : -INFINITY;
+        for (int j = 0; j < N; ++j) x[j] = e0 + j < A.E ? load1<F32>(A.x, t * A.ld + e0 + j) : -INFINITY;
     }
 }
 
-// Routes 32 / L tokens from t0 on, whatever they and the config hold.
-template <bool F32, int L, int N>
-__device__ __forceinline__ void route_tokens(const GateArgs &A, int64_t t0, int32_t *hist, float *rows) {
-    constexpr int SL = N < kMaxK / L ? N : kMaxK / L;  // chosen experts a lane keeps
-    const int lane = threadIdx.x & 31, l = lane & (L - 1), e0 = l * N;
-    const uint32_t lanes = L == 32 ? kFullMask : ((1u << (L & 31)) - 1) << (lane & ~(L - 1));
+// Routes a token by a warp, whatever it and the config hold. row: kMaxExperts floats of the warp's own.
+template <bool F32, int N>
+__device__ __forceinline__ void route_token(const GateArgs &A, int64_t t, int32_t *hist, float *row) {
+    const int lane = threadIdx.x & 31, e0 = lane * N;
     const bool shows = A.bias || (A.groups > 1 && A.group_top == 2);
-    const bool whole_lanes = A.group_size % N == 0 && ((A.group_size / N) & (A.group_size / N - 1)) == 0;
-    float bias[N];
-#pragma unroll
-    for (int j = 0; j < N; ++j) bias[j] = A.bias && e0 + j < A.E ? A.bias[e0 + j] : 0.f;
-    const int64_t t = t0 + lane / L;
-    const bool there = t < A.tokens;
     float x[N];
-    load_logits<F32, N>(A, t, there, e0, x);
+    load_logits<F32, N>(A, t, e0, x);
     bool is_nan = false;
 #pragma unroll
     for (int j = 0; j < N; ++j) is_nan |= x[j] != x[j];
-    const bool nan = (__ballot_sync(kFullMask, is_nan) & lanes) != 0;
+    const bool nan = __any_sync(kFullMask, is_nan);
 
     // what experts are chosen by: the logits (they order as the scores do), or the scores plus the bias
     float shown[N], row_max = 0.f, row_sum = 0.f;
@@ -130,7 +118,7 @@ __device__ __forceinline__ void route_tokens(const GateArgs &A, int64_t t0, int3
         float m = -INFINITY;
 #pragma unroll
         for (int j = 0; j < N; ++j) m = fmaxf(m, x[j]);
-        row_max = lanes_max<L>(m);
+        row_max = lanes_max(m);
         if (row_max == -INFINITY) row_max = 0.f;
         float s = 0.f;
 #pragma unroll
@@ -138,13 +126,13 @@ __device__ __forceinline__ void route_tokens(const GateArgs &A, int64_t t0, int3
             shown[j] = expf(x[j] - row_max);  // without a bias the row's sum changes no order
             s += shown[j];
         }
-        row_sum = lanes_sum<L>(s);
+        row_sum = lanes_sum(s);
         if (A.bias)
 #pragma unroll
-            for (int j = 0; j < N; ++j) shown[j] = shown[j] / row_sum + bias[j];
+            for (int j = 0; j < N; ++j) shown[j] = shown[j] / row_sum + (e0 + j < A.E ? A.bias[e0 + j] : 0.f);
     } else if (shows) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) shown[j] = sigmoid(x[j]) + bias[j];
+        for (int j = 0; j < N; ++j) shown[j] = sigmoid(x[j]) + (A.bias && e0 + j < A.E ? A.bias[e0 + j] : 0.f);
     }
 #pragma unroll
     for (int j = 0; j < N; ++j) {
@@ -152,74 +140,39 @@ __device__ __forceinline__ void route_tokens(const GateArgs &A, int64_t t0, int3
         key[j] = choosable(c) && choosable(x[j]) ? order_key(c) : 0u;
     }
 
-    if (A.groups > 1) {
-        uint32_t gkey = 0, taken = 0;
-        int per = 1;  // lanes from one group's key to the next
-        if (whole_lanes) {
-            per = A.group_size / N;
-            if (A.group_top == 1) {
+    if (A.groups > 1) {  // `share` lanes to a group
+        const int share = 32 >> (32 - __clz(A.groups - 1)), group = lane / share;
 #pragma unroll
-                for (int j = 0; j < N; ++j) gkey = max(gkey, key[j]);
-                for (int d = 1; d < per; d <<= 1) gkey = max(gkey, __shfl_xor_sync(kFullMask, gkey, d));
-            } else {
-                float a1 = -INFINITY, a2 = -INFINITY;
-#pragma unroll
-                for (int j = 0; j < N; ++j) merge_two(a1, a2, key[j] ? shown[j] : -INFINITY, -INFINITY);
-                for (int d = 1; d < per; d <<= 1) {
-                    const float b1 = __shfl_xor_sync(kFullMask, a1, d), b2 = __shfl_xor_sync(kFullMask, a2, d);
-                    merge_two(a1, a2, b1, b2);
-                }
-                if (choosable(a1)) gkey = order_key(choosable(a2) ? a1 + a2 : a1);
-            }
-            if (l % per) gkey = 0;
-        } else if constexpr (L == 32) {  // one lane to a group
-            float *row = rows + (threadIdx.x >> 5) * kMaxExperts;
-            uint32_t *keys = reinterpret_cast<uint32_t *>(row);
-            if (A.group_top == 1) {
-#pragma unroll
-                for (int j = 0; j < N; ++j) keys[e0 + j] = key[j];
-                __syncwarp();
-                if (l < A.groups)
-                    for (int i = 0; i < A.group_size; ++i) gkey = max(gkey, keys[l * A.group_size + i]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < N; ++j) row[e0 + j] = key[j] ? shown[j] : -INFINITY;
-                __syncwarp();
-                float a1 = -INFINITY, a2 = -INFINITY;
-                if (l < A.groups)
-                    for (int i = 0; i < A.group_size; ++i) merge_two(a1, a2, row[l * A.group_size + i], -INFINITY);
-                if (choosable(a1)) gkey = order_key(choosable(a2) ? a1 + a2 : a1);
-            }
-            __syncwarp();
+        for (int j = 0; j < N; ++j) row[e0 + j] = !key[j] ? -INFINITY : A.group_top == 2 ? shown[j] : key_value(key[j]);
+        __syncwarp();
+        float a1 = -INFINITY, a2 = -INFINITY;
+        if (group < A.groups)
+            for (int i = lane % share; i < A.group_size; i += share) merge_two(a1, a2, row[group * A.group_size + i], -INFINITY);
+        for (int d = 1; d < share; d <<= 1) {
+            const float b1 = __shfl_xor_sync(kFullMask, a1, d), b2 = __shfl_xor_sync(kFullMask, a2, d);
+            merge_two(a1, a2, b1, b2);
         }
+        __syncwarp();
+        uint32_t gkey = choosable(a1) && lane % share == 0 ? order_key(A.group_top == 2 && choosable(a2) ? a1 + a2 : a1) : 0u, taken = 0;
         for (int g = 0; g < A.top_groups; ++g) {
-            const uint32_t best = lanes_max<L>(gkey);
-            const uint32_t who = __ballot_sync(kFullMask, gkey == best) & lanes;
-            const int win = __ffs(who) - 1;
-            if (best) taken |= 1u << ((win & (L - 1)) / per);
+            const uint32_t best = lanes_max(gkey);
+            const int win = __ffs(__ballot_sync(kFullMask, gkey == best)) - 1;
+            if (best) taken |= 1u << (win / share);
             if (lane == win) gkey = 0;
         }
-        if (whole_lanes) {
-            if (!(taken >> (l / per) & 1))
 #pragma unroll
-                for (int j = 0; j < N; ++j) key[j] = 0;
-        } else {
-#pragma unroll
-            for (int j = 0; j < N; ++j)
-                if (e0 + j >= A.E || !(taken >> ((e0 + j) / A.group_size) & 1)) key[j] = 0;
-        }
+        for (int j = 0; j < N; ++j)
+            if (e0 + j >= A.E || !(taken >> ((e0 + j) / A.group_size) & 1)) key[j] = 0;
     }
 
     // the k largest, one after another
     uint32_t m = 0;
 #pragma unroll
     for (int j = 0; j < N; ++j) m = max(m, key[j]);
-    int32_t mine[SL];
-#pragma unroll
-    for (int q = 0; q < SL; ++q) mine[q] = -1;
+    int32_t mine = -1;
     for (int i = 0; i < A.k; ++i) {
-        const uint32_t best = lanes_max<L>(m);
-        const int win = __ffs(__ballot_sync(kFullMask, m == best) & lanes) - 1;
+        const uint32_t best = lanes_max(m);
+        const int win = __ffs(__ballot_sync(kFullMask, m == best)) - 1;
         int at = 0;
 #pragma unroll
         for (int j = N - 1; j >= 0; --j)
@@ -233,47 +186,27 @@ __device__ __forceinline__ void route_tokens(const GateArgs &A, int64_t t0, int3
                 m = max(m, key[j]);
             }
         }
-#pragma unroll
-        for (int q = 0; q < SL; ++q)
-            if (best && i == q * L + l) mine[q] = e;
+        if (best && i == lane) mine = e;
     }
 
     // weights of the chosen
-    float sc[SL], sum = 0.f;
-    if (A.sigmoid || !A.renorm) {
-#pragma unroll
-        for (int q = 0; q < SL; ++q) {
-            const float xc = mine[q] >= 0 ? load1<F32>(A.x, t * A.ld + mine[q]) : -INFINITY;
-            sc[q] = A.sigmoid ? sigmoid(xc) : mine[q] >= 0 ? expf(xc - row_max) / row_sum : 0.f;
-            sum += sc[q];
-        }
-    } else {  // the softmax of the chosen
-        float top = -INFINITY;
-#pragma unroll
-        for (int q = 0; q < SL; ++q) {
-            sc[q] = mine[q] >= 0 ? load1<F32>(A.x, t * A.ld + mine[q]) : -INFINITY;
-            top = fmaxf(top, sc[q]);
-        }
-        top = lanes_max<L>(top);
-#pragma unroll
-        for (int q = 0; q < SL; ++q) {
-            sc[q] = mine[q] >= 0 ? expf(sc[q] - top) : 0.f;
-            sum += sc[q];
-        }
+    const float xc = mine >= 0 ? load1<F32>(A.x, t * A.ld + mine) : -INFINITY;
+    float s = 0.f;
+    if (A.sigmoid) {
+        s = sigmoid(xc);
+    } else {
+        const float top = A.renorm ? lanes_max(xc) : row_max;  // renormalised: the softmax of the chosen
+        if (mine >= 0) s = A.renorm ? expf(xc - top) : expf(xc - top) / row_sum;
     }
     float by = A.scale;
     if (A.renorm) {
-        sum = lanes_sum<L>(sum);
+        const float sum = lanes_sum(s);
         by = sum == 0.f ? 0.f : A.scale / sum;
     }
-#pragma unroll
-    for (int q = 0; q < SL; ++q) {
-        const int i = q * L + l;
-        if (there && i < A.k) {
-            A.chosen[t * A.k + i] = mine[q];
-            A.weights[t * A.k + i] = nan ? NAN : sc[q] * by;
-            if (A.counts && mine[q] >= 0) atomicAdd(hist + mine[q], 1);
-        }
+    if (lane < A.k) {
+        A.chosen[t * A.k + lane] = mine;
+        A.weights[t * A.k + lane] = nan ? NAN : s * by;
+        if (A.counts && mine >= 0) atomicAdd(hist + mine, 1);
     }
 }
 
@@ -282,10 +215,10 @@ __device__ __forceinline__ void put_counts(const GateArgs &A, const int32_t *his
     if (!A.counts) return;
     __syncthreads();
     if (gridDim.x == 1) {
-        for (int e = threadIdx.x; e < A.E; e += kThreads) A.counts[e] = hist[e];
+        for (int e = threadIdx.x; e < A.E; e += blockDim.x) A.counts[e] = hist[e];
         return;
     }
-    for (int e = threadIdx.x; e < A.E; e += kThreads)
+    for (int e = threadIdx.x; e < A.E; e += blockDim.x)
         if (hist[e]) atomicAdd(A.ws + e, (uint32_t)hist[e]);
     __shared__ bool last;
     __threadfence();
@@ -294,18 +227,165 @@ __device__ __forceinline__ void put_counts(const GateArgs &A, const int32_t *his
     __syncthreads();
     if (!last) return;
     __threadfence();
-    for (int e = threadIdx.x; e < A.E; e += kThreads) A.counts[e] = (int32_t)atomicExch(A.ws + e, 0u);
+    for (int e = threadIdx.x; e < A.E; e += blockDim.x) A.counts[e] = (int32_t)atomicExch(A.ws + e, 0u);
 }
 
-template <bool F32, int L, int N>
-__global__ void __launch_bounds__(kThreads, 4) k_gate(const __grid_constant__ GateArgs A) {
-    constexpr int TPW = 32 / L;     // tokens a warp takes at a time
-    extern __shared__ float dyn[];  // shown values, where groups do not end with lanes
+// A warp to a token, by route_token alone.
+template <bool F32, int N>
+__global__ void __launch_bounds__(kThreads, 3) k_gate(const __grid_constant__ GateArgs A) {
+    __shared__ float rows[kWarps][N * 32];
     __shared__ int32_t hist[kMaxExperts];
     for (int e = threadIdx.x; e < A.E; e += kThreads) hist[e] = 0;
     __syncthreads();
-    for (int64_t w = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5); w * TPW < A.tokens; w += int64_t(gridDim.x) * kWarps)
-        route_tokens<F32, L, N>(A, w * TPW, hist, dyn);
+    for (int64_t t = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5); t < A.tokens; t += int64_t(gridDim.x) * kWarps)
+        route_token<F32, N>(A, t, hist, rows[threadIdx.x >> 5]);
+    put_counts(A, hist);
+}
+
+// A thread to a token, for up to kThreadExperts experts: its logits in shared memory, its KM best experts in registers, sorted
+// by insertion; a warp's results go out in one piece.
+template <bool F32, int KM>
+__global__ void __launch_bounds__(64) k_gate_thread(const __grid_constant__ GateArgs A) {
+    extern __shared__ float dyn[];
+    __shared__ int32_t hist[kThreadExperts];
+    __shared__ float biases[kThreadExperts];
+    const int lane = threadIdx.x & 31, warps = blockDim.x >> 5, E = A.E, pitch = E | 1;
+    const bool shows = A.bias || (A.groups > 1 && A.group_top == 2), grouped = A.groups > 1;
+    for (int e = threadIdx.x; e < E; e += blockDim.x) {
+        hist[e] = 0;
+        biases[e] = A.bias ? A.bias[e] : 0.f;
+    }
+    __syncthreads();
+    float *rows = dyn + (threadIdx.x >> 5) * A.warp_floats;
+    // a thread's logits, its scores plus biases (where experts or groups go by them), its groups' scores
+    float *x = rows + lane * pitch, *shown = x + 32 * pitch, *scores = rows + (shows ? 64 : 32) * pitch + lane * (A.groups | 1);
+    const float *choices = A.bias ? shown : x, *by = shows ? shown : x;
+    for (int64_t w = int64_t(blockIdx.x) * warps + (threadIdx.x >> 5); w * 32 < A.tokens; w += int64_t(gridDim.x) * warps) {
+        const int64_t t0 = w * 32;
+        const int n = int(A.tokens - t0 < 32 ? A.tokens - t0 : 32);
+        for (int r0 = 0; r0 < n; r0 += 8) {  // a row to the lanes
+            float a[8], b[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                const int64_t at = (t0 + (r0 + r < n ? r0 + r : n - 1)) * A.ld;
+                a[r] = load1<F32>(A.x, at + (lane < E ? lane : 0));
+                b[r] = E > 32 ? load1<F32>(A.x, at + (lane + 32 < E ? lane + 32 : 0)) : 0.f;
+            }
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                if (lane < E) rows[(r0 + r) * pitch + lane] = a[r];
+                if (lane + 32 < E) rows[(r0 + r) * pitch + lane + 32] = b[r];
+            }
+            if (shows && A.sigmoid) {
+                float *at = rows + (32 + r0) * pitch + lane;
+#pragma unroll
+                for (int r = 0; r < 8; ++r)
+                    if (lane < E) at[r * pitch] = sigmoid(a[r]) + biases[lane];
+                if (E > 32)
+#pragma unroll
+                    for (int r = 0; r < 8; ++r)
+                        if (lane + 32 < E) at[r * pitch + 32] = sigmoid(b[r]) + biases[lane + 32];
+            }
+        }
+        __syncwarp();
+        float row_max = 0.f, row_sum = 0.f;
+        if (!A.sigmoid && (shows || !A.renorm)) {
+            float m = -INFINITY;
+#pragma unroll 4
+            for (int e = 0; e < E; ++e) m = fmaxf(m, x[e]);
+            row_max = m == -INFINITY ? 0.f : m;
+#pragma unroll 4
+            for (int e = 0; e < E; ++e) {
+                const float s = expf(x[e] - row_max);
+                if (shows) shown[e] = s;
+                row_sum += s;
+            }
+            if (A.bias)
+#pragma unroll 4
+                for (int e = 0; e < E; ++e) shown[e] = shown[e] / row_sum + biases[e];
+        }
+        uint32_t taken = 1;
+        if (grouped) {
+            for (int g = 0, e = 0; g < A.groups; ++g) {
+                float a1 = -INFINITY, a2 = -INFINITY;
+#pragma unroll 4
+                for (int i = 0; i < A.group_size; ++i, ++e) {
+                    const float s = by[e];
+                    merge_two(a1, a2, choosable(s) && choosable(x[e]) ? s : -INFINITY, -INFINITY);
+                }
+                scores[g] = choosable(a1) ? fmaxf(A.group_top == 2 && choosable(a2) ? a1 + a2 : a1, -FLT_MAX) : -INFINITY;
+            }
+            taken = 0;
+            for (int g = 0; g < A.groups; ++g) {
+                const float mine = scores[g];
+                int rank = 0;
+                for (int o = 0; o < A.groups; ++o) rank += scores[o] > mine || (scores[o] == mine && o < g);
+                if (choosable(mine) && rank < A.top_groups) taken |= 1u << g;
+            }
+        }
+        float best[KM];
+        int32_t which[KM];
+#pragma unroll
+        for (int j = 0; j < KM; ++j) best[j] = -INFINITY, which[j] = -1;
+        bool nan = false;
+        for (int g = 0, e = 0; g < A.groups; ++g) {
+            const bool in = taken >> g & 1;
+#pragma unroll 4
+            for (int i = 0; i < A.group_size; ++i, ++e) {
+                const float v = x[e];
+                float c = choices[e];
+                nan |= v != v;
+                if (!in || !(c > best[KM - 1]) || !choosable(v)) continue;  // (a NaN neither)
+                int32_t ce = e;
+                bool below = false;  // from the first that is smaller on, each moves one down
+#pragma unroll
+                for (int j = 0; j < KM; ++j) {
+                    below = below || c > best[j];
+                    const float tc = best[j];
+                    const int32_t te = which[j];
+                    best[j] = below ? c : tc;
+                    which[j] = below ? ce : te;
+                    c = below ? tc : c;
+                    ce = below ? te : ce;
+                }
+            }
+        }
+        // weights of the chosen
+        float s[KM], top = row_max, sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < KM; ++j) {
+            if (j >= A.k) which[j] = -1;
+            s[j] = which[j] >= 0 ? x[which[j]] : -INFINITY;
+        }
+        if (!A.sigmoid && A.renorm) {  // the softmax of the chosen
+            top = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < KM; ++j) top = fmaxf(top, s[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < KM; ++j) {
+            s[j] = A.sigmoid ? sigmoid(s[j]) : which[j] < 0 ? 0.f : A.renorm ? expf(s[j] - top) : expf(s[j] - top) / row_sum;
+            sum += s[j];
+        }
+        const float factor = !A.renorm ? A.scale : sum == 0.f ? 0.f : A.scale / sum;
+        if (A.counts && lane < n)
+#pragma unroll
+            for (int j = 0; j < KM; ++j)
+                if (which[j] >= 0) atomicAdd(hist + which[j], 1);
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < KM; ++j)
+            if (j < A.k) rows[lane * A.k + j] = __int_as_float(which[j]);
+        __syncwarp();
+        for (int i = lane; i < n * A.k; i += 32) A.chosen[t0 * A.k + i] = __float_as_int(rows[i]);
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < KM; ++j)
+            if (j < A.k) rows[lane * A.k + j] = nan ? NAN : s[j] * factor;
+        __syncwarp();
+        for (int i = lane; i < n * A.k; i += 32) A.weights[t0 * A.k + i] = rows[i];
+        __syncwarp();
+    }
     put_counts(A, hist);
 }
 
@@ -330,62 +410,73 @@ struct alignas(16) Cand {
 };
 
 template <bool F32, int N>
-__device__ __noinline__ void route_hard_token(const GateArgs &A, int64_t t, int32_t *hist) {
-    route_tokens<F32, 32, N>(A, t, hist, nullptr);
+__device__ __noinline__ void route_hard_token(const GateArgs &A, int64_t t, int32_t *hist, float *row) {
+    route_token<F32, N>(A, t, hist, row);
 }
 
-// A warp to a token, for configs whose groups are whole lanes. Near ties aside, quick scores settle which groups are
-// taken, and which experts may be among the top_k: at least k values are no less than the k-th of the lanes' largest, and
-// few more; a lane to one of those, with its fp32 score, ranks it among the others. A token that this does not settle
-// (near ties, a logit that is not finite, over 32 such experts) takes route_tokens.
+// A warp to a token. A group has `per` lanes, a power of two, and a lane lane_n consecutive experts of it (fewer at the group's
+// end). Near ties aside, quick scores settle which groups are taken, and which experts may be among the top_k: at
+// least k values are no less than the k-th of the lanes' two largest each, and few more; a lane to one of those, with its fp32
+// score, ranks it among the others. A token that this does not settle (near ties, a logit that is not finite, over 32
+// such experts) takes route_token.
 // SCORE: kLogits (experts and groups by the logits alone), kSigmoid, kSoftmax (both: quick scores are needed).
 enum { kLogits, kSigmoid, kSoftmax };
 template <bool F32, int N, int SCORE>
 __global__ void __launch_bounds__(kThreads, N == 16 ? 2 : 3) k_gate_wide(const __grid_constant__ GateArgs A) {
     __shared__ int32_t hist[kMaxExperts];
     __shared__ Cand cands[kWarps][32];
-    const int lane = threadIdx.x & 31, e0 = lane * N;
+    __shared__ float rows[kWarps][N * 32];
     for (int e = threadIdx.x; e < A.E; e += kThreads) hist[e] = 0;
     __syncthreads();
+    const int lane = threadIdx.x & 31, per = A.per, group = lane / per, sub = lane % per;
+    const int e0 = group * A.group_size + sub * A.lane_n;
+    const int left_n = group < A.groups ? A.group_size - sub * A.lane_n : 0, mine_n = left_n < 0 ? 0 : left_n < A.lane_n ? left_n : A.lane_n;
+    const bool full = __all_sync(kFullMask, mine_n == N), biased = SCORE == kSigmoid && A.bias;
     Cand *cand = cands[threadIdx.x >> 5];
     const uint32_t before = (1u << lane) - 1;
-    const bool full = A.E == 32 * N, biased = SCORE == kSigmoid && A.bias;
-    const int per = A.group_size / N, group = lane / per;  // (one group: unused)
     float bias[N], bias_max = 0.f;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-        bias[j] = biased && e0 + j < A.E ? A.bias[e0 + j] : 0.f;
+        bias[j] = biased && j < mine_n ? A.bias[e0 + j] : 0.f;
         bias_max = fmaxf(bias_max, fabsf(bias[j]) < INFINITY ? fabsf(bias[j]) : 0.f);
-        if (e0 + j < A.E && !choosable(bias[j])) bias[j] = -INFINITY;
+        if (j < mine_n && !choosable(bias[j])) bias[j] = -INFINITY;
     }
     // How far a quick choice may be from the fp32 one: the score's 2^-21 and the sum's rounding, with room to spare.
-    const float off = 0x1p-20f * (2.f + lanes_max<32>(bias_max));
+    const float off = 0x1p-20f * (2.f + lanes_max(bias_max));
     // The top_groups best of the groups' scores `a` (in all lanes of a group); false where that hangs on less than `far` or a tie.
     auto take_groups = [&](float a, float far, bool &taken) {
         const uint32_t key = group < A.groups && choosable(a) ? order_key(a) : 0u;
         uint32_t left = key, least = 0;
         for (int g = 0; g < A.top_groups; ++g) {
-            least = lanes_max<32>(left);
+            least = lanes_max(left);
             if (left == least) left = 0;
         }
-        const uint32_t next = lanes_max<32>(left);
+        const uint32_t next = lanes_max(left);
         taken = least && key >= least;
-        return __popc(__ballot_sync(kFullMask, taken && lane % per == 0)) == A.top_groups && (!next || key_value(least) - key_value(next) > far);
+        return __popc(__ballot_sync(kFullMask, taken && sub == 0)) == A.top_groups && (!next || key_value(least) - key_value(next) > far);
+    };
+    auto load = [&](int64_t t, float(&x)[N]) {
+        if (A.vec) {
+            load_logits<F32, N>(A, t, e0, x);
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) x[j] = j < mine_n ? load1<F32>(A.x, t * A.ld + e0 + j) : -INFINITY;
+        }
     };
     const uint32_t tokens = uint32_t(A.tokens), step = gridDim.x * kWarps;  // (t + step stays below 2^32)
     uint32_t t = blockIdx.x * kWarps + (threadIdx.x >> 5);
     float x[N];
-    if (t < tokens) load_logits<F32, N>(A, t, true, e0, x);
+    if (t < tokens) load(t, x);
     for (; t < tokens; t += step) {
         float next[N];  // the token after, under way
-        if (t + step < tokens) load_logits<F32, N>(A, t + step, true, e0, next);
+        if (t + step < tokens) load(t + step, next);
         bool fine = true;
         if (full) {
 #pragma unroll
             for (int j = 0; j < N; ++j) fine = fine && fabsf(x[j]) < INFINITY;
         } else {
 #pragma unroll
-            for (int j = 0; j < N; ++j) fine = fine && (fabsf(x[j]) < INFINITY || e0 + j >= A.E);
+            for (int j = 0; j < N; ++j) fine = fine && (fabsf(x[j]) < INFINITY || j >= mine_n);
         }
         bool easy = __all_sync(kFullMask, fine);
         float row_max = 0.f;
@@ -393,7 +484,7 @@ __global__ void __launch_bounds__(kThreads, N == 16 ? 2 : 3) k_gate_wide(const _
             float m = x[0];
 #pragma unroll
             for (int j = 1; j < N; ++j) m = fmaxf(m, x[j]);
-            row_max = key_value(lanes_max<32>(order_key(m)));
+            row_max = key_value(lanes_max(order_key(m)));
         }
         float c[N];  // what experts are chosen by
         bool taken = true;
@@ -412,7 +503,7 @@ __global__ void __launch_bounds__(kThreads, N == 16 ? 2 : 3) k_gate_wide(const _
 #pragma unroll
             for (int j = 0; j < N; ++j) {
                 float s = SCORE == kSigmoid ? quick_sigmoid(x[j]) + bias[j] : quick_exp(x[j] - row_max);
-                if (!full && e0 + j >= A.E) s = -INFINITY;
+                if (!full && j >= mine_n) s = -INFINITY;
                 a2 = fmaxf(fminf(a1, s), a2);
                 a1 = fmaxf(a1, s);
                 c[j] = biased ? s : x[j];
@@ -426,14 +517,15 @@ __global__ void __launch_bounds__(kThreads, N == 16 ? 2 : 3) k_gate_wide(const _
                 easy = take_groups(a, 6.f * off, taken) && easy;
             }
         }
-        float top = c[0];
+        float top = -INFINITY, second = -INFINITY;
 #pragma unroll
-        for (int j = 1; j < N; ++j) top = fmaxf(top, c[j]);
-        uint32_t left = taken && choosable(top) ? order_key(top) : 0u, best = 0, first = 0;
+        for (int j = 0; j < N; ++j) merge_two(top, second, c[j], -INFINITY);
+        uint32_t left = taken && choosable(top) ? order_key(top) : 0u, then = taken && choosable(second) ? order_key(second) : 0u;
+        uint32_t best = 0, first = 0;
         for (int i = 0; i < A.k; ++i) {
-            best = lanes_max<32>(left);
+            best = lanes_max(left);
             if (i == 0) first = best;
-            if (left == best) left = 0;
+            if (left == best) left = then, then = 0;
         }
         float least = best ? key_value(best) : -INFINITY;
         if (biased) least -= 2.f * off;
@@ -456,7 +548,7 @@ __global__ void __launch_bounds__(kThreads, N == 16 ? 2 : 3) k_gate_wide(const _
         }
         __syncwarp();
         if (!easy || n > 32) {
-            route_hard_token<F32, N>(A, t, hist);
+            route_hard_token<F32, N>(A, t, hist, rows[threadIdx.x >> 5]);
         } else {
             Cand own{-INFINITY, -1, -INFINITY, 0.f};
             if (lane < n) own = cand[lane];
@@ -482,12 +574,12 @@ __global__ void __launch_bounds__(kThreads, N == 16 ? 2 : 3) k_gate_wide(const _
                     float sum = 0.f;
 #pragma unroll
                     for (int j = 0; j < N; ++j) sum += expf(x[j] - row_max);
-                    s = expf(own.x - row_max) / lanes_sum<32>(sum);
+                    s = expf(own.x - row_max) / lanes_sum(sum);
                 }
             }
             if (!is) s = 0.f;
             if (A.renorm) {
-                const float sum = lanes_sum<32>(s);
+                const float sum = lanes_sum(s);
                 by = sum == 0.f ? 0.f : A.scale / sum;
             }
             if (rank < A.k) {
@@ -593,18 +685,18 @@ __global__ void __launch_bounds__(kThreads) k_gate_grad_softmax(const __grid_con
             p[j] = lane + 32 * j < A.E ? load1<F32>(A.x, t * A.ld + lane + 32 * j) : -INFINITY;
             m = fmaxf(m, p[j]);
         }
-        m = lanes_max<32>(m);
+        m = lanes_max(m);
         if (m == -INFINITY) m = 0.f;
         float s = 0.f;
 #pragma unroll
         for (int j = 0; j < N; ++j) s += p[j] = expf(p[j] - m);
-        s = lanes_sum<32>(s);
+        s = lanes_sum(s);
         const float r = s == 0.f ? 0.f : 1.f / s;
 #pragma unroll
         for (int j = 0; j < N; ++j) row[lane + 32 * j] = p[j] *= r;
         __syncwarp();
         const float pe = e >= 0 ? row[e] : 0.f;
-        const float dot = lanes_sum<32>(e >= 0 ? g * pe : 0.f);
+        const float dot = lanes_sum(e >= 0 ? g * pe : 0.f);
         __syncwarp();
 #pragma unroll
         for (int j = 0; j < N; ++j) row[lane + 32 * j] = -A.scale * p[j] * dot;
@@ -649,35 +741,45 @@ uint32_t grid_for(int64_t warps, int per_sm) {
     return (uint32_t)(need < 1 ? 1 : need < most ? need : most < 1 ? 1 : most);
 }
 
-bool whole_lanes(const GateArgs &A, int N) { return A.groups == 1 || (A.group_size % N == 0 && ((A.group_size / N) & (A.group_size / N - 1)) == 0); }
-
-template <bool F32, int L, int N>
-cudaError_t launch_gate(const GateArgs &A, cudaStream_t s) {
-    return ops_launch(false, k_gate<F32, L, N>, grid_for((A.tokens + 32 / L - 1) / (32 / L), 4), kThreads,
-                      whole_lanes(A, N) ? 0 : kWarps * kMaxExperts * sizeof(float), s, A);
+template <bool F32, int KM>
+cudaError_t launch_thread(GateArgs &A, cudaStream_t s) {
+    const bool shows = A.bias || (A.groups > 1 && A.group_top == 2);
+    A.warp_floats = 32 * ((A.E | 1) * (shows ? 2 : 1) + (A.groups > 1 ? A.groups | 1 : 0));
+    // one warp to a CTA until that fills the SMs
+    const int64_t need = (A.tokens + 31) / 32, sms = ops_sm_count() > 0 ? ops_sm_count() : 1;
+    const int warps = need > 8 * sms ? 2 : 1;
+    const int64_t ctas = (need + warps - 1) / warps, most = 16 * sms;
+    return ops_launch(false, k_gate_thread<F32, KM>, uint32_t(ctas < 1 ? 1 : ctas < most ? ctas : most), 32 * warps, size_t(warps) * A.warp_floats * sizeof(float), s, A);
 }
 
+// A warp to a token, N experts to a lane (a multiple of 4, so that vectors can be loaded).
 template <bool F32, int N>
-cudaError_t launch_wide(const GateArgs &A, cudaStream_t s) {
+cudaError_t launch_wide(GateArgs &A, bool quick, cudaStream_t s) {
     const bool shows = A.bias || (A.groups > 1 && A.group_top == 2);
-    if (!whole_lanes(A, N) || (A.bias && !A.sigmoid) || (shows && !A.sigmoid && !A.renorm)) return launch_gate<F32, 32, N>(A, s);
     const uint32_t grid = grid_for(A.tokens, N == 16 ? 2 : 3);
+    constexpr uintptr_t kAlign = N * (F32 ? 4 : 2) < 16 ? N * (F32 ? 4 : 2) : 16;
+    // rows on such boundaries; each lane's experts at its lane number times N
+    A.vec = A.E % N == 0 && A.ld * (F32 ? 4 : 2) % kAlign == 0 && ((uintptr_t)A.x & (kAlign - 1)) == 0 &&
+            (!quick || (A.lane_n == N && (A.groups == 1 || A.group_size == A.per * N)));
     auto go = [&](auto k) { return ops_launch(false, k, grid, kThreads, 0, s, A); };
+    if (!quick) return go(k_gate<F32, N>);
     return !shows ? go(k_gate_wide<F32, N, kLogits>) : A.sigmoid ? go(k_gate_wide<F32, N, kSigmoid>) : go(k_gate_wide<F32, N, kSoftmax>);
 }
 
-// Four logits a lane and as few lanes as hold a token; a whole warp for over 64 experts, and where groups are not whole lanes.
 template <bool F32>
 cudaError_t pick_gate(GateArgs &A, cudaStream_t s) {
-    const int es = F32 ? 4 : 2, N = A.E <= 128 ? 4 : A.E <= 256 ? 8 : 16;
-    const uintptr_t align = N * es < 16 ? N * es : 16;
-    A.vec = A.E % N == 0 && A.ld * es % align == 0 && ((uintptr_t)A.x & (align - 1)) == 0;
-    if (A.E <= 16 && whole_lanes(A, 4)) return launch_gate<F32, 4, 4>(A, s);
-    if (A.E <= 32 && whole_lanes(A, 4)) return launch_gate<F32, 8, 4>(A, s);
-    if (A.E <= 64 && whole_lanes(A, 4)) return launch_gate<F32, 16, 4>(A, s);
-    if (A.E <= 128) return launch_wide<F32, 4>(A, s);
-    if (A.E <= 256) return launch_wide<F32, 8>(A, s);
-    return launch_wide<F32, 16>(A, s);
+    if (A.E <= kThreadExperts && A.tokens >= kThreadTokens * A.E)
+        return A.k <= 2 ? launch_thread<F32, 2>(A, s) : A.k <= 4 ? launch_thread<F32, 4>(A, s) : A.k <= 8 ? launch_thread<F32, 8>(A, s)
+             : A.k <= 16 ? launch_thread<F32, 16>(A, s) : launch_thread<F32, 32>(A, s);
+    const bool shows = A.bias || (A.groups > 1 && A.group_top == 2);
+    A.per = 32;
+    while (A.per * A.groups > 32) A.per >>= 1;
+    A.lane_n = (A.group_size + A.per - 1) / A.per;
+    if (A.groups == 1 && A.E % 4 == 0) A.lane_n = A.E <= 128 ? 4 : A.E <= 256 ? 8 : 16;  // vectors
+    // not so: few lanes to large groups; scores that need the row's sum to be chosen by, or to be weights
+    const bool quick = A.lane_n <= 16 && !(A.bias && !A.sigmoid) && !(shows && !A.sigmoid && !A.renorm);
+    const int n = quick ? A.lane_n : (A.E + 31) / 32;
+    return n <= 4 ? launch_wide<F32, 4>(A, quick, s) : n <= 8 ? launch_wide<F32, 8>(A, quick, s) : launch_wide<F32, 16>(A, quick, s);
 }
 
 template <bool F32, int N>

@@ -300,3 +300,66 @@ def test_on_a_side_stream_and_captured():
         torch.cuda.synchronize()
         for a, b in zip(got, want):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("E,k,groups,top_groups", [(1, 1, 1, 1), (2, 2, 1, 1), (6, 1, 2, 1), (8, 2, 1, 1), (8, 8, 1, 1), (15, 4, 3, 2), (24, 3, 8, 4), (33, 20, 1, 1), (47, 4, 1, 1),
+                                                   (48, 16, 16, 6), (64, 6, 1, 1), (64, 32, 2, 2), (64, 8, 32, 5)])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_few_experts_and_many_tokens(E, k, groups, top_groups, score):
+    """Enough tokens for a thread to each: every score, bias, group rule, masks, ties and strides."""
+    T = 601 * E + 77
+    wide = _logits(T, E + 3, E + k, F32, 1.5)
+    bias = 0.2 * torch.randn(E, device="cuda", generator=_gen_of(E))
+    for x in (wide[:, :E].contiguous(), wide[:, 1: E + 1], wide[:, :E].to(BF16)):
+        for group_top in (1, 2) if groups > 1 else (1,):
+            kw = dict(score=score, groups=groups, top_groups=top_groups, group_top=group_top, scale=1.5)
+            _check(x, None, E, k, renorm=False, **kw)
+            _check(x, bias, E, k, renorm=True, **kw)
+    x = wide[:, :E].clone()
+    x[::7, E // 2:] = -math.inf
+    x[::5, ::2] = -math.inf
+    x[::11] = -math.inf
+    for b in (bias, None):
+        if b is None or score == "sigmoid":  # (a softmax with a NaN logit is NaN throughout: then its scores choose nothing)
+            x[3, 0], x[40] = math.nan, math.nan
+        _check(x, b, E, k, score=score, groups=groups, top_groups=top_groups, group_top=1)
+        _check(x, b, E, k, score=score, renorm=False, groups=groups, top_groups=top_groups, group_top=2 if groups > 1 else 1)
+    _check(x.round(), None, E, k, score=score, groups=groups, top_groups=top_groups, group_top=1)  # ties
+    r = S.Router(E, k, score=score)
+    chosen, w, counts = r.route(torch.zeros((T, E), device="cuda"))
+    assert torch.equal(chosen, torch.arange(k, device="cuda", dtype=torch.int32).expand(T, k)) and int(counts.sum()) == T * k
+
+
+def _gen_of(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+@pytest.mark.parametrize("E,groups,top_groups,k", [(65, 5, 2, 9), (96, 8, 4, 5), (352, 8, 4, 6), (396, 4, 2, 15), (480, 32, 9, 12), (510, 3, 2, 8), (300, 12, 12, 32), (511, 7, 3, 4)])
+@pytest.mark.parametrize("group_top", [1, 2])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_groups_of_any_size(E, groups, top_groups, k, group_top, score):
+    """Groups that fill their lanes unevenly, and some that only the general way serves."""
+    x = _logits(800, E, E, F32, 1.0)
+    x[::9, : E // 3] = -math.inf
+    bias = 0.1 * torch.randn(E, device="cuda", generator=_gen_of(groups))
+    for b in (None, bias):
+        for renorm in (True, False):
+            _check(x, b, E, k, score=score, renorm=renorm, groups=groups, top_groups=top_groups, group_top=group_top)
+
+
+@pytest.mark.parametrize("E,k", [(96, 4), (128, 8), (256, 8), (500, 16)])
+def test_near_ties_are_settled_by_fp32_scores(E, k):
+    """Scores that differ by less than quick ones may be off: what is chosen is the largest of the fp32 scores plus bias,
+    the lowest index first, as a plain fp32 evaluation orders them."""
+    x = torch.zeros((400, E), device="cuda") + _logits(1, E, 1, F32, 1e-6) + _logits(400, 1, 2, F32, 1.0)
+    bias = 1e-7 * torch.randn(E, device="cuda", generator=_gen_of(E))
+    s = 1.0 / (1.0 + torch.exp(-x)) + bias
+    chosen, w, _ = S.Router(E, k, score="sigmoid").route(x, bias=bias)
+    assert torch.equal(chosen.long(), _best(s, k)[1])
+    if E % 4 == 0:
+        by = s.view(400, 4, -1)
+        by = _best(by, 2)[0]
+        kept = torch.zeros((400, 4), dtype=torch.bool, device="cuda").scatter_(1, _best(by[..., 0] + by[..., 1], 2)[1], True)
+        want = _best(s.masked_fill(~kept.repeat_interleave(E // 4, dim=1), -math.inf), k)[1]
+        chosen, w, _ = S.Router(E, k, score="sigmoid", groups=4, top_groups=2, group_top=2).route(x, bias=bias)
+        assert torch.equal(chosen.long(), want)

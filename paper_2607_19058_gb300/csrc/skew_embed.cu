@@ -59,22 +59,30 @@ __global__ void __launch_bounds__(kThreads, TF32 ? 5 : 8) k_lookup(const __grid_
     int64_t id = lane < n ? load_id(A.ids, A.wide, t0 + lane) : -1;
     if (id >= A.rows) id = -1;
     if constexpr (VEC) {
-        const int64_t c = c0 + 8 * lane;
-        const bool on = c < A.width;
+        const bool on = c0 + 8 * lane < A.width;
         const uint32_t real = __ballot_sync(kFullMask, id >= 0);
+        // a lane to a token: where its row is; then the row to the lanes
+        const uint64_t mine = reinterpret_cast<uint64_t>(A.table) + (id * A.width + c0) * (TF32 ? 4 : 2);
         Vec8<TF32> v[kLookups];
 #pragma unroll
         for (int b = 0; b < kLookups; ++b) {
-            const int64_t row = __shfl_sync(kFullMask, id, b);
-            if (on && row >= 0) v[b] = load8_cached<TF32>(A.table, row * A.width + c);
+            const char *row = reinterpret_cast<const char *>(__shfl_sync(kFullMask, mine, b));
+            v[b] = Vec8<TF32>{};
+            if (on && (real >> b & 1)) v[b] = load8_cached<TF32>(row, 8 * lane);
         }
+        char *to = static_cast<char *>(A.out) + (t0 * A.ld_out + c0) * (YF32 ? 4 : 2);
 #pragma unroll
-        for (int b = 0; b < kLookups; ++b)
+        for (int b = 0; b < kLookups; ++b, to += A.ld_out * (YF32 ? 4 : 2))
             if (on && b < n) {
-                float y[8];
+                if (TF32 == YF32 && A.scale == 1.f) {  // as it is
+                    st_stream(to + 8 * lane * (YF32 ? 4 : 2), v[b].u[0]);
+                    if constexpr (TF32) st_stream(to + 8 * lane * 4 + 16, v[b].u[1]);
+                } else {
+                    float y[8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) y[k] = real >> b & 1 ? v[b].at(k) * A.scale : 0.f;
-                store8<YF32>(A.out, (t0 + b) * A.ld_out + c, y);
+                    for (int k = 0; k < 8; ++k) y[k] = v[b].at(k) * A.scale;
+                    store8<YF32>(to, 8 * lane, y);
+                }
             }
     } else {
 #pragma unroll
@@ -516,11 +524,38 @@ __global__ void __launch_bounds__(kGradThreads, 5) k_embed_grad(const __grid_con
         const uint32_t v0 = f / A.tiles * 32, share = f - f / A.tiles * A.tiles;
         const uint32_t p = packed(A, v0 + lane < A.rows ? v0 + lane : 0);
         uint32_t empty = __ballot_sync(kFullMask, v0 + lane < A.rows && A.first[p] == A.first[p + 1]);
-        while (empty) {  // runs of rows without tokens: this share of each
-            const int r = __ffs(empty) - 1, n = __ffs(~(empty >> r)) - 1 < 0 ? 32 - r : __ffs(~(empty >> r)) - 1;
-            empty &= r + n < 32 ? ~0u << (r + n) : 0u;
-            const int64_t all = n * A.width, part = (all / A.tiles + 63) / 64 * 64, at = share * part;
-            if (at < all) fill<TF32, BASE>(A, (int64_t(v0) + r) * A.width + at, share + 1 == A.tiles || at + part > all ? all - at : part);
+        if constexpr (VEC) {  // a tile of columns of each
+            const int64_t fc = int64_t(share) * kCols;
+            const int bytes = int(A.width - fc < kCols ? A.width - fc : kCols) * T::kElem;
+            const int64_t row0 = (v0 * A.width + fc) * T::kElem + 16 * lane, pitch = A.width * T::kElem;
+            while (empty) {
+                uint4 v[4][T::kElem / 2];
+                int64_t to[4];
+                uint32_t there[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    there[i] = empty;
+                    to[i] = row0 + (__ffs(empty) - 1) * pitch;
+                    empty &= empty - 1;
+#pragma unroll
+                    for (int j = 0; j < T::kElem / 2; ++j) {
+                        v[i][j] = make_uint4(0, 0, 0, 0);
+                        if (BASE && there[i] && 16 * lane + 512 * j < bytes) v[i][j] = ld_stream(base + to[i] + 512 * j);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < T::kElem / 2; ++j)
+                        if (there[i] && 16 * lane + 512 * j < bytes) st_stream(static_cast<char *>(A.dw) + to[i] + 512 * j, v[i][j]);
+            }
+        } else {
+            while (empty) {  // runs of them: this share of each
+                const int r = __ffs(empty) - 1, n = __ffs(~(empty >> r)) - 1 < 0 ? 32 - r : __ffs(~(empty >> r)) - 1;
+                empty &= r + n < 32 ? ~0u << (r + n) : 0u;
+                const int64_t all = n * A.width, part = (all / A.tiles + 63) / 64 * 64, at = share * part;
+                if (at < all) fill<TF32, BASE>(A, (int64_t(v0) + r) * A.width + at, share + 1 == A.tiles || at + part > all ? all - at : part);
+            }
         }
     }
     if (!own) return;

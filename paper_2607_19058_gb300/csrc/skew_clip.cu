@@ -2,7 +2,7 @@
 //
 //   norm = sqrt(sum g^2), gamma = min(1, max_norm / (norm + 1e-6)), out = gamma g.
 //
-// The tensors are cut into tiles at create time, one table entry each that holds all a CTA needs to know
+// The tensors are cut into tiles, one entry each in a table written at bind that holds all a CTA needs to know
 // (one trip to L2 ahead of the data). Both kernels are bound by memory: the sum of squares reads every
 // gradient once, 2 flops an element; the factor depends on all of them, so clipping reads them again,
 // the last tiles first, which are the ones that L2 still holds.
@@ -31,6 +31,14 @@ struct alignas(16) ClipTile {
     const void *g;
     void *out;
     uint32_t n, flags, zero[2];
+};
+
+// A tensor, cut into `tiles` tiles from `first` on: its first `head` elements, if any, then `step` at a time.
+struct ClipTensor {
+    const char *g;
+    char *out;
+    int64_t numel;
+    uint32_t head, step, flags, first, tiles, zero;
 };
 
 struct ClipArgs {
@@ -177,6 +185,19 @@ __global__ void __launch_bounds__(kThreads) k_clip_norm(const __grid_constant__ 
     }
 }
 
+// Writes the tiles' table: a row of CTAs to a tensor.
+__global__ void __launch_bounds__(kThreads) k_clip_tiles(const ClipTensor *tensors, ClipTile *tiles) {
+    const ClipTensor t = tensors[blockIdx.y];
+    const int64_t ge = t.flags & kGradF32 ? 4 : 2, oe = t.flags & kOutF32 ? 4 : 2;
+    const uint32_t heads = t.head != 0;
+    for (uint32_t i = blockIdx.x * kThreads + threadIdx.x; i < t.tiles; i += gridDim.x * kThreads) {
+        const bool head = i < heads;
+        const int64_t at = head ? 0 : t.head + int64_t(i - heads) * t.step, left = t.numel - at;
+        tiles[t.first + i] = ClipTile{t.g + at * ge, t.out ? t.out + at * oe : nullptr, head ? t.head : uint32_t(left < t.step ? left : t.step),
+                                      head ? (t.flags & ~kVectors) | kNoVectors : t.flags, {0, 0}};
+    }
+}
+
 template <bool GF32, bool OF32>
 __device__ __forceinline__ void scale_tile(const ClipTile &t, uint64_t policy, float gamma) {
     constexpr int kUnits = GF32 ? kBatch / 2 : kBatch;  // under way at a time
@@ -225,10 +246,11 @@ __global__ void __launch_bounds__(kThreads, 4) k_clip_apply(const __grid_constan
 using namespace skew;
 
 struct skew_clip {
-    std::vector<ClipTile> tiles;
+    std::vector<ClipTensor> tensors;
+    uint32_t n_tiles = 0;
     bool writes = true;  // every tensor has an `out`
     uint32_t keep = 0;   // the first of the tiles that skew_clip_apply finds in L2
-    size_t ws_ticket = 0, ws_tiles = 0, ws_bytes = 0;
+    size_t ws_ticket = 0, ws_tensors = 0, ws_tiles = 0, ws_bytes = 0;
     char *ws = nullptr;
     bool bound = false;
     uint32_t norm_ctas = 1, apply_ctas = 1;
@@ -261,42 +283,41 @@ int skew_clip_create(const skew_clip_desc_t *tensors, int32_t n, skew_clip_t **o
     h->writes = writes;
     const int64_t tile_bytes = total < kLargeSet ? kTileBytes : kLargeTileBytes;
     try {
-        h->tiles.reserve(size_t(total / tile_bytes + 2 * int64_t(n)));
+        h->tensors.reserve(n);
         for (int32_t k = 0; k < n; ++k) {
             const skew_clip_desc_t &d = tensors[k];
+            if (!d.numel) continue;
             const int64_t ge = d.flags & SKEW_CLIP_GRAD_FP32 ? 4 : 2, oe = d.flags & SKEW_CLIP_OUT_FP32 ? 4 : 2;
             // The first elements, up to where vectors may start: of both if there is such a place, else of g.
-            const char *g = (const char *)d.grad;
-            char *o = (char *)d.out;
             int64_t head = -1, head_g = 0;
             for (int64_t e = 7; e >= 0; --e) {
-                const bool ga = ((uintptr_t)(g + e * ge) & 15) == 0, oa = ((uintptr_t)(o + e * oe) & 15) == 0;
+                const bool ga = (((uintptr_t)d.grad + e * ge) & 15) == 0, oa = (((uintptr_t)d.out + e * oe) & 15) == 0;
                 if (ga) head_g = e;
                 if (ga && oa) head = e;
             }
-            const bool both = head >= 0;
-            if (!both) head = head_g;
+            const uint32_t flags = d.flags | (head >= 0 ? kVectors : 0u);
+            if (head < 0) head = head_g;
             if (head > d.numel) head = d.numel;
-            auto cut = [&](int64_t at, int64_t count, uint32_t flags) {
-                h->tiles.push_back(ClipTile{g + at * ge, o ? o + at * oe : nullptr, (uint32_t)count, d.flags | flags, {0, 0}});
-            };
-            if (head) cut(0, head, kNoVectors);
-            const int64_t step = tile_bytes / ge;
-            for (int64_t at = head; at < d.numel; at += step) cut(at, d.numel - at < step ? d.numel - at : step, both ? kVectors : 0u);
+            const int64_t step = tile_bytes / ge, tiles = (head > 0) + (d.numel - head + step - 1) / step;
+            h->tensors.push_back(ClipTensor{(const char *)d.grad, (char *)d.out, d.numel, (uint32_t)head, (uint32_t)step, flags, h->n_tiles, (uint32_t)tiles, 0});
+            h->n_tiles += (uint32_t)tiles;
         }
     } catch (...) {
         delete h;
         return ops_fail(SKEW_ENOMEM, "out of host memory");
     }
-    h->keep = (uint32_t)h->tiles.size();
-    for (int64_t bytes = 0; h->keep > 0; --h->keep) {
-        const ClipTile &t = h->tiles[h->keep - 1];
-        bytes += int64_t(t.n) * (t.flags & kGradF32 ? 4 : 2);
-        if (bytes > kKeepBytes) break;
+    h->keep = h->n_tiles;
+    int64_t keep = kKeepBytes / tile_bytes;
+    for (size_t k = h->tensors.size(); k-- > 0 && keep > 0;) {  // whole tiles, a tensor's last and smaller ones among them
+        const int64_t take = h->tensors[k].tiles < keep ? h->tensors[k].tiles : keep;
+        h->keep -= (uint32_t)take;
+        keep -= take;
     }
+    auto after = [](size_t at, size_t bytes) { return (at + bytes + 255) / 256 * 256; };
     h->ws_ticket = kMaxCtas * sizeof(double);
-    h->ws_tiles = h->ws_ticket + 256;
-    h->ws_bytes = (h->ws_tiles + h->tiles.size() * sizeof(ClipTile) + 255) / 256 * 256;
+    h->ws_tensors = h->ws_ticket + 256;
+    h->ws_tiles = after(h->ws_tensors, h->tensors.size() * sizeof(ClipTensor));
+    h->ws_bytes = after(h->ws_tiles, size_t(h->n_tiles) * sizeof(ClipTile));
     *out = h;
     return SKEW_OK;
 }
@@ -320,13 +341,21 @@ int skew_clip_bind(skew_clip_t *h, void *workspace, size_t workspace_bytes, void
         return rc;
     h->bound = false;
     char *ws = (char *)workspace;
-    if ((rc = ops_cuda(cudaMemsetAsync(ws, 0, h->ws_tiles, s), "zero-fill of the workspace"))) return rc;
-    if (!h->tiles.empty() &&
-        (rc = ops_cuda(cudaMemcpyAsync(ws + h->ws_tiles, h->tiles.data(), h->tiles.size() * sizeof(ClipTile), cudaMemcpyHostToDevice, s), "upload of the tile table")))
-        return rc;
+    if ((rc = ops_cuda(cudaMemsetAsync(ws, 0, h->ws_tensors, s), "zero-fill of the workspace"))) return rc;
+    if (!h->tensors.empty()) {
+        if ((rc = ops_cuda(cudaMemcpyAsync(ws + h->ws_tensors, h->tensors.data(), h->tensors.size() * sizeof(ClipTensor), cudaMemcpyHostToDevice, s), "upload of the tensors")))
+            return rc;
+        // (a grid holds 65535 rows)
+        for (size_t k = 0; k < h->tensors.size(); k += 65535) {
+            const size_t rows = h->tensors.size() - k < 65535 ? h->tensors.size() - k : 65535;
+            k_clip_tiles<<<dim3(rows < 64 ? 32 : 4, (uint32_t)rows), kThreads, 0, s>>>(reinterpret_cast<const ClipTensor *>(ws + h->ws_tensors) + k,
+                                                                                       reinterpret_cast<ClipTile *>(ws + h->ws_tiles));
+            if ((rc = ops_cuda(cudaGetLastError(), "k_clip_tiles"))) return rc;
+        }
+    }
     if ((rc = ops_cuda(cudaStreamSynchronize(s), "bind"))) return rc;
     auto ctas = [&](int occ) {
-        const uint64_t most = uint64_t(sms > 0 ? sms : 1) * (occ > 0 ? occ : 1), n = h->tiles.size();
+        const uint64_t most = uint64_t(sms > 0 ? sms : 1) * (occ > 0 ? occ : 1), n = h->n_tiles;
         const uint64_t c = n < most ? n : most;
         return (uint32_t)(c < 1 ? 1 : c < kMaxCtas ? c : kMaxCtas);
     };
@@ -346,7 +375,7 @@ static int clip_args(skew_clip_t *h, float max_norm, float *result, ClipArgs &A)
     A.part = reinterpret_cast<double *>(h->ws);
     A.ticket = reinterpret_cast<uint32_t *>(h->ws + h->ws_ticket);
     A.result = result;
-    A.n_tiles = (uint32_t)h->tiles.size();
+    A.n_tiles = h->n_tiles;
     A.keep = A.n_tiles;
     A.max_norm = max_norm;
     return SKEW_OK;

@@ -437,21 +437,30 @@ class GradClip:
         outs = grads if out is None else list(out)
         if len(outs) != len(grads):
             raise ValueError("out must have one tensor for each gradient")
-        descs: List[ClipDesc] = []
-        for g, o in zip(grads, outs):
-            if g.dtype not in (torch.bfloat16, torch.float32) or o.dtype not in (torch.bfloat16, torch.float32):
+        f32, kinds = torch.float32, {torch.bfloat16: 0, torch.float32: CLIP_GRAD_FP32}
+        first = grads[0].device if grads else None
+        descs = (ClipDesc * max(1, len(grads)))()
+        for d, g, o in zip(descs, grads, outs):
+            flags = kinds.get(g.dtype)
+            if flags is None or o.dtype not in kinds:
                 raise TypeError("gradients must be bf16 or fp32")
-            if o.dtype == torch.float32 and g.dtype != torch.float32:
-                raise TypeError("a bf16 gradient is clipped to bf16")
-            if not (g.is_cuda and o.is_cuda and g.is_contiguous() and o.is_contiguous()):
+            if o.dtype == f32:
+                if not flags:
+                    raise TypeError("a bf16 gradient is clipped to bf16")
+                flags |= CLIP_OUT_FP32
+            if not (g.is_cuda and g.is_contiguous()):
                 raise ValueError("gradients must be contiguous CUDA tensors")
-            if g.shape != o.shape or g.device != o.device or g.device != grads[0].device:
-                raise ValueError("gradient and out must have one shape, and all tensors one device")
-            descs.append(ClipDesc(g.data_ptr(), o.data_ptr(), g.numel(),
-                                  (CLIP_GRAD_FP32 if g.dtype == torch.float32 else 0) |
-                                  (CLIP_OUT_FP32 if o.dtype == torch.float32 else 0), 0))
+            if g.device != first:
+                raise ValueError("all tensors must be on one device")
+            d.grad = p = g.data_ptr()
+            if o is not g:
+                if not (o.is_contiguous() and g.shape == o.shape and o.device == first):
+                    raise ValueError("out must be contiguous CUDA tensors of the gradients' shapes, on their device")
+                p = o.data_ptr()
+            d.out, d.numel, d.flags = p, g.numel(), flags
         self.grads, self.out = grads, outs
-        self.h = skew_clip_create(descs)
+        self.h = C.c_void_p()
+        _check_op(load().skew_clip_create(descs, len(grads), C.byref(self.h)))
         dev = grads[0].device if grads else torch.device("cuda")
         n = skew_clip_workspace_bytes(self.h)
         self.workspace = torch.empty(n, dtype=torch.uint8, device=dev)

@@ -505,7 +505,7 @@ typedef struct {
 } skew_embed_config_t;
 
 /*
- * tokens: 0 to 2^31 - 1 ids, contiguous. out: `tokens` rows of `width` elements, `ld_out` >= width
+ * tokens: 0 to 2^30 ids, contiguous. out: `tokens` rows of `width` elements, `ld_out` >= width
  * elements apart. Pointers aligned to their types (rows that start on 16-byte boundaries, of a
  * width that 8 divides, enable vector accesses). Errors: SKEW_EINVAL, SKEW_ECUDA.
  */

@@ -5,7 +5,8 @@
 // The tensors are cut into tiles, one entry each in a table written at bind that holds all a CTA needs to know
 // (one trip to L2 ahead of the data). Both kernels are bound by memory: the sum of squares reads every
 // gradient once, 2 flops an element; the factor depends on all of them, so clipping reads them again,
-// the last tiles first, which are the ones that L2 still holds.
+// the last tiles first, which are the ones that L2 still holds. One GB300: norm of 13.6 GB in 408 tensors
+// 1.81 ms (7.5 TB/s); norm and clipping of 168 MB 74 us, of 1.07 GB of fp32 to bf16 397 us (2.6 GB, 6.6 TB/s).
 #include "skew_ops.h"
 
 #include <cmath>
@@ -22,6 +23,7 @@ constexpr int kBatch = 4;             // 8-element units a thread loads before i
 // Bytes of gradient in a tile: smaller ones where tiles are few for the SMs, larger ones where reading the table tells
 // (16 and 32 KiB, us: norm of 13.6 GB 1854 1810, norm and clipping of 1.07 GB of fp32 399 410).
 constexpr int64_t kTileBytes = 16384, kLargeTileBytes = 32768, kLargeSet = int64_t(2) << 30;
+// What the norm's pass asks L2 to keep for clipping (0, 48, 64, 96 and 112 MiB, us for 168 MB: 81.8 77.6 77.7 78.9 79.5).
 constexpr int64_t kKeepBytes = 64 << 20;
 
 enum : uint32_t { kGradF32 = SKEW_CLIP_GRAD_FP32, kOutF32 = SKEW_CLIP_OUT_FP32, kVectors = 4u, kNoVectors = 8u };
@@ -274,10 +276,9 @@ int skew_clip_create(const skew_clip_desc_t *tensors, int32_t n, skew_clip_t **o
         if ((uintptr_t)d.grad & (ge - 1) || (uintptr_t)d.out & (oe - 1)) return ops_fail(SKEW_EINVAL, "tensor %d: pointers must be aligned to their type", k);
         if (d.out == d.grad && d.grad && oe != ge) return ops_fail(SKEW_EINVAL, "tensor %d: in place needs one type", k);
         if (d.numel) (d.out ? reads_only : writes) = false;
-        total += d.numel * ge;
+        if ((total += d.numel * ge) > int64_t(1) << 46) return ops_fail(SKEW_EINVAL, "too many elements");
     }
     if (!writes && !reads_only) return ops_fail(SKEW_EINVAL, "`out` is given for some tensors and not for others");
-    if (total > int64_t(1) << 46) return ops_fail(SKEW_EINVAL, "too many elements");
     skew_clip *h = new (std::nothrow) skew_clip();
     if (!h) return ops_fail(SKEW_ENOMEM, "out of host memory");
     h->writes = writes;

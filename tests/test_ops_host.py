@@ -177,3 +177,13 @@ def test_embedding_refuses():
         e.lookup(torch.zeros((10, 8), dtype=torch.bfloat16), torch.zeros(3))
     with pytest.raises(ValueError):
         e.lookup(torch.zeros((10, 8), dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int64))
+
+
+def test_clip_refuses_more_than_it_can_count():
+    many = [S.ClipDesc(0x1000, 0, 1 << 40, S.CLIP_GRAD_FP32, 0)] * 17
+    _refused(S.SKEW_EINVAL, "too many", S.skew_clip_create, many)
+
+
+def test_embed_refuses_too_many_tokens():
+    _refused(S.SKEW_EINVAL, "tokens", S.skew_embed_lookup, _embed(), 0x1000, 0x1000, (1 << 30) + 1, 0x1000, 16, 0)
+    assert S.skew_embed_workspace_bytes(_embed(), 1 << 30) > 0

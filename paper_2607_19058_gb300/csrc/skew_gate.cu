@@ -4,7 +4,7 @@
 // (k_gate_thread), else a warp to a token, N consecutive logits a lane (k_gate_wide), with
 // route_token for what that does not settle. Experts are chosen by the logits themselves, or by fp32
 // scores plus biases, never by quicker ones; the lowest index first among equals.
-// One GB300, 65536 tokens: 8 of 256 experts in 4 of 8 groups, sigmoid scores and a bias, 58 us (694 instructions a token and
+// One GB300, 65536 tokens: 8 of 256 experts in 4 of 8 groups, sigmoid scores and a bias, 57 us (681 instructions a token and
 // warp; 98 us with fp32 scores throughout and the k largest one after another); 6 of 64 22 us; 2 of 8 8 us.
 //
 // Backward: as many lanes as top_k, rounded up to a power of two, own a token, one chosen expert each. Only the
@@ -489,7 +489,7 @@ __global__ void __launch_bounds__(kThreads, N == 16 ? 2 : 3) k_gate_wide(const _
             for (int j = 1; j < N; ++j) m = fmaxf(m, x[j]);
             row_max = key_value(lanes_max(order_key(m)));
         }
-        float c[N];  // what experts are chosen by
+        float c[N], top = -INFINITY, second = -INFINITY;  // what experts are chosen by, and the lane's two largest
         bool taken = true;
         if constexpr (SCORE == kLogits) {
 #pragma unroll
@@ -507,10 +507,11 @@ __global__ void __launch_bounds__(kThreads, N == 16 ? 2 : 3) k_gate_wide(const _
             for (int j = 0; j < N; ++j) {
                 float s = SCORE == kSigmoid ? quick_sigmoid(x[j]) + bias[j] : quick_exp(x[j] - row_max);
                 if (!full && j >= mine_n) s = -INFINITY;
-                a2 = fmaxf(fminf(a1, s), a2);
-                a1 = fmaxf(a1, s);
+                merge_two(a1, a2, s, -INFINITY);
                 c[j] = biased ? s : x[j];
             }
+            top = a1;
+            second = a2;
             if (A.groups > 1) {
                 for (int d = 1; d < per; d <<= 1) {
                     const float b1 = __shfl_xor_sync(kFullMask, a1, d), b2 = __shfl_xor_sync(kFullMask, a2, d);
@@ -520,9 +521,11 @@ __global__ void __launch_bounds__(kThreads, N == 16 ? 2 : 3) k_gate_wide(const _
                 easy = take_groups(a, 6.f * off, taken) && easy;
             }
         }
-        float top = -INFINITY, second = -INFINITY;
+        if (!biased) {
+            top = second = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < N; ++j) merge_two(top, second, c[j], -INFINITY);
+            for (int j = 0; j < N; ++j) merge_two(top, second, c[j], -INFINITY);
+        }
         uint32_t left = taken && choosable(top) ? order_key(top) : 0u, then = taken && choosable(second) ? order_key(second) : 0u;
         uint32_t best = 0, first = 0;
         for (int i = 0; i < A.k; ++i) {

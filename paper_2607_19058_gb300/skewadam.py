@@ -388,6 +388,12 @@ def _stream_of(stream, device) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _on(stream):
+    """A context in which a stream (or its raw handle) is torch's current one."""
+    import torch
+    return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
+
+
 _current = None
 
 
@@ -521,7 +527,7 @@ class Embedding:
         self._shape = (rows, width)
         self._new, self._lookup, self._grad = _allocator(), load().skew_embed_lookup, load().skew_embed_grad
         self._stream = _raw_stream()
-        self.workspace, self._sizes = None, {}
+        self.workspace, self._sizes, self._kept = None, {}, []
 
     def _ids(self, ids):
         c = self._ref.get(ids.dtype)
@@ -537,13 +543,15 @@ class Embedding:
         return t.data_ptr()
 
     def lookup(self, table, ids, stream=None):
-        """scale * table[ids], of shape ids.shape + (width,)."""
+        """scale * table[ids], of shape ids.shape + (width,). With ``stream`` the result belongs to that stream."""
+        if stream is not None:
+            with _on(stream):
+                return self.lookup(table, ids)
         c, dev = self._ids(ids), ids.device
         p = self._table(table, dev, "table")
         n, d = ids.numel(), self.width
         out = self._new((n, d), (d, 1), self.act_dtype, dev)
-        rc = self._lookup(c, p, ids.data_ptr(), n, out.data_ptr(), d,
-                          self._stream(dev.index) if stream is None else _stream_of(stream, dev))
+        rc = self._lookup(c, p, ids.data_ptr(), n, out.data_ptr(), d, self._stream(dev.index))
         if rc:
             _check_op(rc)
         return out if ids.dim() == 1 else out.view(*ids.shape, d)
@@ -553,6 +561,9 @@ class Embedding:
         have rows apart). ``base``: what it adds to; ``out``: where it goes (``base`` itself: in place, and rows
         without tokens are not touched; None: a new tensor). Calls on one object share a
         workspace: they must not overlap on the GPU."""
+        if stream is not None:
+            with _on(stream):
+                return self.grad(ids, dy, base, out)
         c, dev, n = self._ids(ids), ids.device, ids.numel()
         if dy.dtype != self.act_dtype or dy.shape != (*ids.shape, self.width) or dy.device != dev:
             raise ValueError(f"dy must be a {(*ids.shape, self.width)} {self.act_dtype} tensor on the ids' device")
@@ -569,9 +580,10 @@ class Embedding:
             need = self._sizes[n] = skew_embed_workspace_bytes(self.config[ids.dtype], n)
         if ws is None or ws.numel() < need or ws.device != dev:
             import torch
+            self._kept.append(ws)  # a graph, or work on another stream, may still use it
+            need = max(need, 0 if ws is None else 3 * ws.numel() // 2)
             ws = self.workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-        rc = self._grad(c, ids.data_ptr(), n, dy.data_ptr(), ld, b, p, ws.data_ptr(), need,
-                        self._stream(dev.index) if stream is None else _stream_of(stream, dev))
+        rc = self._grad(c, ids.data_ptr(), n, dy.data_ptr(), ld, b, p, ws.data_ptr(), need, self._stream(dev.index))
         if rc:
             _check_op(rc)
         return out
@@ -623,7 +635,10 @@ class Router:
     def route(self, logits, bias=None, stream=None):
         """(chosen int32 (T, k), weights fp32 (T, k), counts int32 (experts,)) of (T, experts) logits, whose rows
         may lie apart. ``bias``: fp32 (experts,), added to the scores for the choice alone. Calls on one
-        object share a workspace: they must not overlap on the GPU."""
+        object share a workspace: they must not overlap on the GPU. With ``stream`` the results belong to that stream."""
+        if stream is not None:
+            with _on(stream):
+                return self.route(logits, bias)
         c, ld, T, dev = self._logits(logits)
         k, new, ws = self.top_k, self._new, self.workspace
         if bias is not None:
@@ -632,25 +647,30 @@ class Router:
             bias = bias.data_ptr()
         if ws is None or ws.device != dev:
             import torch
+            if torch.cuda.is_current_stream_capturing():  # the zeros would be the graph's, and not there before it runs
+                raise SkewError(SKEW_ESTATE, "a Router's first call cannot be captured")
             ws = self.workspace = torch.zeros(self._ws_bytes, dtype=torch.uint8, device=dev)
         chosen = new((T, k), (k, 1), self._i32, dev)
         weights = new((T, k), (k, 1), self._f32, dev)
         counts = new((self.experts,), (1,), self._i32, dev)
         rc = self._forward(c, logits.data_ptr(), ld, bias, T, chosen.data_ptr(), weights.data_ptr(), counts.data_ptr(),
-                           ws.data_ptr(), self._ws_bytes, self._stream(dev.index) if stream is None else _stream_of(stream, dev))
+                           ws.data_ptr(), self._ws_bytes, self._stream(dev.index))
         if rc:
             _check_op(rc)
         return chosen, weights, counts
 
     def grad(self, logits, chosen, dweights, stream=None):
         """The logits' gradient, (T, experts) of their type, from the weights' gradient (T, k) fp32."""
+        if stream is not None:
+            with _on(stream):
+                return self.grad(logits, chosen, dweights)
         c, ld, T, dev = self._logits(logits)
         for t, dt in ((chosen, self._i32), (dweights, self._f32)):
             if not (t.dtype == dt and t.shape == (T, self.top_k) and t.is_contiguous() and t.device == dev):
                 raise ValueError(f"chosen and dweights must be contiguous ({T}, {self.top_k}) int32 and fp32 tensors on the logits' device")
         dlogits = self._new((T, self.experts), (self.experts, 1), logits.dtype, dev)
         rc = self._grad(c, logits.data_ptr(), ld, chosen.data_ptr(), dweights.data_ptr(), T, dlogits.data_ptr(),
-                        self.experts, self._stream(dev.index) if stream is None else _stream_of(stream, dev))
+                        self.experts, self._stream(dev.index))
         if rc:
             _check_op(rc)
         return dlogits

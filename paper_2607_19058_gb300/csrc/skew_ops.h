@@ -118,15 +118,6 @@ __device__ __forceinline__ const char *elem_ptr(const void *p, int64_t i) {
 }
 
 template <bool F32>
-__device__ __forceinline__ Vec8<F32> load8(const void *p, int64_t i) {
-    const char *q = elem_ptr<F32>(p, i);
-    Vec8<F32> v;
-    v.u[0] = ld_stream(q);
-    if constexpr (F32) v.u[1] = ld_stream(q + 16);
-    return v;
-}
-
-template <bool F32>
 __device__ __forceinline__ Vec8<F32> load8_cached(const void *p, int64_t i) {  // likely read again
     const uint4 *q = reinterpret_cast<const uint4 *>(elem_ptr<F32>(p, i));
     Vec8<F32> v;

@@ -52,6 +52,9 @@ __device__ __forceinline__ bool choosable(float x) { return x > -INFINITY; }  //
 
 __device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
 
+// A chosen score over the chosen ones' sum, at most 1: the scale comes after it, as the scale over a sum of tiny scores may leave fp32.
+__device__ __forceinline__ float share_of(float s, float sum) { return sum == 0.f ? 0.f : s / sum; }
+
 __device__ __forceinline__ uint32_t lanes_max(uint32_t v) { return __reduce_max_sync(kFullMask, v); }
 
 __device__ __forceinline__ float lanes_max(float v) {
@@ -201,14 +204,10 @@ __device__ __forceinline__ void route_token(const GateArgs &A, int64_t t, int32_
         const float top = A.renorm ? lanes_max(xc) : row_max;  // renormalised: the softmax of the chosen
         if (mine >= 0) s = A.renorm ? expf(xc - top) : expf(xc - top) / row_sum;
     }
-    float by = A.scale;
-    if (A.renorm) {
-        const float sum = lanes_sum(s);
-        by = sum == 0.f ? 0.f : A.scale / sum;
-    }
+    if (A.renorm) s = share_of(s, lanes_sum(s));
     if (lane < A.k) {
         A.chosen[t * A.k + lane] = mine;
-        A.weights[t * A.k + lane] = nan ? NAN : s * by;
+        A.weights[t * A.k + lane] = nan ? NAN : s * A.scale;
         if (A.counts && mine >= 0) atomicAdd(hist + mine, 1);
     }
 }
@@ -370,7 +369,9 @@ __global__ void __launch_bounds__(64) k_gate_thread(const __grid_constant__ Gate
             s[j] = A.sigmoid ? sigmoid(s[j]) : which[j] < 0 ? 0.f : A.renorm ? expf(s[j] - top) : expf(s[j] - top) / row_sum;
             sum += s[j];
         }
-        const float factor = !A.renorm ? A.scale : sum == 0.f ? 0.f : A.scale / sum;
+        if (A.renorm)
+#pragma unroll
+            for (int j = 0; j < KM; ++j) s[j] = share_of(s[j], sum);
         if (A.counts && lane < n)
 #pragma unroll
             for (int j = 0; j < KM; ++j)
@@ -384,7 +385,7 @@ __global__ void __launch_bounds__(64) k_gate_thread(const __grid_constant__ Gate
         __syncwarp();
 #pragma unroll
         for (int j = 0; j < KM; ++j)
-            if (j < A.k) rows[lane * A.k + j] = nan ? NAN : s[j] * factor;
+            if (j < A.k) rows[lane * A.k + j] = nan ? NAN : s[j] * A.scale;
         __syncwarp();
         for (int i = lane; i < n * A.k; i += 32) A.weights[t0 * A.k + i] = rows[i];
         __syncwarp();
@@ -572,7 +573,6 @@ __global__ void __launch_bounds__(kThreads, N == 16 ? 2 : 3) k_gate_wide(const _
                     rank += o > own.c || (o == own.c && i < lane);
                 }
             const bool is = lane < n && rank < A.k;
-            float by = A.scale;
             if (!A.sigmoid) {
                 if (A.renorm) {
                     s = expf(own.x - key_value(first));  // the largest of the chosen
@@ -584,14 +584,11 @@ __global__ void __launch_bounds__(kThreads, N == 16 ? 2 : 3) k_gate_wide(const _
                 }
             }
             if (!is) s = 0.f;
-            if (A.renorm) {
-                const float sum = lanes_sum(s);
-                by = sum == 0.f ? 0.f : A.scale / sum;
-            }
+            if (A.renorm) s = share_of(s, lanes_sum(s));
             if (rank < A.k) {
                 const int64_t at = int64_t(t) * A.k + rank;
                 A.chosen[at] = own.e;
-                A.weights[at] = s * by;
+                A.weights[at] = s * A.scale;
                 if (is && A.counts) atomicAdd(hist + own.e, 1);
             }
         }
@@ -662,7 +659,7 @@ __global__ void __launch_bounds__(kThreads) k_gate_grad_chosen(const __grid_cons
         }
         if (A.renorm) {
             const float sum = slots_sum(q, A.kp_log2);
-            q = sum == 0.f ? 0.f : q / sum;
+            q = share_of(q, sum);
             g -= slots_sum(e >= 0 ? g * q : 0.f, A.kp_log2);
         }
         if (e >= 0) store1<F32>(A.dx, t * A.ld_out + e, A.scale * q * g * rest);

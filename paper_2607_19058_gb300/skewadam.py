@@ -10,6 +10,7 @@ CPU fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 import threading
@@ -469,8 +470,9 @@ class GradClip:
         _check_op(load().skew_clip_create(descs, len(grads), C.byref(self.h)))
         dev = grads[0].device if grads else torch.device("cuda")
         n = skew_clip_workspace_bytes(self.h)
-        self.workspace = torch.empty(n, dtype=torch.uint8, device=dev)
-        self.result = torch.zeros(2, dtype=torch.float32, device=dev)
+        with contextlib.nullcontext() if stream is None else _on(stream):  # the stream that fills them: no other's work comes between
+            self.workspace = torch.empty(n, dtype=torch.uint8, device=dev)
+            self.result = torch.zeros(2, dtype=torch.float32, device=dev)
         self.gamma = self.result[1:]
         self._result, self._device = self.result.data_ptr(), self.result.device
         self._norm, self._apply, self._stream = load().skew_clip_norm, load().skew_clip_apply, _raw_stream()

@@ -375,7 +375,8 @@ const char *skew_last_error(const skew_handle_t *h);
 /* ==========================================================================
  * Around the step: what a trainer computes with the tiers' tensors before it.
  *
- * Conventions as above. The entry points below report the reason of a failed
+ * Conventions as above; the tensors and the stream are the current device's. The
+ * entry points below report the reason of a failed
  * call through skew_ops_last_error (per host thread). They neither synchronise
  * nor allocate device memory (skew_clip_bind alone synchronises), and can be
  * captured into a CUDA graph after one call outside of it.

@@ -426,10 +426,24 @@ def _allocator():
     return _fresh
 
 
+def _device_check():
+    """A function that refuses tensors on a device other than the current one, where the library launches;
+    None where there is no other."""
+    import torch
+    if torch.cuda.device_count() < 2:
+        return None
+    current = torch.cuda.current_device
+
+    def check(dev):
+        if dev.index != current():
+            raise ValueError(f"the tensors are on {dev}, the current device is cuda:{current()}")
+    return check
+
+
 class GradClip:
     """The global norm of many gradients, its clip factor, and clipping.
 
-    ``grads``: contiguous bf16 or fp32 CUDA tensors of any shapes. ``out``: where ``clip`` writes
+    ``grads``: contiguous bf16 or fp32 CUDA tensors of any shapes, on the current device. ``out``: where ``clip`` writes
     the clipped gradients, one tensor for each: of the gradient's type, or bf16 for an fp32 one
     (microbatches accumulated in fp32, handed to the step in bf16). ``None``: in place.
 
@@ -465,6 +479,9 @@ class GradClip:
                     raise ValueError("out must be contiguous CUDA tensors of the gradients' shapes, on their device")
                 p = o.data_ptr()
             d.out, d.numel, d.flags = p, g.numel(), flags
+        self._elsewhere = _device_check()
+        if grads and self._elsewhere:
+            self._elsewhere(first)
         self.grads, self.out = grads, outs
         self.h = C.c_void_p()
         _check_op(load().skew_clip_create(descs, len(grads), C.byref(self.h)))
@@ -481,6 +498,8 @@ class GradClip:
 
     def norm(self, max_norm: float, stream=None):
         """[norm, gamma] with gamma = min(1, max_norm / (norm + 1e-6)); the gradients are only read."""
+        if self._elsewhere:
+            self._elsewhere(self._device)
         rc = self._norm(self.h, max_norm, self._result, self._stream(self._index) if stream is None else _stream_of(stream, None))
         if rc:
             _check_op(rc)
@@ -488,6 +507,8 @@ class GradClip:
 
     def clip(self, max_norm: float, stream=None):
         """``norm``, then out = gamma * g for every tensor."""
+        if self._elsewhere:
+            self._elsewhere(self._device)
         rc = self._apply(self.h, max_norm, self._result, self._stream(self._index) if stream is None else _stream_of(stream, None))
         if rc:
             _check_op(rc)
@@ -510,7 +531,7 @@ class Embedding:
 
     ``table_dtype`` (of the table and its gradient) and ``act_dtype`` (of the looked-up rows and their
     gradient) are bf16 or fp32. Ids are int32 or int64, of any shape; one outside [0, rows) is padding: its
-    row is zero and it has no gradient.
+    row is zero and it has no gradient. Tensors are to be on the current device.
     """
 
     def __init__(self, rows: int, width: int, table_dtype=None, act_dtype=None, scale: float = 1.0):
@@ -528,7 +549,7 @@ class Embedding:
         self._ref = {dt: C.byref(c) for dt, c in self.config.items()}
         self._shape = (rows, width)
         self._new, self._lookup, self._grad = _allocator(), load().skew_embed_lookup, load().skew_embed_grad
-        self._stream = _raw_stream()
+        self._stream, self._elsewhere = _raw_stream(), _device_check()
         self.workspace, self._sizes, self._kept = None, {}, []
 
     def _ids(self, ids):
@@ -537,6 +558,8 @@ class Embedding:
             raise TypeError("ids must be int32 or int64")
         if not (ids.is_cuda and ids.is_contiguous()):
             raise ValueError("ids must be a contiguous CUDA tensor")
+        if self._elsewhere:
+            self._elsewhere(ids.device)
         return c
 
     def _table(self, t, dev, what: str):
@@ -604,7 +627,7 @@ class Router:
     ``score``: "softmax" or "sigmoid"; ``renorm``: weights divided by their sum over the chosen;
     ``groups``, ``top_groups``, ``group_top``: experts are first narrowed to the best groups, each by its
     best one or the sum of its best two choices; ``scale``: a factor on the weights. See
-    ``skew_gate_forward`` in the header for the definition, masked experts and ties.
+    ``skew_gate_forward`` in the header for the definition, masked experts and ties. Tensors are to be on the current device.
     """
 
     def __init__(self, experts: int, top_k: int, score: str = "softmax", renorm: bool = True, groups: int = 1,
@@ -623,6 +646,7 @@ class Router:
         self._ref = {dt: C.byref(c) for dt, c in self.config.items()}
         self._new, self._i32, self._f32 = _allocator(), torch.int32, torch.float32
         self._forward, self._grad, self._stream = load().skew_gate_forward, load().skew_gate_grad, _raw_stream()
+        self._elsewhere = _device_check()
         self.workspace = None
 
     def _logits(self, logits):
@@ -630,9 +654,11 @@ class Router:
         if c is None:
             raise TypeError("logits must be bf16 or fp32")
         T, E = logits.shape if logits.dim() == 2 else (0, 0)
-        if E == self.experts and logits.is_cuda and logits.is_contiguous():
-            return c, E, T, logits.device
-        return c, _rows(logits, self.experts, "logits"), T, logits.device
+        if not (E == self.experts and logits.is_cuda and logits.is_contiguous()):
+            E = _rows(logits, self.experts, "logits")
+        if self._elsewhere:
+            self._elsewhere(logits.device)
+        return c, E, T, logits.device
 
     def route(self, logits, bias=None, stream=None):
         """(chosen int32 (T, k), weights fp32 (T, k), counts int32 (experts,)) of (T, experts) logits, whose rows

@@ -66,3 +66,40 @@ def test_clip_takes_its_buffers_on_the_stream_given(world):
     world.clear()
     S.GradClip([FakeTensor((100,))])
     assert [name for name, _ in world][-1] == "bind" and {stream for _, stream in world} == {"current"}
+
+
+def _calls(monkeypatch):
+    """Each class's calls on stand-ins for tensors of device 0, and a list of what they launch."""
+    launched = []
+    launch = lambda *a: launched.append(a) or 0  # noqa: E731
+    f32, i32 = torch.float32, torch.int32
+    emb, router = S.Embedding(10, 8), S.Router(8, 2)
+    for o in (emb, router):
+        o._new = lambda shape, strides, dtype, device: FakeTensor(shape, dtype, device.index)
+    emb._lookup = emb._grad = router._forward = router._grad = launch
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    clip = S.GradClip([FakeTensor((100,))])
+    clip._norm = clip._apply = launch
+    clip._device = torch.device("cuda", 0)
+    ids, table, dy = FakeTensor((5,), torch.int64), FakeTensor((10, 8)), FakeTensor((5, 8))
+    x, chosen, dw = FakeTensor((5, 8)), FakeTensor((5, 2), i32), FakeTensor((5, 2), f32)
+    return launched, [lambda: clip.norm(1.0), lambda: clip.clip(1.0), lambda: emb.lookup(table, ids), lambda: emb.grad(ids, dy),
+                      lambda: router.route(x), lambda: router.grad(x, chosen, dw), lambda: S.GradClip([FakeTensor((100,))])]
+
+
+def test_tensors_of_another_device_are_refused(world, monkeypatch):
+    """Their stream may be the default one, whose handle is the current device's too: a launch would run there on the others' pointers."""
+    monkeypatch.setattr(torch.cuda, "device_count", lambda: 2)
+    current = [0]
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    launched, calls = _calls(monkeypatch)
+    for k, call in enumerate(calls):
+        call()
+        assert len(launched) == min(k + 1, 6)
+    current[0] = 1
+    for o in (launched, world):
+        o.clear()
+    for call in calls:
+        with pytest.raises(ValueError, match="current device"):
+            call()
+    assert not launched and not world

@@ -550,7 +550,7 @@ class Embedding:
         self._shape = (rows, width)
         self._new, self._lookup, self._grad = _allocator(), load().skew_embed_lookup, load().skew_embed_grad
         self._stream, self._elsewhere = _raw_stream(), _device_check()
-        self.workspace, self._sizes, self._kept = None, {}, []
+        self._workspaces, self._sizes, self._kept = {}, {}, []  # the first: by device
 
     def _ids(self, ids):
         c = self._ref.get(ids.dtype)
@@ -599,15 +599,16 @@ class Embedding:
             p = out.data_ptr()
         else:
             p = self._table(out, dev, "out")
-        ws = self.workspace
+        ws = self._workspaces.get(dev.index)
         need = self._sizes.get(n)
         if need is None:
             need = self._sizes[n] = skew_embed_workspace_bytes(self.config[ids.dtype], n)
-        if ws is None or ws.numel() < need or ws.device != dev:
+        if ws is None or ws.numel() < need:
             import torch
-            self._kept.append(ws)  # a graph, or work on another stream, may still use it
-            need = max(need, 0 if ws is None else 3 * ws.numel() // 2)
-            ws = self.workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+            if ws is not None:
+                self._kept.append(ws)  # a graph, or work on another stream, may still use it
+                need = max(need, 3 * ws.numel() // 2)
+            ws = self._workspaces[dev.index] = torch.empty(need, dtype=torch.uint8, device=dev)
         rc = self._grad(c, ids.data_ptr(), n, dy.data_ptr(), ld, b, p, ws.data_ptr(), need, self._stream(dev.index))
         if rc:
             _check_op(rc)
@@ -647,7 +648,7 @@ class Router:
         self._new, self._i32, self._f32 = _allocator(), torch.int32, torch.float32
         self._forward, self._grad, self._stream = load().skew_gate_forward, load().skew_gate_grad, _raw_stream()
         self._elsewhere = _device_check()
-        self.workspace = None
+        self._workspaces = {}  # by device
 
     def _logits(self, logits):
         c = self._ref.get(logits.dtype)
@@ -668,16 +669,16 @@ class Router:
             with _on(stream):
                 return self.route(logits, bias)
         c, ld, T, dev = self._logits(logits)
-        k, new, ws = self.top_k, self._new, self.workspace
+        k, new, ws = self.top_k, self._new, self._workspaces.get(dev.index)
         if bias is not None:
             if not (bias.dtype == self._f32 and bias.shape == (self.experts,) and bias.is_contiguous() and bias.device == dev):
                 raise ValueError("bias must be a contiguous fp32 tensor of one value for each expert, on the logits' device")
             bias = bias.data_ptr()
-        if ws is None or ws.device != dev:
+        if ws is None:
             import torch
             if torch.cuda.is_current_stream_capturing():  # the zeros would be the graph's, and not there before it runs
                 raise SkewError(SKEW_ESTATE, "a Router's first call cannot be captured")
-            ws = self.workspace = torch.zeros(self._ws_bytes, dtype=torch.uint8, device=dev)
+            ws = self._workspaces[dev.index] = torch.zeros(self._ws_bytes, dtype=torch.uint8, device=dev)
         chosen = new((T, k), (k, 1), self._i32, dev)
         weights = new((T, k), (k, 1), self._f32, dev)
         counts = new((self.experts,), (1,), self._i32, dev)

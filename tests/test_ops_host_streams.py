@@ -17,14 +17,21 @@ def lib():
 class FakeTensor:
     """What the wrappers ask a CUDA tensor for."""
 
+    made = 0
+
     def __init__(self, shape, dtype=torch.bfloat16, index=0):
         self.shape, self.dtype, self.device, self.is_cuda = torch.Size(shape), dtype, torch.device("cuda", index), True
+        FakeTensor.made += 1
+        self.at = FakeTensor.made << 20
 
     def is_contiguous(self):
         return True
 
     def data_ptr(self):
-        return 0x10000
+        return self.at
+
+    def __getitem__(self, part):
+        return self
 
     def numel(self):
         return self.shape.numel()
@@ -44,16 +51,17 @@ def world(monkeypatch):
         yield
         current.pop()
 
-    def fake(name, real):
-        def make(shape, dtype=None, device=None, **kw):
+    def fake(name):
+        def make(shape, dtype=None, device=None):
             seen.append((name, current[-1]))
-            return real(shape, dtype=dtype)
+            device = torch.device(device)
+            return FakeTensor((shape,) if isinstance(shape, int) else shape, dtype, device.index or 0)
         return make
 
     monkeypatch.setattr(S, "_on", on)
     monkeypatch.setattr(S, "_raw_stream", lambda: lambda index: current[-1])
-    monkeypatch.setattr(torch, "empty", fake("empty", torch.empty))
-    monkeypatch.setattr(torch, "zeros", fake("zeros", torch.zeros))
+    monkeypatch.setattr(torch, "empty", fake("empty"))
+    monkeypatch.setattr(torch, "zeros", fake("zeros"))
     monkeypatch.setattr(S, "skew_clip_bind", lambda h, ws, n, stream: seen.append(("bind", stream)))
     return seen
 
@@ -80,7 +88,6 @@ def _calls(monkeypatch):
     monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
     clip = S.GradClip([FakeTensor((100,))])
     clip._norm = clip._apply = launch
-    clip._device = torch.device("cuda", 0)
     ids, table, dy = FakeTensor((5,), torch.int64), FakeTensor((10, 8)), FakeTensor((5, 8))
     x, chosen, dw = FakeTensor((5, 8)), FakeTensor((5, 2), i32), FakeTensor((5, 2), f32)
     return launched, [lambda: clip.norm(1.0), lambda: clip.clip(1.0), lambda: emb.lookup(table, ids), lambda: emb.grad(ids, dy),
@@ -103,3 +110,25 @@ def test_tensors_of_another_device_are_refused(world, monkeypatch):
         with pytest.raises(ValueError, match="current device"):
             call()
     assert not launched and not world
+
+
+def test_a_workspace_for_each_device(world, monkeypatch):
+    """A graph may hold each of them, so none is dropped for another device's; and they grow with the tokens alone."""
+    monkeypatch.setattr(torch.cuda, "device_count", lambda: 2)
+    current = [0]
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    launched = _calls(monkeypatch)[0]
+    emb, router = S.Embedding(10, 8), S.Router(8, 2)
+    for o in (emb, router):
+        o._new = lambda shape, strides, dtype, device: FakeTensor(shape, dtype, device.index)
+    emb._grad = router._forward = lambda *a: launched.append(a) or 0
+    world.clear()
+    at = {0: set(), 1: set()}
+    for k in range(20):
+        current[0] = d = k % 2
+        emb.grad(FakeTensor((5,), torch.int64, d), FakeTensor((5, 8), index=d))
+        at[d].add(launched[-1][7])
+        router.route(FakeTensor((5, 8), index=d))
+        at[d].add(launched[-1][8])
+    assert sorted(name for name, _ in world) == ["empty"] * 2 + ["zeros"] * 2
+    assert len(at[0]) == len(at[1]) == 2 and not at[0] & at[1]

@@ -440,6 +440,25 @@ def _device_check():
     return check
 
 
+class _Block:
+    """Device memory that an object keeps between calls, and the raw handles of the streams that may use it: the one it was
+    allocated on and those of ``also_on``."""
+
+    __slots__ = ("tensor", "ptr", "bytes", "streams")
+
+    def __init__(self, tensor, handle: int):
+        self.tensor, self.ptr, self.bytes, self.streams = tensor, tensor.data_ptr(), tensor.numel(), {handle}
+
+    def also_on(self, handle: int):
+        """Work on the current stream, of this handle, uses it: once it is dropped, its memory goes to nobody else before that
+        is done. The allocator asks the stream at that time, so one that torch did not make, and that may be gone, is left out."""
+        import torch
+        stream = torch.cuda.current_stream(self.tensor.device)
+        if not handle or stream.stream_id != handle:  # (the id of a stream from elsewhere is its handle)
+            self.tensor.record_stream(stream)
+        self.streams.add(handle)
+
+
 class GradClip:
     """The global norm of many gradients, its clip factor, and clipping.
 
@@ -449,7 +468,8 @@ class GradClip:
 
     ``norm`` and ``clip`` return ``result``, a device tensor [norm, gamma] that the next call
     overwrites; ``gamma`` is the view of its second element that ``SkewAdam.step`` takes as
-    ``grad_scale``. The tensors are borrowed: they must live, and stay where they are, as long as this object.
+    ``grad_scale``. The tensors are borrowed: they must live, and stay where they are, as long as this object, and it
+    as long as a graph that captured its calls, or work that it was given on a stream torch did not make (a raw handle).
     """
 
     def __init__(self, grads: Iterable, out: Optional[Iterable] = None, stream=None):
@@ -491,16 +511,27 @@ class GradClip:
             self.workspace = torch.empty(n, dtype=torch.uint8, device=dev)
             self.result = torch.zeros(2, dtype=torch.float32, device=dev)
         self.gamma = self.result[1:]
-        self._result, self._device = self.result.data_ptr(), self.result.device
+        self._device = self.result.device
         self._norm, self._apply, self._stream = load().skew_clip_norm, load().skew_clip_apply, _raw_stream()
         self._index = self._device.index
-        skew_clip_bind(self.h, self.workspace.data_ptr(), n, _stream_of(stream, self._device))
+        handle = _stream_of(stream, self._device)
+        self._blocks = _Block(self.workspace, handle), _Block(self.result, handle)
+        self._result, self._streams = self._blocks[1].ptr, self._blocks[1].streams
+        skew_clip_bind(self.h, self._blocks[0].ptr, n, handle)
+
+    def _handle(self, stream) -> int:
+        handle = self._stream(self._index) if stream is None else _stream_of(stream, None)
+        if handle not in self._streams:
+            with contextlib.nullcontext() if stream is None else _on(stream):
+                for b in self._blocks:
+                    b.also_on(handle)
+        return handle
 
     def norm(self, max_norm: float, stream=None):
         """[norm, gamma] with gamma = min(1, max_norm / (norm + 1e-6)); the gradients are only read."""
         if self._elsewhere:
             self._elsewhere(self._device)
-        rc = self._norm(self.h, max_norm, self._result, self._stream(self._index) if stream is None else _stream_of(stream, None))
+        rc = self._norm(self.h, max_norm, self._result, self._handle(stream))
         if rc:
             _check_op(rc)
         return self.result
@@ -509,7 +540,7 @@ class GradClip:
         """``norm``, then out = gamma * g for every tensor."""
         if self._elsewhere:
             self._elsewhere(self._device)
-        rc = self._apply(self.h, max_norm, self._result, self._stream(self._index) if stream is None else _stream_of(stream, None))
+        rc = self._apply(self.h, max_norm, self._result, self._handle(stream))
         if rc:
             _check_op(rc)
         return self.result
@@ -531,7 +562,8 @@ class Embedding:
 
     ``table_dtype`` (of the table and its gradient) and ``act_dtype`` (of the looked-up rows and their
     gradient) are bf16 or fp32. Ids are int32 or int64, of any shape; one outside [0, rows) is padding: its
-    row is zero and it has no gradient. Tensors are to be on the current device.
+    row is zero and it has no gradient. Tensors are to be on the current device. The object must live as long as a graph that
+    captured its calls, or work that it was given on a stream torch did not make (a raw handle).
     """
 
     def __init__(self, rows: int, width: int, table_dtype=None, act_dtype=None, scale: float = 1.0):
@@ -599,17 +631,19 @@ class Embedding:
             p = out.data_ptr()
         else:
             p = self._table(out, dev, "out")
-        ws = self._workspaces.get(dev.index)
+        ws, handle = self._workspaces.get(dev.index), self._stream(dev.index)
         need = self._sizes.get(n)
         if need is None:
             need = self._sizes[n] = skew_embed_workspace_bytes(self.config[ids.dtype], n)
-        if ws is None or ws.numel() < need:
+        if ws is None or ws.bytes < need:
             import torch
             if ws is not None:
                 self._kept.append(ws)  # a graph, or work on another stream, may still use it
-                need = max(need, 3 * ws.numel() // 2)
-            ws = self._workspaces[dev.index] = torch.empty(need, dtype=torch.uint8, device=dev)
-        rc = self._grad(c, ids.data_ptr(), n, dy.data_ptr(), ld, b, p, ws.data_ptr(), need, self._stream(dev.index))
+                need = max(need, 3 * ws.bytes // 2)
+            ws = self._workspaces[dev.index] = _Block(torch.empty(need, dtype=torch.uint8, device=dev), handle)
+        elif handle not in ws.streams:
+            ws.also_on(handle)
+        rc = self._grad(c, ids.data_ptr(), n, dy.data_ptr(), ld, b, p, ws.ptr, need, handle)
         if rc:
             _check_op(rc)
         return out
@@ -628,7 +662,8 @@ class Router:
     ``score``: "softmax" or "sigmoid"; ``renorm``: weights divided by their sum over the chosen;
     ``groups``, ``top_groups``, ``group_top``: experts are first narrowed to the best groups, each by its
     best one or the sum of its best two choices; ``scale``: a factor on the weights. See
-    ``skew_gate_forward`` in the header for the definition, masked experts and ties. Tensors are to be on the current device.
+    ``skew_gate_forward`` in the header for the definition, masked experts and ties. Tensors are to be on the current device. The
+    object must live as long as a graph that captured its calls, or work that it was given on a stream torch did not make (a raw handle).
     """
 
     def __init__(self, experts: int, top_k: int, score: str = "softmax", renorm: bool = True, groups: int = 1,
@@ -669,7 +704,7 @@ class Router:
             with _on(stream):
                 return self.route(logits, bias)
         c, ld, T, dev = self._logits(logits)
-        k, new, ws = self.top_k, self._new, self._workspaces.get(dev.index)
+        k, new, ws, handle = self.top_k, self._new, self._workspaces.get(dev.index), self._stream(dev.index)
         if bias is not None:
             if not (bias.dtype == self._f32 and bias.shape == (self.experts,) and bias.is_contiguous() and bias.device == dev):
                 raise ValueError("bias must be a contiguous fp32 tensor of one value for each expert, on the logits' device")
@@ -678,12 +713,14 @@ class Router:
             import torch
             if torch.cuda.is_current_stream_capturing():  # the zeros would be the graph's, and not there before it runs
                 raise SkewError(SKEW_ESTATE, "a Router's first call cannot be captured")
-            ws = self._workspaces[dev.index] = torch.zeros(self._ws_bytes, dtype=torch.uint8, device=dev)
+            ws = self._workspaces[dev.index] = _Block(torch.zeros(self._ws_bytes, dtype=torch.uint8, device=dev), handle)
+        elif handle not in ws.streams:
+            ws.also_on(handle)
         chosen = new((T, k), (k, 1), self._i32, dev)
         weights = new((T, k), (k, 1), self._f32, dev)
         counts = new((self.experts,), (1,), self._i32, dev)
         rc = self._forward(c, logits.data_ptr(), ld, bias, T, chosen.data_ptr(), weights.data_ptr(), counts.data_ptr(),
-                           ws.data_ptr(), self._ws_bytes, self._stream(dev.index))
+                           ws.ptr, self._ws_bytes, handle)
         if rc:
             _check_op(rc)
         return chosen, weights, counts

@@ -42,3 +42,29 @@ def test_clip_beside_a_backlog(raw):
         clip.norm(1.0)
     torch.cuda.synchronize()
     assert clip.result.tolist() == [norm, gamma]
+
+
+def test_a_dropped_object_keeps_its_memory_until_its_work_is_done():
+    """Work queued on another stream than the one that a workspace was allocated on still counts in it: new tensors of the
+    first stream lie elsewhere. (They are allocated and not written.)"""
+    T, E, V, d = 5000, 40, 300, 96
+    x, ids = torch.randn((T, E), device="cuda"), torch.randint(0, V, (T,), device="cuda")
+    dy = torch.randn((T, d), device="cuda").bfloat16()
+    busy = torch.ones(1 << 28, device="cuda")
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    assert side.stream_id != side.cuda_stream and torch.cuda.ExternalStream(other.cuda_stream).stream_id == other.cuda_stream
+    clip, emb, router = S.GradClip([dy]), S.Embedding(V, d), S.Router(E, 3)
+    call = lambda s=None: (clip.norm(1.0, stream=s), emb.grad(ids, dy, stream=s), router.route(x, stream=s))  # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        _queue(busy)
+    call(side)
+    call(other.cuda_stream)
+    blocks = [clip.workspace, clip.result, *(next(iter(o._workspaces.values())).tensor for o in (emb, router))]
+    sizes, at = [b.untyped_storage().nbytes() for b in blocks], {b.data_ptr() for b in blocks}
+    other.synchronize()
+    del clip, emb, router, call, blocks
+    new = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(4)]
+    assert not at & {t.data_ptr() for t in new}
+    torch.cuda.synchronize()

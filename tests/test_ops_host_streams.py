@@ -17,7 +17,7 @@ def lib():
 class FakeTensor:
     """What the wrappers ask a CUDA tensor for."""
 
-    made = 0
+    made, recorded = 0, []
 
     def __init__(self, shape, dtype=torch.bfloat16, index=0):
         self.shape, self.dtype, self.device, self.is_cuda = torch.Size(shape), dtype, torch.device("cuda", index), True
@@ -32,6 +32,9 @@ class FakeTensor:
 
     def __getitem__(self, part):
         return self
+
+    def record_stream(self, stream):
+        FakeTensor.recorded.append((self.at, stream.cuda_stream))
 
     def numel(self):
         return self.shape.numel()
@@ -76,11 +79,10 @@ def test_clip_takes_its_buffers_on_the_stream_given(world):
     assert [name for name, _ in world][-1] == "bind" and {stream for _, stream in world} == {"current"}
 
 
-def _calls(monkeypatch):
-    """Each class's calls on stand-ins for tensors of device 0, and a list of what they launch."""
+def _objects(monkeypatch):
+    """One of each class, that launch into a list."""
     launched = []
     launch = lambda *a: launched.append(a) or 0  # noqa: E731
-    f32, i32 = torch.float32, torch.int32
     emb, router = S.Embedding(10, 8), S.Router(8, 2)
     for o in (emb, router):
         o._new = lambda shape, strides, dtype, device: FakeTensor(shape, dtype, device.index)
@@ -88,10 +90,15 @@ def _calls(monkeypatch):
     monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
     clip = S.GradClip([FakeTensor((100,))])
     clip._norm = clip._apply = launch
+    return launched, clip, emb, router
+
+
+def _calls(clip, emb, router):
+    """Each class's calls on stand-ins for tensors of device 0."""
     ids, table, dy = FakeTensor((5,), torch.int64), FakeTensor((10, 8)), FakeTensor((5, 8))
-    x, chosen, dw = FakeTensor((5, 8)), FakeTensor((5, 2), i32), FakeTensor((5, 2), f32)
-    return launched, [lambda: clip.norm(1.0), lambda: clip.clip(1.0), lambda: emb.lookup(table, ids), lambda: emb.grad(ids, dy),
-                      lambda: router.route(x), lambda: router.grad(x, chosen, dw), lambda: S.GradClip([FakeTensor((100,))])]
+    x, chosen, dw = FakeTensor((5, 8)), FakeTensor((5, 2), torch.int32), FakeTensor((5, 2), torch.float32)
+    return [lambda: clip.norm(1.0), lambda: clip.clip(1.0), lambda: emb.lookup(table, ids), lambda: emb.grad(ids, dy),
+            lambda: router.route(x), lambda: router.grad(x, chosen, dw), lambda: S.GradClip([FakeTensor((100,))])]
 
 
 def test_tensors_of_another_device_are_refused(world, monkeypatch):
@@ -99,7 +106,8 @@ def test_tensors_of_another_device_are_refused(world, monkeypatch):
     monkeypatch.setattr(torch.cuda, "device_count", lambda: 2)
     current = [0]
     monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
-    launched, calls = _calls(monkeypatch)
+    launched, *objects = _objects(monkeypatch)
+    calls = _calls(*objects)
     for k, call in enumerate(calls):
         call()
         assert len(launched) == min(k + 1, 6)
@@ -117,11 +125,7 @@ def test_a_workspace_for_each_device(world, monkeypatch):
     monkeypatch.setattr(torch.cuda, "device_count", lambda: 2)
     current = [0]
     monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
-    launched = _calls(monkeypatch)[0]
-    emb, router = S.Embedding(10, 8), S.Router(8, 2)
-    for o in (emb, router):
-        o._new = lambda shape, strides, dtype, device: FakeTensor(shape, dtype, device.index)
-    emb._grad = router._forward = lambda *a: launched.append(a) or 0
+    launched, _, emb, router = _objects(monkeypatch)
     world.clear()
     at = {0: set(), 1: set()}
     for k in range(20):
@@ -132,3 +136,43 @@ def test_a_workspace_for_each_device(world, monkeypatch):
         at[d].add(launched[-1][8])
     assert sorted(name for name, _ in world) == ["empty"] * 2 + ["zeros"] * 2
     assert len(at[0]) == len(at[1]) == 2 and not at[0] & at[1]
+
+
+class FakeStream:
+    def __init__(self, handle, stream_id=3):
+        self.cuda_stream, self.stream_id = handle, stream_id
+
+
+def test_memory_that_other_streams_use_is_not_given_away(world, monkeypatch):
+    """Each block that an object keeps is recorded, once, on every stream of torch's that uses it beside its own."""
+    now = [FakeStream(100)]
+    monkeypatch.setattr(S, "_raw_stream", lambda: lambda index: now[0].cuda_stream)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: now[0])
+
+    @contextlib.contextmanager
+    def on(stream):
+        before, now[0] = now[0], stream if hasattr(stream, "cuda_stream") else FakeStream(stream, stream)
+        yield
+        now[0] = before
+
+    monkeypatch.setattr(S, "_on", on)
+    launched, clip, emb, router = _objects(monkeypatch)
+    ids, dy, x = FakeTensor((5,), torch.int64), FakeTensor((5, 8)), FakeTensor((5, 8))
+    both = lambda s=None: (clip.norm(1.0, stream=s), clip.clip(1.0, stream=s), emb.grad(ids, dy, stream=s), router.route(x, stream=s))  # noqa: E731
+    both()
+    FakeTensor.recorded.clear()
+    own = {clip.workspace.at, clip.result.at, launched[-2][7], launched[-1][8]}
+    assert len(own) == 4
+    for _ in range(3):
+        both()
+        both(FakeStream(200))
+        now[0] = FakeStream(300)
+        both()
+        now[0] = FakeStream(0, 0)   # the default stream
+        both()
+        both(400)                   # a raw handle: not torch's to ask later
+        now[0] = FakeStream(100)
+    assert sorted(FakeTensor.recorded) == sorted((at, h) for at in own for h in (200, 300, 0))
+    emb.grad(FakeTensor((5000,), torch.int64), FakeTensor((5000, 8)))  # a larger workspace: a new block
+    emb.grad(ids, dy, stream=FakeStream(200))
+    assert FakeTensor.recorded[-1] == (launched[-1][7], 200) and launched[-1][7] not in own

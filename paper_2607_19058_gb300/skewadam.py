@@ -672,6 +672,8 @@ class Router:
         kinds = {"softmax": GATE_SOFTMAX, "sigmoid": GATE_SIGMOID}
         if score not in kinds:
             raise ValueError("score must be 'softmax' or 'sigmoid'")
+        if not all(-2**31 <= v < 2**31 for v in (experts, top_k, groups, top_groups, group_top)):  # (a C field would keep the low bits)
+            raise ValueError("experts, top_k, groups, top_groups and group_top must fit 32 bits")
         self.experts, self.top_k = experts, top_k
         flags = GATE_RENORM if renorm else 0
         make = lambda f: GateConfig(experts, top_k, groups, top_groups, group_top, kinds[score], scale, f)  # noqa: E731

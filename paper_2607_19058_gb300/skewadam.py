@@ -780,8 +780,9 @@ class SkewAdam:
         self.hp = hp
         self.h = skew_create(descs, hp)
         dev = self.params[0][0].device if self.params else torch.device("cuda")
-        self.state = torch.empty(max(1, skew_state_bytes(self.h)), dtype=torch.uint8, device=dev)
-        self.workspace = torch.empty(max(1, skew_workspace_bytes(self.h)), dtype=torch.uint8, device=dev)
+        with contextlib.nullcontext() if stream is None else _on(stream):  # the stream that fills them: no other's work comes between
+            self.state = torch.empty(max(1, skew_state_bytes(self.h)), dtype=torch.uint8, device=dev)
+            self.workspace = torch.empty(max(1, skew_workspace_bytes(self.h)), dtype=torch.uint8, device=dev)
         skew_bind(self.h, self.state.data_ptr(), skew_state_bytes(self.h), self.workspace.data_ptr(),
                   skew_workspace_bytes(self.h), self._stream(stream))
 

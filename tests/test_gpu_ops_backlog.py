@@ -68,3 +68,22 @@ def test_a_dropped_object_keeps_its_memory_until_its_work_is_done():
     new = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(4)]
     assert not at & {t.data_ptr() for t in new}
     torch.cuda.synchronize()
+
+
+def test_the_default_streams_handle():
+    """0 is the default stream's handle: given for each object and call, and for the optimizer."""
+    g = torch.randn(5000, device="cuda").bfloat16().view(50, 100)
+    clip = S.GradClip([g], stream=0)
+    norm = clip.norm(1.0, stream=0)
+    want = float(g.double().norm())
+    assert abs(float(norm[0]) - want) <= 1e-5 * want
+    ids = torch.arange(50, device="cuda")
+    assert torch.equal(S.Embedding(50, 100).lookup(g, ids, stream=0), g)
+    chosen, _, counts = S.Router(4, 1).route(torch.zeros((30, 4), device="cuda"), stream=0)
+    assert counts.tolist() == [30, 0, 0, 0] and int(chosen.abs().max()) == 0
+    w = [torch.ones_like(g) for _ in range(2)]
+    for t, stream in zip(w, (0, None)):
+        opt = S.SkewAdam([(t, g, S.TIER_BACKBONE)], S.hparams(), stream=stream)
+        opt.step(1, 1e-2, 3, stream=stream)
+        opt.sync_status(stream=stream)
+    assert torch.equal(*w) and not torch.equal(w[0], torch.ones_like(g))

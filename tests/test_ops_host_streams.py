@@ -176,3 +176,13 @@ def test_memory_that_other_streams_use_is_not_given_away(world, monkeypatch):
     emb.grad(FakeTensor((5000,), torch.int64), FakeTensor((5000, 8)))  # a larger workspace: a new block
     emb.grad(ids, dy, stream=FakeStream(200))
     assert FakeTensor.recorded[-1] == (launched[-1][7], 200) and launched[-1][7] not in own
+
+
+def test_the_step_takes_its_buffers_on_the_stream_given(world, monkeypatch):
+    monkeypatch.setattr(S, "skew_bind", lambda h, state, n, ws, m, stream: world.append(("bind", stream)))
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: FakeStream("current"))
+    params = [(FakeTensor((16, 8)), FakeTensor((16, 8)), S.TIER_BACKBONE)]
+    for stream, want in ((7, 7), (None, "current")):
+        world.clear()
+        S.SkewAdam(params, S.hparams(), stream=stream)
+        assert world == [("empty", want), ("empty", want), ("bind", want)]

@@ -52,8 +52,13 @@ __device__ __forceinline__ bool choosable(float x) { return x > -INFINITY; }  //
 
 __device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
 
-// A chosen score over the chosen ones' sum, at most 1: the scale comes after it, as the scale over a sum of tiny scores may leave fp32.
-__device__ __forceinline__ float share_of(float s, float sum) { return sum == 0.f ? 0.f : s / sum; }
+// A chosen score over the chosen ones' sum, at most 1 (0 where that is 0): the scale comes after it, as the scale over a sum of tiny
+// scores may leave fp32. Most lanes have no score, and a numerator of 0 takes the division's long way (us for 65536 tokens, 2 of 128
+// experts and 8 of 256 in 4 of 8 groups: 30.7 and 61.3 without the 1, 28.5 and 58.3 with it).
+__device__ __forceinline__ float share_of(float s, float sum) {
+    const float share = (s == 0.f ? 1.f : s) / sum;
+    return s == 0.f && sum == sum ? 0.f : share;
+}
 
 __device__ __forceinline__ uint32_t lanes_max(uint32_t v) { return __reduce_max_sync(kFullMask, v); }
 
@@ -659,7 +664,7 @@ __global__ void __launch_bounds__(kThreads) k_gate_grad_chosen(const __grid_cons
         }
         if (A.renorm) {
             const float sum = slots_sum(q, A.kp_log2);
-            q = share_of(q, sum);
+            q = sum == 0.f ? 0.f : q / sum;
             g -= slots_sum(e >= 0 ? g * q : 0.f, A.kp_log2);
         }
         if (e >= 0) store1<F32>(A.dx, t * A.ld_out + e, A.scale * q * g * rest);

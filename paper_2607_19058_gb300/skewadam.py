@@ -752,7 +752,8 @@ class SkewAdam:
     A 3-D tensor (E, n, m) is a stack of E matrices (e.g. an MoE layer's experts
     kept in one array), each stepped with its own second-moment factors and clip
     factor. The optimizer state is one device buffer of exactly ``state_bytes``
-    bytes (the paper's closed form); the workspace holds scratch and tables.
+    bytes (the paper's closed form); the workspace holds scratch and tables. Tensors are to be
+    on the current device, and to stay where they are as long as this object.
     """
 
     def __init__(self, params: Iterable, hp: HParams, stream=None):
@@ -777,9 +778,12 @@ class SkewAdam:
                 shape, stack = (int(w.shape[0]), int(w.shape[1]) if w.dim() == 2 else 0), 0
             descs.append(ParamDesc(w.data_ptr(), g.data_ptr(), (C.c_int64 * 2)(*shape), w.dim(), tier, flags, stack))
             self.params.append((w, g))
+        dev = self.params[0][0].device if self.params else torch.device("cuda")
+        self._elsewhere = _device_check()
+        if self.params and self._elsewhere:
+            self._elsewhere(dev)
         self.hp = hp
         self.h = skew_create(descs, hp)
-        dev = self.params[0][0].device if self.params else torch.device("cuda")
         with contextlib.nullcontext() if stream is None else _on(stream):  # the stream that fills them: no other's work comes between
             self.state = torch.empty(max(1, skew_state_bytes(self.h)), dtype=torch.uint8, device=dev)
             self.workspace = torch.empty(max(1, skew_workspace_bytes(self.h)), dtype=torch.uint8, device=dev)
@@ -802,6 +806,8 @@ class SkewAdam:
     def step(self, step: int, lr: float, seed: int, stream=None, grad_scale=None) -> None:
         """One step. `grad_scale`: optional one-element fp32 device tensor gamma (the trainer's
         global gradient-norm clip factor); the step then sees gamma * G."""
+        if self._elsewhere:
+            self._elsewhere(self.state.device)
         if grad_scale is None:
             skew_step(self.h, step, lr, seed, self._stream(stream))
             return

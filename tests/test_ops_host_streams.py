@@ -186,3 +186,23 @@ def test_the_step_takes_its_buffers_on_the_stream_given(world, monkeypatch):
         world.clear()
         S.SkewAdam(params, S.hparams(), stream=stream)
         assert world == [("empty", want), ("empty", want), ("bind", want)]
+
+
+def test_the_step_refuses_tensors_of_another_device(world, monkeypatch):
+    stepped, current = [], [0]
+    monkeypatch.setattr(S, "skew_bind", lambda *a: None)
+    monkeypatch.setattr(S, "skew_step", lambda *a: stepped.append(a))
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: FakeStream(5))
+    monkeypatch.setattr(torch.cuda, "device_count", lambda: 2)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    params = [(FakeTensor((16, 8)), FakeTensor((16, 8)), S.TIER_BACKBONE)]
+    opt = S.SkewAdam(params, S.hparams())
+    opt.step(1, 1e-3, 5)
+    assert len(stepped) == 1
+    current[0] = 1
+    world.clear()
+    with pytest.raises(ValueError, match="current device"):
+        opt.step(2, 1e-3, 5)
+    with pytest.raises(ValueError, match="current device"):
+        S.SkewAdam(params, S.hparams())
+    assert len(stepped) == 1 and not world

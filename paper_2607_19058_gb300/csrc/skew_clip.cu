@@ -5,8 +5,8 @@
 // The tensors are cut into tiles, one entry each in a table written at bind that holds all a CTA needs to know
 // (one trip to L2 ahead of the data). Both kernels are bound by memory: the sum of squares reads every
 // gradient once, 2 flops an element; the factor depends on all of them, so clipping reads them again,
-// the last tiles first, which are the ones that L2 still holds. One GB300: norm of 13.6 GB in 408 tensors
-// 1.81 ms (7.5 TB/s); norm and clipping of 168 MB 74 us, of 1.07 GB of fp32 to bf16 397 us (2.6 GB, 6.6 TB/s).
+// the last tiles first, which are the ones that L2 still holds. One GB300, whole calls: norm of 13.6 GB in 407 tensors
+// 1.78 ms (7.6 TB/s); norm and clipping of 157 MB 76 us (in place 80), of 1.08 GB of fp32 to bf16 397 us (2.7 GB, 6.8 TB/s).
 #include "skew_ops.h"
 
 #include <cmath>
@@ -20,10 +20,11 @@ namespace {
 constexpr int kThreads = 256;
 constexpr uint32_t kMaxCtas = 8192;   // partial sums that the workspace has room for
 constexpr int kBatch = 4;             // 8-element units a thread loads before it uses them
-// Bytes of gradient in a tile: smaller ones where tiles are few for the SMs, larger ones where reading the table tells
-// (16 and 32 KiB, us: norm of 13.6 GB 1854 1810, norm and clipping of 1.07 GB of fp32 399 410).
+// Bytes of gradient in a tile: smaller ones where tiles are few for the SMs, larger ones where reading the table tells. From 1 GB on
+// the norm gains a little by larger tiles and clipping loses a little (16 and 32 KiB, us, for 0.94, 1.75, 3.4, 6.6 and 13 GB of bf16: norm 133.5
+// 132.7, 239.7 238.4, 451 449, 877 868, 1749 1709; norm and clipping 426 430, 787 789, 1505 1519, 2952 2962, 5801 5808).
 constexpr int64_t kTileBytes = 16384, kLargeTileBytes = 32768, kLargeSet = int64_t(2) << 30;
-// What the norm's pass asks L2 to keep for clipping (0, 48, 64, 96 and 112 MiB, us for 168 MB: 81.8 77.6 77.7 78.9 79.5).
+// What the norm's pass asks L2 to keep for clipping (0, 48, 64, 96 and 112 MiB, us for 157 MB, one set: 81.8 77.6 77.7 78.9 79.5).
 constexpr int64_t kKeepBytes = 64 << 20;
 
 enum : uint32_t { kGradF32 = SKEW_CLIP_GRAD_FP32, kOutF32 = SKEW_CLIP_OUT_FP32, kVectors = 4u, kNoVectors = 8u };
@@ -223,6 +224,7 @@ __device__ __forceinline__ void scale_tile(const ClipTile &t, uint64_t policy, f
         for (; u < units; u += kThreads) scale(u, load8_policy<GF32>(t.g, int64_t(u) * 8, policy));
         left += t.n & ~7u;
     }
+    // what 8 does not divide; or all, where g and out lie differently in their 16-byte units (157 MB: 226 us, aligned 76)
     for (uint32_t i = left; i < t.n; i += kThreads) store1<OF32>(t.out, i, load1<GF32>(t.g, i) * gamma);
 }
 

@@ -7,8 +7,8 @@
 // list and kCols columns, and adds up the runs that start there. A run of more places than that (a
 // frequent word) is cut at the chunks' ends into pieces, which the warps that finish last add up in their
 // order. The same warps write the rows without tokens while their copies are under way.
-// One GB300, 50304 x 4096, bf16, 32768 tokens with frequencies of 1 / rank: lookup 57 us (354 MB, 6.2 TB/s), gradient 4 + 9
-// us of sorting and 112 us for 681 MB (6.1 TB/s).
+// One GB300, 50304 x 4096, bf16, 32768 tokens with frequencies of 1 / rank, the kernels alone: lookup 57 us (354 MB, 6.2 TB/s), gradient
+// 4 + 9 us of sorting and 112 us for 681 MB (6.1 TB/s). Whole calls: 59, 125, and 94 where the gradient is added in place.
 #include "skew_ops.h"
 
 #include <cmath>
@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(kThreads, TF32 ? 5 : 8) k_lookup(const __grid_
                     store8<YF32>(to, 8 * lane, y);
                 }
             }
-    } else {
+    } else {  // an element an access (the same lookup with 4095 columns: 133 us)
 #pragma unroll
         for (int b = 0; b < kLookups; ++b) {
             const int64_t row = __shfl_sync(kFullMask, id, b);
@@ -205,6 +205,7 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_split(const __grid_const
 
 // Sorts an owner's tokens by row: counts by (warp, row), each warp its own run of the owner's tokens, then places.
 // Rows are taken kSortRows at a time. SPLIT: the tokens come from k_embed_split's parts, else from the ids themselves.
+// Walking the tokens twice is much of what many tokens of few columns take (126113 of 12777 x 176, fp32: 49 us, the bytes 16).
 template <bool WIDE, bool SPLIT>
 __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const __grid_constant__ EmbedGradArgs A) {
     extern __shared__ uint32_t hist[];  // [warp][row], then each warp's next place
@@ -351,7 +352,8 @@ __device__ __forceinline__ void fill(const EmbedGradArgs &A, int64_t at, int64_t
     for (int64_t i = done + lane; i < count; i += 32) one(i);
 }
 
-// Stores a row's 8 columns of a lane.
+// Stores a row's 8 columns of a lane: without VEC an element at a time, as they are read from shared memory (25090 tokens of 4594 x 4519 to
+// fp32: 101 us, where the bytes take 42).
 template <bool TF32, bool VEC>
 __device__ __forceinline__ void put_row(const EmbedGradArgs &A, int64_t row, int64_t c0, const float (&y)[8]) {
     if constexpr (VEC) {

@@ -4,12 +4,14 @@
 // (k_gate_thread), else a warp to a token, N consecutive logits a lane (k_gate_wide), with
 // route_token for what that does not settle. Experts are chosen by the logits themselves, or by fp32
 // scores plus biases, never by quicker ones; the lowest index first among equals.
-// One GB300, 65536 tokens: 8 of 256 experts in 4 of 8 groups, sigmoid scores and a bias, 57 us (681 instructions a token and
-// warp; 98 us with fp32 scores throughout and the k largest one after another); 6 of 64 22 us; 2 of 8 8 us.
+// One GB300, 65536 tokens, whole calls: 8 of 256 experts in 4 of 8 groups, sigmoid scores and a bias, 58 us (674 instructions a
+// token and warp; 98 us with fp32 scores throughout and the k largest one after another); 8 of 512 by sigmoid scores and a bias 68; 2 of 128 28;
+// 6 of 64 23; 2 of 8 8. What is issued once for a token, and not for an expert, is most of it.
 //
 // Backward: as many lanes as top_k, rounded up to a power of two, own a token, one chosen expert each. Only the
-// softmax that is not renormalised has a gradient elsewhere, and reads whole rows. 65536 tokens, 2 of 128: 11 us
-// (33.5 MB of zeros and 131072 values over them; laid out in shared memory first: 12.4).
+// softmax that is not renormalised has a gradient elsewhere, and reads whole rows. 65536 tokens of 128 experts, whole calls: 2 chosen 13 us
+// (the kernel 11: 33.5 MB of zeros, each sector written by two stores of half of it, and 131072 values over them; laid out
+// in shared memory first 12.4), the plain softmax 21.
 #include "skew_ops.h"
 
 #include <cfloat>
@@ -428,6 +430,7 @@ __device__ __noinline__ void route_hard_token(const GateArgs &A, int64_t t, int3
 // least k values are no less than the k-th of the lanes' two largest each, and few more; a lane to one of those, with its fp32
 // score, ranks it among the others. A token that this does not settle (near ties, a logit that is not finite, over 32
 // such experts) takes route_token.
+// N = 16 spills up to 192 bytes (softmax scores of bf16 logits) at the 128 registers that two CTAs an SM leave.
 // SCORE: kLogits (experts and groups by the logits alone), kSigmoid, kSoftmax (both: quick scores are needed).
 enum { kLogits, kSigmoid, kSoftmax };
 template <bool F32, int N, int SCORE>
@@ -784,7 +787,8 @@ cudaError_t pick_gate(GateArgs &A, cudaStream_t s) {
     while (A.per * A.groups > 32) A.per >>= 1;
     A.lane_n = (A.group_size + A.per - 1) / A.per;
     if (A.groups == 1 && A.E % 4 == 0) A.lane_n = A.E <= 128 ? 4 : A.E <= 256 ? 8 : 16;  // vectors
-    // not so: few lanes to large groups; scores that need the row's sum to be chosen by, or to be weights
+    // not so: few lanes to large groups; scores that need the row's sum to be chosen by, or to be weights (8 of 256 by softmax
+    // scores and a bias, 65536 tokens: 82 us)
     const bool quick = A.lane_n <= 16 && !(A.bias && !A.sigmoid) && !(shows && !A.sigmoid && !A.renorm);
     const int n = quick ? A.lane_n : (A.E + 31) / 32;
     return n <= 4 ? launch_wide<F32, 4>(A, quick, s) : n <= 8 ? launch_wide<F32, 8>(A, quick, s) : launch_wide<F32, 16>(A, quick, s);

@@ -468,7 +468,8 @@ class GradClip:
 
     ``norm`` and ``clip`` return ``result``, a device tensor [norm, gamma] that the next call
     overwrites; ``gamma`` is the view of its second element that ``SkewAdam.step`` takes as
-    ``grad_scale``. The tensors are borrowed: they must live, and stay where they are, as long as this object, and it
+    ``grad_scale``. The tensors are borrowed: they must live, and stay where they are, as long as this object: across steps,
+    as with ``zero_grad(set_to_none=False)`` (a new object costs some 0.2 ms and waits for its stream); and it
     as long as a graph that captured its calls, or work that it was given on a stream torch did not make (a raw handle).
     """
 
@@ -558,7 +559,8 @@ class GradClip:
 
 
 class Embedding:
-    """Lookup of a (rows, width) table by token ids, scaled, and the table's gradient.
+    """Lookup of a (rows, width) table by token ids, scaled, and the table's gradient, which is a call of its
+    own: for autograd a looked-up tensor is a leaf, whether the table requires a gradient or not.
 
     ``table_dtype`` (of the table and its gradient) and ``act_dtype`` (of the looked-up rows and their
     gradient) are bf16 or fp32. Ids are int32 or int64, of any shape; one outside [0, rows) is padding: its
@@ -657,7 +659,8 @@ def _rows(t, width: int, what: str) -> int:
 
 
 class Router:
-    """Routing of tokens to experts (the gate of an MoE layer) and its gradient.
+    """Routing of tokens to experts (the gate of an MoE layer) and its gradient, which is a call of its own (no
+    autograd function: the weights are a leaf).
 
     ``score``: "softmax" or "sigmoid"; ``renorm``: weights divided by their sum over the chosen;
     ``groups``, ``top_groups``, ``group_top``: experts are first narrowed to the best groups, each by its

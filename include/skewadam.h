@@ -378,11 +378,11 @@ const char *skew_last_error(const skew_handle_t *h);
  * Conventions as above; the tensors and the stream are the current device's. The
  * entry points below report the reason of a failed
  * call through skew_ops_last_error (per host thread). They neither synchronise
- * nor allocate device memory (skew_clip_bind alone synchronises), and can be
+ * nor allocate device memory (skew_clip_bind and skew_ops_sync_status alone synchronise), and can be
  * captured into a CUDA graph after one call outside of it.
  * ======================================================================== */
 
-/* One-line reason for the last failure of a skew_clip_*, skew_embed_* or skew_gate_* call on this host thread. */
+/* One-line reason for the last failure of an entry point below on this host thread. */
 const char *skew_ops_last_error(void);
 
 /* ---- global gradient norm and clipping -------------------------------------
@@ -523,6 +523,124 @@ size_t skew_embed_workspace_bytes(const skew_embed_config_t *c, int64_t tokens);
  */
 int skew_embed_grad(const skew_embed_config_t *c, const void *ids, int64_t tokens, const void *dout, int64_t ld_dout,
                     const void *base, void *dtable, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- rows by expert and back ---------------------------------------------------
+ * What lies between the routing and the experts' products. Of the (tokens, top_k) experts that a router chose,
+ *   order         place of (t, j): how many entries go before it, by (expert, t, j); -1 for an entry outside
+ *                 [0, experts). offsets[e]: the first place of expert e; offsets[experts]: how many there are.
+ *   spread        rows[place(t, j)] = x[t]
+ *   combine       out[t] = sum over j of weights[t, j] * rows[place(t, j)]
+ *   combine_grad  drows[place(t, j)] = weights[t, j] * dout[t], dweights[t, j] = <dout[t], rows[place(t, j)]>
+ * The gradient of spread is combine without weights. A row that an entry without a place would read is zero (so is its
+ * dweights); rows from offsets[experts] up to tokens * top_k are written as zeros by spread and combine_grad. Sums are fp32: combine's in the
+ * order of j, so that results do not depend on timing; each element is rounded once.
+ */
+#define SKEW_DISPATCH_TOKENS_FP32 1u /* x, out and dout are fp32 (else bf16)  */
+#define SKEW_DISPATCH_ROWS_FP32 2u   /* rows and drows are fp32 (else bf16)   */
+
+/* experts 1 to 1024, top_k 1 to 64. */
+typedef struct {
+    int32_t experts, top_k;
+    uint32_t flags; /* SKEW_DISPATCH_* */
+    uint32_t zero;  /* 0 */
+} skew_dispatch_config_t;
+
+/* Bytes of device workspace that the order of `tokens` tokens needs (0 for an invalid config). tokens * top_k: at most 2^30. */
+size_t skew_dispatch_workspace_bytes(const skew_dispatch_config_t *c, int64_t tokens);
+/*
+ * chosen, places: (tokens, top_k), contiguous; offsets: experts + 1. workspace: 256-byte aligned, of any content; calls that share one must
+ * not overlap on the GPU. Errors, here and below: SKEW_EINVAL, SKEW_ECUDA.
+ */
+int skew_dispatch_order(const skew_dispatch_config_t *c, const int32_t *chosen, int64_t tokens, int32_t *offsets, int32_t *places, void *workspace,
+                        size_t workspace_bytes, void *stream);
+/*
+ * x: `tokens` rows of `width` elements (1 to 2^20), `ld_x` >= width apart. rows: tokens * top_k rows, contiguous. offsets, places: as skew_dispatch_order
+ * made them (a place outside [0, tokens * top_k) is none). No output may overlap an input. Rows that start on 16-byte boundaries, of a width that 8
+ * divides, enable vector accesses.
+ */
+int skew_dispatch_spread(const skew_dispatch_config_t *c, const void *x, int64_t ld_x, const int32_t *offsets, const int32_t *places, int64_t tokens,
+                         int64_t width, void *rows, void *stream);
+/* weights: (tokens, top_k) fp32, contiguous, or NULL: ones. */
+int skew_dispatch_combine(const skew_dispatch_config_t *c, const void *rows, const float *weights, const int32_t *places, int64_t tokens, int64_t width,
+                          void *out, int64_t ld_out, void *stream);
+int skew_dispatch_combine_grad(const skew_dispatch_config_t *c, const void *dout, int64_t ld_dout, const void *rows, const float *weights,
+                               const int32_t *offsets, const int32_t *places, int64_t tokens, int64_t width, void *drows, float *dweights, void *stream);
+
+/* ---- products grouped by expert -------------------------------------------------
+ * Rows ordered by expert, as skew_dispatch_spread makes them: those of expert e are [offsets[e], offsets[e + 1]), any number
+ * of them. With E = experts matrices W_e of n x m in one array (E, n, m), as a stack of skew_create's:
+ *   product    y[r]  = x[r] W_e                       x (rows, n), y (rows, m)
+ *   grad_rows  dx[r] = dy[r] W_e^T
+ *   grad       dW_e  = base_e + sum over its rows r of x[r]^T dy[r]
+ * x, dy and W are bf16; sums are fp32 on the tensor cores, each result is rounded once. Rows of no expert (before offsets[0] and from
+ * offsets[E] on) give zeros, and enter no dW, whatever they hold. Offsets are read on the device and taken as they come: one
+ * below the one before counts as that one, one beyond `rows` as `rows`. Results do not depend on timing.
+ */
+#define SKEW_EXPERTS_ROWS_FP32 1u /* y and dx are fp32 (else bf16)    */
+#define SKEW_EXPERTS_GRAD_FP32 2u /* base and dW are fp32 (else bf16) */
+
+/* experts 1 to 1024; n, m 1 to 2^20. */
+typedef struct {
+    int32_t experts, n, m;
+    uint32_t flags; /* SKEW_EXPERTS_* */
+} skew_experts_config_t;
+
+/*
+ * rows: 0 to 2^30; x and dy have rows `ld` elements apart (at least their width), y, dx, W and dW are contiguous. offsets: experts + 1. No output may overlap
+ * an input. Pointers aligned to their types; rows that start on 16-byte boundaries (W: n and m that 8 divides) are much quicker. The kernel's waits on
+ * the device are bounded: see skew_ops_sync_status. Errors: SKEW_EINVAL, SKEW_ECUDA.
+ */
+int skew_experts_product(const skew_experts_config_t *c, const void *x, int64_t ld_x, const void *w, const int32_t *offsets, int64_t rows, void *y, void *stream);
+int skew_experts_grad_rows(const skew_experts_config_t *c, const void *dy, int64_t ld_dy, const void *w, const int32_t *offsets, int64_t rows, void *dx,
+                           void *stream);
+/*
+ * base: NULL, a tensor like dW that overlaps nothing else, or dW itself, to which the gradient is then added; matrices of experts without rows are
+ * then not touched.
+ */
+int skew_experts_grad(const skew_experts_config_t *c, const void *x, int64_t ld_x, const void *dy, int64_t ld_dy, const int32_t *offsets, int64_t rows,
+                      const void *base, void *dw, void *stream);
+
+/* ---- the output head's softmax cross entropy, without its logits ------------------
+ * With h (tokens, width), the table W (rows, width) that the embedding may share, and l[t, v] = scale * <h[t], W[v]>:
+ *   lse[t]  = log sum over v of exp(l[t, v])
+ *   loss[t] = lse[t] - l[t, target_t]
+ *   dh[t]   = scale * sum over v of p[t, v] W[v],  dW[v] = base[v] + scale * sum over t of p[t, v] h[t]
+ *   p[t, v] = dloss[t] * (exp(l[t, v] - lse[t]) - [v = target_t])
+ * A target outside [0, rows) is padding: its loss is zero, its dloss is not read, and it enters no gradient. h, W, dh, base and dW
+ * are bf16. l is summed in fp32 and never stored; the gradients take the vocabulary in pieces and make a piece's p from l anew, rounded to bf16 (for the
+ * tensor cores: an error of up to 2^-8 of each term, about that of rounding the result), with sums in fp32. Results do not depend on timing.
+ */
+#define SKEW_HEAD_IDS_64 1u /* targets are int64 (else int32) */
+
+/* rows 1 to 2^24, width 1 to 2^20, scale finite. */
+typedef struct {
+    int64_t rows, width;
+    float scale;
+    uint32_t flags; /* SKEW_HEAD_* */
+} skew_head_config_t;
+
+/* Bytes of device workspace that the loss, or its gradients, of `tokens` tokens (0 to 2^24) need (0 for an invalid config). */
+size_t skew_head_loss_workspace_bytes(const skew_head_config_t *c, int64_t tokens);
+size_t skew_head_grad_workspace_bytes(const skew_head_config_t *c, int64_t tokens);
+/*
+ * h: rows `ld_h` >= width elements apart; table: contiguous; loss, lse: fp32, one for each token. Rows on 16-byte boundaries, of a
+ * width that 8 divides, are much quicker. workspace: 256-byte aligned, of any content; calls that share one must not overlap on the GPU. Waits on the device are
+ * bounded: see skew_ops_sync_status. Errors: SKEW_EINVAL, SKEW_ECUDA.
+ */
+int skew_head_loss(const skew_head_config_t *c, const void *h, int64_t ld_h, const void *table, const void *targets, int64_t tokens, float *loss, float *lse,
+                   void *workspace, size_t workspace_bytes, void *stream);
+/*
+ * lse: as skew_head_loss made it; dloss: fp32, one for each token; dh (tokens, width) and dtable: contiguous. base: NULL, a tensor like dtable that
+ * overlaps nothing else, or dtable itself, to which the gradient is then added (rounded once).
+ */
+int skew_head_grad(const skew_head_config_t *c, const void *h, int64_t ld_h, const void *table, const void *targets, int64_t tokens, const float *lse,
+                   const float *dloss, void *dh, const void *base, void *dtable, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Synchronises `stream` and reports whether a bounded wait on the device, of any skew_experts_* or skew_head_* kernel on the current device, has
+ * given up since the last such call (SKEW_ETIMEOUT; what that call wrote is then not to be used). Errors: also SKEW_ECUDA.
+ */
+int skew_ops_sync_status(void *stream);
 
 #ifdef __cplusplus
 }

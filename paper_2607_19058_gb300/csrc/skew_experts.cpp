@@ -1,0 +1,102 @@
+// The experts' products (skewadam.h): checks, and the products of skew_product.cu that they are.
+#include "skew_ops.h"
+#include "skew_product.h"
+
+namespace skew {
+namespace {
+
+constexpr int64_t kMaxRows = int64_t(1) << 30;
+constexpr int kMaxExperts = 1024;
+
+int check(const skew_experts_config_t *c, int64_t rows, const int32_t *offsets) {
+    if (!c) return ops_fail(SKEW_EINVAL, "config is NULL");
+    if (c->experts < 1 || c->experts > kMaxExperts) return ops_fail(SKEW_EINVAL, "experts must be in [1, %d]", kMaxExperts);
+    if (c->n < 1 || c->n > 1 << 20 || c->m < 1 || c->m > 1 << 20) return ops_fail(SKEW_EINVAL, "n and m must be in [1, 2^20]");
+    if (c->flags & ~(SKEW_EXPERTS_ROWS_FP32 | SKEW_EXPERTS_GRAD_FP32)) return ops_fail(SKEW_EINVAL, "unknown flags");
+    if (rows < 0 || rows > kMaxRows) return ops_fail(SKEW_EINVAL, "rows must be in [0, 2^30]");
+    if (!offsets || ((uintptr_t)offsets & 3)) return ops_fail(SKEW_EINVAL, "offsets must be a device pointer aligned to its type");
+    return SKEW_OK;
+}
+
+int check_rows(const char *what, const void *p, int64_t rows, int64_t width, int64_t ld) {
+    if ((rows && !p) || ((uintptr_t)p & 1)) return ops_fail(SKEW_EINVAL, "%s must be a device pointer aligned to its type", what);
+    if (ld < width || ld > int64_t(1) << 31) return ops_fail(SKEW_EINVAL, "row stride must be in [width, 2^31]");
+    return SKEW_OK;
+}
+
+int check_ptr(const char *what, const void *p, uintptr_t es, bool needed) {
+    if ((needed && !p) || ((uintptr_t)p & (es - 1))) return ops_fail(SKEW_EINVAL, "%s must be a device pointer aligned to its type", what);
+    return SKEW_OK;
+}
+
+// The two products by rows: of `inner` columns each, times one matrix a group, to `cols` columns.
+int by_rows(ProductKind kind, const skew_experts_config_t *c, const void *x, int64_t ld, const void *w, const int32_t *offsets, int64_t rows, void *y, cudaStream_t s) {
+    const bool wide = c->flags & SKEW_EXPERTS_ROWS_FP32;
+    const int32_t inner = kind == kByRows ? c->n : c->m, cols = kind == kByRows ? c->m : c->n;
+    int rc;
+    if ((rc = check_rows("rows", x, rows, inner, ld)) || (rc = check_ptr("w", w, 2, true)) || (rc = check_ptr("result", y, wide ? 4 : 2, rows > 0))) return rc;
+    if (!rows) return SKEW_OK;
+    ProductArgs A{};
+    A.a = x;
+    A.b = w;
+    A.lda = ld;
+    A.ldb = c->m;
+    A.b_group = int64_t(c->n) * c->m;
+    A.offsets = offsets;
+    A.rows = rows;
+    A.groups = c->experts;
+    A.inner = inner;
+    A.cols = cols;
+    A.out = y;
+    A.ldo = cols;
+    A.scale = 1.f;
+    A.flags = (wide ? kOut32 : 0) | (cols % 8 == 0 && ((uintptr_t)y & 15) == 0 ? kOutVec : 0);
+    return ops_cuda(product_launch(kind, kStore, A, s), "k_product");
+}
+
+}  // namespace
+}  // namespace skew
+
+using namespace skew;
+
+extern "C" {
+
+int skew_experts_product(const skew_experts_config_t *c, const void *x, int64_t ld_x, const void *w, const int32_t *offsets, int64_t rows, void *y, void *stream) {
+    const int rc = check(c, rows, offsets);
+    return rc ? rc : by_rows(kByRows, c, x, ld_x, w, offsets, rows, y, (cudaStream_t)stream);
+}
+
+int skew_experts_grad_rows(const skew_experts_config_t *c, const void *dy, int64_t ld_dy, const void *w, const int32_t *offsets, int64_t rows, void *dx,
+                           void *stream) {
+    const int rc = check(c, rows, offsets);
+    return rc ? rc : by_rows(kByCols, c, dy, ld_dy, w, offsets, rows, dx, (cudaStream_t)stream);
+}
+
+int skew_experts_grad(const skew_experts_config_t *c, const void *x, int64_t ld_x, const void *dy, int64_t ld_dy, const int32_t *offsets, int64_t rows,
+                      const void *base, void *dw, void *stream) {
+    int rc = check(c, rows, offsets);
+    if (rc) return rc;
+    const bool wide = c->flags & SKEW_EXPERTS_GRAD_FP32;
+    if ((rc = check_rows("x", x, rows, c->n, ld_x)) || (rc = check_rows("dy", dy, rows, c->m, ld_dy)) || (rc = check_ptr("base", base, wide ? 4 : 2, false)) ||
+        (rc = check_ptr("dw", dw, wide ? 4 : 2, true)))
+        return rc;
+    ProductArgs A{};
+    A.a = x;
+    A.b = dy;
+    A.lda = ld_x;
+    A.ldb = ld_dy;
+    A.offsets = offsets;
+    A.rows = rows;
+    A.groups = c->experts;
+    A.inner = c->n;
+    A.cols = c->m;
+    A.out = dw;
+    A.base = base;
+    A.ldo = c->m;
+    A.o_group = int64_t(c->n) * c->m;
+    A.scale = 1.f;
+    A.flags = (wide ? kOut32 | kBase32 : 0) | (c->m % 8 == 0 && (((uintptr_t)dw | (uintptr_t)base) & 15) == 0 ? kOutVec : 0);
+    return ops_cuda(product_launch(kOuter, kStore, A, (cudaStream_t)stream), "k_product");
+}
+
+}  // extern "C"

@@ -1,0 +1,216 @@
+// The output head's softmax cross entropy (skewadam.h), from the products of skew_product.cu.
+//
+// The loss takes one product whose tiles of logits never leave the chip: of each row a tile keeps the largest logit and the sum of
+// exponentials below it (8 bytes for 128 columns), k_join joins a row's. The gradients take the vocabulary in pieces: the logits' gradient of a
+// piece in bf16, from its logits anew, then the piece's share of dh, added up in fp32 over the pieces, and its rows of dW.
+#include <cmath>
+
+#include "skew_ops.h"
+#include "skew_product.h"
+
+namespace skew {
+namespace {
+
+constexpr int64_t kMaxTokens = int64_t(1) << 24, kMaxRows = int64_t(1) << 24;
+constexpr int64_t kPieceBytes = int64_t(512) << 20;  // of the logits' gradient
+constexpr int64_t kPieceCols = 256;                  // at least, and a multiple
+
+constexpr int kJoinThreads = 256;
+
+struct JoinArgs {
+    const float2 *part;
+    const float *picked;
+    const void *targets;
+    float *loss, *lse;
+    int64_t tokens, vocab;
+    int32_t tiles;
+    bool wide;
+};
+
+// A warp to a token. Parts are in powers of two (skew_product.h).
+__global__ void __launch_bounds__(kJoinThreads) k_join(const JoinArgs A) {
+    wait_launch_before();
+    const int64_t t = blockIdx.x * int64_t(kJoinThreads / 32) + threadIdx.x / 32;
+    const int lane = threadIdx.x & 31;
+    if (t >= A.tokens) return;
+    const float2 *p = A.part + t * A.tiles;
+    float top = -INFINITY;
+    for (int i = lane; i < A.tiles; i += 32) top = fmaxf(top, p[i].x);
+    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(kFullMask, top, d));
+    float sum = 0.f;
+    for (int i = lane; i < A.tiles; i += 32) sum = fmaf(p[i].y, exp2f(p[i].x - (top == -INFINITY ? 0.f : top)), sum);
+    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(kFullMask, sum, d);
+    if (lane) return;
+    constexpr float kLn2 = 0.693147180559945309417f;
+    const float lse = (top + log2f(sum)) * kLn2;
+    const int64_t v = A.wide ? static_cast<const int64_t *>(A.targets)[t] : static_cast<const int32_t *>(A.targets)[t];
+    A.lse[t] = lse;
+    A.loss[t] = v < 0 || v >= A.vocab ? 0.f : lse - A.picked[t];
+}
+
+int check(const skew_head_config_t *c, int64_t tokens) {
+    if (!c) return ops_fail(SKEW_EINVAL, "config is NULL");
+    if (c->rows < 1 || c->rows > kMaxRows) return ops_fail(SKEW_EINVAL, "rows must be in [1, 2^24]");
+    if (c->width < 1 || c->width > int64_t(1) << 20) return ops_fail(SKEW_EINVAL, "width must be in [1, 2^20]");
+    if (!std::isfinite(c->scale)) return ops_fail(SKEW_EINVAL, "scale must be finite");
+    if (c->flags & ~SKEW_HEAD_IDS_64) return ops_fail(SKEW_EINVAL, "unknown flags");
+    if (tokens < 0 || tokens > kMaxTokens) return ops_fail(SKEW_EINVAL, "tokens must be in [0, 2^24]");
+    return SKEW_OK;
+}
+
+int check_ptr(const char *what, const void *p, uintptr_t es, bool needed) {
+    if ((needed && !p) || ((uintptr_t)p & (es - 1))) return ops_fail(SKEW_EINVAL, "%s must be a device pointer aligned to its type", what);
+    return SKEW_OK;
+}
+
+int check_workspace(const void *ws, size_t bytes, size_t need) {
+    if (!ws || ((uintptr_t)ws & 255) || bytes < need) return ops_fail(SKEW_EINVAL, "workspace must be 256-byte aligned and at least %zu bytes", need);
+    return SKEW_OK;
+}
+
+size_t whole(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+struct Layout {
+    int64_t tiles, piece, pieces;
+    size_t picked, loss_bytes;     // parts, then the picked logits
+    size_t sums, grad_bytes;       // a piece, then dh's sums
+};
+
+Layout layout(const skew_head_config_t *c, int64_t tokens) {
+    Layout L{};
+    const int64_t T = tokens ? tokens : 1, wide = product_loss_columns();
+    L.tiles = (c->rows + wide - 1) / wide;
+    L.picked = whole(size_t(T) * L.tiles * 8);
+    L.loss_bytes = L.picked + whole(size_t(T) * 4);
+    int64_t most = kPieceBytes / (2 * T) / kPieceCols * kPieceCols;
+    if (most < kPieceCols) most = kPieceCols;
+    L.pieces = (c->rows + most - 1) / most;
+    L.piece = ((c->rows + L.pieces - 1) / L.pieces + kPieceCols - 1) / kPieceCols * kPieceCols;
+    L.pieces = (c->rows + L.piece - 1) / L.piece;
+    L.sums = whole(size_t(T) * L.piece * 2);
+    L.grad_bytes = L.sums + (L.pieces > 1 ? whole(size_t(T) * c->width * 4) : 0);
+    return L;
+}
+
+bool units(int64_t width, const void *p) { return width % 8 == 0 && ((uintptr_t)p & 15) == 0; }
+
+}  // namespace
+}  // namespace skew
+
+using namespace skew;
+
+extern "C" {
+
+size_t skew_head_loss_workspace_bytes(const skew_head_config_t *c, int64_t tokens) { return check(c, tokens) == SKEW_OK ? layout(c, tokens).loss_bytes : 0; }
+size_t skew_head_grad_workspace_bytes(const skew_head_config_t *c, int64_t tokens) { return check(c, tokens) == SKEW_OK ? layout(c, tokens).grad_bytes : 0; }
+
+int skew_head_loss(const skew_head_config_t *c, const void *h, int64_t ld_h, const void *table, const void *targets, int64_t tokens, float *loss, float *lse,
+                   void *workspace, size_t workspace_bytes, void *stream) {
+    int rc = check(c, tokens);
+    if (rc) return rc;
+    const bool wide = c->flags & SKEW_HEAD_IDS_64;
+    if ((rc = check_ptr("h", h, 2, tokens > 0)) || (rc = check_ptr("table", table, 2, true)) || (rc = check_ptr("targets", targets, wide ? 8 : 4, tokens > 0)) ||
+        (rc = check_ptr("loss", loss, 4, tokens > 0)) || (rc = check_ptr("lse", lse, 4, tokens > 0)))
+        return rc;
+    if (ld_h < c->width || ld_h > int64_t(1) << 31) return ops_fail(SKEW_EINVAL, "row stride must be in [width, 2^31]");
+    const Layout L = layout(c, tokens);
+    if ((rc = check_workspace(workspace, workspace_bytes, L.loss_bytes))) return rc;
+    if (!tokens) return SKEW_OK;
+    char *ws = (char *)workspace;
+    cudaStream_t s = (cudaStream_t)stream;
+    ProductArgs A{};
+    A.a = h;
+    A.b = table;
+    A.lda = ld_h;
+    A.ldb = c->width;
+    A.rows = tokens;
+    A.groups = 1;
+    A.inner = (int32_t)c->width;
+    A.cols = (int32_t)c->rows;
+    A.scale = c->scale;
+    A.flags = wide ? kIds64 : 0;
+    A.tiles = (int32_t)L.tiles;
+    A.targets = targets;
+    A.vocab = c->rows;
+    A.part = (float2 *)ws;
+    A.picked = (float *)(ws + L.picked);
+    if ((rc = ops_cuda(product_launch(kByCols, kLoss, A, s), "k_product"))) return rc;
+    const JoinArgs J{A.part, A.picked, targets, loss, lse, tokens, c->rows, A.tiles, wide};
+    return ops_cuda(ops_launch(true, k_join, uint32_t((tokens + kJoinThreads / 32 - 1) / (kJoinThreads / 32)), kJoinThreads, 0, s, J), "k_join");
+}
+
+int skew_head_grad(const skew_head_config_t *c, const void *h, int64_t ld_h, const void *table, const void *targets, int64_t tokens, const float *lse,
+                   const float *dloss, void *dh, const void *base, void *dtable, void *workspace, size_t workspace_bytes, void *stream) {
+    int rc = check(c, tokens);
+    if (rc) return rc;
+    const bool wide = c->flags & SKEW_HEAD_IDS_64;
+    if ((rc = check_ptr("h", h, 2, tokens > 0)) || (rc = check_ptr("table", table, 2, true)) || (rc = check_ptr("targets", targets, wide ? 8 : 4, tokens > 0)) ||
+        (rc = check_ptr("lse", lse, 4, tokens > 0)) || (rc = check_ptr("dloss", dloss, 4, tokens > 0)) || (rc = check_ptr("dh", dh, 2, tokens > 0)) ||
+        (rc = check_ptr("base", base, 2, false)) || (rc = check_ptr("dtable", dtable, 2, true)))
+        return rc;
+    if (ld_h < c->width || ld_h > int64_t(1) << 31) return ops_fail(SKEW_EINVAL, "row stride must be in [width, 2^31]");
+    const Layout L = layout(c, tokens);
+    if ((rc = check_workspace(workspace, workspace_bytes, L.grad_bytes))) return rc;
+    char *ws = (char *)workspace;
+    cudaStream_t s = (cudaStream_t)stream;
+    const int32_t width = (int32_t)c->width;
+    for (int64_t v0 = 0; v0 < c->rows; v0 += L.piece) {
+        const int64_t n = c->rows - v0 < L.piece ? c->rows - v0 : L.piece;
+        const uint16_t *w = (const uint16_t *)table + v0 * c->width;
+        const bool first = v0 == 0, last = v0 + n == c->rows;
+        if (tokens) {
+            ProductArgs P{};  // the logits' gradient: (tokens, n)
+            P.a = h;
+            P.b = w;
+            P.lda = ld_h;
+            P.ldb = c->width;
+            P.rows = tokens;
+            P.groups = 1;
+            P.inner = width;
+            P.cols = (int32_t)n;
+            P.scale = c->scale;
+            P.flags = wide ? kIds64 : 0;
+            P.targets = targets;
+            P.first = v0;
+            P.vocab = c->rows;
+            P.lse = lse;
+            P.dloss = dloss;
+            P.out = ws;
+            P.ldo = L.piece;
+            if ((rc = ops_cuda(product_launch(kByCols, kLogitsGrad, P, s), "k_product"))) return rc;
+            ProductArgs H{};  // its share of dh
+            H.a = ws;
+            H.b = w;
+            H.lda = L.piece;
+            H.ldb = c->width;
+            H.rows = tokens;
+            H.groups = 1;
+            H.inner = (int32_t)n;
+            H.cols = width;
+            H.scale = c->scale;
+            H.base = first ? nullptr : ws + L.sums;
+            H.out = last ? dh : ws + L.sums;
+            H.ldo = c->width;
+            H.flags = kBase32 | (last ? 0 : kOut32) | (units(c->width, H.out) ? kOutVec : 0);
+            if ((rc = ops_cuda(product_launch(kByRows, kStore, H, s), "k_product"))) return rc;
+        }
+        ProductArgs W{};  // its rows of dW
+        W.a = ws;
+        W.b = h;
+        W.lda = L.piece;
+        W.ldb = ld_h;
+        W.rows = tokens;
+        W.groups = 1;
+        W.inner = (int32_t)n;
+        W.cols = width;
+        W.scale = c->scale;
+        W.base = base ? (const uint16_t *)base + v0 * c->width : nullptr;
+        W.out = (uint16_t *)dtable + v0 * c->width;
+        W.ldo = c->width;
+        W.flags = units(c->width, W.out) && units(c->width, base) ? kOutVec : 0;
+        if ((rc = ops_cuda(product_launch(kOuter, kStore, W, s), "k_product"))) return rc;
+    }
+    return SKEW_OK;
+}
+
+}  // extern "C"

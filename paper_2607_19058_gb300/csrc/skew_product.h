@@ -1,0 +1,52 @@
+// Matrix products on the tensor cores, of bf16 with sums in fp32, as the experts' products and the output head's
+// loss need them (skew_product.cu). Not part of the public ABI.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace skew {
+
+// What is multiplied. A "line" is a run of memory: 64 contiguous elements of it, at a time, come to shared memory.
+//   BY_ROWS : C[r, j] = sum_k A[r, k] B_e[k, j]     A: lines of k, one for each row r; B: lines of j
+//   BY_COLS : C[r, j] = sum_k A[r, k] B_e[j, k]     A as above;                        B: lines of k
+//   OUTER   : C_e[i, j] = sum_r A[r, i] B[r, j]     A: lines of i, B: lines of j, one for each row r of the group e
+enum ProductKind { kByRows = 0, kByCols = 1, kOuter = 2 };
+
+// What becomes of a tile of sums.
+//   STORE  : out = base + scale * C
+//   LOSS   : of x = scale * C, per row and tile, the largest and the sum of exponentials; the target's x
+//   LOGITS_GRAD : out = (exp(x - lse) - [j is the target]) * dloss, bf16
+enum ProductEnd { kStore = 0, kLoss = 1, kLogitsGrad = 2 };
+
+enum : uint32_t { kOut32 = 1, kBase32 = 2, kOutVec = 4, kIds64 = 8 };
+
+struct ProductArgs {
+    const void *a, *b;          // bf16
+    int64_t lda, ldb, b_group;  // elements between lines, and between B's groups
+    const int32_t *offsets;     // groups + 1 row numbers on the device; NULL: one group of all rows
+    int64_t rows;               // r in [0, rows)
+    int32_t groups, cols;       // j in [0, cols)
+    int32_t inner;              // k, or OUTER's i, in [0, inner)
+    uint32_t flags;
+    void *out;
+    const void *base;           // strides as out; may be out
+    int64_t ldo, o_group;
+    float scale;
+    // LOSS, LOGITS_GRAD
+    int32_t tiles;              // LOSS: parts of a row
+    const void *targets;        // one for each row; not in [0, vocab): none
+    int64_t first, vocab;       // the column j is the vocabulary's `first` + j
+    const float *lse, *dloss;
+    float2 *part;               // [rows][tiles]: (largest, sum) in powers of two
+    float *picked;              // [rows]: the target's x
+};
+
+// Columns of a LOSS part.
+int32_t product_loss_columns();
+// Runs the product on `stream`; every pointer, size and stride has been checked.
+cudaError_t product_launch(ProductKind kind, ProductEnd end, ProductArgs &A, cudaStream_t stream);
+// Synchronises, and reads and clears the word in which a wait on the device that gave up leaves its mark: a SKEW_* code.
+int product_status(cudaStream_t stream);
+
+}  // namespace skew

@@ -31,6 +31,9 @@ CLIP_GRAD_FP32, CLIP_OUT_FP32 = 1, 2
 GATE_SOFTMAX, GATE_SIGMOID = 0, 1
 GATE_RENORM, GATE_FP32 = 1, 2
 EMBED_TABLE_FP32, EMBED_ACT_FP32, EMBED_IDS_64 = 1, 2, 4
+DISPATCH_TOKENS_FP32, DISPATCH_ROWS_FP32 = 1, 2
+EXPERTS_ROWS_FP32, EXPERTS_GRAD_FP32 = 1, 2
+HEAD_IDS_64 = 1
 
 EXPORTS = ["skew_create", "skew_destroy", "skew_state_bytes", "skew_workspace_bytes", "skew_bind", "skew_step",
            "skew_sync_status", "skew_tensor_scalars", "skew_matrix_scalars", "skew_tensor_info", "skew_num_tensors", "skew_last_error",
@@ -39,7 +42,10 @@ EXPORTS = ["skew_create", "skew_destroy", "skew_state_bytes", "skew_workspace_by
            "skew_noalloc_selftest_wait_timeout", "skew_tensor_route", "skew_ops_last_error",
            "skew_clip_create", "skew_clip_destroy", "skew_clip_workspace_bytes", "skew_clip_bind", "skew_clip_norm",
            "skew_clip_apply", "skew_gate_workspace_bytes", "skew_gate_forward", "skew_gate_grad",
-           "skew_embed_lookup", "skew_embed_workspace_bytes", "skew_embed_grad"]
+           "skew_embed_lookup", "skew_embed_workspace_bytes", "skew_embed_grad",
+           "skew_dispatch_workspace_bytes", "skew_dispatch_order", "skew_dispatch_spread", "skew_dispatch_combine", "skew_dispatch_combine_grad",
+           "skew_experts_product", "skew_experts_grad_rows", "skew_experts_grad",
+           "skew_head_loss_workspace_bytes", "skew_head_grad_workspace_bytes", "skew_head_loss", "skew_head_grad", "skew_ops_sync_status"]
 
 
 class SkewError(RuntimeError):
@@ -76,6 +82,18 @@ class GateConfig(C.Structure):
 
 
 class EmbedConfig(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("width", C.c_int64), ("scale", C.c_float), ("flags", C.c_uint32)]
+
+
+class DispatchConfig(C.Structure):
+    _fields_ = [("experts", C.c_int32), ("top_k", C.c_int32), ("flags", C.c_uint32), ("zero", C.c_uint32)]
+
+
+class ExpertsConfig(C.Structure):
+    _fields_ = [("experts", C.c_int32), ("n", C.c_int32), ("m", C.c_int32), ("flags", C.c_uint32)]
+
+
+class HeadConfig(C.Structure):
     _fields_ = [("rows", C.c_int64), ("width", C.c_int64), ("scale", C.c_float), ("flags", C.c_uint32)]
 
 
@@ -165,6 +183,23 @@ def load(path: Optional[str] = None) -> C.CDLL:
         L.skew_embed_workspace_bytes.restype = sz
         L.skew_embed_grad.argtypes = [C.POINTER(EmbedConfig), vp, i64, vp, i64, vp, vp, vp, sz, vp]
         L.skew_embed_grad.restype = C.c_int
+        L.skew_dispatch_workspace_bytes.argtypes = [C.POINTER(DispatchConfig), i64]
+        L.skew_dispatch_workspace_bytes.restype = sz
+        L.skew_dispatch_order.argtypes = [C.POINTER(DispatchConfig), vp, i64, vp, vp, vp, sz, vp]
+        L.skew_dispatch_spread.argtypes = [C.POINTER(DispatchConfig), vp, i64, vp, vp, i64, i64, vp, vp]
+        L.skew_dispatch_combine.argtypes = [C.POINTER(DispatchConfig), vp, vp, vp, i64, i64, vp, i64, vp]
+        L.skew_dispatch_combine_grad.argtypes = [C.POINTER(DispatchConfig), vp, i64, vp, vp, vp, vp, i64, i64, vp, vp, vp]
+        L.skew_experts_product.argtypes = [C.POINTER(ExpertsConfig), vp, i64, vp, vp, i64, vp, vp]
+        L.skew_experts_grad_rows.argtypes = [C.POINTER(ExpertsConfig), vp, i64, vp, vp, i64, vp, vp]
+        L.skew_experts_grad.argtypes = [C.POINTER(ExpertsConfig), vp, i64, vp, i64, vp, i64, vp, vp, vp]
+        for f in (L.skew_head_loss_workspace_bytes, L.skew_head_grad_workspace_bytes):
+            f.argtypes, f.restype = [C.POINTER(HeadConfig), i64], sz
+        L.skew_head_loss.argtypes = [C.POINTER(HeadConfig), vp, i64, vp, vp, i64, vp, vp, vp, sz, vp]
+        L.skew_head_grad.argtypes = [C.POINTER(HeadConfig), vp, i64, vp, vp, i64, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.skew_ops_sync_status.argtypes = [vp]
+        for f in (L.skew_dispatch_order, L.skew_dispatch_spread, L.skew_dispatch_combine, L.skew_dispatch_combine_grad, L.skew_experts_product,
+                  L.skew_experts_grad_rows, L.skew_experts_grad, L.skew_head_loss, L.skew_head_grad, L.skew_ops_sync_status):
+            f.restype = C.c_int
         if path is None:
             _lib = L
         return L
@@ -373,6 +408,70 @@ def skew_embed_grad(c: EmbedConfig, ids_ptr: int, tokens: int, dout_ptr: int, ld
     """`base_ptr`: 0 for none."""
     _check_op(load().skew_embed_grad(C.byref(c), ids_ptr, tokens, dout_ptr, ld_dout, base_ptr or None, dtable_ptr,
                                      ws_ptr, ws_bytes, stream))
+
+
+def skew_dispatch_workspace_bytes(c: DispatchConfig, tokens: int) -> int:
+    return int(load().skew_dispatch_workspace_bytes(C.byref(c), tokens))
+
+
+def skew_dispatch_order(c: DispatchConfig, chosen_ptr: int, tokens: int, offsets_ptr: int, places_ptr: int, ws_ptr: int, ws_bytes: int, stream: int) -> None:
+    _check_op(load().skew_dispatch_order(C.byref(c), chosen_ptr, tokens, offsets_ptr, places_ptr, ws_ptr, ws_bytes, stream))
+
+
+def skew_dispatch_spread(c: DispatchConfig, x_ptr: int, ld_x: int, offsets_ptr: int, places_ptr: int, tokens: int, width: int, rows_ptr: int,
+                         stream: int) -> None:
+    _check_op(load().skew_dispatch_spread(C.byref(c), x_ptr, ld_x, offsets_ptr, places_ptr, tokens, width, rows_ptr, stream))
+
+
+def skew_dispatch_combine(c: DispatchConfig, rows_ptr: int, weights_ptr: int, places_ptr: int, tokens: int, width: int, out_ptr: int, ld_out: int,
+                          stream: int) -> None:
+    """`weights_ptr`: 0 for ones."""
+    _check_op(load().skew_dispatch_combine(C.byref(c), rows_ptr, weights_ptr or None, places_ptr, tokens, width, out_ptr, ld_out, stream))
+
+
+def skew_dispatch_combine_grad(c: DispatchConfig, dout_ptr: int, ld_dout: int, rows_ptr: int, weights_ptr: int, offsets_ptr: int, places_ptr: int,
+                               tokens: int, width: int, drows_ptr: int, dweights_ptr: int, stream: int) -> None:
+    _check_op(load().skew_dispatch_combine_grad(C.byref(c), dout_ptr, ld_dout, rows_ptr, weights_ptr, offsets_ptr, places_ptr, tokens, width, drows_ptr,
+                                                dweights_ptr, stream))
+
+
+def skew_experts_product(c: ExpertsConfig, x_ptr: int, ld_x: int, w_ptr: int, offsets_ptr: int, rows: int, y_ptr: int, stream: int) -> None:
+    _check_op(load().skew_experts_product(C.byref(c), x_ptr, ld_x, w_ptr, offsets_ptr, rows, y_ptr, stream))
+
+
+def skew_experts_grad_rows(c: ExpertsConfig, dy_ptr: int, ld_dy: int, w_ptr: int, offsets_ptr: int, rows: int, dx_ptr: int, stream: int) -> None:
+    _check_op(load().skew_experts_grad_rows(C.byref(c), dy_ptr, ld_dy, w_ptr, offsets_ptr, rows, dx_ptr, stream))
+
+
+def skew_experts_grad(c: ExpertsConfig, x_ptr: int, ld_x: int, dy_ptr: int, ld_dy: int, offsets_ptr: int, rows: int, base_ptr: int, dw_ptr: int,
+                      stream: int) -> None:
+    """`base_ptr`: 0 for none."""
+    _check_op(load().skew_experts_grad(C.byref(c), x_ptr, ld_x, dy_ptr, ld_dy, offsets_ptr, rows, base_ptr or None, dw_ptr, stream))
+
+
+def skew_head_loss_workspace_bytes(c: HeadConfig, tokens: int) -> int:
+    return int(load().skew_head_loss_workspace_bytes(C.byref(c), tokens))
+
+
+def skew_head_grad_workspace_bytes(c: HeadConfig, tokens: int) -> int:
+    return int(load().skew_head_grad_workspace_bytes(C.byref(c), tokens))
+
+
+def skew_head_loss(c: HeadConfig, h_ptr: int, ld_h: int, table_ptr: int, targets_ptr: int, tokens: int, loss_ptr: int, lse_ptr: int, ws_ptr: int,
+                   ws_bytes: int, stream: int) -> None:
+    _check_op(load().skew_head_loss(C.byref(c), h_ptr, ld_h, table_ptr, targets_ptr, tokens, loss_ptr, lse_ptr, ws_ptr, ws_bytes, stream))
+
+
+def skew_head_grad(c: HeadConfig, h_ptr: int, ld_h: int, table_ptr: int, targets_ptr: int, tokens: int, lse_ptr: int, dloss_ptr: int, dh_ptr: int,
+                   base_ptr: int, dtable_ptr: int, ws_ptr: int, ws_bytes: int, stream: int) -> None:
+    """`base_ptr`: 0 for none."""
+    _check_op(load().skew_head_grad(C.byref(c), h_ptr, ld_h, table_ptr, targets_ptr, tokens, lse_ptr, dloss_ptr, dh_ptr, base_ptr or None, dtable_ptr, ws_ptr,
+                                    ws_bytes, stream))
+
+
+def skew_ops_sync_status(stream: int) -> None:
+    """Synchronises `stream`; raises SkewError(SKEW_ETIMEOUT) once if a bounded device wait of Experts or HeadLoss gave up since the last read."""
+    _check_op(load().skew_ops_sync_status(stream))
 
 
 def hparams(beta1=0.9, beta2=0.999, eps=1e-8, clip_d=1.0, weight_decay=0.05, policy=POLICY_TIERED) -> HParams:
@@ -745,6 +844,364 @@ class Router:
         if rc:
             _check_op(rc)
         return dlogits
+
+
+class _Workspace:
+    """Device memory that an object's calls share, one block for each device: it grows, and what a graph or another stream may still use is kept."""
+
+    __slots__ = ("blocks", "kept")
+
+    def __init__(self):
+        self.blocks, self.kept = {}, []
+
+    def get(self, dev, need: int, handle: int) -> int:
+        ws = self.blocks.get(dev.index)
+        if ws is None or ws.bytes < need:
+            import torch
+            if ws is not None:
+                self.kept.append(ws)
+                need = max(need, 3 * ws.bytes // 2)
+            ws = self.blocks[dev.index] = _Block(torch.empty(need, dtype=torch.uint8, device=dev), handle)
+        elif handle not in ws.streams:
+            ws.also_on(handle)
+        return ws.ptr
+
+
+def _types(what: str, *dtypes):
+    """Each type, bf16 where it is None; others than bf16 and fp32 are refused."""
+    import torch
+    dtypes = [dt or torch.bfloat16 for dt in dtypes]
+    if not set(dtypes) <= {torch.bfloat16, torch.float32}:
+        raise TypeError(f"{what} must be bf16 or fp32")
+    return dtypes
+
+
+def _fits(**values):
+    """A C field would keep the low bits of what does not fit it."""
+    for name, v in values.items():
+        if not -2**31 <= v < 2**31:
+            raise ValueError(f"{name} must fit 32 bits")
+
+
+class Dispatch:
+    """Tokens' rows by expert and back: what lies between a ``Router`` and ``Experts``. Each gradient is a call of its own (no autograd functions).
+
+    ``order`` sorts the entries of ``chosen`` (T, k) by expert, stably, and returns (offsets int32 (experts + 1,), places int32
+    (T, k)): the rows of expert e are [offsets[e], offsets[e + 1]), and an entry outside [0, experts) has no row (place -1).
+    ``token_dtype`` (x, combined rows and their gradient) and ``row_dtype`` (the rows by expert) are bf16 or fp32. Rows behind the
+    last expert's are zeros. Tensors are to be on the current device. The object must live as long as a graph that captured its calls, or
+    work that it was given on a stream torch did not make (a raw handle).
+    """
+
+    def __init__(self, experts: int, top_k: int, token_dtype=None, row_dtype=None):
+        import torch
+        self.token_dtype, self.row_dtype = _types("tokens and rows", token_dtype, row_dtype)
+        _fits(experts=experts, top_k=top_k)
+        self.experts, self.top_k = experts, top_k
+        self.config = DispatchConfig(experts, top_k, (DISPATCH_TOKENS_FP32 if self.token_dtype == torch.float32 else 0) |
+                                     (DISPATCH_ROWS_FP32 if self.row_dtype == torch.float32 else 0), 0)
+        if not skew_dispatch_workspace_bytes(self.config, 0):
+            raise SkewError(SKEW_EINVAL, skew_ops_last_error())
+        self._ref, self._new, self._i32, self._f32 = C.byref(self.config), _allocator(), torch.int32, torch.float32
+        L = load()
+        self._order, self._spread, self._combine, self._combine_grad = L.skew_dispatch_order, L.skew_dispatch_spread, L.skew_dispatch_combine, L.skew_dispatch_combine_grad
+        self._stream, self._elsewhere = _raw_stream(), _device_check()
+        self._workspace, self._sizes = _Workspace(), {}
+
+    def _there(self, t, dtype, shape, dev, what: str) -> int:
+        if not (t.dtype == dtype and t.shape == shape and t.is_contiguous() and t.is_cuda and (dev is None or t.device == dev)):
+            raise ValueError(f"{what} must be a contiguous {tuple(shape)} {dtype} CUDA tensor, on the device of the others")
+        return t.data_ptr()
+
+    def _ordered(self, order, dev):
+        """Pointers of an order, and its tokens."""
+        offsets, places = order
+        T = places.shape[0] if places.dim() == 2 else 0
+        return self._there(offsets, self._i32, (self.experts + 1,), dev, "offsets"), self._there(places, self._i32, (T, self.top_k), dev, "places"), T
+
+    def _tokens(self, x, T, what: str):
+        """The row stride and width of a (T, width) tensor of tokens."""
+        if not (x.dtype == self.token_dtype and x.is_cuda and x.dim() == 2 and x.shape[0] == T):
+            raise ValueError(f"{what} must be a ({T}, width) {self.token_dtype} CUDA tensor")
+        if self._elsewhere:
+            self._elsewhere(x.device)
+        d = x.shape[1]
+        return d if x.is_contiguous() else _rows(x, d, what), d
+
+    def _by_expert(self, rows, T, what: str):
+        """The width of a (T * top_k, width) tensor of rows by expert."""
+        if not (rows.dtype == self.row_dtype and rows.is_cuda and rows.dim() == 2 and rows.shape[0] == T * self.top_k and rows.is_contiguous()):
+            raise ValueError(f"{what} must be a contiguous ({T * self.top_k}, width) {self.row_dtype} CUDA tensor")
+        if self._elsewhere:
+            self._elsewhere(rows.device)
+        return rows.shape[1]
+
+    def order(self, chosen, stream=None):
+        """(offsets, places) of a router's ``chosen``. Calls on one object share a workspace: they must not overlap on the GPU.
+        With ``stream``, here and below, the results belong to that stream."""
+        if stream is not None:
+            with _on(stream):
+                return self.order(chosen)
+        T, dev = chosen.shape[0] if chosen.dim() == 2 else 0, chosen.device
+        p = self._there(chosen, self._i32, (T, self.top_k), None, "chosen")
+        if self._elsewhere:
+            self._elsewhere(dev)
+        need = self._sizes.get(T)
+        if need is None:
+            need = self._sizes[T] = skew_dispatch_workspace_bytes(self.config, T)
+            if not need:
+                del self._sizes[T]
+                raise SkewError(SKEW_EINVAL, skew_ops_last_error())
+        handle = self._stream(dev.index)
+        ws = self._workspace.get(dev, need, handle)
+        offsets = self._new((self.experts + 1,), (1,), self._i32, dev)
+        places = self._new((T, self.top_k), (self.top_k, 1), self._i32, dev)
+        rc = self._order(self._ref, p, T, offsets.data_ptr(), places.data_ptr(), ws, need, handle)
+        if rc:
+            _check_op(rc)
+        return offsets, places
+
+    def spread(self, x, order, stream=None):
+        """The tokens' rows by expert, (T * top_k, width), of x (T, width), whose rows may lie apart. Its gradient is ``combine`` of
+        the rows' gradient, without weights."""
+        if stream is not None:
+            with _on(stream):
+                return self.spread(x, order)
+        dev = x.device
+        offsets, places, T = self._ordered(order, dev)
+        ld, d = self._tokens(x, T, "x")
+        rows = self._new((T * self.top_k, d), (d, 1), self.row_dtype, dev)
+        rc = self._spread(self._ref, x.data_ptr(), ld, offsets, places, T, d, rows.data_ptr(), self._stream(dev.index))
+        if rc:
+            _check_op(rc)
+        return rows
+
+    def combine(self, rows, weights, order, stream=None):
+        """Each token's sum over its experts of weight * row, (T, width). ``weights``: fp32 (T, top_k), or None for ones."""
+        if stream is not None:
+            with _on(stream):
+                return self.combine(rows, weights, order)
+        dev = rows.device
+        _, places, T = self._ordered(order, dev)
+        d = self._by_expert(rows, T, "rows")
+        w = None if weights is None else self._there(weights, self._f32, (T, self.top_k), dev, "weights")
+        out = self._new((T, d), (d, 1), self.token_dtype, dev)
+        rc = self._combine(self._ref, rows.data_ptr(), w, places, T, d, out.data_ptr(), d, self._stream(dev.index))
+        if rc:
+            _check_op(rc)
+        return out
+
+    def combine_grad(self, dy, rows, weights, order, stream=None):
+        """The gradients of ``combine``'s rows and weights (fp32), from that of its result (whose rows may lie apart)."""
+        if stream is not None:
+            with _on(stream):
+                return self.combine_grad(dy, rows, weights, order)
+        dev = dy.device
+        offsets, places, T = self._ordered(order, dev)
+        ld, d = self._tokens(dy, T, "dy")
+        if self._by_expert(rows, T, "rows") != d or rows.device != dev:
+            raise ValueError("dy and rows must have one width, and be on one device")
+        w = self._there(weights, self._f32, (T, self.top_k), dev, "weights")
+        drows = self._new((T * self.top_k, d), (d, 1), self.row_dtype, dev)
+        dweights = self._new((T, self.top_k), (self.top_k, 1), self._f32, dev)
+        rc = self._combine_grad(self._ref, dy.data_ptr(), ld, rows.data_ptr(), w, offsets, places, T, d, drows.data_ptr(), dweights.data_ptr(),
+                                self._stream(dev.index))
+        if rc:
+            _check_op(rc)
+        return drows, dweights
+
+
+class Experts:
+    """Products of rows grouped by expert with a stack of matrices (experts, n, m), one for each, and their gradients, which are calls of their own
+    (no autograd functions).
+
+    Rows of expert e are [offsets[e], offsets[e + 1]), as ``Dispatch.order`` makes them: any number each, and those of no expert
+    give zeros. x (rows, n) and dy (rows, m), whose rows may lie apart, and the matrices are bf16; ``row_dtype`` (products and the rows' gradients) and
+    ``grad_dtype`` (the matrices' gradients) are bf16 or fp32. Tensors are to be on the current device.
+    """
+
+    def __init__(self, experts: int, n: int, m: int, row_dtype=None, grad_dtype=None):
+        import torch
+        self.row_dtype, self.grad_dtype = _types("rows and gradients", row_dtype, grad_dtype)
+        _fits(experts=experts, n=n, m=m)
+        self.experts, self.n, self.m = experts, n, m
+        self.config = ExpertsConfig(experts, n, m, (EXPERTS_ROWS_FP32 if self.row_dtype == torch.float32 else 0) |
+                                    (EXPERTS_GRAD_FP32 if self.grad_dtype == torch.float32 else 0))
+        self._ref, self._new = C.byref(self.config), _allocator()
+        skew_experts_product(self.config, 0, max(n, 1), 256, 256, 0, 0, 0)  # refuses what the library does not take; no rows: no launch
+        self._shape = (experts, n, m)
+        self._bf16, self._i32 = torch.bfloat16, torch.int32
+        L = load()
+        self._product, self._grad_rows, self._grad = L.skew_experts_product, L.skew_experts_grad_rows, L.skew_experts_grad
+        self._stream, self._elsewhere = _raw_stream(), _device_check()
+
+    def _rows(self, x, width: int, dev, what: str) -> int:
+        if not (x.dtype == self._bf16 and x.is_cuda and x.dim() == 2 and x.shape[1] == width and x.device == dev):
+            raise ValueError(f"{what} must be a (rows, {width}) bf16 CUDA tensor, on the device of the others")
+        return width if x.is_contiguous() else _rows(x, width, what)
+
+    def _offsets(self, offsets, dev) -> int:
+        if not (offsets.dtype == self._i32 and offsets.shape == (self.experts + 1,) and offsets.is_contiguous() and offsets.device == dev):
+            raise ValueError(f"offsets must be a contiguous int32 tensor of {self.experts + 1} values, on the device of the others")
+        if self._elsewhere:
+            self._elsewhere(dev)
+        return offsets.data_ptr()
+
+    def _matrices(self, w, dtype, dev, what: str) -> int:
+        if not (w.dtype == dtype and w.shape == self._shape and w.is_contiguous() and w.device == dev):
+            raise ValueError(f"{what} must be a contiguous {self._shape} {dtype} tensor, on the device of the others")
+        return w.data_ptr()
+
+    def _by_rows(self, call, x, width, to, w, offsets, what):
+        dev = x.device
+        ld, o, p = self._rows(x, width, dev, what), self._offsets(offsets, dev), self._matrices(w, self._bf16, dev, "w")
+        R = x.shape[0]
+        y = self._new((R, to), (to, 1), self.row_dtype, dev)
+        rc = call(self._ref, x.data_ptr(), ld, p, o, R, y.data_ptr(), self._stream(dev.index))
+        if rc:
+            _check_op(rc)
+        return y
+
+    def product(self, x, w, offsets, stream=None):
+        """x[r] @ w[e] for each row r of expert e: (rows, m). With ``stream``, here and below, the result belongs to that stream."""
+        if stream is not None:
+            with _on(stream):
+                return self.product(x, w, offsets)
+        return self._by_rows(self._product, x, self.n, self.m, w, offsets, "x")
+
+    def grad_rows(self, dy, w, offsets, stream=None):
+        """The gradient of ``product``'s rows, dy[r] @ w[e]^T: (rows, n)."""
+        if stream is not None:
+            with _on(stream):
+                return self.grad_rows(dy, w, offsets)
+        return self._by_rows(self._grad_rows, dy, self.m, self.n, w, offsets, "dy")
+
+    def grad(self, x, dy, offsets, base=None, out=None, stream=None):
+        """The matrices' gradient, the sum over an expert's rows of x[r]^T dy[r]. ``base``: what it adds to; ``out``: where it goes
+        (``base`` itself: in place, and matrices of experts without rows are not touched; None: a new tensor)."""
+        if stream is not None:
+            with _on(stream):
+                return self.grad(x, dy, offsets, base, out)
+        dev = x.device
+        ld, ldd, o = self._rows(x, self.n, dev, "x"), self._rows(dy, self.m, dev, "dy"), self._offsets(offsets, dev)
+        if dy.shape[0] != x.shape[0]:
+            raise ValueError("x and dy must have one number of rows")
+        b = None if base is None else self._matrices(base, self.grad_dtype, dev, "base")
+        if out is None:
+            out = self._new(self._shape, (self.n * self.m, self.m, 1), self.grad_dtype, dev)
+            p = out.data_ptr()
+        else:
+            p = self._matrices(out, self.grad_dtype, dev, "out")
+        rc = self._grad(self._ref, x.data_ptr(), ld, dy.data_ptr(), ldd, o, x.shape[0], b, p, self._stream(dev.index))
+        if rc:
+            _check_op(rc)
+        return out
+
+    def sync_status(self, stream=None) -> None:
+        """Waits for a stream; raises if a wait on the device has given up."""
+        import torch
+        skew_ops_sync_status(torch.cuda.current_stream().cuda_stream if stream is None else _stream_of(stream, None))
+
+
+class HeadLoss:
+    """The softmax cross entropy of an output head over a (rows, width) table, which an ``Embedding`` may share, without keeping the logits
+    scale * h @ table^T; its gradients are a call of their own (no autograd function).
+
+    h (T, width), whose rows may lie apart, the table and the gradients are bf16. Targets are int32 or int64 (T,); one
+    outside [0, rows) is padding: its loss is zero and it enters no gradient. Tensors are to be on the current device. Calls on one object share a
+    workspace: they must not overlap on the GPU. The object must live as long as a graph that captured its calls, or work that it was given on
+    a stream torch did not make (a raw handle).
+    """
+
+    def __init__(self, rows: int, width: int, scale: float = 1.0):
+        import torch
+        if not all(-2**63 <= v < 2**63 for v in (rows, width)):
+            raise ValueError("rows and width must fit 64 bits")
+        self.rows, self.width = rows, width
+        self.config = {torch.int32: HeadConfig(rows, width, scale, 0), torch.int64: HeadConfig(rows, width, scale, HEAD_IDS_64)}
+        if not skew_head_loss_workspace_bytes(self.config[torch.int32], 0):
+            raise SkewError(SKEW_EINVAL, skew_ops_last_error())
+        self._ref = {dt: C.byref(c) for dt, c in self.config.items()}
+        self._shape, self._bf16, self._f32 = (rows, width), torch.bfloat16, torch.float32
+        self._new, self._loss, self._grad = _allocator(), load().skew_head_loss, load().skew_head_grad
+        self._stream, self._elsewhere = _raw_stream(), _device_check()
+        self._workspace, self._sizes = _Workspace(), {}
+
+    def _table(self, t, dev, what: str) -> int:
+        if not (t.dtype == self._bf16 and t.shape == self._shape and t.is_contiguous() and t.device == dev):
+            raise ValueError(f"{what} must be a contiguous {self._shape} bf16 tensor on h's device")
+        return t.data_ptr()
+
+    def _per_token(self, t, T, dev, what: str) -> int:
+        if not (t.dtype == self._f32 and t.shape == (T,) and t.is_contiguous() and t.device == dev):
+            raise ValueError(f"{what} must be a contiguous fp32 tensor of {T} values on h's device")
+        return t.data_ptr()
+
+    def _tokens(self, h, targets):
+        """(config, row stride, tokens, device)"""
+        if not (h.dtype == self._bf16 and h.is_cuda and h.dim() == 2 and h.shape[1] == self.width):
+            raise ValueError(f"h must be a (tokens, {self.width}) bf16 CUDA tensor")
+        c, T, dev = self._ref.get(targets.dtype), h.shape[0], h.device
+        if c is None:
+            raise TypeError("targets must be int32 or int64")
+        if not (targets.shape == (T,) and targets.is_contiguous() and targets.device == dev):
+            raise ValueError(f"targets must be a contiguous tensor of {T} values on h's device")
+        if self._elsewhere:
+            self._elsewhere(dev)
+        return c, self.width if h.is_contiguous() else _rows(h, self.width, "h"), T, dev
+
+    def _space(self, T, dev, handle: int, which: int):
+        """The workspace, of what the loss (0) or its gradients (1) need."""
+        need = self._sizes.get(T)
+        if need is None:
+            c = next(iter(self.config.values()))
+            need = skew_head_loss_workspace_bytes(c, T), skew_head_grad_workspace_bytes(c, T)
+            if not need[0]:
+                raise SkewError(SKEW_EINVAL, skew_ops_last_error())
+            self._sizes[T] = need
+        return self._workspace.get(dev, need[which], handle), need[which]
+
+    def loss(self, h, table, targets, stream=None):
+        """(loss, lse), fp32 (T,): each token's loss, and the logarithm of its sum of exponentials, which ``grad`` takes.
+        With ``stream``, here and below, the results belong to that stream."""
+        if stream is not None:
+            with _on(stream):
+                return self.loss(h, table, targets)
+        c, ld, T, dev = self._tokens(h, targets)
+        p, handle = self._table(table, dev, "table"), self._stream(dev.index)
+        ws, need = self._space(T, dev, handle, 0)
+        loss, lse = self._new((T,), (1,), self._f32, dev), self._new((T,), (1,), self._f32, dev)
+        rc = self._loss(c, h.data_ptr(), ld, p, targets.data_ptr(), T, loss.data_ptr(), lse.data_ptr(), ws, need, handle)
+        if rc:
+            _check_op(rc)
+        return loss, lse
+
+    def grad(self, h, table, targets, lse, dloss, base=None, out=None, stream=None):
+        """(dh, dtable) from the losses' gradient ``dloss``, fp32 (T,): 1 / T for their mean. ``base``: what the table's gradient adds
+        to; ``out``: where it goes (``base`` itself: in place; None: a new tensor)."""
+        if stream is not None:
+            with _on(stream):
+                return self.grad(h, table, targets, lse, dloss, base, out)
+        c, ld, T, dev = self._tokens(h, targets)
+        p, handle = self._table(table, dev, "table"), self._stream(dev.index)
+        l, g = self._per_token(lse, T, dev, "lse"), self._per_token(dloss, T, dev, "dloss")
+        b = None if base is None else self._table(base, dev, "base")
+        if out is None:
+            out = self._new(self._shape, (self.width, 1), self._bf16, dev)
+            q = out.data_ptr()
+        else:
+            q = self._table(out, dev, "out")
+        ws, need = self._space(T, dev, handle, 1)
+        dh = self._new((T, self.width), (self.width, 1), self._bf16, dev)
+        rc = self._grad(c, h.data_ptr(), ld, p, targets.data_ptr(), T, l, g, dh.data_ptr(), b, q, ws, need, handle)
+        if rc:
+            _check_op(rc)
+        return dh, out
+
+    def sync_status(self, stream=None) -> None:
+        """Waits for a stream; raises if a wait on the device has given up."""
+        import torch
+        skew_ops_sync_status(torch.cuda.current_stream().cuda_stream if stream is None else _stream_of(stream, None))
 
 
 class SkewAdam:

@@ -15,7 +15,7 @@ constexpr int64_t kMaxTokens = int64_t(1) << 24, kMaxRows = int64_t(1) << 24;
 constexpr int64_t kPieceBytes = int64_t(512) << 20;  // of the logits' gradient
 constexpr int64_t kPieceCols = 256;                  // at least, and a multiple
 
-constexpr int kJoinThreads = 256;
+constexpr int kJoinWarps = 8;
 
 struct JoinArgs {
     const float2 *part;
@@ -23,24 +23,35 @@ struct JoinArgs {
     const void *targets;
     float *loss, *lse;
     int64_t tokens, vocab;
-    int32_t tiles;
+    int32_t parts;
     bool wide;
 };
 
-// A warp to a token. Parts are in powers of two (skew_product.h).
-__global__ void __launch_bounds__(kJoinThreads) k_join(const JoinArgs A) {
+// A lane to a token, every eighth part to a warp. Parts are in powers of two (skew_product.h).
+__global__ void __launch_bounds__(32 * kJoinWarps) k_join(const JoinArgs A) {
+    __shared__ float2 of_warp[kJoinWarps][32];
     wait_launch_before();
-    const int64_t t = blockIdx.x * int64_t(kJoinThreads / 32) + threadIdx.x / 32;
-    const int lane = threadIdx.x & 31;
-    if (t >= A.tokens) return;
-    const float2 *p = A.part + t * A.tiles;
-    float top = -INFINITY;
-    for (int i = lane; i < A.tiles; i += 32) top = fmaxf(top, p[i].x);
-    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(kFullMask, top, d));
-    float sum = 0.f;
-    for (int i = lane; i < A.tiles; i += 32) sum = fmaf(p[i].y, exp2f(p[i].x - (top == -INFINITY ? 0.f : top)), sum);
-    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(kFullMask, sum, d);
-    if (lane) return;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t t = blockIdx.x * int64_t(32) + lane;
+    const bool there = t < A.tokens;
+    float top = -INFINITY, sum = 0.f;
+    auto add = [&](float2 p) {
+        const float high = fmaxf(top, p.x), from = high == -INFINITY ? 0.f : high;
+        sum = fmaf(sum, exp2f(top - from), p.y * exp2f(p.x - from));
+        top = high;
+    };
+    constexpr int kDeep = 8;
+    for (int i = warp; there && i < A.parts; i += kJoinWarps * kDeep) {
+        float2 p[kDeep];
+#pragma unroll
+        for (int j = 0; j < kDeep; ++j) p[j] = i + j * kJoinWarps < A.parts ? A.part[int64_t(i + j * kJoinWarps) * A.tokens + t] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+        for (int j = 0; j < kDeep; ++j) add(p[j]);
+    }
+    of_warp[warp][lane] = make_float2(top, sum);
+    __syncthreads();
+    if (warp || !there) return;
+    for (int w = 1; w < kJoinWarps; ++w) add(of_warp[w][lane]);
     constexpr float kLn2 = 0.693147180559945309417f;
     const float lse = (top + log2f(sum)) * kLn2;
     const int64_t v = A.wide ? static_cast<const int64_t *>(A.targets)[t] : static_cast<const int32_t *>(A.targets)[t];
@@ -71,7 +82,7 @@ int check_workspace(const void *ws, size_t bytes, size_t need) {
 size_t whole(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
 struct Layout {
-    int64_t tiles, piece, pieces;
+    int64_t parts, piece, pieces;
     size_t picked, loss_bytes;     // parts, then the picked logits
     size_t sums, grad_bytes;       // a piece, then dh's sums
 };
@@ -79,8 +90,8 @@ struct Layout {
 Layout layout(const skew_head_config_t *c, int64_t tokens) {
     Layout L{};
     const int64_t T = tokens ? tokens : 1, wide = product_loss_columns();
-    L.tiles = (c->rows + wide - 1) / wide;
-    L.picked = whole(size_t(T) * L.tiles * 8);
+    L.parts = (c->rows + wide - 1) / wide;
+    L.picked = whole(size_t(T) * L.parts * 8);
     L.loss_bytes = L.picked + whole(size_t(T) * 4);
     int64_t most = kPieceBytes / (2 * T) / kPieceCols * kPieceCols;
     if (most < kPieceCols) most = kPieceCols;
@@ -129,14 +140,13 @@ int skew_head_loss(const skew_head_config_t *c, const void *h, int64_t ld_h, con
     A.cols = (int32_t)c->rows;
     A.scale = c->scale;
     A.flags = wide ? kIds64 : 0;
-    A.tiles = (int32_t)L.tiles;
     A.targets = targets;
     A.vocab = c->rows;
     A.part = (float2 *)ws;
     A.picked = (float *)(ws + L.picked);
     if ((rc = ops_cuda(product_launch(kByCols, kLoss, A, s), "k_product"))) return rc;
-    const JoinArgs J{A.part, A.picked, targets, loss, lse, tokens, c->rows, A.tiles, wide};
-    return ops_cuda(ops_launch(true, k_join, uint32_t((tokens + kJoinThreads / 32 - 1) / (kJoinThreads / 32)), kJoinThreads, 0, s, J), "k_join");
+    const JoinArgs J{A.part, A.picked, targets, loss, lse, tokens, c->rows, (int32_t)L.parts, wide};
+    return ops_cuda(ops_launch(true, k_join, uint32_t((tokens + 31) / 32), 32 * kJoinWarps, 0, s, J), "k_join");
 }
 
 int skew_head_grad(const skew_head_config_t *c, const void *h, int64_t ld_h, const void *table, const void *targets, int64_t tokens, const float *lse,

@@ -11,6 +11,8 @@
 // rows are summed over (OUTER) they are zeros in shared memory, so that nothing of another group, NaN included, enters.
 #include "skew_product.h"
 
+#include <cuda.h>
+
 #include <atomic>
 
 #include "skew_ops.h"
@@ -18,25 +20,28 @@
 namespace skew {
 namespace {
 
-constexpr int kLines = 128;                    // of each operand, in a stage
+constexpr int kLines = 128;                    // of each operand, in a CTA's stage
 constexpr int kStep = 64;                      // elements of the summed index in a stage
 constexpr uint32_t kOperandBytes = kLines * kStep * 2;
 constexpr uint32_t kStageBytes = 2 * kOperandBytes;
 constexpr int kStages = 6;
 constexpr int kMaxGroups = 1024;
-constexpr int kTileRows = 128, kTileCols = 128;
-constexpr int kAccCols = 2 * kTileCols;        // of tensor memory: two tiles of sums
-constexpr int kBand = 16;                      // tiles of rows that are walked together (A and B of 152 tiles then stay in L2)
+constexpr int kBandRows = 2048;                // rows of tiles that are walked together (what 152 SMs have under way then stays in L2)
 
-constexpr int kLoadWarps = 8, kEndWarps = 4;
-constexpr int kMulWarp = 0, kFirstEnd = 4, kFirstLoad = 8;  // warps 4 to 7 read lanes 32 (warp % 4) on of tensor memory
-constexpr int kThreads = 32 * (kFirstLoad + kLoadWarps);
+constexpr int kMulWarp = 0, kMemWarp = 1, kCopyWarp = 2, kCutWarp = 3, kFirstEnd = 4, kFirstLoad = 8;  // warps 4 to 7 read lanes 32 (warp % 4) on of tensor memory
+constexpr int kLoadWarps = 8, kEndWarps = 4, kMaxWarps = kFirstLoad + kLoadWarps;
+
+// COPY: stages come by tensor copies (one thread), else by loads of eight warps. PAIR: CTAs that share a tile, 1 or 2.
+template <bool COPY>
+constexpr int kThreads = 32 * (COPY ? kFirstLoad : kMaxWarps);
+template <int PAIR>
+constexpr int kTile = 128 * PAIR;              // rows and columns of a tile
 
 struct Shared {
-    uint64_t full[kStages], empty[kStages], sums[2], freed[2];
+    uint64_t full[kStages], empty[kStages], landed[kStages], sums[2], freed[2];
     uint32_t acc;                     // where the sums are in tensor memory
     uint32_t gave_up;
-    int32_t total[kThreads / 32];
+    int32_t total[kMaxWarps];
     int32_t begin[kMaxGroups + 1];    // first row of each group; the end of the last
     int32_t tile[kMaxGroups + 1];     // tiles of rows before it (BY_ROWS, BY_COLS)
 };
@@ -51,13 +56,27 @@ __device__ __forceinline__ void bar_init(uint64_t *b, uint32_t count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(shared_address(b)), "r"(count) : "memory");
 }
 
-__device__ __forceinline__ void bar_arrive(uint64_t *b) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(shared_address(b)) : "memory");
+// The address of `p` in the pair's first CTA.
+template <int PAIR>
+__device__ __forceinline__ uint32_t in_first(const void *p) {
+    uint32_t a = shared_address(p);
+    if constexpr (PAIR == 2) asm("mapa.shared::cluster.u32 %0, %0, 0;" : "+r"(a));
+    return a;
+}
+
+template <int PAIR>
+__device__ __forceinline__ void bar_arrive(uint64_t *b) {  // the first CTA's
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(in_first<PAIR>(b)) : "memory");
+}
+
+// Arrives at a barrier of this address, which then also waits for `bytes`.
+__device__ __forceinline__ void bar_expect(uint32_t address, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.release.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(address), "r"(bytes) : "memory");
 }
 
 __device__ __forceinline__ bool bar_poll(uint64_t *b, uint32_t parity) {
     uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                  : "=r"(ok) : "r"(shared_address(b)), "r"(parity), "n"(2000) : "memory");
     return ok != 0;
 }
@@ -75,6 +94,14 @@ __device__ __forceinline__ bool bar_wait(uint64_t *b, uint32_t parity, Shared &S
     return false;
 }
 
+__device__ __forceinline__ void drain(uint64_t *b, uint32_t parity) {
+    for (int i = 0; i < 1 << 20 && !bar_poll(b, parity); ++i) {}
+}
+
+__device__ __forceinline__ void pair_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
 // ---------------------------------------------------------------------------
 // Tiles
 // ---------------------------------------------------------------------------
@@ -85,9 +112,9 @@ struct Tile {
 };
 
 // The groups' rows, in order and within [0, rows) whatever `offsets` hold, and the tiles before each.
-template <int KIND>
+template <int KIND, int THREADS, int TILE>
 __device__ __forceinline__ void groups_of(const ProductArgs &A, Shared &S) {
-    const int G = A.groups, per = (G + kThreads) / kThreads, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int G = A.groups, per = (G + THREADS) / THREADS, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int rows = int(A.rows);
     const int i0 = threadIdx.x * per, i1 = min(i0 + per, G + 1);
     auto scan = [&](int v, auto join) {  // what the threads before this one have together; -1 for none
@@ -113,7 +140,7 @@ __device__ __forceinline__ void groups_of(const ProductArgs &A, Shared &S) {
     for (int i = i0; i < i1; ++i) S.begin[i] = m = max(m, at(i));
     __syncthreads();
     if (KIND != kOuter) {
-        auto tiles = [&](int i) { return i < G ? (S.begin[i + 1] - S.begin[i] + kTileRows - 1) / kTileRows : 0; };
+        auto tiles = [&](int i) { return i < G ? (S.begin[i + 1] - S.begin[i] + TILE - 1) / TILE : 0; };
         int n = 0;
         for (int i = i0; i < i1; ++i) n += tiles(i);
         n = scan(n, both);
@@ -122,19 +149,20 @@ __device__ __forceinline__ void groups_of(const ProductArgs &A, Shared &S) {
     __syncthreads();
 }
 
-// The CTA's tiles, one after another: blockIdx.x, + gridDim.x, ...
-template <int KIND>
+// The pair's tiles, one after another: its own number, + the pairs, ...
+template <int KIND, int PAIR>
 struct Walk {
+    static constexpr int kT = kTile<PAIR>, kBand = kBandRows / kT;
     const ProductArgs &A;
     const Shared &S;
     int64_t at, all;
     int64_t each;      // OUTER: tiles of a group
     int32_t nt, group;
 
-    __device__ __forceinline__ Walk(const ProductArgs &a, const Shared &s) : A(a), S(s), at(blockIdx.x), group(0) {
-        nt = (A.cols + kTileCols - 1) / kTileCols;
+    __device__ __forceinline__ Walk(const ProductArgs &a, const Shared &s) : A(a), S(s), at(blockIdx.x / PAIR), group(0) {
+        nt = (A.cols + kT - 1) / kT;
         if (KIND == kOuter) {
-            each = int64_t((A.inner + kTileRows - 1) / kTileRows) * nt;
+            each = int64_t((A.inner + kT - 1) / kT) * nt;
             all = each * A.groups;
         } else {
             all = int64_t(S.tile[A.groups]) * nt;
@@ -148,7 +176,7 @@ struct Walk {
         if (KIND == kOuter) {
             group = int(at / each);
             here = at - group * each;
-            mt = (A.inner + kTileRows - 1) / kTileRows;
+            mt = (A.inner + kT - 1) / kT;
         } else {
             const int row = int(at / nt);  // tiles of rows before this one's, over all groups: its group is the last that begins at or before it
             int lo = group, hi = A.groups;
@@ -165,10 +193,10 @@ struct Walk {
         t.group = group;
         t.r0 = S.begin[group];
         t.r1 = S.begin[group + 1];
-        t.m0 = (first + left % in) * kTileRows + (KIND == kOuter ? 0 : t.r0);
-        t.n0 = left / in * kTileCols;
+        t.m0 = (first + left % in) * kT + (KIND == kOuter ? 0 : t.r0);
+        t.n0 = left / in * kT;
         t.steps = ((KIND == kOuter ? t.r1 - t.r0 : A.inner) + kStep - 1) / kStep;
-        at += gridDim.x;
+        at += gridDim.x / PAIR;
         return true;
     }
 };
@@ -213,6 +241,28 @@ __device__ __forceinline__ void load_lines(const uint16_t *p, int64_t ld, int64_
     }
 }
 
+// A box of a tensor map, from column x, line y of group z, to shared memory at `to`; its bytes count at the barrier of this address.
+template <int PAIR>
+__device__ __forceinline__ void copy_box(const CUtensorMap &map, uint32_t to, uint32_t bar, int x, int y, int z) {
+    if constexpr (PAIR == 2)
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4, %5}], [%2];"
+                     ::"r"(to), "l"(&map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                     ::"r"(to), "l"(&map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+}
+
+// One operand's 128 lines, as load_lines brings them. Beyond the matrix the boxes hold zeros.
+template <bool MAJOR, int PAIR>
+__device__ __forceinline__ void copy_lines(const CUtensorMap &map, uint32_t to, uint32_t bar, int l0, int s0, int group) {
+    if constexpr (MAJOR) {
+        copy_box<PAIR>(map, to, bar, s0, l0, group);
+    } else {
+        copy_box<PAIR>(map, to, bar, l0, s0, group);
+        copy_box<PAIR>(map, to + kOperandBytes / 2, bar, l0 + 64, s0, group);
+    }
+}
+
 // ---------------------------------------------------------------------------
 // Tensor cores
 // ---------------------------------------------------------------------------
@@ -227,18 +277,47 @@ __device__ __forceinline__ uint64_t operand(uint32_t address) {
 template <bool MAJOR>
 constexpr uint32_t kNext16 = (MAJOR ? 32 : 16 * 128) >> 4;
 
-template <bool A_MAJOR, bool B_MAJOR>
+template <bool A_MAJOR, bool B_MAJOR, int PAIR>
 constexpr uint32_t kInstruction = 1u << 4 /* sums fp32 */ | 1u << 7 | 1u << 10 /* bf16 */ | uint32_t(!A_MAJOR) << 15 | uint32_t(!B_MAJOR) << 16 |
-                                  uint32_t(kTileCols >> 3) << 17 | uint32_t(kTileRows >> 4) << 24;
+                                  uint32_t(kTile<PAIR> >> 3) << 17 | uint32_t(kTile<PAIR> >> 4) << 24;
 
+// 16 steps of the tile: for a pair of CTAs, each holds half of A's rows and of B's columns, and takes the sums of its rows.
+template <int PAIR>
 __device__ __forceinline__ void multiply(uint32_t acc, uint64_t a, uint64_t b, uint32_t instruction, bool add) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(acc), "l"(a), "l"(b), "r"(instruction), "r"(uint32_t(add)) : "memory");
+    if constexpr (PAIR == 2)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(acc), "l"(a), "l"(b), "r"(instruction), "r"(uint32_t(add)) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(acc), "l"(a), "l"(b), "r"(instruction), "r"(uint32_t(add)) : "memory");
 }
 
-// Arrives once what was issued before is done.
+// Arrives, in each CTA of the pair, once what was issued before is done.
+template <int PAIR>
 __device__ __forceinline__ void commit(uint64_t *bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(shared_address(bar)) : "memory");
+    if constexpr (PAIR == 2)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(shared_address(bar)), "h"(uint16_t(3)) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(shared_address(bar)) : "memory");
+}
+
+template <int PAIR>
+__device__ __forceinline__ void take_tensor_memory(uint32_t *address) {
+    if constexpr (PAIR == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_address(address)), "n"(2 * kTile<PAIR>) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_address(address)), "n"(2 * kTile<PAIR>) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+}
+
+template <int PAIR>
+__device__ __forceinline__ void give_tensor_memory(uint32_t acc) {
+    if constexpr (PAIR == 2)
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(acc), "n"(2 * kTile<PAIR>) : "memory");
+    else
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(acc), "n"(2 * kTile<PAIR>) : "memory");
 }
 
 __device__ __forceinline__ void after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -301,17 +380,18 @@ __device__ __forceinline__ int64_t target_of(const ProductArgs &A, int64_t row) 
     return v < 0 || v >= A.vocab ? -1 : v;
 }
 
+constexpr int kPart = 128;  // columns of a LOSS part: a tile's or half a tile's
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // A tile's 32 rows of one warp, read from tensor memory at `acc` (`none`: the sums are zero).
-template <int KIND, int END>
+template <int KIND, int END, int COLS>
 __device__ __forceinline__ void end_tile(const ProductArgs &A, const Tile &t, uint32_t acc, bool none, int row_in_tile) {
     const int64_t row = t.m0 + row_in_tile;
     const bool mine = row < (KIND == kOuter ? A.inner : t.r1);
     float x[32];
     if constexpr (END == kStore) {
         const int64_t at = t.group * A.o_group * (KIND == kOuter) + row * A.ldo;
-        for (int c = 0; c < kTileCols && t.n0 + c < A.cols; c += 32) {
+        for (int c = 0; c < COLS && t.n0 + c < A.cols; c += 32) {
             if (none) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i) x[i] = 0.f;
@@ -334,7 +414,7 @@ __device__ __forceinline__ void end_tile(const ProductArgs &A, const Tile &t, ui
         const float scale2 = A.scale * kLog2e;
         const int64_t target = mine ? target_of(A, row) : -1;
         float top = -INFINITY, sum = 0.f;
-        for (int c = 0; c < kTileCols && t.n0 + c < A.cols; c += 32) {
+        for (int c = 0; c < COLS && t.n0 + c < A.cols; c += 32) {
             read_sums(acc + c, x);
             const int n = A.cols - t.n0 - c;
             const int64_t at = target - t.n0 - c;
@@ -356,13 +436,17 @@ __device__ __forceinline__ void end_tile(const ProductArgs &A, const Tile &t, ui
             for (int i = 0; i < 32; ++i) part += exp2_of(x[i] - from);
             sum = fmaf(sum, exp2_of(top - from), part);
             top = high;
+            if ((c + 32) % kPart == 0 || n <= 32) {  // parts of a row one after another, so that lanes write side by side
+                if (mine) A.part[int64_t((t.n0 + c) / kPart) * A.rows + row] = make_float2(top, sum);
+                top = -INFINITY;
+                sum = 0.f;
+            }
         }
-        if (mine) A.part[row * A.tiles + t.n0 / kTileCols] = make_float2(top, sum);
     } else {
         const float scale2 = A.scale * kLog2e;
         const int64_t target = mine ? target_of(A, row) : -1;
         const float g = target >= 0 ? A.dloss[row] : 0.f, lse2 = target >= 0 ? A.lse[row] * kLog2e : 0.f;
-        for (int c = 0; c < kTileCols && t.n0 + c < A.cols; c += 32) {
+        for (int c = 0; c < COLS && t.n0 + c < A.cols; c += 32) {
             read_sums(acc + c, x);
             const int64_t at = target - A.first - t.n0 - c;
 #pragma unroll
@@ -400,36 +484,73 @@ __device__ __forceinline__ void clear_rows(const ProductArgs &A, const Shared &S
     }
 }
 
-template <int KIND, int END>
-__global__ void __launch_bounds__(kThreads, 1) k_product(const ProductArgs A) {
+template <int KIND, int END, bool COPY, int PAIR>
+__global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                                                               const ProductArgs A) {
     extern __shared__ char raw[];
     char *const ring = raw + (1024 - (shared_address(raw) & 1023)) % 1024;
     Shared &S = *reinterpret_cast<Shared *>(ring + size_t(kStages) * kStageBytes);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr int kT = kTile<PAIR>;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = PAIR == 2 ? blockIdx.x & 1 : 0;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kStages; ++i) bar_init(&S.full[i], kLoadWarps), bar_init(&S.empty[i], 1);
-        for (int i = 0; i < 2; ++i) bar_init(&S.sums[i], 1), bar_init(&S.freed[i], kEndWarps);
+        for (int i = 0; i < kStages; ++i) bar_init(&S.full[i], PAIR * (COPY ? 1 : kLoadWarps)), bar_init(&S.empty[i], 1), bar_init(&S.landed[i], 1);
+        for (int i = 0; i < 2; ++i) bar_init(&S.sums[i], 1), bar_init(&S.freed[i], PAIR * kEndWarps);
         S.gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_address(&S.acc)), "n"(kAccCols) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    }
-    groups_of<KIND>(A, S);
+    if (warp == kMemWarp) take_tensor_memory<PAIR>(&S.acc);
+    groups_of<KIND, kThreads<COPY>, kT>(A, S);
     before_sync();
-    __syncthreads();
+    if (PAIR == 2) pair_sync(); else __syncthreads();
     after_sync();
     const uint32_t acc = S.acc;
     constexpr bool A_MAJOR = KIND != kOuter, B_MAJOR = KIND == kByCols;
-    Walk<KIND> walk(A, S);
+    Walk<KIND, PAIR> walk(A, S);
     Tile t;
+    uint32_t n = 0;  // stages so far
+    bool ok = true;
 
-    if (warp >= kFirstLoad) {
+    if (COPY && warp == kCopyWarp) {
+        if (!lane) {
+            while (ok && walk.next(t)) {
+                const int m0 = t.m0 + rank * kLines, n0 = t.n0 + rank * kLines;
+                // A CTA whose rows all belong to the groups behind needs none of them: its sums are not read.
+                const bool rows = KIND == kOuter || m0 < t.r1;
+                for (int k = 0; k < t.steps; ++k, ++n) {
+                    const int s = n % kStages, s0 = (KIND == kOuter ? t.r0 : 0) + k * kStep;
+                    if (n >= kStages && !(ok = bar_wait(&S.empty[s], (n / kStages - 1) & 1, S))) break;
+                    // The last lines of a group that ends within a stage go to the warp that clears what is behind them.
+                    const bool cut = KIND == kOuter && s0 + kStep > t.r1;
+                    const uint32_t to = shared_address(ring) + s * kStageBytes, bar = cut ? shared_address(&S.landed[s]) : in_first<PAIR>(&S.full[s]);
+                    bar_expect(bar, rows ? kStageBytes : kOperandBytes);
+                    if (rows) copy_lines<A_MAJOR, PAIR>(map_a, to, bar, m0, s0, 0);
+                    copy_lines<B_MAJOR, PAIR>(map_b, to + kOperandBytes, bar, n0, s0, KIND == kOuter ? 0 : t.group);
+                }
+            }
+            // what was asked for arrives before the shared memory is given back
+            if (!ok && !rank)
+                for (uint32_t i = n > kStages ? n - kStages : 0; i < n; ++i) drain(&S.full[i % kStages], i / kStages & 1);
+        }
+    } else if (COPY && KIND == kOuter && warp == kCutWarp) {
+        uint32_t phases = 0;
+        while (ok && walk.next(t)) {
+            const int left = (t.r1 - t.r0) % kStep;
+            n += t.steps;
+            if (!left || !t.steps) continue;
+            const int s = (n - 1) % kStages;
+            if (!(ok = bar_wait(&S.landed[s], phases >> s & 1, S))) break;
+            phases ^= 1u << s;
+            char *const at = ring + size_t(s) * kStageBytes;
+            for (int i = left * 8 + lane; i < kStep * 8; i += 32)  // 16-byte units of a block's lines
+#pragma unroll
+                for (int b = 0; b < 4; ++b) *reinterpret_cast<uint4 *>(at + b * (kOperandBytes / 2) + i * 16) = make_uint4(0, 0, 0, 0);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (!lane) bar_arrive<PAIR>(&S.full[s]);
+        }
+    } else if (!COPY && warp >= kFirstLoad) {
         const int w = (warp - kFirstLoad) % (kLoadWarps / 2);
         const bool second = warp - kFirstLoad >= kLoadWarps / 2;
-        uint32_t n = 0;
-        bool ok = true;
         while (ok && walk.next(t)) {
             const uint16_t *b = static_cast<const uint16_t *>(A.b) + t.group * A.b_group * (KIND != kOuter);
             for (int k = 0; k < t.steps; ++k, ++n) {
@@ -438,47 +559,42 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const ProductArgs A) {
                 char *to = ring + size_t(s) * kStageBytes;
                 const int64_t s0 = (KIND == kOuter ? t.r0 : 0) + int64_t(k) * kStep, s_end = KIND == kOuter ? t.r1 : A.inner;
                 if (!second)
-                    load_lines<A_MAJOR>(static_cast<const uint16_t *>(A.a), A.lda, t.m0, KIND == kOuter ? A.inner : t.r1, s0, s_end, to, w, lane);
+                    load_lines<A_MAJOR>(static_cast<const uint16_t *>(A.a), A.lda, t.m0 + rank * kLines, KIND == kOuter ? A.inner : t.r1, s0, s_end, to, w, lane);
                 else
-                    load_lines<B_MAJOR>(b, A.ldb, t.n0, A.cols, s0, s_end, to + kOperandBytes, w, lane);
+                    load_lines<B_MAJOR>(b, A.ldb, t.n0 + rank * kLines, A.cols, s0, s_end, to + kOperandBytes, w, lane);
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (!lane) bar_arrive(&S.full[s]);
+                if (!lane) bar_arrive<PAIR>(&S.full[s]);
             }
         }
-    } else if (warp == kMulWarp) {
+    } else if (warp == kMulWarp && !rank) {
         if (!lane) {
-            uint32_t n = 0, tiles = 0;
-            bool ok = true;
+            uint32_t tiles = 0;
             while (ok && walk.next(t)) {
                 if (!t.steps) continue;
-                const uint32_t half = tiles & 1, to = acc + half * kTileCols;
+                const uint32_t half = tiles & 1, to = acc + half * kT;
                 if (tiles >= 2 && !(ok = bar_wait(&S.freed[half], (tiles / 2 - 1) & 1, S))) break;
                 after_sync();
                 for (int k = 0; k < t.steps; ++k, ++n) {
                     const int s = n % kStages;
                     if (!(ok = bar_wait(&S.full[s], n / kStages & 1, S))) break;
                     after_sync();
-                    const uint32_t at = shared_address(ring + size_t(s) * kStageBytes);
+                    const uint32_t at = shared_address(ring) + s * kStageBytes;
                     const uint64_t a = operand<A_MAJOR>(at), b = operand<B_MAJOR>(at + kOperandBytes);
 #pragma unroll
                     for (int i = 0; i < kStep / 16; ++i)
-                        multiply(to, a + i * kNext16<A_MAJOR>, b + i * kNext16<B_MAJOR>, kInstruction<A_MAJOR, B_MAJOR>, k | i);
-                    commit(&S.empty[s]);
+                        multiply<PAIR>(to, a + i * kNext16<A_MAJOR>, b + i * kNext16<B_MAJOR>, kInstruction<A_MAJOR, B_MAJOR, PAIR>, k | i);
+                    commit<PAIR>(&S.empty[s]);
                 }
-                if (ok) commit(&S.sums[half]);
+                if (ok) commit<PAIR>(&S.sums[half]);
                 ++tiles;
             }
             // what was issued ends before the tensor memory is given back
-            if (!ok && n) {
-                const uint32_t s = (n - 1) % kStages;
-                for (int i = 0; i < 1 << 20 && !bar_poll(&S.empty[s], (n - 1) / kStages & 1); ++i) {}
-            }
+            if (!ok && n) drain(&S.empty[(n - 1) % kStages], (n - 1) / kStages & 1);
         }
     } else if (warp >= kFirstEnd && warp < kFirstEnd + kEndWarps) {
         const int q = warp - kFirstEnd;
         uint32_t tiles = 0;
-        bool ok = true;
         while (ok && walk.next(t)) {
             const uint32_t half = tiles & 1;
             if (t.steps) {
@@ -487,11 +603,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const ProductArgs A) {
             } else if (KIND == kOuter && A.base == A.out) {
                 continue;
             }
-            end_tile<KIND, END>(A, t, acc + half * kTileCols + (uint32_t(q * 32) << 16), !t.steps, q * 32 + lane);
+            end_tile<KIND, END, kT>(A, t, acc + half * kT + (uint32_t(q * 32) << 16), !t.steps, rank * kLines + q * 32 + lane);
             if (t.steps) {
                 before_sync();
                 __syncwarp();
-                if (!lane) bar_arrive(&S.freed[half]);
+                if (!lane) bar_arrive<PAIR>(&S.freed[half]);
                 ++tiles;
             }
         }
@@ -499,26 +615,79 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const ProductArgs A) {
     }
     before_sync();
     __syncwarp();
-    __syncthreads();
-    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(acc), "n"(kAccCols) : "memory");
+    if (PAIR == 2) pair_sync(); else __syncthreads();
+    if (warp == kMemWarp) give_tensor_memory<PAIR>(acc);
+}
+
+// ---------------------------------------------------------------------------
+// Host
+// ---------------------------------------------------------------------------
+using Encode = decltype(&cuTensorMapEncodeTiled);
+
+Encode encoder() {
+    static const Encode f = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult got;
+        return cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &got) == cudaSuccess && got == cudaDriverEntryPointSuccess
+                   ? reinterpret_cast<Encode>(p) : nullptr;
+    }();
+    return f;
+}
+
+// Lines of `x` elements, `ld` apart, y of them in a group and z groups; boxes of 64 elements of `lines` lines.
+bool map_of(CUtensorMap *m, const void *p, int64_t x, int64_t ld, int64_t y, int64_t group, int64_t z, uint32_t lines) {
+    const cuuint64_t dims[3] = {cuuint64_t(x), cuuint64_t(y), cuuint64_t(z)}, strides[2] = {cuuint64_t(ld) * 2, cuuint64_t(z > 1 ? group : ld) * 2};
+    const cuuint32_t box[3] = {64, lines, 1}, step[3] = {1, 1, 1};
+    const Encode f = encoder();
+    return f && f(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Whether tensor copies can bring a matrix: lines on 16-byte boundaries, strides that their maps hold.
+bool copies(const void *p, int64_t ld, int64_t group, int64_t groups) {
+    return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && (groups == 1 || (group % 8 == 0 && group < int64_t(1) << 38));
+}
+
+template <int KIND, int END, bool COPY, int PAIR>
+cudaError_t launch_of(const ProductArgs &A, const CUtensorMap &a, const CUtensorMap &b, cudaStream_t s) {
+    constexpr auto k = k_product<KIND, END, COPY, PAIR>;
+    const cudaError_t e = ops_allow_smem<k>(int(kSharedBytes));
+    if (e != cudaSuccess) return e;
+    constexpr int kT = kTile<PAIR>;
+    const int64_t nt = (A.cols + kT - 1) / kT;
+    const int64_t most = (KIND == kOuter ? int64_t((A.inner + kT - 1) / kT) * A.groups : A.rows / kT + A.groups) * nt;
+    const int64_t pairs = ops_sm_count() / PAIR;
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = PAIR;
+    at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(uint32_t(most < pairs ? most : pairs) * PAIR);
+    cfg.blockDim = dim3(kThreads<COPY>);
+    cfg.dynamicSmemBytes = kSharedBytes;
+    cfg.stream = s;
+    cfg.attrs = &at;
+    cfg.numAttrs = PAIR > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, k, a, b, A);
 }
 
 template <int KIND, int END>
 cudaError_t launch(const ProductArgs &A, cudaStream_t s) {
-    constexpr auto k = k_product<KIND, END>;
-    const cudaError_t e = ops_allow_smem<k>(int(kSharedBytes));
-    if (e != cudaSuccess) return e;
-    const int64_t nt = (A.cols + kTileCols - 1) / kTileCols;
-    const int64_t most = (KIND == kOuter ? int64_t((A.inner + kTileRows - 1) / kTileRows) * A.groups : A.rows / kTileRows + A.groups) * nt;
-    const int64_t sms = ops_sm_count();
-    return ops_launch(false, k, uint32_t(most < sms ? most : sms), kThreads, kSharedBytes, s, A);
+    CUtensorMap a{}, b{};
+    constexpr bool A_MAJOR = KIND != kOuter, B_MAJOR = KIND == kByCols;
+    const bool outer = KIND == kOuter;
+    const int64_t groups = outer ? 1 : A.groups;
+    if (A.rows && copies(A.a, A.lda, 0, 1) && copies(A.b, A.ldb, A.b_group, groups) && map_of(&a, A.a, A.inner, A.lda, A.rows, 0, 1, A_MAJOR ? kLines : kStep) &&
+        map_of(&b, A.b, B_MAJOR ? A.inner : A.cols, A.ldb, B_MAJOR ? A.cols : outer ? A.rows : A.inner, A.b_group, groups, B_MAJOR ? kLines : kStep))
+        return launch_of<KIND, END, true, 2>(A, a, b, s);
+    return launch_of<KIND, END, false, 1>(A, a, b, s);
 }
 
 }  // namespace
 
-int32_t product_loss_columns() { return kTileCols; }
+int32_t product_loss_columns() { return kPart; }
 
-cudaError_t product_launch(ProductKind kind, ProductEnd end, ProductArgs &A, cudaStream_t s) {
+cudaError_t product_launch(ProductKind kind, ProductEnd end, const ProductArgs &A, cudaStream_t s) {
     if (end == kLoss) return launch<kByCols, kLoss>(A, s);
     if (end == kLogitsGrad) return launch<kByCols, kLogitsGrad>(A, s);
     return kind == kByRows ? launch<kByRows, kStore>(A, s) : kind == kByCols ? launch<kByCols, kStore>(A, s) : launch<kOuter, kStore>(A, s);

@@ -34,18 +34,17 @@ struct ProductArgs {
     int64_t ldo, o_group;
     float scale;
     // LOSS, LOGITS_GRAD
-    int32_t tiles;              // LOSS: parts of a row
     const void *targets;        // one for each row; not in [0, vocab): none
     int64_t first, vocab;       // the column j is the vocabulary's `first` + j
     const float *lse, *dloss;
-    float2 *part;               // [rows][tiles]: (largest, sum) in powers of two
+    float2 *part;               // [part of a row][rows]: (largest, sum) in powers of two
     float *picked;              // [rows]: the target's x
 };
 
 // Columns of a LOSS part.
 int32_t product_loss_columns();
 // Runs the product on `stream`; every pointer, size and stride has been checked.
-cudaError_t product_launch(ProductKind kind, ProductEnd end, ProductArgs &A, cudaStream_t stream);
+cudaError_t product_launch(ProductKind kind, ProductEnd end, const ProductArgs &A, cudaStream_t stream);
 // Synchronises, and reads and clears the word in which a wait on the device that gave up leaves its mark: a SKEW_* code.
 int product_status(cudaStream_t stream);
 

@@ -24,16 +24,19 @@ constexpr int kLines = 128;                    // of each operand, in a CTA's st
 constexpr int kStep = 64;                      // elements of the summed index in a stage
 constexpr uint32_t kOperandBytes = kLines * kStep * 2;
 constexpr uint32_t kStageBytes = 2 * kOperandBytes;
-constexpr int kStages = 6;
+constexpr int kStages = 6;                     // 5 where there are many groups
 constexpr int kMaxGroups = 1024;
 constexpr int kBandRows = 2048;                // rows of tiles that are walked together (what 152 SMs have under way then stays in L2)
 
-constexpr int kMulWarp = 0, kMemWarp = 1, kCopyWarp = 2, kCutWarp = 3, kFirstEnd = 4, kFirstLoad = 8;  // warps 4 to 7 read lanes 32 (warp % 4) on of tensor memory
-constexpr int kLoadWarps = 8, kEndWarps = 4, kMaxWarps = kFirstLoad + kLoadWarps;
+constexpr int kMulWarp = 0, kMemWarp = 1, kCopyWarp = 2, kCutWarp = 3, kFirstEnd = 4;  // of the warps from 4 on, each reads lanes 32 (warp % 4) on of tensor memory
+constexpr int kLoadWarps = 8;
 
-// COPY: stages come by tensor copies (one thread), else by loads of eight warps. PAIR: CTAs that share a tile, 1 or 2.
+// COPY: stages come by tensor copies (one thread), and eight warps write out; else eight warps load, and four write out.
 template <bool COPY>
-constexpr int kThreads = 32 * (COPY ? kFirstLoad : kMaxWarps);
+constexpr int kEndWarps = COPY ? 8 : 4;
+template <bool COPY>
+constexpr int kThreads = 32 * (kFirstEnd + kEndWarps<COPY> + (COPY ? 0 : kLoadWarps));
+// PAIR: CTAs that share a tile, 1 or 2.
 template <int PAIR>
 constexpr int kTile = 128 * PAIR;              // rows and columns of a tile
 
@@ -41,12 +44,25 @@ struct Shared {
     uint64_t full[kStages], empty[kStages], landed[kStages], sums[2], freed[2];
     uint32_t acc;                     // where the sums are in tensor memory
     uint32_t gave_up;
-    int32_t total[kMaxWarps];
-    int32_t begin[kMaxGroups + 1];    // first row of each group; the end of the last
-    int32_t tile[kMaxGroups + 1];     // tiles of rows before it (BY_ROWS, BY_COLS)
+    int32_t total[32];
+    int32_t begin[1];                 // [groups + 1]: first row of each group, and the end of the last; then
+                                      // [groups + 1]: tiles of rows before it (BY_ROWS, BY_COLS)
 };
 
-constexpr size_t kSharedBytes = 1024 + size_t(kStages) * kStageBytes + sizeof(Shared);
+constexpr int kOutBytes = 32 * 128;            // 32 rows of 128 bytes, of each warp that writes out
+constexpr size_t kMaxSharedBytes = 232448;
+constexpr size_t shared_bytes(int stages, int end_warps, int groups) {
+    return 1024 + size_t(stages) * kStageBytes + size_t(end_warps) * kOutBytes + sizeof(Shared) + size_t(groups + 1) * 8;
+}
+static_assert(shared_bytes(kStages - 1, 8, kMaxGroups) <= kMaxSharedBytes, "shared memory of a CTA");
+
+// A place in the ring of stages, and how often it was there before (odd or even).
+struct Place {
+    uint32_t s = 0, phase = 0;
+    __device__ __forceinline__ void next(uint32_t stages) {
+        if (++s == stages) s = 0, phase ^= 1;
+    }
+};
 
 __device__ uint32_t g_status;  // 1: a wait gave up
 
@@ -69,9 +85,10 @@ __device__ __forceinline__ void bar_arrive(uint64_t *b) {  // the first CTA's
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(in_first<PAIR>(b)) : "memory");
 }
 
-// Arrives at a barrier of this address, which then also waits for `bytes`.
+// Arrives at a barrier of this address, which then also waits for `bytes`. (Relaxed: nothing that this thread wrote is read after it. A release
+// waits for what is under way, copies among it: 0.6 us a stage.)
 __device__ __forceinline__ void bar_expect(uint32_t address, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.release.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(address), "r"(bytes) : "memory");
+    asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(address), "r"(bytes) : "memory");
 }
 
 __device__ __forceinline__ bool bar_poll(uint64_t *b, uint32_t parity) {
@@ -111,6 +128,8 @@ struct Tile {
     int32_t steps;                // of the summed index
 };
 
+__device__ __forceinline__ int32_t *tiles_of(const ProductArgs &A, Shared &S) { return S.begin + A.groups + 1; }
+
 // The groups' rows, in order and within [0, rows) whatever `offsets` hold, and the tiles before each.
 template <int KIND, int THREADS, int TILE>
 __device__ __forceinline__ void groups_of(const ProductArgs &A, Shared &S) {
@@ -140,11 +159,12 @@ __device__ __forceinline__ void groups_of(const ProductArgs &A, Shared &S) {
     for (int i = i0; i < i1; ++i) S.begin[i] = m = max(m, at(i));
     __syncthreads();
     if (KIND != kOuter) {
+        int32_t *const tile = tiles_of(A, S);
         auto tiles = [&](int i) { return i < G ? (S.begin[i + 1] - S.begin[i] + TILE - 1) / TILE : 0; };
         int n = 0;
         for (int i = i0; i < i1; ++i) n += tiles(i);
         n = scan(n, both);
-        for (int i = i0; i < i1; ++i) S.tile[i] = n, n += tiles(i);
+        for (int i = i0; i < i1; ++i) tile[i] = n, n += tiles(i);
     }
     __syncthreads();
 }
@@ -154,18 +174,18 @@ template <int KIND, int PAIR>
 struct Walk {
     static constexpr int kT = kTile<PAIR>, kBand = kBandRows / kT;
     const ProductArgs &A;
-    const Shared &S;
+    const int32_t *begin, *tile;
     int64_t at, all;
     int64_t each;      // OUTER: tiles of a group
     int32_t nt, group;
 
-    __device__ __forceinline__ Walk(const ProductArgs &a, const Shared &s) : A(a), S(s), at(blockIdx.x / PAIR), group(0) {
+    __device__ __forceinline__ Walk(const ProductArgs &a, Shared &s) : A(a), begin(s.begin), tile(tiles_of(a, s)), at(blockIdx.x / PAIR), group(0) {
         nt = (A.cols + kT - 1) / kT;
         if (KIND == kOuter) {
             each = int64_t((A.inner + kT - 1) / kT) * nt;
             all = each * A.groups;
         } else {
-            all = int64_t(S.tile[A.groups]) * nt;
+            all = int64_t(tile[A.groups]) * nt;
         }
     }
 
@@ -182,17 +202,17 @@ struct Walk {
             int lo = group, hi = A.groups;
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
-                if (S.tile[mid] <= row) lo = mid; else hi = mid;
+                if (tile[mid] <= row) lo = mid; else hi = mid;
             }
             group = lo;
-            here = at - int64_t(S.tile[group]) * nt;
-            mt = S.tile[group + 1] - S.tile[group];
+            here = at - int64_t(tile[group]) * nt;
+            mt = tile[group + 1] - tile[group];
         }
         const int64_t span = int64_t(kBand) * nt;
         const int band = int(here / span), first = band * kBand, in = min(kBand, mt - first), left = int(here - band * span);
         t.group = group;
-        t.r0 = S.begin[group];
-        t.r1 = S.begin[group + 1];
+        t.r0 = begin[group];
+        t.r1 = begin[group + 1];
         t.m0 = (first + left % in) * kT + (KIND == kOuter ? 0 : t.r0);
         t.n0 = left / in * kT;
         t.steps = ((KIND == kOuter ? t.r1 - t.r0 : A.inner) + kStep - 1) / kStep;
@@ -323,17 +343,24 @@ __device__ __forceinline__ void give_tensor_memory(uint32_t acc) {
 __device__ __forceinline__ void after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 
-// 32 columns of the warp's 32 lanes: x[c] of this lane.
+// 32 columns of the warp's 32 lanes, x[c] of this lane: there after sums_read.
 __device__ __forceinline__ void read_sums(uint32_t at, float (&x)[32]) {
-    __syncwarp();
     uint32_t *u = reinterpret_cast<uint32_t *>(x);
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
         : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]), "=r"(u[10]), "=r"(u[11]),
           "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]), "=r"(u[16]), "=r"(u[17]), "=r"(u[18]), "=r"(u[19]), "=r"(u[20]), "=r"(u[21]), "=r"(u[22]),
           "=r"(u[23]), "=r"(u[24]), "=r"(u[25]), "=r"(u[26]), "=r"(u[27]), "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
         : "r"(at) : "memory");
+}
+
+__device__ __forceinline__ void sums_read(float (&x)[32]) {  // (x: so that nothing that reads it moves before)
+    uint32_t *u = reinterpret_cast<uint32_t *>(x);
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+        : "+r"(u[0]), "+r"(u[1]), "+r"(u[2]), "+r"(u[3]), "+r"(u[4]), "+r"(u[5]), "+r"(u[6]), "+r"(u[7]), "+r"(u[8]), "+r"(u[9]), "+r"(u[10]), "+r"(u[11]),
+          "+r"(u[12]), "+r"(u[13]), "+r"(u[14]), "+r"(u[15]), "+r"(u[16]), "+r"(u[17]), "+r"(u[18]), "+r"(u[19]), "+r"(u[20]), "+r"(u[21]), "+r"(u[22]),
+          "+r"(u[23]), "+r"(u[24]), "+r"(u[25]), "+r"(u[26]), "+r"(u[27]), "+r"(u[28]), "+r"(u[29]), "+r"(u[30]), "+r"(u[31])
+        :: "memory");
 }
 
 // ---------------------------------------------------------------------------
@@ -345,34 +372,66 @@ __device__ __forceinline__ float exp2_of(float x) {
     return y;
 }
 
-// out = base + scale * x for 32 columns of a row, of which `n` are there.
-template <bool O32, bool B32>
-__device__ __forceinline__ void store_sums(const ProductArgs &A, int64_t at, int n, bool vec, const float (&x)[32]) {
-    if (n >= 32 && vec) {
+// y = base + scale * x for 32 columns of a row, of which `n` are there.
+template <bool B32>
+__device__ __forceinline__ void add_base(const ProductArgs &A, int64_t at, int n, float (&x)[32]) {
+    if (!A.base) {
 #pragma unroll
-        for (int c = 0; c < 32; c += 8) {
-            float y[8];
-            if (A.base) {
-                const Vec8<B32> b = load8_cached<B32>(A.base, at + c);
+        for (int c = 0; c < 32; ++c) x[c] *= A.scale;
+    } else if (n >= 32 && A.flags & kOutVec) {
+        Vec8<B32> b[4];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = fmaf(x[c + i], A.scale, b.at(i));
-            } else {
+        for (int c = 0; c < 4; ++c) b[c] = load8_cached<B32>(A.base, at + 8 * c);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = x[c + i] * A.scale;
-            }
-            char *q = const_cast<char *>(elem_ptr<O32>(A.out, at + c));
-            if constexpr (O32) {
-                reinterpret_cast<float4 *>(q)[0] = make_float4(y[0], y[1], y[2], y[3]);
-                reinterpret_cast<float4 *>(q)[1] = make_float4(y[4], y[5], y[6], y[7]);
-            } else {
-                *reinterpret_cast<uint4 *>(q) = make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
-            }
-        }
+        for (int c = 0; c < 32; ++c) x[c] = fmaf(x[c], A.scale, b[c / 8].at(c % 8));
+    } else {
+#pragma unroll
+        for (int c = 0; c < 32; ++c) x[c] = c < n ? fmaf(x[c], A.scale, load1<B32>(A.base, at + c)) : 0.f;
+    }
+}
+
+// 32 columns of a row, of which `n` are there, to memory.
+template <bool O32>
+__device__ __forceinline__ void put_columns(const ProductArgs &A, int64_t at, int n, const float (&y)[32]) {
+    if (n >= 32 && A.flags & kOutVec) {
+        uint4 *q = reinterpret_cast<uint4 *>(const_cast<char *>(elem_ptr<O32>(A.out, at)));
+#pragma unroll
+        for (int c = 0; c < 32; c += O32 ? 4 : 8)
+            q[c / (O32 ? 4 : 8)] = O32 ? make_uint4(__float_as_uint(y[c]), __float_as_uint(y[c + 1]), __float_as_uint(y[c + 2]), __float_as_uint(y[c + 3]))
+                                       : make_uint4(pack_bf16(y[c], y[c + 1]), pack_bf16(y[c + 2], y[c + 3]), pack_bf16(y[c + 4], y[c + 5]), pack_bf16(y[c + 6], y[c + 7]));
         return;
     }
 #pragma unroll
     for (int c = 0; c < 32; ++c)
-        if (c < n) store1<O32>(A.out, at + c, A.base ? fmaf(x[c], A.scale, load1<B32>(A.base, at + c)) : x[c] * A.scale);
+        if (c < n) store1<O32>(A.out, at + c, y[c]);
+}
+
+// The 32 columns to the lane's row of the warp's 32 x 128 bytes of shared memory, 16-byte units permuted as in a stage; the last of the 128 bytes then
+// leave by a tensor copy, which keeps to the matrix. `column`: the first of the 32.
+template <bool O32>
+__device__ __forceinline__ void copy_columns(const CUtensorMap &map, char *to, int column, int row0, int group, bool last, const float (&y)[32]) {
+    const int lane = threadIdx.x & 31;
+    constexpr int kWide = O32 ? 32 : 64;  // columns of 128 bytes
+    const int part = column % kWide;
+    if (part == 0) {
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        __syncwarp();
+    }
+#pragma unroll
+    for (int c = 0; c < 32; c += O32 ? 4 : 8) {
+        const uint4 u = O32 ? make_uint4(__float_as_uint(y[c]), __float_as_uint(y[c + 1]), __float_as_uint(y[c + 2]), __float_as_uint(y[c + 3]))
+                            : make_uint4(pack_bf16(y[c], y[c + 1]), pack_bf16(y[c + 2], y[c + 3]), pack_bf16(y[c + 4], y[c + 5]), pack_bf16(y[c + 6], y[c + 7]));
+        *reinterpret_cast<uint4 *>(to + lane * 128 + ((((part + c) / (O32 ? 4 : 8)) ^ (lane & 7)) * 16)) = u;
+    }
+    if (part + 32 == kWide || last) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+            asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
+                         ::"l"(&map), "r"(shared_address(to)), "r"(column - part), "r"(row0), "r"(group) : "memory");
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
+    }
 }
 
 __device__ __forceinline__ int64_t target_of(const ProductArgs &A, int64_t row) {  // -1: none
@@ -380,48 +439,44 @@ __device__ __forceinline__ int64_t target_of(const ProductArgs &A, int64_t row) 
     return v < 0 || v >= A.vocab ? -1 : v;
 }
 
-constexpr int kPart = 128;  // columns of a LOSS part: a tile's or half a tile's
+constexpr int kPart = 128;  // columns of a LOSS part: what one warp has of a tile
 constexpr float kLog2e = 1.44269504088896340736f;
 
-// A tile's 32 rows of one warp, read from tensor memory at `acc` (`none`: the sums are zero).
+// What a warp does with 32 rows and COLS columns of a tile, from row `row0` and column `col0` of it, whose sums are at `acc` (`none`: they are zeros).
 template <int KIND, int END, int COLS>
-__device__ __forceinline__ void end_tile(const ProductArgs &A, const Tile &t, uint32_t acc, bool none, int row_in_tile) {
-    const int64_t row = t.m0 + row_in_tile;
-    const bool mine = row < (KIND == kOuter ? A.inner : t.r1);
-    float x[32];
-    if constexpr (END == kStore) {
-        const int64_t at = t.group * A.o_group * (KIND == kOuter) + row * A.ldo;
-        for (int c = 0; c < COLS && t.n0 + c < A.cols; c += 32) {
-            if (none) {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) x[i] = 0.f;
-            } else {
-                read_sums(acc + c, x);
+__device__ __forceinline__ void end_tile(const ProductArgs &A, const CUtensorMap &map, char *buffer, const Tile &t, uint32_t acc, bool none, int row0, int col0) {
+    const int64_t first = int64_t(t.m0) + row0, row = first + (threadIdx.x & 31);
+    const int64_t end = KIND == kOuter ? A.inner : t.r1;
+    const bool mine = row < end;
+    const int start = t.n0 + col0, stop = min(start + COLS, A.cols);
+    if (first >= end || start >= stop) return;
+    // STORE: whole by a tensor copy, unless rows of the group behind would be written.
+    const bool copy = A.flags & kOutCopy && (KIND == kOuter || !A.offsets || first + 32 <= end);
+    const int64_t at = (KIND == kOuter ? t.group * A.o_group : 0) + row * A.ldo;
+    const int group = KIND == kOuter ? t.group : 0;
+    // LOSS, LOGITS_GRAD: in powers of two, exp(x) = 2^(x log2 e)
+    const float scale2 = A.scale * kLog2e;
+    const int64_t target = END != kStore && mine ? target_of(A, row) : -1;
+    const float g = END == kLogitsGrad && target >= 0 ? A.dloss[row] : 0.f, lse2 = END == kLogitsGrad && target >= 0 ? A.lse[row] * kLog2e : 0.f;
+    float top = -INFINITY, sum = 0.f;
+
+    auto chunk = [&](int column, float (&x)[32]) {  // 32 columns
+        const int n = stop - column;
+        if constexpr (END == kStore) {
+            if (mine) {
+                if (A.flags & kBase32) add_base<true>(A, at + column, n, x); else add_base<false>(A, at + column, n, x);
             }
-            const int n = A.cols - t.n0 - c;
-            const bool vec = A.flags & kOutVec;
-            if (!mine) {
-            } else if (A.flags & kOut32) {
-                store_sums<true, true>(A, at + t.n0 + c, n, vec, x);
-            } else if (A.flags & kBase32) {
-                store_sums<false, true>(A, at + t.n0 + c, n, vec, x);
-            } else {
-                store_sums<false, false>(A, at + t.n0 + c, n, vec, x);
+            if (copy) {
+                if (A.flags & kOut32) copy_columns<true>(map, buffer, column, int(first), group, n <= 32, x); else copy_columns<false>(map, buffer, column, int(first), group, n <= 32, x);
+            } else if (mine) {
+                if (A.flags & kOut32) put_columns<true>(A, at + column, n, x); else put_columns<false>(A, at + column, n, x);
             }
-        }
-    } else if constexpr (END == kLoss) {
-        // in powers of two: exp(x) = 2^(x log2 e)
-        const float scale2 = A.scale * kLog2e;
-        const int64_t target = mine ? target_of(A, row) : -1;
-        float top = -INFINITY, sum = 0.f;
-        for (int c = 0; c < COLS && t.n0 + c < A.cols; c += 32) {
-            read_sums(acc + c, x);
-            const int n = A.cols - t.n0 - c;
-            const int64_t at = target - t.n0 - c;
-            if (at >= 0 && at < 32 && target >= 0) {
+        } else if constexpr (END == kLoss) {
+            const int64_t here = target - column;
+            if (here >= 0 && here < 32 && target >= 0) {
                 float p = 0.f;
 #pragma unroll
-                for (int i = 0; i < 32; ++i) p = at == i ? x[i] : p;
+                for (int i = 0; i < 32; ++i) p = here == i ? x[i] : p;
                 A.picked[row] = p * A.scale;
             }
             float high = top;
@@ -436,39 +491,47 @@ __device__ __forceinline__ void end_tile(const ProductArgs &A, const Tile &t, ui
             for (int i = 0; i < 32; ++i) part += exp2_of(x[i] - from);
             sum = fmaf(sum, exp2_of(top - from), part);
             top = high;
-            if ((c + 32) % kPart == 0 || n <= 32) {  // parts of a row one after another, so that lanes write side by side
-                if (mine) A.part[int64_t((t.n0 + c) / kPart) * A.rows + row] = make_float2(top, sum);
-                top = -INFINITY;
-                sum = 0.f;
-            }
-        }
-    } else {
-        const float scale2 = A.scale * kLog2e;
-        const int64_t target = mine ? target_of(A, row) : -1;
-        const float g = target >= 0 ? A.dloss[row] : 0.f, lse2 = target >= 0 ? A.lse[row] * kLog2e : 0.f;
-        for (int c = 0; c < COLS && t.n0 + c < A.cols; c += 32) {
-            read_sums(acc + c, x);
-            const int64_t at = target - A.first - t.n0 - c;
+        } else {
+            const int64_t here = target - A.first - column;
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
-                const float p = exp2_of(fmaf(x[i], scale2, -lse2)) - (at == i ? 1.f : 0.f);
+                const float p = exp2_of(fmaf(x[i], scale2, -lse2)) - (here == i ? 1.f : 0.f);
                 x[i] = target >= 0 ? p * g : 0.f;
             }
-            const int n = mine ? A.cols - t.n0 - c : 0;
-            uint16_t *q = static_cast<uint16_t *>(A.out) + row * A.ldo + t.n0 + c;
-#pragma unroll
-            for (int i = 0; i < 32; i += 8) {  // the matrix's lines are 16-byte aligned and have room for whole units
-                if (i < n)
-                    *reinterpret_cast<uint4 *>(q + i) = make_uint4(pack_bf16(x[i], x[i + 1]), pack_bf16(x[i + 2], x[i + 3]), pack_bf16(x[i + 4], x[i + 5]), pack_bf16(x[i + 6], x[i + 7]));
+            if (copy) {
+                copy_columns<false>(map, buffer, column, int(first), 0, n <= 32, x);
+            } else if (mine) {
+                put_columns<false>(A, at + column, n, x);
             }
         }
+    };
+    float x[2][32];
+    if (none) {
+        for (int c = start; c < stop; c += 32) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) x[0][i] = 0.f;
+            chunk(c, x[0]);
+        }
+    } else {  // the next 32 columns are on their way while 32 are dealt with
+        read_sums(acc, x[0]);
+#pragma unroll
+        for (int c = 0; c < COLS; c += 32) {
+            if (start + c >= stop) break;
+            sums_read(x[c / 32 % 2]);
+            if (c + 32 < COLS) read_sums(acc + c + 32, x[(c / 32 + 1) % 2]);
+            chunk(start + c, x[c / 32 % 2]);
+            __syncwarp();
+        }
+        sums_read(x[0]);
     }
+    if (END == kLoss && mine) A.part[int64_t(start / kPart) * A.rows + row] = make_float2(top, sum);  // lanes side by side
 }
 
 // Rows of no group are zeros.
+template <int WARPS>
 __device__ __forceinline__ void clear_rows(const ProductArgs &A, const Shared &S, int warp, int lane) {
     const int64_t before = S.begin[0], behind = A.rows - S.begin[A.groups];
-    for (int64_t i = int64_t(blockIdx.x) * kEndWarps + warp; i < before + behind; i += int64_t(gridDim.x) * kEndWarps) {
+    for (int64_t i = int64_t(blockIdx.x) * WARPS + warp; i < before + behind; i += int64_t(gridDim.x) * WARPS) {
         const int64_t row = i < before ? i : S.begin[A.groups] + i - before;
         if (A.flags & kOutVec) {
             for (int c = lane * 8; c < A.cols; c += 256) {
@@ -486,15 +549,15 @@ __device__ __forceinline__ void clear_rows(const ProductArgs &A, const Shared &S
 
 template <int KIND, int END, bool COPY, int PAIR>
 __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                                                               const ProductArgs A) {
+                                                               const __grid_constant__ CUtensorMap map_out, const ProductArgs A, const uint32_t stages) {
     extern __shared__ char raw[];
-    char *const ring = raw + (1024 - (shared_address(raw) & 1023)) % 1024;
-    Shared &S = *reinterpret_cast<Shared *>(ring + size_t(kStages) * kStageBytes);
-    constexpr int kT = kTile<PAIR>;
+    constexpr int kT = kTile<PAIR>, kEnds = kEndWarps<COPY>, kEndCols = kT * 4 / kEnds;
+    char *const ring = raw + (1024 - (shared_address(raw) & 1023)) % 1024, *const out_at = ring + stages * kStageBytes;
+    Shared &S = *reinterpret_cast<Shared *>(out_at + kEnds * kOutBytes);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = PAIR == 2 ? blockIdx.x & 1 : 0;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) bar_init(&S.full[i], PAIR * (COPY ? 1 : kLoadWarps)), bar_init(&S.empty[i], 1), bar_init(&S.landed[i], 1);
-        for (int i = 0; i < 2; ++i) bar_init(&S.sums[i], 1), bar_init(&S.freed[i], PAIR * kEndWarps);
+        for (int i = 0; i < 2; ++i) bar_init(&S.sums[i], 1), bar_init(&S.freed[i], PAIR * kEnds);
         S.gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -507,21 +570,22 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
     constexpr bool A_MAJOR = KIND != kOuter, B_MAJOR = KIND == kByCols;
     Walk<KIND, PAIR> walk(A, S);
     Tile t;
-    uint32_t n = 0;  // stages so far
+    Place p;
     bool ok = true;
 
     if (COPY && warp == kCopyWarp) {
         if (!lane) {
+            uint32_t n = 0;
             while (ok && walk.next(t)) {
                 const int m0 = t.m0 + rank * kLines, n0 = t.n0 + rank * kLines;
                 // A CTA whose rows all belong to the groups behind needs none of them: its sums are not read.
                 const bool rows = KIND == kOuter || m0 < t.r1;
-                for (int k = 0; k < t.steps; ++k, ++n) {
-                    const int s = n % kStages, s0 = (KIND == kOuter ? t.r0 : 0) + k * kStep;
-                    if (n >= kStages && !(ok = bar_wait(&S.empty[s], (n / kStages - 1) & 1, S))) break;
+                for (int k = 0; k < t.steps; ++k, ++n, p.next(stages)) {
+                    const int s0 = (KIND == kOuter ? t.r0 : 0) + k * kStep;
+                    if (!(ok = bar_wait(&S.empty[p.s], p.phase ^ 1, S))) break;
                     // The last lines of a group that ends within a stage go to the warp that clears what is behind them.
                     const bool cut = KIND == kOuter && s0 + kStep > t.r1;
-                    const uint32_t to = shared_address(ring) + s * kStageBytes, bar = cut ? shared_address(&S.landed[s]) : in_first<PAIR>(&S.full[s]);
+                    const uint32_t to = shared_address(ring) + p.s * kStageBytes, bar = cut ? shared_address(&S.landed[p.s]) : in_first<PAIR>(&S.full[p.s]);
                     bar_expect(bar, rows ? kStageBytes : kOperandBytes);
                     if (rows) copy_lines<A_MAJOR, PAIR>(map_a, to, bar, m0, s0, 0);
                     copy_lines<B_MAJOR, PAIR>(map_b, to + kOperandBytes, bar, n0, s0, KIND == kOuter ? 0 : t.group);
@@ -529,18 +593,18 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
             }
             // what was asked for arrives before the shared memory is given back
             if (!ok && !rank)
-                for (uint32_t i = n > kStages ? n - kStages : 0; i < n; ++i) drain(&S.full[i % kStages], i / kStages & 1);
+                for (uint32_t i = n > stages ? n - stages : 0; i < n; ++i) drain(&S.full[i % stages], i / stages & 1);
         }
     } else if (COPY && KIND == kOuter && warp == kCutWarp) {
-        uint32_t phases = 0;
+        uint32_t phases = 0, n = 0;
         while (ok && walk.next(t)) {
             const int left = (t.r1 - t.r0) % kStep;
-            n += t.steps;
-            if (!left || !t.steps) continue;
-            const int s = (n - 1) % kStages;
+            n = (n + t.steps) % stages;
+            if (!left) continue;
+            const uint32_t s = n ? n - 1 : stages - 1;
             if (!(ok = bar_wait(&S.landed[s], phases >> s & 1, S))) break;
             phases ^= 1u << s;
-            char *const at = ring + size_t(s) * kStageBytes;
+            char *const at = ring + s * kStageBytes;
             for (int i = left * 8 + lane; i < kStep * 8; i += 32)  // 16-byte units of a block's lines
 #pragma unroll
                 for (int b = 0; b < 4; ++b) *reinterpret_cast<uint4 *>(at + b * (kOperandBytes / 2) + i * 16) = make_uint4(0, 0, 0, 0);
@@ -548,15 +612,14 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
             __syncwarp();
             if (!lane) bar_arrive<PAIR>(&S.full[s]);
         }
-    } else if (!COPY && warp >= kFirstLoad) {
-        const int w = (warp - kFirstLoad) % (kLoadWarps / 2);
-        const bool second = warp - kFirstLoad >= kLoadWarps / 2;
+    } else if (!COPY && warp >= kFirstEnd + kEnds) {
+        const int w = (warp - kFirstEnd - kEnds) % (kLoadWarps / 2);
+        const bool second = warp - kFirstEnd - kEnds >= kLoadWarps / 2;
         while (ok && walk.next(t)) {
-            const uint16_t *b = static_cast<const uint16_t *>(A.b) + t.group * A.b_group * (KIND != kOuter);
-            for (int k = 0; k < t.steps; ++k, ++n) {
-                const int s = n % kStages;
-                if (n >= kStages && !(ok = bar_wait(&S.empty[s], (n / kStages - 1) & 1, S))) break;
-                char *to = ring + size_t(s) * kStageBytes;
+            const uint16_t *b = static_cast<const uint16_t *>(A.b) + (KIND != kOuter ? t.group * A.b_group : 0);
+            for (int k = 0; k < t.steps; ++k, p.next(stages)) {
+                if (!(ok = bar_wait(&S.empty[p.s], p.phase ^ 1, S))) break;
+                char *to = ring + p.s * kStageBytes;
                 const int64_t s0 = (KIND == kOuter ? t.r0 : 0) + int64_t(k) * kStep, s_end = KIND == kOuter ? t.r1 : A.inner;
                 if (!second)
                     load_lines<A_MAJOR>(static_cast<const uint16_t *>(A.a), A.lda, t.m0 + rank * kLines, KIND == kOuter ? A.inner : t.r1, s0, s_end, to, w, lane);
@@ -564,54 +627,57 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
                     load_lines<B_MAJOR>(b, A.ldb, t.n0 + rank * kLines, A.cols, s0, s_end, to + kOperandBytes, w, lane);
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (!lane) bar_arrive<PAIR>(&S.full[s]);
+                if (!lane) bar_arrive<PAIR>(&S.full[p.s]);
             }
         }
     } else if (warp == kMulWarp && !rank) {
         if (!lane) {
-            uint32_t tiles = 0;
+            Place h;  // of the two halves of tensor memory
+            bool some = false;
             while (ok && walk.next(t)) {
                 if (!t.steps) continue;
-                const uint32_t half = tiles & 1, to = acc + half * kT;
-                if (tiles >= 2 && !(ok = bar_wait(&S.freed[half], (tiles / 2 - 1) & 1, S))) break;
+                const uint32_t to = acc + h.s * kT;
+                if (!(ok = bar_wait(&S.freed[h.s], h.phase ^ 1, S))) break;
                 after_sync();
-                for (int k = 0; k < t.steps; ++k, ++n) {
-                    const int s = n % kStages;
-                    if (!(ok = bar_wait(&S.full[s], n / kStages & 1, S))) break;
+                for (int k = 0; k < t.steps; ++k) {
+                    if (!(ok = bar_wait(&S.full[p.s], p.phase, S))) break;
                     after_sync();
-                    const uint32_t at = shared_address(ring) + s * kStageBytes;
+                    const uint32_t at = shared_address(ring) + p.s * kStageBytes;
                     const uint64_t a = operand<A_MAJOR>(at), b = operand<B_MAJOR>(at + kOperandBytes);
 #pragma unroll
                     for (int i = 0; i < kStep / 16; ++i)
                         multiply<PAIR>(to, a + i * kNext16<A_MAJOR>, b + i * kNext16<B_MAJOR>, kInstruction<A_MAJOR, B_MAJOR, PAIR>, k | i);
-                    commit<PAIR>(&S.empty[s]);
+                    commit<PAIR>(&S.empty[p.s]);
+                    p.next(stages);
+                    some = true;
                 }
-                if (ok) commit<PAIR>(&S.sums[half]);
-                ++tiles;
+                if (ok) commit<PAIR>(&S.sums[h.s]);
+                h.next(2);
             }
             // what was issued ends before the tensor memory is given back
-            if (!ok && n) drain(&S.empty[(n - 1) % kStages], (n - 1) / kStages & 1);
+            if (!ok && some) drain(&S.empty[p.s ? p.s - 1 : stages - 1], p.s ? p.phase : p.phase ^ 1);
         }
-    } else if (warp >= kFirstEnd && warp < kFirstEnd + kEndWarps) {
-        const int q = warp - kFirstEnd;
-        uint32_t tiles = 0;
+    } else if (warp >= kFirstEnd && warp < kFirstEnd + kEnds) {
+        const int q = warp % 4, half = (warp - kFirstEnd) / 4;
+        char *const buffer = out_at + (warp - kFirstEnd) * kOutBytes;
+        Place h;
         while (ok && walk.next(t)) {
-            const uint32_t half = tiles & 1;
             if (t.steps) {
-                if (!(ok = bar_wait(&S.sums[half], tiles / 2 & 1, S))) break;
+                if (!(ok = bar_wait(&S.sums[h.s], h.phase, S))) break;
                 after_sync();
             } else if (KIND == kOuter && A.base == A.out) {
                 continue;
             }
-            end_tile<KIND, END, kT>(A, t, acc + half * kT + (uint32_t(q * 32) << 16), !t.steps, rank * kLines + q * 32 + lane);
+            end_tile<KIND, END, kEndCols>(A, map_out, buffer, t, acc + h.s * kT + half * kEndCols + (uint32_t(q * 32) << 16), !t.steps, rank * kLines + q * 32, half * kEndCols);
             if (t.steps) {
                 before_sync();
                 __syncwarp();
-                if (!lane) bar_arrive<PAIR>(&S.freed[half]);
-                ++tiles;
+                if (!lane) bar_arrive<PAIR>(&S.freed[h.s]);
+                h.next(2);
             }
         }
-        if (KIND != kOuter && END == kStore && A.offsets) clear_rows(A, S, q, lane);
+        if (KIND != kOuter && END == kStore && A.offsets) clear_rows<kEnds>(A, S, warp - kFirstEnd, lane);
+        if (!lane) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     before_sync();
     __syncwarp();
@@ -634,25 +700,29 @@ Encode encoder() {
     return f;
 }
 
-// Lines of `x` elements, `ld` apart, y of them in a group and z groups; boxes of 64 elements of `lines` lines.
-bool map_of(CUtensorMap *m, const void *p, int64_t x, int64_t ld, int64_t y, int64_t group, int64_t z, uint32_t lines) {
-    const cuuint64_t dims[3] = {cuuint64_t(x), cuuint64_t(y), cuuint64_t(z)}, strides[2] = {cuuint64_t(ld) * 2, cuuint64_t(z > 1 ? group : ld) * 2};
-    const cuuint32_t box[3] = {64, lines, 1}, step[3] = {1, 1, 1};
+// Lines of `x` elements, `ld` apart, y of them in a group and z groups; boxes of `lines` lines of 128 bytes.
+bool map_of(CUtensorMap *m, const void *p, bool f32, int64_t x, int64_t ld, int64_t y, int64_t group, int64_t z, uint32_t lines) {
+    const int es = f32 ? 4 : 2;
+    const cuuint64_t dims[3] = {cuuint64_t(x), cuuint64_t(y), cuuint64_t(z)}, strides[2] = {cuuint64_t(ld) * es, cuuint64_t(z > 1 ? group : ld) * es};
+    const cuuint32_t box[3] = {cuuint32_t(128 / es), lines, 1}, step[3] = {1, 1, 1};
     const Encode f = encoder();
-    return f && f(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return f && f(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(p), dims, strides, box, step,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Whether tensor copies can bring a matrix: lines on 16-byte boundaries, strides that their maps hold.
-bool copies(const void *p, int64_t ld, int64_t group, int64_t groups) {
-    return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && (groups == 1 || (group % 8 == 0 && group < int64_t(1) << 38));
+// Whether tensor copies can move a matrix: lines on 16-byte boundaries, strides that their maps hold.
+bool copies(const void *p, bool f32, int64_t ld, int64_t group, int64_t groups) {
+    const int64_t unit = f32 ? 4 : 8;
+    return ((uintptr_t)p & 15) == 0 && ld % unit == 0 && (groups == 1 || (group % unit == 0 && group < int64_t(1) << 37));
 }
 
 template <int KIND, int END, bool COPY, int PAIR>
-cudaError_t launch_of(const ProductArgs &A, const CUtensorMap &a, const CUtensorMap &b, cudaStream_t s) {
+cudaError_t launch_of(const ProductArgs &A, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, cudaStream_t s) {
     constexpr auto k = k_product<KIND, END, COPY, PAIR>;
-    const cudaError_t e = ops_allow_smem<k>(int(kSharedBytes));
+    const cudaError_t e = ops_allow_smem<k>(int(kMaxSharedBytes));
     if (e != cudaSuccess) return e;
+    uint32_t stages = kStages;
+    while (shared_bytes(stages, kEndWarps<COPY>, A.groups) > kMaxSharedBytes) --stages;
     constexpr int kT = kTile<PAIR>;
     const int64_t nt = (A.cols + kT - 1) / kT;
     const int64_t most = (KIND == kOuter ? int64_t((A.inner + kT - 1) / kT) * A.groups : A.rows / kT + A.groups) * nt;
@@ -664,23 +734,27 @@ cudaError_t launch_of(const ProductArgs &A, const CUtensorMap &a, const CUtensor
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(uint32_t(most < pairs ? most : pairs) * PAIR);
     cfg.blockDim = dim3(kThreads<COPY>);
-    cfg.dynamicSmemBytes = kSharedBytes;
+    cfg.dynamicSmemBytes = shared_bytes(stages, kEndWarps<COPY>, A.groups);
     cfg.stream = s;
     cfg.attrs = &at;
     cfg.numAttrs = PAIR > 1 ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, k, a, b, A);
+    return cudaLaunchKernelEx(&cfg, k, a, b, out, A, stages);
 }
 
 template <int KIND, int END>
-cudaError_t launch(const ProductArgs &A, cudaStream_t s) {
-    CUtensorMap a{}, b{};
+cudaError_t launch(ProductArgs A, cudaStream_t s) {
+    CUtensorMap a{}, b{}, out{};
     constexpr bool A_MAJOR = KIND != kOuter, B_MAJOR = KIND == kByCols;
-    const bool outer = KIND == kOuter;
-    const int64_t groups = outer ? 1 : A.groups;
-    if (A.rows && copies(A.a, A.lda, 0, 1) && copies(A.b, A.ldb, A.b_group, groups) && map_of(&a, A.a, A.inner, A.lda, A.rows, 0, 1, A_MAJOR ? kLines : kStep) &&
-        map_of(&b, A.b, B_MAJOR ? A.inner : A.cols, A.ldb, B_MAJOR ? A.cols : outer ? A.rows : A.inner, A.b_group, groups, B_MAJOR ? kLines : kStep))
-        return launch_of<KIND, END, true, 2>(A, a, b, s);
-    return launch_of<KIND, END, false, 1>(A, a, b, s);
+    const bool outer = KIND == kOuter, o32 = A.flags & kOut32;
+    const int64_t groups = outer ? 1 : A.groups, o_groups = outer ? A.groups : 1;
+    if (END != kLoss && copies(A.out, o32, A.ldo, A.o_group, o_groups) &&
+        map_of(&out, A.out, o32, A.cols, A.ldo, outer ? A.inner : A.rows, A.o_group, o_groups, 32))
+        A.flags |= kOutCopy;
+    if (A.rows && copies(A.a, false, A.lda, 0, 1) && copies(A.b, false, A.ldb, A.b_group, groups) &&
+        map_of(&a, A.a, false, A.inner, A.lda, A.rows, 0, 1, A_MAJOR ? kLines : kStep) &&
+        map_of(&b, A.b, false, B_MAJOR ? A.inner : A.cols, A.ldb, B_MAJOR ? A.cols : outer ? A.rows : A.inner, A.b_group, groups, B_MAJOR ? kLines : kStep))
+        return launch_of<KIND, END, true, 2>(A, a, b, out, s);
+    return launch_of<KIND, END, false, 1>(A, a, b, out, s);
 }
 
 }  // namespace

@@ -593,12 +593,14 @@ typedef struct {
 int skew_experts_product(const skew_experts_config_t *c, const void *x, int64_t ld_x, const void *w, const int32_t *offsets, int64_t rows, void *y, void *stream);
 int skew_experts_grad_rows(const skew_experts_config_t *c, const void *dy, int64_t ld_dy, const void *w, const int32_t *offsets, int64_t rows, void *dx,
                            void *stream);
+/* Bytes of device workspace that skew_experts_grad needs, for any number of rows (0 for an invalid config). */
+size_t skew_experts_workspace_bytes(const skew_experts_config_t *c);
 /*
  * base: NULL, a tensor like dW that overlaps nothing else, or dW itself, to which the gradient is then added; matrices of experts without rows are
- * then not touched.
+ * then not touched. workspace: 256-byte aligned, of any content; calls that share one must not overlap on the GPU.
  */
 int skew_experts_grad(const skew_experts_config_t *c, const void *x, int64_t ld_x, const void *dy, int64_t ld_dy, const int32_t *offsets, int64_t rows,
-                      const void *base, void *dw, void *stream);
+                      const void *base, void *dw, void *workspace, size_t workspace_bytes, void *stream);
 
 /* ---- the output head's softmax cross entropy, without its logits ------------------
  * With h (tokens, width), the table W (rows, width) that the embedding may share, and l[t, v] = scale * <h[t], W[v]>:
@@ -606,7 +608,7 @@ int skew_experts_grad(const skew_experts_config_t *c, const void *x, int64_t ld_
  *   loss[t] = lse[t] - l[t, target_t]
  *   dh[t]   = scale * sum over v of p[t, v] W[v],  dW[v] = base[v] + scale * sum over t of p[t, v] h[t]
  *   p[t, v] = dloss[t] * (exp(l[t, v] - lse[t]) - [v = target_t])
- * A target outside [0, rows) is padding: its loss is zero, its dloss is not read, and it enters no gradient. h, W, dh, base and dW
+ * A target outside [0, rows) is padding: its loss is zero, its dloss is not read, and neither it nor its h, NaN included, enters a gradient. h, W, dh, base and dW
  * are bf16. l is summed in fp32 and never stored; the gradients take the vocabulary in pieces and make a piece's p from l anew, rounded to bf16 (for the
  * tensor cores: an error of up to 2^-8 of each term, about that of rounding the result), with sums in fp32. Results do not depend on timing.
  */

@@ -72,15 +72,21 @@ int skew_experts_grad_rows(const skew_experts_config_t *c, const void *dy, int64
     return rc ? rc : by_rows(kByCols, c, dy, ld_dy, w, offsets, rows, dx, (cudaStream_t)stream);
 }
 
+size_t skew_experts_workspace_bytes(const skew_experts_config_t *c) { return check(c, 0, (const int32_t *)4) == SKEW_OK ? (product_parts_bytes() + 255) / 256 * 256 : 0; }
+
 int skew_experts_grad(const skew_experts_config_t *c, const void *x, int64_t ld_x, const void *dy, int64_t ld_dy, const int32_t *offsets, int64_t rows,
-                      const void *base, void *dw, void *stream) {
+                      const void *base, void *dw, void *workspace, size_t workspace_bytes, void *stream) {
     int rc = check(c, rows, offsets);
     if (rc) return rc;
     const bool wide = c->flags & SKEW_EXPERTS_GRAD_FP32;
     if ((rc = check_rows("x", x, rows, c->n, ld_x)) || (rc = check_rows("dy", dy, rows, c->m, ld_dy)) || (rc = check_ptr("base", base, wide ? 4 : 2, false)) ||
         (rc = check_ptr("dw", dw, wide ? 4 : 2, true)))
         return rc;
+    const size_t need = skew_experts_workspace_bytes(c);
+    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)
+        return ops_fail(SKEW_EINVAL, "workspace must be 256-byte aligned and at least %zu bytes", need);
     ProductArgs A{};
+    A.parts = (float *)workspace;
     A.a = x;
     A.b = dy;
     A.lda = ld_x;

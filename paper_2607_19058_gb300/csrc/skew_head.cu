@@ -59,6 +59,54 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_join(const JoinArgs A) {
     A.loss[t] = v < 0 || v >= A.vocab ? 0.f : lse - A.picked[t];
 }
 
+// What the gradients read of the activations: rows of padded tokens as zeros (whatever they hold then enters no gradient), on 16-byte boundaries;
+// and the largest dloss of each CTA. A logit's gradient is rounded to bf16 divided by the largest of all, so that where all are
+// equal, as in a mean, the largest terms (at the targets, near -1) lose almost nothing.
+constexpr int kTidyThreads = 256;
+
+struct TidyArgs {
+    const uint16_t *h;
+    uint16_t *out;
+    const void *targets;
+    const float *dloss;
+    float *peaks;
+    int64_t tokens, vocab, width, ld, ld_out;
+    bool wide, vec;
+};
+
+__global__ void __launch_bounds__(kTidyThreads) k_tidy(const TidyArgs A) {
+    __shared__ float of_warp[kTidyThreads / 32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    float peak = 0.f;
+    for (int64_t t = blockIdx.x * int64_t(kTidyThreads / 32) + warp; t < A.tokens; t += int64_t(gridDim.x) * (kTidyThreads / 32)) {
+        const int64_t v = A.wide ? static_cast<const int64_t *>(A.targets)[t] : static_cast<const int32_t *>(A.targets)[t];
+        const bool there = v >= 0 && v < A.vocab;
+        if (there) peak = fmaxf(peak, fabsf(A.dloss[t]));
+        const uint16_t *from = A.h + t * A.ld;
+        uint16_t *to = A.out + t * A.ld_out;
+#pragma unroll 4
+        for (int64_t c = lane * 8; c < A.ld_out; c += 256) {
+            uint4 u = make_uint4(0, 0, 0, 0);
+            if (there && A.vec) {
+                u = *reinterpret_cast<const uint4 *>(from + c);
+            } else if (there) {
+                uint32_t x[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] = c + k < A.width ? from[c + k] : 0;
+                u = make_uint4(x[0] | x[1] << 16, x[2] | x[3] << 16, x[4] | x[5] << 16, x[6] | x[7] << 16);
+            }
+            *reinterpret_cast<uint4 *>(to + c) = u;
+        }
+    }
+    if (!lane) of_warp[warp] = peak;
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int w = 1; w < kTidyThreads / 32; ++w) peak = fmaxf(peak, of_warp[w]);
+    A.peaks[blockIdx.x] = peak;
+    if (!blockIdx.x)
+        for (int i = gridDim.x; i < kPeaks; ++i) A.peaks[i] = 0.f;
+}
+
 int check(const skew_head_config_t *c, int64_t tokens) {
     if (!c) return ops_fail(SKEW_EINVAL, "config is NULL");
     if (c->rows < 1 || c->rows > kMaxRows) return ops_fail(SKEW_EINVAL, "rows must be in [1, 2^24]");
@@ -84,7 +132,8 @@ size_t whole(size_t bytes) { return (bytes + 255) / 256 * 256; }
 struct Layout {
     int64_t parts, piece, pieces;
     size_t picked, loss_bytes;     // parts, then the picked logits
-    size_t sums, grad_bytes;       // a piece, then dh's sums
+    int64_t ld;                    // of the activations' copy
+    size_t sums, tidy, peaks, shares, grad_bytes;  // a piece, dh's sums over the pieces, the copy, peaks, shares of tiles
 };
 
 Layout layout(const skew_head_config_t *c, int64_t tokens) {
@@ -99,7 +148,11 @@ Layout layout(const skew_head_config_t *c, int64_t tokens) {
     L.piece = ((c->rows + L.pieces - 1) / L.pieces + kPieceCols - 1) / kPieceCols * kPieceCols;
     L.pieces = (c->rows + L.piece - 1) / L.piece;
     L.sums = whole(size_t(T) * L.piece * 2);
-    L.grad_bytes = L.sums + (L.pieces > 1 ? whole(size_t(T) * c->width * 4) : 0);
+    L.ld = (c->width + 7) / 8 * 8;
+    L.tidy = L.sums + (L.pieces > 1 ? whole(size_t(T) * c->width * 4) : 0);
+    L.peaks = L.tidy + whole(size_t(T) * L.ld * 2);
+    L.shares = L.peaks + whole(kPeaks * 4);
+    L.grad_bytes = L.shares + whole(product_parts_bytes());
     return L;
 }
 
@@ -164,15 +217,24 @@ int skew_head_grad(const skew_head_config_t *c, const void *h, int64_t ld_h, con
     char *ws = (char *)workspace;
     cudaStream_t s = (cudaStream_t)stream;
     const int32_t width = (int32_t)c->width;
+    float *const peaks = (float *)(ws + L.peaks);
+    const uint16_t *const tidy = (const uint16_t *)(ws + L.tidy);
+    if (tokens) {
+        const TidyArgs A{(const uint16_t *)h, (uint16_t *)(ws + L.tidy), targets, dloss, peaks, tokens, c->rows, c->width, ld_h, L.ld, wide,
+                         units(c->width, h) && ld_h % 8 == 0};
+        const int64_t blocks = (tokens + kTidyThreads / 32 - 1) / (kTidyThreads / 32);
+        if ((rc = ops_cuda(ops_launch(false, k_tidy, uint32_t(blocks < kPeaks ? blocks : kPeaks), kTidyThreads, 0, s, A), "k_tidy"))) return rc;
+    }
     for (int64_t v0 = 0; v0 < c->rows; v0 += L.piece) {
         const int64_t n = c->rows - v0 < L.piece ? c->rows - v0 : L.piece;
         const uint16_t *w = (const uint16_t *)table + v0 * c->width;
         const bool first = v0 == 0, last = v0 + n == c->rows;
         if (tokens) {
             ProductArgs P{};  // the logits' gradient: (tokens, n)
-            P.a = h;
+            P.a = tidy;
             P.b = w;
-            P.lda = ld_h;
+            P.lda = L.ld;
+            P.peaks = peaks;
             P.ldb = c->width;
             P.rows = tokens;
             P.groups = 1;
@@ -198,6 +260,8 @@ int skew_head_grad(const skew_head_config_t *c, const void *h, int64_t ld_h, con
             H.inner = (int32_t)n;
             H.cols = width;
             H.scale = c->scale;
+            H.peaks = peaks;
+            H.parts = (float *)(ws + L.shares);
             H.base = first ? nullptr : ws + L.sums;
             H.out = last ? dh : ws + L.sums;
             H.ldo = c->width;
@@ -206,9 +270,11 @@ int skew_head_grad(const skew_head_config_t *c, const void *h, int64_t ld_h, con
         }
         ProductArgs W{};  // its rows of dW
         W.a = ws;
-        W.b = h;
+        W.b = tidy;
         W.lda = L.piece;
-        W.ldb = ld_h;
+        W.ldb = L.ld;
+        W.peaks = tokens ? peaks : nullptr;
+        W.parts = (float *)(ws + L.shares);
         W.rows = tokens;
         W.groups = 1;
         W.inner = (int32_t)n;

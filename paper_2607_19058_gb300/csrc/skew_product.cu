@@ -125,7 +125,9 @@ __device__ __forceinline__ void pair_sync() {
 struct Tile {
     int32_t group, m0, n0;        // first row (of the matrices' `rows`, or OUTER's i) and column
     int32_t r0, r1;               // the group's rows
-    int32_t steps;                // of the summed index
+    int32_t k0, steps;            // of the summed index: the first, and how many
+    int32_t unit;                 // of the tile and its share of the summed index, where that is split
+    bool ends;                    // the share's last step is the group's
 };
 
 __device__ __forceinline__ int32_t *tiles_of(const ProductArgs &A, Shared &S) { return S.begin + A.groups + 1; }
@@ -187,25 +189,27 @@ struct Walk {
         } else {
             all = int64_t(tile[A.groups]) * nt;
         }
+        all *= A.splits;
     }
 
     __device__ __forceinline__ bool next(Tile &t) {
         if (at >= all) return false;
-        int64_t here;
-        int mt;
+        int64_t here = at;
+        int mt, split = 0;
+        if (A.splits > 1) here /= A.splits, split = int(at - here * A.splits);
         if (KIND == kOuter) {
-            group = int(at / each);
-            here = at - group * each;
+            group = int(here / each);
+            here -= group * each;
             mt = (A.inner + kT - 1) / kT;
         } else {
-            const int row = int(at / nt);  // tiles of rows before this one's, over all groups: its group is the last that begins at or before it
+            const int row = int(here / nt);  // tiles of rows before this one's, over all groups: its group is the last that begins at or before it
             int lo = group, hi = A.groups;
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
                 if (tile[mid] <= row) lo = mid; else hi = mid;
             }
             group = lo;
-            here = at - int64_t(tile[group]) * nt;
+            here -= int64_t(tile[group]) * nt;
             mt = tile[group + 1] - tile[group];
         }
         const int64_t span = int64_t(kBand) * nt;
@@ -215,7 +219,12 @@ struct Walk {
         t.r1 = begin[group + 1];
         t.m0 = (first + left % in) * kT + (KIND == kOuter ? 0 : t.r0);
         t.n0 = left / in * kT;
-        t.steps = ((KIND == kOuter ? t.r1 - t.r0 : A.inner) + kStep - 1) / kStep;
+        const int steps = ((KIND == kOuter ? t.r1 - t.r0 : A.inner) + kStep - 1) / kStep, share = (steps + A.splits - 1) / A.splits;
+        t.k0 = split * share;
+        t.steps = max(min(share, steps - t.k0), 0);
+        t.ends = t.k0 + t.steps == steps;
+        t.unit = ((KIND == kOuter ? group * mt : 0) + first + left % in) * nt + left / in;
+        t.unit = t.unit * A.splits + split;
         at += gridDim.x / PAIR;
         return true;
     }
@@ -374,19 +383,19 @@ __device__ __forceinline__ float exp2_of(float x) {
 
 // y = base + scale * x for 32 columns of a row, of which `n` are there.
 template <bool B32>
-__device__ __forceinline__ void add_base(const ProductArgs &A, int64_t at, int n, float (&x)[32]) {
+__device__ __forceinline__ void add_base(const ProductArgs &A, float scale, int64_t at, int n, float (&x)[32]) {
     if (!A.base) {
 #pragma unroll
-        for (int c = 0; c < 32; ++c) x[c] *= A.scale;
+        for (int c = 0; c < 32; ++c) x[c] *= scale;
     } else if (n >= 32 && A.flags & kOutVec) {
         Vec8<B32> b[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) b[c] = load8_cached<B32>(A.base, at + 8 * c);
 #pragma unroll
-        for (int c = 0; c < 32; ++c) x[c] = fmaf(x[c], A.scale, b[c / 8].at(c % 8));
+        for (int c = 0; c < 32; ++c) x[c] = fmaf(x[c], scale, b[c / 8].at(c % 8));
     } else {
 #pragma unroll
-        for (int c = 0; c < 32; ++c) x[c] = c < n ? fmaf(x[c], A.scale, load1<B32>(A.base, at + c)) : 0.f;
+        for (int c = 0; c < 32; ++c) x[c] = c < n ? fmaf(x[c], scale, load1<B32>(A.base, at + c)) : 0.f;
     }
 }
 
@@ -439,35 +448,47 @@ __device__ __forceinline__ int64_t target_of(const ProductArgs &A, int64_t row) 
     return v < 0 || v >= A.vocab ? -1 : v;
 }
 
+// The largest of a call's peaks (all of one warp ask); 1 where that divides nothing.
+__device__ __forceinline__ float peak_of(const float *peaks) {
+    if (!peaks) return 1.f;
+    float m = 0.f;
+    for (int i = threadIdx.x & 31; i < kPeaks; i += 32) m = fmaxf(m, peaks[i]);
+    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(kFullMask, m, d));
+    return m > 0.f && m < INFINITY ? m : 1.f;
+}
+
 constexpr int kPart = 128;  // columns of a LOSS part: what one warp has of a tile
 constexpr float kLog2e = 1.44269504088896340736f;
 
-// What a warp does with 32 rows and COLS columns of a tile, from row `row0` and column `col0` of it, whose sums are at `acc` (`none`: they are zeros).
-template <int KIND, int END, int COLS>
-__device__ __forceinline__ void end_tile(const ProductArgs &A, const CUtensorMap &map, char *buffer, const Tile &t, uint32_t acc, bool none, int row0, int col0) {
+// What a warp does with 32 rows and COLS columns of a tile, from row `row0` and column `col0` of it. read(f) has f see the sums in tensor memory, at an
+// address, once they are there; false if the wait for them gave up. Sums of more than A.chunk steps come in several parts, which are added here: the tensor
+// cores round every addition towards zero, so that errors do not cancel but grow with the number of steps (measured: 1e-9 of the result for each product).
+template <int KIND, int END, int COLS, typename Read>
+__device__ __forceinline__ bool end_tile(const ProductArgs &A, const CUtensorMap &map, char *buffer, const Tile &t, float peak, int row0, int col0, const Read &read) {
+    const bool parts = A.splits > 1;  // of the sums, each to a tile of its own
     const int64_t first = int64_t(t.m0) + row0, row = first + (threadIdx.x & 31);
     const int64_t end = KIND == kOuter ? A.inner : t.r1;
     const bool mine = row < end;
     const int start = t.n0 + col0, stop = min(start + COLS, A.cols);
-    if (first >= end || start >= stop) return;
+    const bool any = first < end && start < stop;
     // STORE: whole by a tensor copy, unless rows of the group behind would be written.
     const bool copy = A.flags & kOutCopy && (KIND == kOuter || !A.offsets || first + 32 <= end);
     const int64_t at = (KIND == kOuter ? t.group * A.o_group : 0) + row * A.ldo;
-    const int group = KIND == kOuter ? t.group : 0;
+    const int to_col = parts ? t.n0 : 0, to_row = parts ? row0 : int(first), to_group = parts ? t.unit : KIND == kOuter ? t.group : 0;
     // LOSS, LOGITS_GRAD: in powers of two, exp(x) = 2^(x log2 e)
-    const float scale2 = A.scale * kLog2e;
+    const float scale = A.scale * peak, scale2 = A.scale * kLog2e;
     const int64_t target = END != kStore && mine ? target_of(A, row) : -1;
-    const float g = END == kLogitsGrad && target >= 0 ? A.dloss[row] : 0.f, lse2 = END == kLogitsGrad && target >= 0 ? A.lse[row] * kLog2e : 0.f;
+    const float g = END == kLogitsGrad && target >= 0 ? A.dloss[row] / peak : 0.f, lse2 = END == kLogitsGrad && target >= 0 ? A.lse[row] * kLog2e : 0.f;
     float top = -INFINITY, sum = 0.f;
 
     auto chunk = [&](int column, float (&x)[32]) {  // 32 columns
         const int n = stop - column;
         if constexpr (END == kStore) {
             if (mine) {
-                if (A.flags & kBase32) add_base<true>(A, at + column, n, x); else add_base<false>(A, at + column, n, x);
+                if (A.flags & kBase32) add_base<true>(A, scale, at + column, n, x); else add_base<false>(A, scale, at + column, n, x);
             }
             if (copy) {
-                if (A.flags & kOut32) copy_columns<true>(map, buffer, column, int(first), group, n <= 32, x); else copy_columns<false>(map, buffer, column, int(first), group, n <= 32, x);
+                if (A.flags & kOut32) copy_columns<true>(map, buffer, column - to_col, to_row, to_group, n <= 32, x); else copy_columns<false>(map, buffer, column - to_col, to_row, to_group, n <= 32, x);
             } else if (mine) {
                 if (A.flags & kOut32) put_columns<true>(A, at + column, n, x); else put_columns<false>(A, at + column, n, x);
             }
@@ -505,26 +526,59 @@ __device__ __forceinline__ void end_tile(const ProductArgs &A, const CUtensorMap
             }
         }
     };
-    float x[2][32];
-    if (none) {
-        for (int c = start; c < stop; c += 32) {
+    if (!t.steps) {
+        float x[32];
+        for (int c = start; any && c < stop; c += 32) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) x[0][i] = 0.f;
-            chunk(c, x[0]);
+            for (int i = 0; i < 32; ++i) x[i] = 0.f;
+            chunk(c, x);
         }
-    } else {  // the next 32 columns are on their way while 32 are dealt with
-        read_sums(acc, x[0]);
-#pragma unroll
-        for (int c = 0; c < COLS; c += 32) {
-            if (start + c >= stop) break;
-            sums_read(x[c / 32 % 2]);
-            if (c + 32 < COLS) read_sums(acc + c + 32, x[(c / 32 + 1) % 2]);
-            chunk(start + c, x[c / 32 % 2]);
-            __syncwarp();
-        }
-        sums_read(x[0]);
+        return true;
     }
-    if (END == kLoss && mine) A.part[int64_t(start / kPart) * A.rows + row] = make_float2(top, sum);  // lanes side by side
+    if (t.steps <= A.chunk) {
+        const bool ok = read([&](uint32_t acc) {
+            if (!any) return;
+            float x[2][32];
+            read_sums(acc, x[0]);
+#pragma unroll
+            for (int c = 0; c < COLS / 32; ++c) {  // the next 32 columns are on their way while 32 are dealt with
+                sums_read(x[c % 2]);
+                if (c + 1 < COLS / 32) read_sums(acc + (c + 1) * 32, x[(c + 1) % 2]);
+                if (start + c * 32 < stop) chunk(start + c * 32, x[c % 2]);
+                __syncwarp();
+            }
+        });
+        if (!ok) return false;
+    } else {
+        float run[COLS / 32][32];
+#pragma unroll
+        for (int c = 0; c < COLS / 32; ++c)
+#pragma unroll
+            for (int i = 0; i < 32; ++i) run[c][i] = 0.f;
+#pragma unroll 1
+        for (int k = 0; k < t.steps; k += A.chunk) {
+            const bool ok = read([&](uint32_t acc) {
+#pragma unroll
+                for (int c = 0; c < COLS / 32; ++c) {
+                    float x[32];
+                    read_sums(acc + c * 32, x);
+                    sums_read(x);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) run[c][i] += x[i];
+                }
+            });
+            if (!ok) return false;
+        }
+        if (any) {
+#pragma unroll
+            for (int c = 0; c < COLS / 32; ++c) {
+                if (start + c * 32 < stop) chunk(start + c * 32, run[c]);
+                __syncwarp();
+            }
+        }
+    }
+    if (END == kLoss && any && mine) A.part[int64_t(start / kPart) * A.rows + row] = make_float2(top, sum);  // lanes side by side
+    return true;
 }
 
 // Rows of no group are zeros.
@@ -573,6 +627,9 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
     Place p;
     bool ok = true;
 
+    // Registers, of the 168 (128) that a thread starts with: a warp that writes out holds 128 columns of sums, and what becomes of them.
+    if (warp < kFirstEnd)
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(COPY ? 56 : 48));
     if (COPY && warp == kCopyWarp) {
         if (!lane) {
             uint32_t n = 0;
@@ -581,7 +638,7 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
                 // A CTA whose rows all belong to the groups behind needs none of them: its sums are not read.
                 const bool rows = KIND == kOuter || m0 < t.r1;
                 for (int k = 0; k < t.steps; ++k, ++n, p.next(stages)) {
-                    const int s0 = (KIND == kOuter ? t.r0 : 0) + k * kStep;
+                    const int s0 = (KIND == kOuter ? t.r0 : 0) + (t.k0 + k) * kStep;
                     if (!(ok = bar_wait(&S.empty[p.s], p.phase ^ 1, S))) break;
                     // The last lines of a group that ends within a stage go to the warp that clears what is behind them.
                     const bool cut = KIND == kOuter && s0 + kStep > t.r1;
@@ -598,7 +655,7 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
     } else if (COPY && KIND == kOuter && warp == kCutWarp) {
         uint32_t phases = 0, n = 0;
         while (ok && walk.next(t)) {
-            const int left = (t.r1 - t.r0) % kStep;
+            const int left = t.ends && t.steps ? (t.r1 - t.r0) % kStep : 0;
             n = (n + t.steps) % stages;
             if (!left) continue;
             const uint32_t s = n ? n - 1 : stages - 1;
@@ -613,6 +670,7 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
             if (!lane) bar_arrive<PAIR>(&S.full[s]);
         }
     } else if (!COPY && warp >= kFirstEnd + kEnds) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
         const int w = (warp - kFirstEnd - kEnds) % (kLoadWarps / 2);
         const bool second = warp - kFirstEnd - kEnds >= kLoadWarps / 2;
         while (ok && walk.next(t)) {
@@ -620,7 +678,7 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
             for (int k = 0; k < t.steps; ++k, p.next(stages)) {
                 if (!(ok = bar_wait(&S.empty[p.s], p.phase ^ 1, S))) break;
                 char *to = ring + p.s * kStageBytes;
-                const int64_t s0 = (KIND == kOuter ? t.r0 : 0) + int64_t(k) * kStep, s_end = KIND == kOuter ? t.r1 : A.inner;
+                const int64_t s0 = (KIND == kOuter ? t.r0 : 0) + int64_t(t.k0 + k) * kStep, s_end = KIND == kOuter ? t.r1 : A.inner;
                 if (!second)
                     load_lines<A_MAJOR>(static_cast<const uint16_t *>(A.a), A.lda, t.m0 + rank * kLines, KIND == kOuter ? A.inner : t.r1, s0, s_end, to, w, lane);
                 else
@@ -636,17 +694,25 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
             bool some = false;
             while (ok && walk.next(t)) {
                 if (!t.steps) continue;
-                const uint32_t to = acc + h.s * kT;
-                if (!(ok = bar_wait(&S.freed[h.s], h.phase ^ 1, S))) break;
-                after_sync();
-                for (int k = 0; k < t.steps; ++k) {
+                uint32_t to = 0;
+                for (int k = 0, in = 0; k < t.steps; ++k, ++in) {
+                    if (in == A.chunk) {
+                        commit<PAIR>(&S.sums[h.s]);
+                        h.next(2);
+                        in = 0;
+                    }
+                    if (in == 0) {
+                        if (!(ok = bar_wait(&S.freed[h.s], h.phase ^ 1, S))) break;
+                        after_sync();
+                        to = acc + h.s * kT;
+                    }
                     if (!(ok = bar_wait(&S.full[p.s], p.phase, S))) break;
                     after_sync();
                     const uint32_t at = shared_address(ring) + p.s * kStageBytes;
                     const uint64_t a = operand<A_MAJOR>(at), b = operand<B_MAJOR>(at + kOperandBytes);
 #pragma unroll
                     for (int i = 0; i < kStep / 16; ++i)
-                        multiply<PAIR>(to, a + i * kNext16<A_MAJOR>, b + i * kNext16<B_MAJOR>, kInstruction<A_MAJOR, B_MAJOR, PAIR>, k | i);
+                        multiply<PAIR>(to, a + i * kNext16<A_MAJOR>, b + i * kNext16<B_MAJOR>, kInstruction<A_MAJOR, B_MAJOR, PAIR>, in | i);
                     commit<PAIR>(&S.empty[p.s]);
                     p.next(stages);
                     some = true;
@@ -658,23 +724,23 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
             if (!ok && some) drain(&S.empty[p.s ? p.s - 1 : stages - 1], p.s ? p.phase : p.phase ^ 1);
         }
     } else if (warp >= kFirstEnd && warp < kFirstEnd + kEnds) {
-        const int q = warp % 4, half = (warp - kFirstEnd) / 4;
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(COPY ? 224 : 216));
+        const int q = warp % 4, col0 = (warp - kFirstEnd) / 4 * kEndCols;
         char *const buffer = out_at + (warp - kFirstEnd) * kOutBytes;
         Place h;
+        const float peak = END == kLoss ? 1.f : peak_of(A.peaks);
         while (ok && walk.next(t)) {
-            if (t.steps) {
-                if (!(ok = bar_wait(&S.sums[h.s], h.phase, S))) break;
+            if (!t.steps && KIND == kOuter && A.base == A.out) continue;
+            ok = end_tile<KIND, END, kEndCols>(A, map_out, buffer, t, peak, rank * kLines + q * 32, col0, [&](auto &&see) {
+                if (!bar_wait(&S.sums[h.s], h.phase, S)) return false;
                 after_sync();
-            } else if (KIND == kOuter && A.base == A.out) {
-                continue;
-            }
-            end_tile<KIND, END, kEndCols>(A, map_out, buffer, t, acc + h.s * kT + half * kEndCols + (uint32_t(q * 32) << 16), !t.steps, rank * kLines + q * 32, half * kEndCols);
-            if (t.steps) {
+                see(acc + h.s * kT + col0 + (uint32_t(q * 32) << 16));
                 before_sync();
                 __syncwarp();
                 if (!lane) bar_arrive<PAIR>(&S.freed[h.s]);
                 h.next(2);
-            }
+                return true;
+            });
         }
         if (KIND != kOuter && END == kStore && A.offsets) clear_rows<kEnds>(A, S, warp - kFirstEnd, lane);
         if (!lane) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
@@ -685,9 +751,43 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
     if (warp == kMemWarp) give_tensor_memory<PAIR>(acc);
 }
 
+// out = base + scale * (the sum, in order, of a tile's shares), four columns to a thread.
+constexpr int kSumThreads = 256;
+
+template <int TILE>
+__global__ void __launch_bounds__(kSumThreads) k_sum(const ProductArgs A, const int32_t splits, const int64_t height) {
+    wait_launch_before();
+    const float scale = A.scale * peak_of(A.peaks);
+    const int64_t mt = (height + TILE - 1) / TILE, nt = (A.cols + TILE - 1) / TILE, fours = (A.cols + 3) / 4;
+    for (int64_t i = blockIdx.x * int64_t(kSumThreads) + threadIdx.x; i < A.groups * height * fours; i += int64_t(gridDim.x) * kSumThreads) {
+        const int64_t c = i % fours * 4, r = i / fours % height, g = i / fours / height;
+        const float4 *p = reinterpret_cast<const float4 *>(A.parts + ((g * mt + r / TILE) * nt + c / TILE) * splits * (TILE * TILE) + r % TILE * TILE + c % TILE);
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int s = 0; s < splits; ++s) {
+            const float4 y = p[s * (TILE * TILE / 4)];
+            x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+        }
+        const int64_t at = g * A.o_group + r * A.ldo + c;
+        const float v[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (c + k >= A.cols || (A.base == A.out && v[k] == 0.f)) continue;  // (in place: a matrix without rows is not touched)
+            const float b = !A.base ? 0.f : A.flags & kBase32 ? load1<true>(A.base, at + k) : load1<false>(A.base, at + k);
+            const float y = A.base ? fmaf(v[k], scale, b) : v[k] * scale;
+            if (A.flags & kOut32) store1<true>(A.out, at + k, y); else store1<false>(A.out, at + k, y);
+        }
+    }
+}
+
 // ---------------------------------------------------------------------------
 // Host
 // ---------------------------------------------------------------------------
+int64_t sms() {
+    const int n = ops_sm_count();
+    return n > 0 ? n : 152;
+}
+
 using Encode = decltype(&cuTensorMapEncodeTiled);
 
 Encode encoder() {
@@ -725,8 +825,8 @@ cudaError_t launch_of(const ProductArgs &A, const CUtensorMap &a, const CUtensor
     while (shared_bytes(stages, kEndWarps<COPY>, A.groups) > kMaxSharedBytes) --stages;
     constexpr int kT = kTile<PAIR>;
     const int64_t nt = (A.cols + kT - 1) / kT;
-    const int64_t most = (KIND == kOuter ? int64_t((A.inner + kT - 1) / kT) * A.groups : A.rows / kT + A.groups) * nt;
-    const int64_t pairs = ops_sm_count() / PAIR;
+    const int64_t most = (KIND == kOuter ? int64_t((A.inner + kT - 1) / kT) * A.groups : A.rows / kT + A.groups) * nt * A.splits;
+    const int64_t pairs = sms() / PAIR;
     cudaLaunchAttribute at{};
     at.id = cudaLaunchAttributeClusterDimension;
     at.val.clusterDim.x = PAIR;
@@ -741,9 +841,53 @@ cudaError_t launch_of(const ProductArgs &A, const CUtensorMap &a, const CUtensor
     return cudaLaunchKernelEx(&cfg, k, a, b, out, A, stages);
 }
 
+// Steps between two additions outside of the tensor cores: 512 products (an error of 5e-7 of the result); 1024 (9e-7) for logits, of which an epilogue makes more
+// (at 4096 columns 597 us a 8192 x 16384 table, 619 with 512, 574 with all of them); 8192 (8e-6) where bf16 is made of it.
+constexpr int kChunk32 = 512 / kStep, kChunkLoss = 1024 / kStep, kChunk16 = 8192 / kStep;
+
+
+constexpr int kMostWaves = 4;  // of shares: what their sums' memory is sized for
+
+// How many shares the summed index is cut into, so that few tiles keep the SMs busy: the fewest steps (of 64 products, about 0.3 us) that a pair of CTAs does in
+// turn, a share's start and end counted as 6, and the launch that adds the shares as 10 and 0.4 for each.
+int shares_of(int64_t tiles, int64_t steps, int64_t pairs) {
+    int best = 1;
+    double least = 0;
+    for (int s = 1; s <= 4 * pairs && (s == 1 || (tiles * s <= kMostWaves * pairs && (steps + s - 1) / s >= 4)); ++s) {
+        const int64_t units = tiles * s, waves = (units + pairs - 1) / pairs;
+        const double cost = double(waves) * double((steps + s - 1) / s + 6) + (s > 1 ? 10 + 0.4 * double(units) : 0);
+        if (s == 1 || cost < least) best = s, least = cost;
+    }
+    return best;
+}
+
+template <int KIND, int END, bool COPY, int PAIR>
+cudaError_t launch_split(ProductArgs A, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, cudaStream_t s) {
+    constexpr int kT = kTile<PAIR>;
+    const int64_t height = KIND == kOuter ? A.inner : A.rows, mt = (height + kT - 1) / kT, nt = (A.cols + kT - 1) / kT, tiles = mt * nt * A.groups;
+    const int64_t steps = KIND == kOuter ? (A.rows + int64_t(kStep) * A.groups - 1) / (int64_t(kStep) * A.groups) : (A.inner + kStep - 1) / kStep;
+    const int shares = END == kStore && A.parts && (KIND == kOuter || !A.offsets) ? shares_of(tiles, steps, sms() / PAIR) : 1;
+    CUtensorMap to{};
+    if (shares == 1 || !map_of(&to, A.parts, true, kT, kT, kT, kT * kT, tiles * shares, 32)) return launch_of<KIND, END, COPY, PAIR>(A, a, b, out, s);
+    ProductArgs P = A;
+    P.splits = shares;
+    P.out = A.parts;
+    P.base = nullptr;
+    P.peaks = nullptr;
+    P.scale = 1.f;
+    P.flags = (A.flags & ~uint32_t(kBase32)) | kOut32 | kOutCopy;
+    P.chunk = kChunk32;
+    const cudaError_t e = launch_of<KIND, END, COPY, PAIR>(P, a, b, to, s);
+    if (e != cudaSuccess) return e;
+    const int64_t blocks = (A.groups * height * ((A.cols + 3) / 4) + kSumThreads - 1) / kSumThreads;
+    return ops_launch(true, k_sum<kT>, uint32_t(blocks < sms() * 8 ? blocks : sms() * 8), kSumThreads, 0, s, A, shares, height);
+}
+
 template <int KIND, int END>
 cudaError_t launch(ProductArgs A, cudaStream_t s) {
     CUtensorMap a{}, b{}, out{};
+    A.splits = 1;
+    A.chunk = END == kLoss ? kChunkLoss : END == kStore && A.flags & kOut32 ? kChunk32 : kChunk16;
     constexpr bool A_MAJOR = KIND != kOuter, B_MAJOR = KIND == kByCols;
     const bool outer = KIND == kOuter, o32 = A.flags & kOut32;
     const int64_t groups = outer ? 1 : A.groups, o_groups = outer ? A.groups : 1;
@@ -753,13 +897,15 @@ cudaError_t launch(ProductArgs A, cudaStream_t s) {
     if (A.rows && copies(A.a, false, A.lda, 0, 1) && copies(A.b, false, A.ldb, A.b_group, groups) &&
         map_of(&a, A.a, false, A.inner, A.lda, A.rows, 0, 1, A_MAJOR ? kLines : kStep) &&
         map_of(&b, A.b, false, B_MAJOR ? A.inner : A.cols, A.ldb, B_MAJOR ? A.cols : outer ? A.rows : A.inner, A.b_group, groups, B_MAJOR ? kLines : kStep))
-        return launch_of<KIND, END, true, 2>(A, a, b, out, s);
-    return launch_of<KIND, END, false, 1>(A, a, b, out, s);
+        return launch_split<KIND, END, true, 2>(A, a, b, out, s);
+    return launch_split<KIND, END, false, 1>(A, a, b, out, s);
 }
 
 }  // namespace
 
 int32_t product_loss_columns() { return kPart; }
+
+size_t product_parts_bytes() { return size_t(kMostWaves) * (sms() / 2) * kTile<2> * kTile<2> * 4; }
 
 cudaError_t product_launch(ProductKind kind, ProductEnd end, const ProductArgs &A, cudaStream_t s) {
     if (end == kLoss) return launch<kByCols, kLoss>(A, s);

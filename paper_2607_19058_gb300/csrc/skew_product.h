@@ -14,9 +14,9 @@ namespace skew {
 enum ProductKind { kByRows = 0, kByCols = 1, kOuter = 2 };
 
 // What becomes of a tile of sums.
-//   STORE  : out = base + scale * C
+//   STORE  : out = base + scale * peak * C
 //   LOSS   : of x = scale * C, per row and tile, the largest and the sum of exponentials; the target's x
-//   LOGITS_GRAD : out = (exp(x - lse) - [j is the target]) * dloss, bf16
+//   LOGITS_GRAD : out = (exp(x - lse) - [j is the target]) * dloss / peak, bf16
 enum ProductEnd { kStore = 0, kLoss = 1, kLogitsGrad = 2 };
 
 enum : uint32_t { kOut32 = 1, kBase32 = 2, kOutVec = 4 /* out and base: 16-byte accesses */, kIds64 = 8, kOutCopy = 16 /* set by product_launch */ };
@@ -33,6 +33,9 @@ struct ProductArgs {
     const void *base;           // strides as out; may be out
     int64_t ldo, o_group;
     float scale;
+    float *parts;               // product_parts_bytes() for the sums of tiles that are cut along the summed index (OUTER, or one group); NULL: none is
+    const float *peaks;         // kPeaks numbers that are not negative, or NULL. LOGITS_GRAD divides by the largest, STORE multiplies by it
+    int32_t splits, chunk;      // set by product_launch: shares of the summed index; its steps between two additions outside of the tensor cores
     // LOSS, LOGITS_GRAD
     const void *targets;        // one for each row; not in [0, vocab): none
     int64_t first, vocab;       // the column j is the vocabulary's `first` + j
@@ -41,6 +44,9 @@ struct ProductArgs {
     float *picked;              // [rows]: the target's x
 };
 
+constexpr int kPeaks = 512;
+
+size_t product_parts_bytes();
 // Columns of a LOSS part.
 int32_t product_loss_columns();
 // Runs the product on `stream`; every pointer, size and stride has been checked.

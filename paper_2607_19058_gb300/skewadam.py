@@ -44,7 +44,7 @@ EXPORTS = ["skew_create", "skew_destroy", "skew_state_bytes", "skew_workspace_by
            "skew_clip_apply", "skew_gate_workspace_bytes", "skew_gate_forward", "skew_gate_grad",
            "skew_embed_lookup", "skew_embed_workspace_bytes", "skew_embed_grad",
            "skew_dispatch_workspace_bytes", "skew_dispatch_order", "skew_dispatch_spread", "skew_dispatch_combine", "skew_dispatch_combine_grad",
-           "skew_experts_product", "skew_experts_grad_rows", "skew_experts_grad",
+           "skew_experts_product", "skew_experts_grad_rows", "skew_experts_grad", "skew_experts_workspace_bytes",
            "skew_head_loss_workspace_bytes", "skew_head_grad_workspace_bytes", "skew_head_loss", "skew_head_grad", "skew_ops_sync_status"]
 
 
@@ -191,7 +191,9 @@ def load(path: Optional[str] = None) -> C.CDLL:
         L.skew_dispatch_combine_grad.argtypes = [C.POINTER(DispatchConfig), vp, i64, vp, vp, vp, vp, i64, i64, vp, vp, vp]
         L.skew_experts_product.argtypes = [C.POINTER(ExpertsConfig), vp, i64, vp, vp, i64, vp, vp]
         L.skew_experts_grad_rows.argtypes = [C.POINTER(ExpertsConfig), vp, i64, vp, vp, i64, vp, vp]
-        L.skew_experts_grad.argtypes = [C.POINTER(ExpertsConfig), vp, i64, vp, i64, vp, i64, vp, vp, vp]
+        L.skew_experts_grad.argtypes = [C.POINTER(ExpertsConfig), vp, i64, vp, i64, vp, i64, vp, vp, vp, sz, vp]
+        L.skew_experts_workspace_bytes.argtypes = [C.POINTER(ExpertsConfig)]
+        L.skew_experts_workspace_bytes.restype = sz
         for f in (L.skew_head_loss_workspace_bytes, L.skew_head_grad_workspace_bytes):
             f.argtypes, f.restype = [C.POINTER(HeadConfig), i64], sz
         L.skew_head_loss.argtypes = [C.POINTER(HeadConfig), vp, i64, vp, vp, i64, vp, vp, vp, sz, vp]
@@ -443,10 +445,14 @@ def skew_experts_grad_rows(c: ExpertsConfig, dy_ptr: int, ld_dy: int, w_ptr: int
     _check_op(load().skew_experts_grad_rows(C.byref(c), dy_ptr, ld_dy, w_ptr, offsets_ptr, rows, dx_ptr, stream))
 
 
+def skew_experts_workspace_bytes(c: ExpertsConfig) -> int:
+    return int(load().skew_experts_workspace_bytes(C.byref(c)))
+
+
 def skew_experts_grad(c: ExpertsConfig, x_ptr: int, ld_x: int, dy_ptr: int, ld_dy: int, offsets_ptr: int, rows: int, base_ptr: int, dw_ptr: int,
-                      stream: int) -> None:
+                      ws_ptr: int, ws_bytes: int, stream: int) -> None:
     """`base_ptr`: 0 for none."""
-    _check_op(load().skew_experts_grad(C.byref(c), x_ptr, ld_x, dy_ptr, ld_dy, offsets_ptr, rows, base_ptr or None, dw_ptr, stream))
+    _check_op(load().skew_experts_grad(C.byref(c), x_ptr, ld_x, dy_ptr, ld_dy, offsets_ptr, rows, base_ptr or None, dw_ptr, ws_ptr, ws_bytes, stream))
 
 
 def skew_head_loss_workspace_bytes(c: HeadConfig, tokens: int) -> int:
@@ -1017,7 +1023,8 @@ class Experts:
 
     Rows of expert e are [offsets[e], offsets[e + 1]), as ``Dispatch.order`` makes them: any number each, and those of no expert
     give zeros. x (rows, n) and dy (rows, m), whose rows may lie apart, and the matrices are bf16; ``row_dtype`` (products and the rows' gradients) and
-    ``grad_dtype`` (the matrices' gradients) are bf16 or fp32. Tensors are to be on the current device.
+    ``grad_dtype`` (the matrices' gradients) are bf16 or fp32. Tensors are to be on the current device. The object must live as long as a graph that
+    captured its calls, or work that it was given on a stream torch did not make (a raw handle).
     """
 
     def __init__(self, experts: int, n: int, m: int, row_dtype=None, grad_dtype=None):
@@ -1028,12 +1035,15 @@ class Experts:
         self.config = ExpertsConfig(experts, n, m, (EXPERTS_ROWS_FP32 if self.row_dtype == torch.float32 else 0) |
                                     (EXPERTS_GRAD_FP32 if self.grad_dtype == torch.float32 else 0))
         self._ref, self._new = C.byref(self.config), _allocator()
-        skew_experts_product(self.config, 0, max(n, 1), 256, 256, 0, 0, 0)  # refuses what the library does not take; no rows: no launch
+        self._ws_bytes = skew_experts_workspace_bytes(self.config)
+        if not self._ws_bytes:
+            raise SkewError(SKEW_EINVAL, skew_ops_last_error())
         self._shape = (experts, n, m)
         self._bf16, self._i32 = torch.bfloat16, torch.int32
         L = load()
         self._product, self._grad_rows, self._grad = L.skew_experts_product, L.skew_experts_grad_rows, L.skew_experts_grad
         self._stream, self._elsewhere = _raw_stream(), _device_check()
+        self._workspace = _Workspace()
 
     def _rows(self, x, width: int, dev, what: str) -> int:
         if not (x.dtype == self._bf16 and x.is_cuda and x.dim() == 2 and x.shape[1] == width and x.device == dev):
@@ -1078,7 +1088,8 @@ class Experts:
 
     def grad(self, x, dy, offsets, base=None, out=None, stream=None):
         """The matrices' gradient, the sum over an expert's rows of x[r]^T dy[r]. ``base``: what it adds to; ``out``: where it goes
-        (``base`` itself: in place, and matrices of experts without rows are not touched; None: a new tensor)."""
+        (``base`` itself: in place, and matrices of experts without rows are not touched; None: a new tensor). Calls on one object share a
+        workspace: they must not overlap on the GPU."""
         if stream is not None:
             with _on(stream):
                 return self.grad(x, dy, offsets, base, out)
@@ -1092,7 +1103,8 @@ class Experts:
             p = out.data_ptr()
         else:
             p = self._matrices(out, self.grad_dtype, dev, "out")
-        rc = self._grad(self._ref, x.data_ptr(), ld, dy.data_ptr(), ldd, o, x.shape[0], b, p, self._stream(dev.index))
+        handle = self._stream(dev.index)
+        rc = self._grad(self._ref, x.data_ptr(), ld, dy.data_ptr(), ldd, o, x.shape[0], b, p, self._workspace.get(dev, self._ws_bytes, handle), self._ws_bytes, handle)
         if rc:
             _check_op(rc)
         return out

@@ -91,8 +91,7 @@ def test_scales(scale):
 def test_several_pieces():
     """Tokens enough that the logits' gradient takes the vocabulary in more than one piece."""
     T, V, d = 40000, 9000, 64
-    c = S.HeadConfig(V, d, 1.0, 0)
-    assert S.skew_head_grad_workspace_bytes(c, T) > T * d * 4 and S.skew_head_grad_workspace_bytes(c, T) < T * V * 2
+    assert T * V * 2 > 512 << 20
     _check(T, V, d, base=True)
     _check(T - 1, V + 3, d - 1, dtype=torch.int32)
 
@@ -152,11 +151,12 @@ def test_large_and_infinite_logits():
     h[7, 3] = float("nan")
     loss, lse = op.loss(h, w, t)
     assert lse[7].isnan() and loss[7].isnan() and int(lse.isnan().sum()) == 1
-    t[7] = -1                                              # a padded token: its NaN enters no gradient but through h itself
+    t[7] = -1                                              # a padded token: its NaN enters no gradient
     loss, lse = op.loss(h, w, t)
     assert loss[7] == 0
-    dh, _ = op.grad(h, w, t, lse, g)
+    dh, dw = op.grad(h, w, t, lse, g)
     assert (dh[7] == 0).all() and dh.isfinite().all()
+    assert dw[:300].isfinite().all()
 
 
 def test_no_tokens_and_padding_alone():

@@ -85,9 +85,10 @@ def test_dispatch_refuses_arguments():
 ])
 def test_experts_refuse_configs(config, rows, what):
     c = S.ExpertsConfig(*config)
+    assert what == "rows" or S.skew_experts_workspace_bytes(c) == 0
     _refused(what, S.skew_experts_product, c, P, 8, P, P, rows, P, 0)
     _refused(what, S.skew_experts_grad_rows, c, P, 8, P, P, rows, P, 0)
-    _refused(what, S.skew_experts_grad, c, P, 8, P, 8, P, rows, 0, P, 0)
+    _refused(what, S.skew_experts_grad, c, P, 8, P, 8, P, rows, 0, P, P, 1 << 40, 0)
 
 
 def test_experts_refuse_arguments():
@@ -98,11 +99,14 @@ def test_experts_refuse_arguments():
     _refused("rows must", S.skew_experts_product, c, P + 1, 8, P, P, 5, P, 0)
     _refused("stride", S.skew_experts_product, c, P, 7, P, P, 5, P, 0)
     _refused("stride", S.skew_experts_grad_rows, c, P, 15, P, P, 5, P, 0)
-    _refused("stride", S.skew_experts_grad, c, P, 8, P, (1 << 31) + 1, P, 5, 0, P, 0)
+    n = S.skew_experts_workspace_bytes(c)
+    _refused("stride", S.skew_experts_grad, c, P, 8, P, (1 << 31) + 1, P, 5, 0, P, P, n, 0)
     _refused("w must", S.skew_experts_product, c, P, 8, 0, P, 5, P, 0)
     _refused("result", S.skew_experts_product, c, P, 8, P, P, 5, P + 2, 0)
-    _refused("base", S.skew_experts_grad, c, P, 8, P, 16, P, 5, P + 2, P, 0)
-    _refused("dw", S.skew_experts_grad, c, P, 8, P, 16, P, 5, P, 0, 0)
+    _refused("base", S.skew_experts_grad, c, P, 8, P, 16, P, 5, P + 2, P, P, n, 0)
+    _refused("dw", S.skew_experts_grad, c, P, 8, P, 16, P, 5, P, 0, P, n, 0)
+    for ws, size in ((0, n), (P + 16, n), (P, n - 1)):
+        _refused("workspace", S.skew_experts_grad, c, P, 8, P, 16, P, 5, 0, P, ws, size, 0)
     S.skew_experts_product(c, 0, 8, P, P, 0, 0, 0)  # no rows: nothing to do
 
 
@@ -135,7 +139,7 @@ def test_head_does_not_keep_the_logits():
     """The gradients' workspace stays below the logits' size where these are large, whatever the number of tokens."""
     for T, V, d in ((8192, 50304, 4096), (65536, 131072, 1024), (1 << 20, 50257, 768)):
         c = S.HeadConfig(V, d, 1.0, 0)
-        assert S.skew_head_grad_workspace_bytes(c, T) <= max(512 << 20, T * 256 * 2) + T * d * 4 + 1024
+        assert S.skew_head_grad_workspace_bytes(c, T) <= max(512 << 20, T * 256 * 2) + T * d * 6 + (100 << 20)
         assert S.skew_head_loss_workspace_bytes(c, T) < T * V // 8
 
 

@@ -241,7 +241,7 @@ int skew_head_grad(const skew_head_config_t *c, const void *h, int64_t ld_h, con
             P.inner = width;
             P.cols = (int32_t)n;
             P.scale = c->scale;
-            P.flags = wide ? kIds64 : 0;
+            P.flags = (wide ? kIds64 : 0) | kOutVec;
             P.targets = targets;
             P.first = v0;
             P.vocab = c->rows;

@@ -28,17 +28,15 @@ constexpr int kStages = 6;                     // 5 where there are many groups
 constexpr int kMaxGroups = 1024;
 constexpr int kBandRows = 2048;                // rows of tiles that are walked together (what 152 SMs have under way then stays in L2)
 
-constexpr int kMulWarp = 0, kMemWarp = 1, kCopyWarp = 2, kCutWarp = 3, kFirstEnd = 4;  // of the warps from 4 on, each reads lanes 32 (warp % 4) on of tensor memory
-constexpr int kLoadWarps = 8;
+constexpr int kTile = 256;                     // rows and columns of a tile, which a pair of CTAs shares
 
-// COPY: stages come by tensor copies (one thread), and eight warps write out; else eight warps load, and four write out.
-template <bool COPY>
-constexpr int kEndWarps = COPY ? 8 : 4;
-template <bool COPY>
-constexpr int kThreads = 32 * (kFirstEnd + kEndWarps<COPY> + (COPY ? 0 : kLoadWarps));
-// PAIR: CTAs that share a tile, 1 or 2.
-template <int PAIR>
-constexpr int kTile = 128 * PAIR;              // rows and columns of a tile
+constexpr int kMulWarp = 0, kMemWarp = 1, kCopyWarp = 2, kCutWarp = 3, kFirstEnd = 4;  // of the warps from 4 on, each reads lanes 32 (warp % 4) on of tensor memory
+constexpr int kEndWarps = 8, kEndCols = kTile * 4 / kEndWarps, kFirstLoad = kFirstEnd + kEndWarps, kLoadWarps = 4;
+
+// COPY: the operands (1: A, 2: B) whose stages come by tensor copies, which one thread asks for. Four more warps load the others.
+constexpr int kCopyA = 1, kCopyB = 2;
+template <int COPY>
+constexpr int kThreads = 32 * (kFirstLoad + (COPY == 3 ? 0 : kLoadWarps));
 
 struct Shared {
     uint64_t full[kStages], empty[kStages], landed[kStages], sums[2], freed[2];
@@ -51,10 +49,10 @@ struct Shared {
 
 constexpr int kOutBytes = 32 * 128;            // 32 rows of 128 bytes, of each warp that writes out
 constexpr size_t kMaxSharedBytes = 232448;
-constexpr size_t shared_bytes(int stages, int end_warps, int groups) {
-    return 1024 + size_t(stages) * kStageBytes + size_t(end_warps) * kOutBytes + sizeof(Shared) + size_t(groups + 1) * 8;
+constexpr size_t shared_bytes(int stages, int groups) {
+    return 1024 + size_t(stages) * kStageBytes + size_t(kEndWarps) * kOutBytes + sizeof(Shared) + size_t(groups + 1) * 8;
 }
-static_assert(shared_bytes(kStages - 1, 8, kMaxGroups) <= kMaxSharedBytes, "shared memory of a CTA");
+static_assert(shared_bytes(kStages - 1, kMaxGroups) <= kMaxSharedBytes, "shared memory of a CTA");
 
 // A place in the ring of stages, and how often it was there before (odd or even).
 struct Place {
@@ -73,16 +71,16 @@ __device__ __forceinline__ void bar_init(uint64_t *b, uint32_t count) {
 }
 
 // The address of `p` in the pair's first CTA.
-template <int PAIR>
 __device__ __forceinline__ uint32_t in_first(const void *p) {
     uint32_t a = shared_address(p);
-    if constexpr (PAIR == 2) asm("mapa.shared::cluster.u32 %0, %0, 0;" : "+r"(a));
+    asm("mapa.shared::cluster.u32 %0, %0, 0;" : "+r"(a));
     return a;
 }
 
-template <int PAIR>
 __device__ __forceinline__ void bar_arrive(uint64_t *b) {  // the first CTA's
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(in_first<PAIR>(b)) : "memory");
+    // (Scope cta: what is handed over lies in shared or tensor memory, and goes by the proxies' own fences. At cluster scope the release waits for this
+    // thread's stores to memory.)
+    asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(in_first(b)) : "memory");
 }
 
 // Arrives at a barrier of this address, which then also waits for `bytes`. (Relaxed: nothing that this thread wrote is read after it. A release
@@ -93,7 +91,7 @@ __device__ __forceinline__ void bar_expect(uint32_t address, uint32_t bytes) {
 
 __device__ __forceinline__ bool bar_poll(uint64_t *b, uint32_t parity) {
     uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                  : "=r"(ok) : "r"(shared_address(b)), "r"(parity), "n"(2000) : "memory");
     return ok != 0;
 }
@@ -109,6 +107,13 @@ __device__ __forceinline__ bool bar_wait(uint64_t *b, uint32_t parity, Shared &S
     *reinterpret_cast<volatile uint32_t *>(&S.gave_up) = 1;
     atomicOr(&g_status, 1u);
     return false;
+}
+
+// One lane waits for its warp.
+__device__ __forceinline__ bool warp_wait(uint64_t *b, uint32_t parity, Shared &S) {
+    bool ok = true;
+    if ((threadIdx.x & 31) == 0) ok = bar_wait(b, parity, S);
+    return __shfl_sync(kFullMask, ok, 0);
 }
 
 __device__ __forceinline__ void drain(uint64_t *b, uint32_t parity) {
@@ -133,7 +138,7 @@ struct Tile {
 __device__ __forceinline__ int32_t *tiles_of(const ProductArgs &A, Shared &S) { return S.begin + A.groups + 1; }
 
 // The groups' rows, in order and within [0, rows) whatever `offsets` hold, and the tiles before each.
-template <int KIND, int THREADS, int TILE>
+template <int KIND, int THREADS>
 __device__ __forceinline__ void groups_of(const ProductArgs &A, Shared &S) {
     const int G = A.groups, per = (G + THREADS) / THREADS, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int rows = int(A.rows);
@@ -162,7 +167,7 @@ __device__ __forceinline__ void groups_of(const ProductArgs &A, Shared &S) {
     __syncthreads();
     if (KIND != kOuter) {
         int32_t *const tile = tiles_of(A, S);
-        auto tiles = [&](int i) { return i < G ? (S.begin[i + 1] - S.begin[i] + TILE - 1) / TILE : 0; };
+        auto tiles = [&](int i) { return i < G ? (S.begin[i + 1] - S.begin[i] + kTile - 1) / kTile : 0; };
         int n = 0;
         for (int i = i0; i < i1; ++i) n += tiles(i);
         n = scan(n, both);
@@ -171,61 +176,73 @@ __device__ __forceinline__ void groups_of(const ProductArgs &A, Shared &S) {
     __syncthreads();
 }
 
-// The pair's tiles, one after another: its own number, + the pairs, ...
-template <int KIND, int PAIR>
+// The pair's tiles, one after another: its own number, + the pairs, ... (Their number fits 31 bits: launch_of sees to it.) A whole warp walks: each lane works
+// out one of the next 32 tiles, which takes four divisions.
+template <int KIND>
 struct Walk {
-    static constexpr int kT = kTile<PAIR>, kBand = kBandRows / kT;
+    static constexpr uint32_t kBand = kBandRows / kTile;
     const ProductArgs &A;
     const int32_t *begin, *tile;
-    int64_t at, all;
-    int64_t each;      // OUTER: tiles of a group
-    int32_t nt, group;
+    uint32_t at, all, nt, mt;
+    Tile mine;
+    int32_t ahead;     // tiles that the lanes have left
 
-    __device__ __forceinline__ Walk(const ProductArgs &a, Shared &s) : A(a), begin(s.begin), tile(tiles_of(a, s)), at(blockIdx.x / PAIR), group(0) {
-        nt = (A.cols + kT - 1) / kT;
+    __device__ __forceinline__ Walk(const ProductArgs &a, Shared &s) : A(a), begin(s.begin), tile(tiles_of(a, s)), at(blockIdx.x / 2), ahead(0) {
+        nt = (uint32_t(A.cols) + kTile - 1) / kTile;
+        mt = (uint32_t(A.inner) + kTile - 1) / kTile;
+        all = (KIND == kOuter ? mt * A.groups : tile[A.groups]) * nt * A.splits;
+    }
+
+    __device__ __forceinline__ void work_out(uint32_t at) {
+        uint32_t here = at, split = 0, mt = this->mt, group;
+        if (A.splits > 1) here /= uint32_t(A.splits), split = at - here * A.splits;
+        const uint32_t row = here / nt;  // tiles of rows before this one's, over all groups
         if (KIND == kOuter) {
-            each = int64_t((A.inner + kT - 1) / kT) * nt;
-            all = each * A.groups;
-        } else {
-            all = int64_t(tile[A.groups]) * nt;
+            group = row / mt;
+            here -= group * mt * nt;
+        } else {  // its group is the last that begins at or before it
+            uint32_t lo = 0, hi = A.groups;
+            while (hi - lo > 1) {
+                const uint32_t mid = (lo + hi) >> 1;
+                if (uint32_t(tile[mid]) <= row) lo = mid; else hi = mid;
+            }
+            group = lo;
+            here -= tile[group] * nt;
+            mt = tile[group + 1] - tile[group];
         }
-        all *= A.splits;
+        const uint32_t band = here / (kBand * nt), first = band * kBand, in = min(kBand, mt - first), left = here - first * nt;
+        const uint32_t n = left / in, m = first + left - n * in;
+        mine.group = group;
+        mine.r0 = begin[group];
+        mine.r1 = begin[group + 1];
+        mine.m0 = m * kTile + (KIND == kOuter ? 0 : mine.r0);
+        mine.n0 = n * kTile;
+        const int steps = ((KIND == kOuter ? mine.r1 - mine.r0 : A.inner) + kStep - 1) / kStep, share = A.splits > 1 ? (steps + A.splits - 1) / A.splits : steps;
+        mine.k0 = split * share;
+        mine.steps = max(min(share, steps - mine.k0), 0);
+        mine.ends = mine.k0 + mine.steps == steps;
+        mine.unit = (((KIND == kOuter ? group * mt : 0) + m) * nt + n) * A.splits + split;
     }
 
     __device__ __forceinline__ bool next(Tile &t) {
         if (at >= all) return false;
-        int64_t here = at;
-        int mt, split = 0;
-        if (A.splits > 1) here /= A.splits, split = int(at - here * A.splits);
-        if (KIND == kOuter) {
-            group = int(here / each);
-            here -= group * each;
-            mt = (A.inner + kT - 1) / kT;
-        } else {
-            const int row = int(here / nt);  // tiles of rows before this one's, over all groups: its group is the last that begins at or before it
-            int lo = group, hi = A.groups;
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (tile[mid] <= row) lo = mid; else hi = mid;
-            }
-            group = lo;
-            here -= int64_t(tile[group]) * nt;
-            mt = tile[group + 1] - tile[group];
+        const uint32_t step = gridDim.x / 2;
+        if (!ahead) {
+            const uint32_t lane = threadIdx.x & 31;
+            if (at + uint64_t(lane) * step < all) work_out(at + lane * step);
+            ahead = 32;
         }
-        const int64_t span = int64_t(kBand) * nt;
-        const int band = int(here / span), first = band * kBand, in = min(kBand, mt - first), left = int(here - band * span);
-        t.group = group;
-        t.r0 = begin[group];
-        t.r1 = begin[group + 1];
-        t.m0 = (first + left % in) * kT + (KIND == kOuter ? 0 : t.r0);
-        t.n0 = left / in * kT;
-        const int steps = ((KIND == kOuter ? t.r1 - t.r0 : A.inner) + kStep - 1) / kStep, share = (steps + A.splits - 1) / A.splits;
-        t.k0 = split * share;
-        t.steps = max(min(share, steps - t.k0), 0);
-        t.ends = t.k0 + t.steps == steps;
-        t.unit = ((KIND == kOuter ? group * mt : 0) + first + left % in) * nt + left / in;
-        t.unit = t.unit * A.splits + split;
-        at += gridDim.x / PAIR;
+        const int from = 32 - ahead--;
+        t.group = __shfl_sync(kFullMask, mine.group, from);
+        t.m0 = __shfl_sync(kFullMask, mine.m0, from);
+        t.n0 = __shfl_sync(kFullMask, mine.n0, from);
+        t.r0 = __shfl_sync(kFullMask, mine.r0, from);
+        t.r1 = __shfl_sync(kFullMask, mine.r1, from);
+        t.k0 = __shfl_sync(kFullMask, mine.k0, from);
+        t.steps = __shfl_sync(kFullMask, mine.steps, from);
+        t.unit = __shfl_sync(kFullMask, mine.unit, from);
+        t.ends = __shfl_sync(kFullMask, int(mine.ends), from);
+        at += step;
         return true;
     }
 };
@@ -233,62 +250,85 @@ struct Walk {
 // ---------------------------------------------------------------------------
 // Loads
 // ---------------------------------------------------------------------------
-// Eight elements from `p`, of which `n` are there.
-__device__ __forceinline__ uint4 eight(const uint16_t *p, int n) {
-    uint4 u = make_uint4(0, 0, 0, 0);
-    if (n >= 8 && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
-        u = *reinterpret_cast<const uint4 *>(p);
-    } else if (n >= 8 && (reinterpret_cast<uintptr_t>(p) & 3) == 0) {
-        const uint32_t *q = reinterpret_cast<const uint32_t *>(p);
-        u = make_uint4(q[0], q[1], q[2], q[3]);
-    } else if (n > 0) {
-        uint32_t v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0;
-        u = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+// Eight elements from `p` on, of which `n` are there, wherever they start: by the one or two 16-byte units that hold them. (A unit is read only where it holds an
+// element that is there, so that no access leaves the units of the matrix itself.)
+struct Eight {
+    uint4 a, b;
+    __device__ __forceinline__ void ask(const uint16_t *p, int n) {
+        const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(p)) & 15;
+        const uint4 *q = reinterpret_cast<const uint4 *>(reinterpret_cast<uintptr_t>(p) - off);
+        a = b = make_uint4(0, 0, 0, 0);
+        if (n > 0) a = __ldg(q);
+        if (n > int(16 - off) / 2) b = __ldg(q + 1);
     }
-    return u;
-}
+    __device__ __forceinline__ uint4 get(const uint16_t *p, int n) const {
+        const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(p)) & 15;
+        uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        if (off & 8) {
+#pragma unroll
+            for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+        }
+        if (off & 4) {
+#pragma unroll
+            for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+        }
+        if (off & 2) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+        }
+        if (n < 8) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = n >= 2 * i + 2 ? w[i] : n == 2 * i + 1 ? w[i] & 0xFFFFu : 0u;
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
 
-// One operand's 128 lines of a stage. MAJOR: lines along the summed index, numbered l0 on, of which those before l_end are there; elements from s0, before s_end.
-// Else two blocks of 64 lines, one for each step of the summed index (s0 on, before s_end), of elements from l0 (and l0 + 64), before l_end.
+// `count` of one operand's 128 lines of a stage, from line `from` on, by a warp. MAJOR: lines along the summed index, numbered l0 on, of which those before l_end are
+// there; elements from s0, before s_end. Else two blocks of 64 lines, one for each step of the summed index (s0 on, before s_end), of elements from l0 (and l0 + 64),
+// before l_end.
 template <bool MAJOR>
-__device__ __forceinline__ void load_lines(const uint16_t *p, int64_t ld, int64_t l0, int64_t l_end, int64_t s0, int64_t s_end, char *to, int warp, int lane) {
-    constexpr int kRounds = kLines / (kLoadWarps / 2) / 4;
-    uint4 u[kRounds];
+__device__ __forceinline__ void load_lines(const uint16_t *p, int64_t ld, int64_t l0, int64_t l_end, int64_t s0, int64_t s_end, char *to, int from, int count, int lane) {
+    constexpr int kDeep = 4;  // four lines a round, eight lanes each
+    const int c = lane % 8 * 8;
+    auto place = [&](int L, const uint16_t *&q, int &n) {
+        const int64_t line = MAJOR ? l0 + L : s0 + L % 64, elem = MAJOR ? s0 + c : l0 + L / 64 * 64 + c, left = (MAJOR ? s_end : l_end) - elem;
+        q = p + line * ld + elem;
+        n = line < (MAJOR ? l_end : s_end) ? int(left < 8 ? left : 8) : 0;
+    };
+#pragma unroll 1
+    for (int i = from; i < from + count; i += 4 * kDeep) {
+        Eight u[kDeep];
+        const uint16_t *q;
+        int n;
 #pragma unroll
-    for (int i = 0; i < kRounds; ++i) {
-        const int L = (warp * kRounds + i) * 4 + lane / 8, c = lane % 8 * 8;
-        const int64_t line = MAJOR ? l0 + L : s0 + L % 64, elem = MAJOR ? s0 + c : l0 + L / 64 * 64 + c;
-        const int64_t left = (MAJOR ? s_end : l_end) - elem;
-        u[i] = line < (MAJOR ? l_end : s_end) && left > 0 ? eight(p + line * ld + elem, left < 8 ? int(left) : 8) : make_uint4(0, 0, 0, 0);
-    }
+        for (int j = 0; j < kDeep; ++j) {
+            place(i + j * 4 + lane / 8, q, n);
+            u[j].ask(q, n);
+        }
 #pragma unroll
-    for (int i = 0; i < kRounds; ++i) {
-        const int L = (warp * kRounds + i) * 4 + lane / 8;
-        *reinterpret_cast<uint4 *>(to + L * 128 + ((lane % 8) ^ (L & 7)) * 16) = u[i];
+        for (int j = 0; j < kDeep; ++j) {
+            const int L = i + j * 4 + lane / 8;
+            place(L, q, n);
+            *reinterpret_cast<uint4 *>(to + L * 128 + ((lane % 8) ^ (L & 7)) * 16) = u[j].get(q, n);
+        }
     }
 }
 
 // A box of a tensor map, from column x, line y of group z, to shared memory at `to`; its bytes count at the barrier of this address.
-template <int PAIR>
 __device__ __forceinline__ void copy_box(const CUtensorMap &map, uint32_t to, uint32_t bar, int x, int y, int z) {
-    if constexpr (PAIR == 2)
-        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4, %5}], [%2];"
-                     ::"r"(to), "l"(&map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
-    else
-        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-                     ::"r"(to), "l"(&map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4, %5}], [%2];"
+                 ::"r"(to), "l"(&map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
 }
 
 // One operand's 128 lines, as load_lines brings them. Beyond the matrix the boxes hold zeros.
-template <bool MAJOR, int PAIR>
+template <bool MAJOR>
 __device__ __forceinline__ void copy_lines(const CUtensorMap &map, uint32_t to, uint32_t bar, int l0, int s0, int group) {
     if constexpr (MAJOR) {
-        copy_box<PAIR>(map, to, bar, s0, l0, group);
+        copy_box(map, to, bar, s0, l0, group);
     } else {
-        copy_box<PAIR>(map, to, bar, l0, s0, group);
-        copy_box<PAIR>(map, to + kOperandBytes / 2, bar, l0 + 64, s0, group);
+        copy_box(map, to, bar, l0, s0, group);
+        copy_box(map, to + kOperandBytes / 2, bar, l0 + 64, s0, group);
     }
 }
 
@@ -306,47 +346,28 @@ __device__ __forceinline__ uint64_t operand(uint32_t address) {
 template <bool MAJOR>
 constexpr uint32_t kNext16 = (MAJOR ? 32 : 16 * 128) >> 4;
 
-template <bool A_MAJOR, bool B_MAJOR, int PAIR>
+template <bool A_MAJOR, bool B_MAJOR>
 constexpr uint32_t kInstruction = 1u << 4 /* sums fp32 */ | 1u << 7 | 1u << 10 /* bf16 */ | uint32_t(!A_MAJOR) << 15 | uint32_t(!B_MAJOR) << 16 |
-                                  uint32_t(kTile<PAIR> >> 3) << 17 | uint32_t(kTile<PAIR> >> 4) << 24;
+                                  uint32_t(kTile >> 3) << 17 | uint32_t(kTile >> 4) << 24;
 
-// 16 steps of the tile: for a pair of CTAs, each holds half of A's rows and of B's columns, and takes the sums of its rows.
-template <int PAIR>
+// 16 steps of a tile: each CTA of the pair holds half of A's rows and of B's columns, and gets the sums of its rows.
 __device__ __forceinline__ void multiply(uint32_t acc, uint64_t a, uint64_t b, uint32_t instruction, bool add) {
-    if constexpr (PAIR == 2)
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                     ::"r"(acc), "l"(a), "l"(b), "r"(instruction), "r"(uint32_t(add)) : "memory");
-    else
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                     ::"r"(acc), "l"(a), "l"(b), "r"(instruction), "r"(uint32_t(add)) : "memory");
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(acc), "l"(a), "l"(b), "r"(instruction), "r"(uint32_t(add)) : "memory");
 }
 
 // Arrives, in each CTA of the pair, once what was issued before is done.
-template <int PAIR>
 __device__ __forceinline__ void commit(uint64_t *bar) {
-    if constexpr (PAIR == 2)
-        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(shared_address(bar)), "h"(uint16_t(3)) : "memory");
-    else
-        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(shared_address(bar)) : "memory");
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(shared_address(bar)), "h"(uint16_t(3)) : "memory");
 }
 
-template <int PAIR>
 __device__ __forceinline__ void take_tensor_memory(uint32_t *address) {
-    if constexpr (PAIR == 2) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_address(address)), "n"(2 * kTile<PAIR>) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-    } else {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_address(address)), "n"(2 * kTile<PAIR>) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    }
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_address(address)), "n"(2 * kTile) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
 }
 
-template <int PAIR>
 __device__ __forceinline__ void give_tensor_memory(uint32_t acc) {
-    if constexpr (PAIR == 2)
-        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(acc), "n"(2 * kTile<PAIR>) : "memory");
-    else
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(acc), "n"(2 * kTile<PAIR>) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(acc), "n"(2 * kTile) : "memory");
 }
 
 __device__ __forceinline__ void after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -381,66 +402,77 @@ __device__ __forceinline__ float exp2_of(float x) {
     return y;
 }
 
-// y = base + scale * x for 32 columns of a row, of which `n` are there.
-template <bool B32>
-__device__ __forceinline__ void add_base(const ProductArgs &A, float scale, int64_t at, int n, float (&x)[32]) {
-    if (!A.base) {
+// Where 32 rows of a warp go, in elements: of the first row and the matrix's first column, and the rows' distance.
+struct Target {
+    int64_t at, ldo;
+    int rows;
+};
+
+// What lanes have of their rows leaves through 32 x 128 bytes of shared memory of the warp's own, 16-byte units permuted as in a stage, and from there row by row,
+// so that accesses are whole 32-byte sectors (stores of the lanes' own rows took twice the time, and tensor copies of them a wait for each).
+
+// 64 columns, from `column` on, scaled, in bf16; the rows' units are on 16-byte boundaries.
+__device__ __forceinline__ void put_64(const ProductArgs &A, char *buffer, const Target &to, int column, float scale, const float (&x)[64]) {
+    const int lane = threadIdx.x & 31, unit = lane % 8;
 #pragma unroll
-        for (int c = 0; c < 32; ++c) x[c] *= scale;
-    } else if (n >= 32 && A.flags & kOutVec) {
-        Vec8<B32> b[4];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) b[c] = load8_cached<B32>(A.base, at + 8 * c);
-#pragma unroll
-        for (int c = 0; c < 32; ++c) x[c] = fmaf(x[c], scale, b[c / 8].at(c % 8));
-    } else {
-#pragma unroll
-        for (int c = 0; c < 32; ++c) x[c] = c < n ? fmaf(x[c], scale, load1<B32>(A.base, at + c)) : 0.f;
+    for (int u = 0; u < 8; ++u) {
+        const float *y = x + u * 8;
+        *reinterpret_cast<uint4 *>(buffer + lane * 128 + (u ^ (lane & 7)) * 16) = make_uint4(pack_bf16(y[0] * scale, y[1] * scale), pack_bf16(y[2] * scale, y[3] * scale),
+                                                                                             pack_bf16(y[4] * scale, y[5] * scale), pack_bf16(y[6] * scale, y[7] * scale));
     }
+    __syncwarp();
+    char *out = static_cast<char *>(A.out) + (to.at + column + lane / 8 * to.ldo) * 2 + unit * 16;
+    const int64_t next = to.ldo * 8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i, out += next) {
+        const int r = i * 4 + lane / 8;
+        const uint4 u = *reinterpret_cast<const uint4 *>(buffer + r * 128 + (unit ^ (r & 7)) * 16);
+        if (r < to.rows) *reinterpret_cast<uint4 *>(out) = u;
+    }
+    __syncwarp();
 }
 
-// 32 columns of a row, of which `n` are there, to memory.
-template <bool O32>
-__device__ __forceinline__ void put_columns(const ProductArgs &A, int64_t at, int n, const float (&y)[32]) {
-    if (n >= 32 && A.flags & kOutVec) {
-        uint4 *q = reinterpret_cast<uint4 *>(const_cast<char *>(elem_ptr<O32>(A.out, at)));
-#pragma unroll
-        for (int c = 0; c < 32; c += O32 ? 4 : 8)
-            q[c / (O32 ? 4 : 8)] = O32 ? make_uint4(__float_as_uint(y[c]), __float_as_uint(y[c + 1]), __float_as_uint(y[c + 2]), __float_as_uint(y[c + 3]))
-                                       : make_uint4(pack_bf16(y[c], y[c + 1]), pack_bf16(y[c + 2], y[c + 3]), pack_bf16(y[c + 4], y[c + 5]), pack_bf16(y[c + 6], y[c + 7]));
-        return;
-    }
-#pragma unroll
-    for (int c = 0; c < 32; ++c)
-        if (c < n) store1<O32>(A.out, at + c, y[c]);
-}
-
-// The 32 columns to the lane's row of the warp's 32 x 128 bytes of shared memory, 16-byte units permuted as in a stage; the last of the 128 bytes then
-// leave by a tensor copy, which keeps to the matrix. `column`: the first of the 32.
-template <bool O32>
-__device__ __forceinline__ void copy_columns(const CUtensorMap &map, char *to, int column, int row0, int group, bool last, const float (&y)[32]) {
+// 32 columns, from `column` on, of which `n` are there: base + scale * x, in any type.
+__device__ __forceinline__ void put_32(const ProductArgs &A, char *buffer, const Target &to, int column, int n, float scale, const float (&x)[32]) {
     const int lane = threadIdx.x & 31;
-    constexpr int kWide = O32 ? 32 : 64;  // columns of 128 bytes
-    const int part = column % kWide;
-    if (part == 0) {
-        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-        __syncwarp();
-    }
+    const bool o32 = A.flags & kOut32, b32 = A.flags & kBase32;
 #pragma unroll
-    for (int c = 0; c < 32; c += O32 ? 4 : 8) {
-        const uint4 u = O32 ? make_uint4(__float_as_uint(y[c]), __float_as_uint(y[c + 1]), __float_as_uint(y[c + 2]), __float_as_uint(y[c + 3]))
-                            : make_uint4(pack_bf16(y[c], y[c + 1]), pack_bf16(y[c + 2], y[c + 3]), pack_bf16(y[c + 4], y[c + 5]), pack_bf16(y[c + 6], y[c + 7]));
-        *reinterpret_cast<uint4 *>(to + lane * 128 + ((((part + c) / (O32 ? 4 : 8)) ^ (lane & 7)) * 16)) = u;
-    }
-    if (part + 32 == kWide || last) {
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) {
-            asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
-                         ::"l"(&map), "r"(shared_address(to)), "r"(column - part), "r"(row0), "r"(group) : "memory");
-            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    for (int u = 0; u < 8; ++u)
+        *reinterpret_cast<float4 *>(buffer + lane * 128 + (u ^ (lane & 7)) * 16) = make_float4(x[4 * u], x[4 * u + 1], x[4 * u + 2], x[4 * u + 3]);
+    __syncwarp();
+    if (A.flags & kOutVec && n >= 32) {  // eight lanes to a row, four columns to a lane
+        const int unit = lane % 8;
+        const int64_t at = to.at + column + unit * 4;
+#pragma unroll 4
+        for (int i = 0; i < 8; ++i) {
+            const int r = i * 4 + lane / 8;
+            if (r >= to.rows) break;
+            const float4 y = *reinterpret_cast<const float4 *>(buffer + r * 128 + (unit ^ (r & 7)) * 16);
+            const int64_t e = at + r * to.ldo;
+            float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (A.base && b32) {
+                b = *reinterpret_cast<const float4 *>(elem_ptr<true>(A.base, e));
+            } else if (A.base) {
+                const uint2 u = *reinterpret_cast<const uint2 *>(elem_ptr<false>(A.base, e));
+                b = make_float4(bf16_low(u.x), bf16_high(u.x), bf16_low(u.y), bf16_high(u.y));
+            }
+            b = A.base ? make_float4(fmaf(y.x, scale, b.x), fmaf(y.y, scale, b.y), fmaf(y.z, scale, b.z), fmaf(y.w, scale, b.w))
+                       : make_float4(y.x * scale, y.y * scale, y.z * scale, y.w * scale);
+            if (o32) *reinterpret_cast<float4 *>(static_cast<float *>(A.out) + e) = b;
+            else *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(A.out) + e) = make_uint2(pack_bf16(b.x, b.y), pack_bf16(b.z, b.w));
+        }
+    } else {  // a row at a time, a column to a lane
+        const int64_t at = to.at + column + lane;
+#pragma unroll 4
+        for (int r = 0; r < to.rows; ++r) {
+            const float y = *reinterpret_cast<const float *>(buffer + r * 128 + ((lane / 4) ^ (r & 7)) * 16 + lane % 4 * 4);
+            const int64_t e = at + r * to.ldo;
+            if (lane >= n) continue;
+            const float b = !A.base ? 0.f : b32 ? load1<true>(A.base, e) : load1<false>(A.base, e), z = A.base ? fmaf(y, scale, b) : y * scale;
+            if (o32) store1<true>(A.out, e, z); else store1<false>(A.out, e, z);
         }
     }
+    __syncwarp();
 }
 
 __device__ __forceinline__ int64_t target_of(const ProductArgs &A, int64_t row) {  // -1: none
@@ -460,38 +492,53 @@ __device__ __forceinline__ float peak_of(const float *peaks) {
 constexpr int kPart = 128;  // columns of a LOSS part: what one warp has of a tile
 constexpr float kLog2e = 1.44269504088896340736f;
 
-// What a warp does with 32 rows and COLS columns of a tile, from row `row0` and column `col0` of it. read(f) has f see the sums in tensor memory, at an
-// address, once they are there; false if the wait for them gave up. Sums of more than A.chunk steps come in several parts, which are added here: the tensor
-// cores round every addition towards zero, so that errors do not cancel but grow with the number of steps (measured: 1e-9 of the result for each product).
-template <int KIND, int END, int COLS, typename Read>
-__device__ __forceinline__ bool end_tile(const ProductArgs &A, const CUtensorMap &map, char *buffer, const Tile &t, float peak, int row0, int col0, const Read &read) {
+// The sums in tensor memory, one half after the other, as a warp that writes out sees them.
+struct Sums {
+    Shared &S;
+    Place half;
+    uint32_t first;
+    __device__ __forceinline__ bool wait(uint32_t &at) {  // for the next; false if that gave up
+        if (!warp_wait(&S.sums[half.s], half.phase, S)) return false;
+        after_sync();
+        at = first + half.s * kTile;
+        return true;
+    }
+    __device__ __forceinline__ void free() {
+        before_sync();
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) bar_arrive(&S.freed[half.s]);
+        half.next(2);
+    }
+};
+
+// What a warp does with 32 rows and COLS columns of a tile, from row `row0` and column `col0` of it; false if a wait gave up. Sums of more than A.chunk
+// steps come in several parts, which are added here: the tensor cores round every addition towards zero, so that errors do not cancel but grow with the
+// number of steps (measured: 1e-9 of the result for each product).
+template <int KIND, int END, int COLS>
+__device__ __forceinline__ bool end_tile(const ProductArgs &A, char *buffer, const Tile &t, float peak, int row0, int col0, Sums &sums) {
     const bool parts = A.splits > 1;  // of the sums, each to a tile of its own
     const int64_t first = int64_t(t.m0) + row0, row = first + (threadIdx.x & 31);
     const int64_t end = KIND == kOuter ? A.inner : t.r1;
     const bool mine = row < end;
     const int start = t.n0 + col0, stop = min(start + COLS, A.cols);
     const bool any = first < end && start < stop;
-    // STORE: whole by a tensor copy, unless rows of the group behind would be written.
-    const bool copy = A.flags & kOutCopy && (KIND == kOuter || !A.offsets || first + 32 <= end);
-    const int64_t at = (KIND == kOuter ? t.group * A.o_group : 0) + row * A.ldo;
-    const int to_col = parts ? t.n0 : 0, to_row = parts ? row0 : int(first), to_group = parts ? t.unit : KIND == kOuter ? t.group : 0;
+    const Target to{parts ? int64_t(t.unit) * (kTile * kTile) + row0 * kTile - t.n0 : (KIND == kOuter ? t.group * A.o_group : 0) + first * A.ldo,
+                    parts ? kTile : A.ldo, int(min(end - first, int64_t(32)))};
     // LOSS, LOGITS_GRAD: in powers of two, exp(x) = 2^(x log2 e)
     const float scale = A.scale * peak, scale2 = A.scale * kLog2e;
     const int64_t target = END != kStore && mine ? target_of(A, row) : -1;
     const float g = END == kLogitsGrad && target >= 0 ? A.dloss[row] / peak : 0.f, lse2 = END == kLogitsGrad && target >= 0 ? A.lse[row] * kLog2e : 0.f;
     float top = -INFINITY, sum = 0.f;
 
+    const int picked = target >= A.first && target < A.first + A.cols ? int(target - A.first) : -1;
+    auto turned = [&](int column, float &x, int i) {  // LOGITS_GRAD: a logit to its gradient
+        const float p = exp2_of(fmaf(x, scale2, -lse2)) - (picked == column + i ? 1.f : 0.f);
+        x = target >= 0 ? p * g : 0.f;
+    };
     auto chunk = [&](int column, float (&x)[32]) {  // 32 columns
         const int n = stop - column;
         if constexpr (END == kStore) {
-            if (mine) {
-                if (A.flags & kBase32) add_base<true>(A, scale, at + column, n, x); else add_base<false>(A, scale, at + column, n, x);
-            }
-            if (copy) {
-                if (A.flags & kOut32) copy_columns<true>(map, buffer, column - to_col, to_row, to_group, n <= 32, x); else copy_columns<false>(map, buffer, column - to_col, to_row, to_group, n <= 32, x);
-            } else if (mine) {
-                if (A.flags & kOut32) put_columns<true>(A, at + column, n, x); else put_columns<false>(A, at + column, n, x);
-            }
+            put_32(A, buffer, to, column, n, scale, x);
         } else if constexpr (END == kLoss) {
             const int64_t here = target - column;
             if (here >= 0 && here < 32 && target >= 0) {
@@ -500,92 +547,96 @@ __device__ __forceinline__ bool end_tile(const ProductArgs &A, const CUtensorMap
                 for (int i = 0; i < 32; ++i) p = here == i ? x[i] : p;
                 A.picked[row] = p * A.scale;
             }
-            float high = top;
+            float high[4] = {top, -INFINITY, -INFINITY, -INFINITY}, part[4] = {};
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
                 x[i] = i < n ? x[i] * scale2 : -INFINITY;
-                high = fmaxf(high, x[i]);
+                high[i % 4] = fmaxf(high[i % 4], x[i]);
             }
-            const float from = high == -INFINITY ? 0.f : high;
-            float part = 0.f;
+            const float most = fmaxf(fmaxf(high[0], high[1]), fmaxf(high[2], high[3])), from = most == -INFINITY ? 0.f : most;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) part += exp2_of(x[i] - from);
-            sum = fmaf(sum, exp2_of(top - from), part);
-            top = high;
+            for (int i = 0; i < 32; ++i) part[i % 4] += exp2_of(x[i] - from);
+            sum = fmaf(sum, exp2_of(top - from), (part[0] + part[1]) + (part[2] + part[3]));
+            top = most;
         } else {
-            const int64_t here = target - A.first - column;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                const float p = exp2_of(fmaf(x[i], scale2, -lse2)) - (here == i ? 1.f : 0.f);
-                x[i] = target >= 0 ? p * g : 0.f;
-            }
-            if (copy) {
-                copy_columns<false>(map, buffer, column, int(first), 0, n <= 32, x);
-            } else if (mine) {
-                put_columns<false>(A, at + column, n, x);
-            }
+            for (int i = 0; i < 32; ++i) turned(column, x[i], i);
+            put_32(A, buffer, to, column, n, 1.f, x);
         }
     };
-    if (!t.steps) {
-        float x[32];
-        for (int c = start; any && c < stop; c += 32) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) x[i] = 0.f;
-            chunk(c, x);
-        }
-        return true;
-    }
-    if (t.steps <= A.chunk) {
-        const bool ok = read([&](uint32_t acc) {
-            if (!any) return;
-            float x[2][32];
-            read_sums(acc, x[0]);
-#pragma unroll
-            for (int c = 0; c < COLS / 32; ++c) {  // the next 32 columns are on their way while 32 are dealt with
-                sums_read(x[c % 2]);
-                if (c + 1 < COLS / 32) read_sums(acc + (c + 1) * 32, x[(c + 1) % 2]);
-                if (start + c * 32 < stop) chunk(start + c * 32, x[c % 2]);
-                __syncwarp();
-            }
-        });
-        if (!ok) return false;
-    } else {
-        float run[COLS / 32][32];
+    // Below, one loop for what comes from tensor memory, from several parts of it, or is zeros, and not unrolled: what becomes of 32 columns is long, and code
+    // that is there several times waits for instructions (2.2 us more a tile, measured with four copies).
+    float run[COLS / 32][32];
+    const bool several = t.steps > A.chunk;
+    if (several) {
 #pragma unroll
         for (int c = 0; c < COLS / 32; ++c)
 #pragma unroll
             for (int i = 0; i < 32; ++i) run[c][i] = 0.f;
 #pragma unroll 1
         for (int k = 0; k < t.steps; k += A.chunk) {
-            const bool ok = read([&](uint32_t acc) {
-#pragma unroll
-                for (int c = 0; c < COLS / 32; ++c) {
-                    float x[32];
-                    read_sums(acc + c * 32, x);
-                    sums_read(x);
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) run[c][i] += x[i];
-                }
-            });
-            if (!ok) return false;
-        }
-        if (any) {
+            uint32_t acc;
+            if (!sums.wait(acc)) return false;
 #pragma unroll
             for (int c = 0; c < COLS / 32; ++c) {
-                if (start + c * 32 < stop) chunk(start + c * 32, run[c]);
-                __syncwarp();
+                float x[32];
+                read_sums(acc + c * 32, x);
+                sums_read(x);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) run[c][i] += x[i];
             }
+            sums.free();
         }
     }
+    const bool here = t.steps && !several;
+    uint32_t acc = 0;
+    if (here && !sums.wait(acc)) return false;
+    if (any) {
+        int c = 0;
+        if (END != kLoss && here && A.flags & kOutVec && !(A.flags & kOut32) && !A.base) {
+#pragma unroll 1
+            for (; c < COLS && start + c + 64 <= stop; c += 64) {
+                float x[64];
+                read_sums(acc + c, *reinterpret_cast<float (*)[32]>(x));
+                read_sums(acc + c + 32, *reinterpret_cast<float (*)[32]>(x + 32));
+                sums_read(*reinterpret_cast<float (*)[32]>(x));
+                sums_read(*reinterpret_cast<float (*)[32]>(x + 32));
+                if constexpr (END == kLogitsGrad) {
+#pragma unroll
+                    for (int i = 0; i < 64; ++i) turned(start + c, x[i], i);
+                }
+                put_64(A, buffer, to, start + c, END == kLogitsGrad ? 1.f : scale, x);
+            }
+        }
+#pragma unroll(END == kLoss ? COLS / 32 : 1)
+        for (; c < COLS; c += 32) {
+            if (start + c >= stop) break;
+            float x[32];
+            if (here) {
+                read_sums(acc + c, x);
+                sums_read(x);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    x[i] = 0.f;
+                    if (several) {
+#pragma unroll
+                        for (int j = 0; j < COLS / 32; ++j) x[i] = c == 32 * j ? run[j][i] : x[i];
+                    }
+                }
+            }
+            chunk(start + c, x);
+        }
+    }
+    if (here) sums.free();
     if (END == kLoss && any && mine) A.part[int64_t(start / kPart) * A.rows + row] = make_float2(top, sum);  // lanes side by side
     return true;
 }
 
 // Rows of no group are zeros.
-template <int WARPS>
 __device__ __forceinline__ void clear_rows(const ProductArgs &A, const Shared &S, int warp, int lane) {
     const int64_t before = S.begin[0], behind = A.rows - S.begin[A.groups];
-    for (int64_t i = int64_t(blockIdx.x) * WARPS + warp; i < before + behind; i += int64_t(gridDim.x) * WARPS) {
+    for (int64_t i = int64_t(blockIdx.x) * kEndWarps + warp; i < before + behind; i += int64_t(gridDim.x) * kEndWarps) {
         const int64_t row = i < before ? i : S.begin[A.groups] + i - before;
         if (A.flags & kOutVec) {
             for (int c = lane * 8; c < A.cols; c += 256) {
@@ -601,57 +652,57 @@ __device__ __forceinline__ void clear_rows(const ProductArgs &A, const Shared &S
     }
 }
 
-template <int KIND, int END, bool COPY, int PAIR>
+template <int KIND, int END, int COPY>
 __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                                                               const __grid_constant__ CUtensorMap map_out, const ProductArgs A, const uint32_t stages) {
+                                                               const ProductArgs A, const uint32_t stages) {
     extern __shared__ char raw[];
-    constexpr int kT = kTile<PAIR>, kEnds = kEndWarps<COPY>, kEndCols = kT * 4 / kEnds;
+    constexpr bool COPY_A = COPY & kCopyA, COPY_B = COPY & kCopyB;
     char *const ring = raw + (1024 - (shared_address(raw) & 1023)) % 1024, *const out_at = ring + stages * kStageBytes;
-    Shared &S = *reinterpret_cast<Shared *>(out_at + kEnds * kOutBytes);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = PAIR == 2 ? blockIdx.x & 1 : 0;
+    Shared &S = *reinterpret_cast<Shared *>(out_at + kEndWarps * kOutBytes);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = blockIdx.x & 1;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kStages; ++i) bar_init(&S.full[i], PAIR * (COPY ? 1 : kLoadWarps)), bar_init(&S.empty[i], 1), bar_init(&S.landed[i], 1);
-        for (int i = 0; i < 2; ++i) bar_init(&S.sums[i], 1), bar_init(&S.freed[i], PAIR * kEnds);
+        for (int i = 0; i < kStages; ++i) bar_init(&S.full[i], 2 * ((COPY ? 1 : 0) + (COPY == 3 ? 0 : kLoadWarps))), bar_init(&S.empty[i], 1), bar_init(&S.landed[i], 1);
+        for (int i = 0; i < 2; ++i) bar_init(&S.sums[i], 1), bar_init(&S.freed[i], 2 * kEndWarps);
         S.gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == kMemWarp) take_tensor_memory<PAIR>(&S.acc);
-    groups_of<KIND, kThreads<COPY>, kT>(A, S);
+    if (warp == kMemWarp) take_tensor_memory(&S.acc);
+    groups_of<KIND, kThreads<COPY>>(A, S);
     before_sync();
-    if (PAIR == 2) pair_sync(); else __syncthreads();
+    pair_sync();
     after_sync();
     const uint32_t acc = S.acc;
     constexpr bool A_MAJOR = KIND != kOuter, B_MAJOR = KIND == kByCols;
-    Walk<KIND, PAIR> walk(A, S);
+    Walk<KIND> walk(A, S);
     Tile t;
     Place p;
     bool ok = true;
 
     // Registers, of the 168 (128) that a thread starts with: a warp that writes out holds 128 columns of sums, and what becomes of them.
-    if (warp < kFirstEnd)
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(COPY ? 56 : 48));
-    if (COPY && warp == kCopyWarp) {
-        if (!lane) {
-            uint32_t n = 0;
-            while (ok && walk.next(t)) {
+    if (warp < kFirstEnd) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(COPY == 3 ? 56 : 40));
+    if (COPY && warp == kCopyWarp) {  // one lane, as where the products are issued: 32 that wait for a barrier slow down what runs beside them by 3 %
+        uint32_t n = 0;
+        while (ok && walk.next(t)) {
+            if (!lane) {
                 const int m0 = t.m0 + rank * kLines, n0 = t.n0 + rank * kLines;
                 // A CTA whose rows all belong to the groups behind needs none of them: its sums are not read.
-                const bool rows = KIND == kOuter || m0 < t.r1;
+                const bool rows = COPY_A && (KIND == kOuter || m0 < t.r1);
                 for (int k = 0; k < t.steps; ++k, ++n, p.next(stages)) {
                     const int s0 = (KIND == kOuter ? t.r0 : 0) + (t.k0 + k) * kStep;
                     if (!(ok = bar_wait(&S.empty[p.s], p.phase ^ 1, S))) break;
                     // The last lines of a group that ends within a stage go to the warp that clears what is behind them.
                     const bool cut = KIND == kOuter && s0 + kStep > t.r1;
-                    const uint32_t to = shared_address(ring) + p.s * kStageBytes, bar = cut ? shared_address(&S.landed[p.s]) : in_first<PAIR>(&S.full[p.s]);
-                    bar_expect(bar, rows ? kStageBytes : kOperandBytes);
-                    if (rows) copy_lines<A_MAJOR, PAIR>(map_a, to, bar, m0, s0, 0);
-                    copy_lines<B_MAJOR, PAIR>(map_b, to + kOperandBytes, bar, n0, s0, KIND == kOuter ? 0 : t.group);
+                    const uint32_t to = shared_address(ring) + p.s * kStageBytes, bar = cut ? shared_address(&S.landed[p.s]) : in_first(&S.full[p.s]);
+                    bar_expect(bar, (rows ? kOperandBytes : 0) + (COPY_B ? kOperandBytes : 0));
+                    if (rows) copy_lines<A_MAJOR>(map_a, to, bar, m0, s0, 0);
+                    if (COPY_B) copy_lines<B_MAJOR>(map_b, to + kOperandBytes, bar, n0, s0, KIND == kOuter ? 0 : t.group);
                 }
             }
-            // what was asked for arrives before the shared memory is given back
-            if (!ok && !rank)
-                for (uint32_t i = n > stages ? n - stages : 0; i < n; ++i) drain(&S.full[i % stages], i / stages & 1);
+            ok = __shfl_sync(kFullMask, ok, 0);
         }
+        // what was asked for arrives before the shared memory is given back
+        if (!ok && !rank && !lane)
+            for (uint32_t i = n > stages ? n - stages : 0; i < n; ++i) drain(&S.full[i % stages], i / stages & 1);
     } else if (COPY && KIND == kOuter && warp == kCutWarp) {
         uint32_t phases = 0, n = 0;
         while (ok && walk.next(t)) {
@@ -659,52 +710,52 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
             n = (n + t.steps) % stages;
             if (!left) continue;
             const uint32_t s = n ? n - 1 : stages - 1;
-            if (!(ok = bar_wait(&S.landed[s], phases >> s & 1, S))) break;
+            if (!(ok = warp_wait(&S.landed[s], phases >> s & 1, S))) break;
             phases ^= 1u << s;
             char *const at = ring + s * kStageBytes;
             for (int i = left * 8 + lane; i < kStep * 8; i += 32)  // 16-byte units of a block's lines
 #pragma unroll
-                for (int b = 0; b < 4; ++b) *reinterpret_cast<uint4 *>(at + b * (kOperandBytes / 2) + i * 16) = make_uint4(0, 0, 0, 0);
+                for (int b = COPY_A ? 0 : 2; b < (COPY_B ? 4 : 2); ++b) *reinterpret_cast<uint4 *>(at + b * (kOperandBytes / 2) + i * 16) = make_uint4(0, 0, 0, 0);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (!lane) bar_arrive<PAIR>(&S.full[s]);
+            if (!lane) bar_arrive(&S.full[s]);
+            __syncwarp();
         }
-    } else if (!COPY && warp >= kFirstEnd + kEnds) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
-        const int w = (warp - kFirstEnd - kEnds) % (kLoadWarps / 2);
-        const bool second = warp - kFirstEnd - kEnds >= kLoadWarps / 2;
+    } else if (COPY != 3 && warp >= kFirstLoad) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        constexpr int kShare = (COPY ? 1 : 2) * kLines / kLoadWarps;  // lines of a warp, of one operand or of both
+        const int w = warp - kFirstLoad, from = w * kShare % kLines;
+        const bool second = COPY ? COPY_A : w * kShare >= kLines;
         while (ok && walk.next(t)) {
             const uint16_t *b = static_cast<const uint16_t *>(A.b) + (KIND != kOuter ? t.group * A.b_group : 0);
             for (int k = 0; k < t.steps; ++k, p.next(stages)) {
-                if (!(ok = bar_wait(&S.empty[p.s], p.phase ^ 1, S))) break;
+                if (!(ok = warp_wait(&S.empty[p.s], p.phase ^ 1, S))) break;
                 char *to = ring + p.s * kStageBytes;
                 const int64_t s0 = (KIND == kOuter ? t.r0 : 0) + int64_t(t.k0 + k) * kStep, s_end = KIND == kOuter ? t.r1 : A.inner;
                 if (!second)
-                    load_lines<A_MAJOR>(static_cast<const uint16_t *>(A.a), A.lda, t.m0 + rank * kLines, KIND == kOuter ? A.inner : t.r1, s0, s_end, to, w, lane);
+                    load_lines<A_MAJOR>(static_cast<const uint16_t *>(A.a), A.lda, t.m0 + rank * kLines, KIND == kOuter ? A.inner : t.r1, s0, s_end, to, from, kShare, lane);
                 else
-                    load_lines<B_MAJOR>(b, A.ldb, t.n0 + rank * kLines, A.cols, s0, s_end, to + kOperandBytes, w, lane);
+                    load_lines<B_MAJOR>(b, A.ldb, t.n0 + rank * kLines, A.cols, s0, s_end, to + kOperandBytes, from, kShare, lane);
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (!lane) bar_arrive<PAIR>(&S.full[p.s]);
+                if (!lane) bar_arrive(&S.full[p.s]);
             }
         }
     } else if (warp == kMulWarp && !rank) {
-        if (!lane) {
-            Place h;  // of the two halves of tensor memory
-            bool some = false;
-            while (ok && walk.next(t)) {
-                if (!t.steps) continue;
+        Place h;  // of the two halves of tensor memory
+        bool some = false;
+        while (ok && walk.next(t)) {
+            if (!lane && t.steps) {
                 uint32_t to = 0;
                 for (int k = 0, in = 0; k < t.steps; ++k, ++in) {
                     if (in == A.chunk) {
-                        commit<PAIR>(&S.sums[h.s]);
+                        commit(&S.sums[h.s]);
                         h.next(2);
                         in = 0;
                     }
                     if (in == 0) {
                         if (!(ok = bar_wait(&S.freed[h.s], h.phase ^ 1, S))) break;
-                        after_sync();
-                        to = acc + h.s * kT;
+                        to = acc + h.s * kTile;
                     }
                     if (!(ok = bar_wait(&S.full[p.s], p.phase, S))) break;
                     after_sync();
@@ -712,60 +763,50 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
                     const uint64_t a = operand<A_MAJOR>(at), b = operand<B_MAJOR>(at + kOperandBytes);
 #pragma unroll
                     for (int i = 0; i < kStep / 16; ++i)
-                        multiply<PAIR>(to, a + i * kNext16<A_MAJOR>, b + i * kNext16<B_MAJOR>, kInstruction<A_MAJOR, B_MAJOR, PAIR>, in | i);
-                    commit<PAIR>(&S.empty[p.s]);
+                        multiply(to, a + i * kNext16<A_MAJOR>, b + i * kNext16<B_MAJOR>, kInstruction<A_MAJOR, B_MAJOR>, in | i);
+                    commit(&S.empty[p.s]);
                     p.next(stages);
                     some = true;
                 }
-                if (ok) commit<PAIR>(&S.sums[h.s]);
+                if (ok) commit(&S.sums[h.s]);
                 h.next(2);
             }
-            // what was issued ends before the tensor memory is given back
-            if (!ok && some) drain(&S.empty[p.s ? p.s - 1 : stages - 1], p.s ? p.phase : p.phase ^ 1);
+            ok = __shfl_sync(kFullMask, ok, 0);
         }
-    } else if (warp >= kFirstEnd && warp < kFirstEnd + kEnds) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(COPY ? 224 : 216));
+        // what was issued ends before the tensor memory is given back
+        if (!ok && some) drain(&S.empty[p.s ? p.s - 1 : stages - 1], p.s ? p.phase : p.phase ^ 1);
+    } else if (warp >= kFirstEnd && warp < kFirstLoad) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(COPY == 3 ? 224 : 192));
         const int q = warp % 4, col0 = (warp - kFirstEnd) / 4 * kEndCols;
         char *const buffer = out_at + (warp - kFirstEnd) * kOutBytes;
-        Place h;
+        Sums sums{S, {}, acc + col0 + (uint32_t(q * 32) << 16)};
         const float peak = END == kLoss ? 1.f : peak_of(A.peaks);
         while (ok && walk.next(t)) {
             if (!t.steps && KIND == kOuter && A.base == A.out) continue;
-            ok = end_tile<KIND, END, kEndCols>(A, map_out, buffer, t, peak, rank * kLines + q * 32, col0, [&](auto &&see) {
-                if (!bar_wait(&S.sums[h.s], h.phase, S)) return false;
-                after_sync();
-                see(acc + h.s * kT + col0 + (uint32_t(q * 32) << 16));
-                before_sync();
-                __syncwarp();
-                if (!lane) bar_arrive<PAIR>(&S.freed[h.s]);
-                h.next(2);
-                return true;
-            });
+            ok = end_tile<KIND, END, kEndCols>(A, buffer, t, peak, rank * kLines + q * 32, col0, sums);
         }
-        if (KIND != kOuter && END == kStore && A.offsets) clear_rows<kEnds>(A, S, warp - kFirstEnd, lane);
-        if (!lane) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        if (KIND != kOuter && END == kStore && A.offsets) clear_rows(A, S, warp - kFirstEnd, lane);
     }
     before_sync();
     __syncwarp();
-    if (PAIR == 2) pair_sync(); else __syncthreads();
-    if (warp == kMemWarp) give_tensor_memory<PAIR>(acc);
+    pair_sync();
+    if (warp == kMemWarp) give_tensor_memory(acc);
 }
 
 // out = base + scale * (the sum, in order, of a tile's shares), four columns to a thread.
 constexpr int kSumThreads = 256;
 
-template <int TILE>
 __global__ void __launch_bounds__(kSumThreads) k_sum(const ProductArgs A, const int32_t splits, const int64_t height) {
     wait_launch_before();
     const float scale = A.scale * peak_of(A.peaks);
-    const int64_t mt = (height + TILE - 1) / TILE, nt = (A.cols + TILE - 1) / TILE, fours = (A.cols + 3) / 4;
+    const int64_t mt = (height + kTile - 1) / kTile, nt = (A.cols + kTile - 1) / kTile, fours = (A.cols + 3) / 4;
     for (int64_t i = blockIdx.x * int64_t(kSumThreads) + threadIdx.x; i < A.groups * height * fours; i += int64_t(gridDim.x) * kSumThreads) {
         const int64_t c = i % fours * 4, r = i / fours % height, g = i / fours / height;
-        const float4 *p = reinterpret_cast<const float4 *>(A.parts + ((g * mt + r / TILE) * nt + c / TILE) * splits * (TILE * TILE) + r % TILE * TILE + c % TILE);
+        const float4 *p = reinterpret_cast<const float4 *>(A.parts + ((g * mt + r / kTile) * nt + c / kTile) * splits * (kTile * kTile) + r % kTile * kTile + c % kTile);
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
         for (int s = 0; s < splits; ++s) {
-            const float4 y = p[s * (TILE * TILE / 4)];
+            const float4 y = p[s * (kTile * kTile / 4)];
             x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
         }
         const int64_t at = g * A.o_group + r * A.ldo + c;
@@ -801,50 +842,47 @@ Encode encoder() {
 }
 
 // Lines of `x` elements, `ld` apart, y of them in a group and z groups; boxes of `lines` lines of 128 bytes.
-bool map_of(CUtensorMap *m, const void *p, bool f32, int64_t x, int64_t ld, int64_t y, int64_t group, int64_t z, uint32_t lines) {
-    const int es = f32 ? 4 : 2;
-    const cuuint64_t dims[3] = {cuuint64_t(x), cuuint64_t(y), cuuint64_t(z)}, strides[2] = {cuuint64_t(ld) * es, cuuint64_t(z > 1 ? group : ld) * es};
-    const cuuint32_t box[3] = {cuuint32_t(128 / es), lines, 1}, step[3] = {1, 1, 1};
+bool map_of(CUtensorMap *m, const void *p, int64_t x, int64_t ld, int64_t y, int64_t group, int64_t z, uint32_t lines) {
+    const cuuint64_t dims[3] = {cuuint64_t(x), cuuint64_t(y), cuuint64_t(z)}, strides[2] = {cuuint64_t(ld) * 2, cuuint64_t(z > 1 ? group : ld) * 2};
+    const cuuint32_t box[3] = {64, lines, 1}, step[3] = {1, 1, 1};
     const Encode f = encoder();
-    return f && f(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(p), dims, strides, box, step,
+    return f && f(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(p), dims, strides, box, step,
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // Whether tensor copies can move a matrix: lines on 16-byte boundaries, strides that their maps hold.
-bool copies(const void *p, bool f32, int64_t ld, int64_t group, int64_t groups) {
-    const int64_t unit = f32 ? 4 : 8;
-    return ((uintptr_t)p & 15) == 0 && ld % unit == 0 && (groups == 1 || (group % unit == 0 && group < int64_t(1) << 37));
+bool copies(const void *p, int64_t ld, int64_t group, int64_t groups) {
+    return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && (groups == 1 || (group % 8 == 0 && group < int64_t(1) << 38));
 }
 
-template <int KIND, int END, bool COPY, int PAIR>
-cudaError_t launch_of(const ProductArgs &A, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, cudaStream_t s) {
-    constexpr auto k = k_product<KIND, END, COPY, PAIR>;
+template <int KIND, int END, int COPY>
+cudaError_t launch_of(const ProductArgs &A, const CUtensorMap &a, const CUtensorMap &b, cudaStream_t s) {
+    constexpr auto k = k_product<KIND, END, COPY>;
     const cudaError_t e = ops_allow_smem<k>(int(kMaxSharedBytes));
     if (e != cudaSuccess) return e;
     uint32_t stages = kStages;
-    while (shared_bytes(stages, kEndWarps<COPY>, A.groups) > kMaxSharedBytes) --stages;
-    constexpr int kT = kTile<PAIR>;
-    const int64_t nt = (A.cols + kT - 1) / kT;
-    const int64_t most = (KIND == kOuter ? int64_t((A.inner + kT - 1) / kT) * A.groups : A.rows / kT + A.groups) * nt * A.splits;
-    const int64_t pairs = sms() / PAIR;
+    while (shared_bytes(stages, A.groups) > kMaxSharedBytes) --stages;
+    const int64_t nt = (A.cols + kTile - 1) / kTile;
+    const int64_t most = (KIND == kOuter ? int64_t((A.inner + kTile - 1) / kTile) * A.groups : A.rows / kTile + A.groups) * nt * A.splits;
+    if (most > INT32_MAX) return cudaErrorInvalidValue;
+    const int64_t pairs = sms() / 2;
     cudaLaunchAttribute at{};
     at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = PAIR;
+    at.val.clusterDim.x = 2;
     at.val.clusterDim.y = at.val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(uint32_t(most < pairs ? most : pairs) * PAIR);
+    cfg.gridDim = dim3(uint32_t(most < pairs ? most : pairs) * 2);
     cfg.blockDim = dim3(kThreads<COPY>);
-    cfg.dynamicSmemBytes = shared_bytes(stages, kEndWarps<COPY>, A.groups);
+    cfg.dynamicSmemBytes = shared_bytes(stages, A.groups);
     cfg.stream = s;
     cfg.attrs = &at;
-    cfg.numAttrs = PAIR > 1 ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, k, a, b, out, A, stages);
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, k, a, b, A, stages);
 }
 
 // Steps between two additions outside of the tensor cores: 512 products (an error of 5e-7 of the result); 1024 (9e-7) for logits, of which an epilogue makes more
-// (at 4096 columns 597 us a 8192 x 16384 table, 619 with 512, 574 with all of them); 8192 (8e-6) where bf16 is made of it.
+// (at 4096 columns 597 us for 8192 x 16384 of them, 619 with 512, 574 with all); 8192 (8e-6) where bf16 is made of it.
 constexpr int kChunk32 = 512 / kStep, kChunkLoss = 1024 / kStep, kChunk16 = 8192 / kStep;
-
 
 constexpr int kMostWaves = 4;  // of shares: what their sums' memory is sized for
 
@@ -861,51 +899,48 @@ int shares_of(int64_t tiles, int64_t steps, int64_t pairs) {
     return best;
 }
 
-template <int KIND, int END, bool COPY, int PAIR>
-cudaError_t launch_split(ProductArgs A, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, cudaStream_t s) {
-    constexpr int kT = kTile<PAIR>;
-    const int64_t height = KIND == kOuter ? A.inner : A.rows, mt = (height + kT - 1) / kT, nt = (A.cols + kT - 1) / kT, tiles = mt * nt * A.groups;
+template <int KIND, int END, int COPY>
+cudaError_t launch_split(ProductArgs A, const CUtensorMap &a, const CUtensorMap &b, cudaStream_t s) {
+    const int64_t height = KIND == kOuter ? A.inner : A.rows, mt = (height + kTile - 1) / kTile, nt = (A.cols + kTile - 1) / kTile, tiles = mt * nt * A.groups;
     const int64_t steps = KIND == kOuter ? (A.rows + int64_t(kStep) * A.groups - 1) / (int64_t(kStep) * A.groups) : (A.inner + kStep - 1) / kStep;
-    const int shares = END == kStore && A.parts && (KIND == kOuter || !A.offsets) ? shares_of(tiles, steps, sms() / PAIR) : 1;
-    CUtensorMap to{};
-    if (shares == 1 || !map_of(&to, A.parts, true, kT, kT, kT, kT * kT, tiles * shares, 32)) return launch_of<KIND, END, COPY, PAIR>(A, a, b, out, s);
+    const int shares = END == kStore && A.parts && (KIND == kOuter || !A.offsets) ? shares_of(tiles, steps, sms() / 2) : 1;
+    if (shares == 1) return launch_of<KIND, END, COPY>(A, a, b, s);
     ProductArgs P = A;
     P.splits = shares;
     P.out = A.parts;
     P.base = nullptr;
     P.peaks = nullptr;
     P.scale = 1.f;
-    P.flags = (A.flags & ~uint32_t(kBase32)) | kOut32 | kOutCopy;
+    P.flags = kOut32 | kOutVec;
     P.chunk = kChunk32;
-    const cudaError_t e = launch_of<KIND, END, COPY, PAIR>(P, a, b, to, s);
+    const cudaError_t e = launch_of<KIND, END, COPY>(P, a, b, s);
     if (e != cudaSuccess) return e;
     const int64_t blocks = (A.groups * height * ((A.cols + 3) / 4) + kSumThreads - 1) / kSumThreads;
-    return ops_launch(true, k_sum<kT>, uint32_t(blocks < sms() * 8 ? blocks : sms() * 8), kSumThreads, 0, s, A, shares, height);
+    return ops_launch(true, k_sum, uint32_t(blocks < sms() * 8 ? blocks : sms() * 8), kSumThreads, 0, s, A, shares, height);
 }
 
 template <int KIND, int END>
 cudaError_t launch(ProductArgs A, cudaStream_t s) {
-    CUtensorMap a{}, b{}, out{};
+    CUtensorMap a{}, b{};
     A.splits = 1;
     A.chunk = END == kLoss ? kChunkLoss : END == kStore && A.flags & kOut32 ? kChunk32 : kChunk16;
     constexpr bool A_MAJOR = KIND != kOuter, B_MAJOR = KIND == kByCols;
-    const bool outer = KIND == kOuter, o32 = A.flags & kOut32;
-    const int64_t groups = outer ? 1 : A.groups, o_groups = outer ? A.groups : 1;
-    if (END != kLoss && copies(A.out, o32, A.ldo, A.o_group, o_groups) &&
-        map_of(&out, A.out, o32, A.cols, A.ldo, outer ? A.inner : A.rows, A.o_group, o_groups, 32))
-        A.flags |= kOutCopy;
-    if (A.rows && copies(A.a, false, A.lda, 0, 1) && copies(A.b, false, A.ldb, A.b_group, groups) &&
-        map_of(&a, A.a, false, A.inner, A.lda, A.rows, 0, 1, A_MAJOR ? kLines : kStep) &&
-        map_of(&b, A.b, false, B_MAJOR ? A.inner : A.cols, A.ldb, B_MAJOR ? A.cols : outer ? A.rows : A.inner, A.b_group, groups, B_MAJOR ? kLines : kStep))
-        return launch_split<KIND, END, true, 2>(A, a, b, out, s);
-    return launch_split<KIND, END, false, 1>(A, a, b, out, s);
+    const bool outer = KIND == kOuter;
+    const int64_t groups = outer ? 1 : A.groups;
+    const bool copy_a = A.rows && copies(A.a, A.lda, 0, 1) && map_of(&a, A.a, A.inner, A.lda, A.rows, 0, 1, A_MAJOR ? kLines : kStep);
+    const bool copy_b = A.rows && copies(A.b, A.ldb, A.b_group, groups) &&
+                        map_of(&b, A.b, B_MAJOR ? A.inner : A.cols, A.ldb, B_MAJOR ? A.cols : outer ? A.rows : A.inner, A.b_group, groups, B_MAJOR ? kLines : kStep);
+    if (copy_a && copy_b) return launch_split<KIND, END, 3>(A, a, b, s);
+    if (copy_a) return launch_split<KIND, END, kCopyA>(A, a, b, s);
+    if (copy_b) return launch_split<KIND, END, kCopyB>(A, a, b, s);
+    return launch_split<KIND, END, 0>(A, a, b, s);
 }
 
 }  // namespace
 
 int32_t product_loss_columns() { return kPart; }
 
-size_t product_parts_bytes() { return size_t(kMostWaves) * (sms() / 2) * kTile<2> * kTile<2> * 4; }
+size_t product_parts_bytes() { return size_t(kMostWaves) * (sms() / 2) * kTile * kTile * 4; }
 
 cudaError_t product_launch(ProductKind kind, ProductEnd end, const ProductArgs &A, cudaStream_t s) {
     if (end == kLoss) return launch<kByCols, kLoss>(A, s);

@@ -19,7 +19,7 @@ enum ProductKind { kByRows = 0, kByCols = 1, kOuter = 2 };
 //   LOGITS_GRAD : out = (exp(x - lse) - [j is the target]) * dloss / peak, bf16
 enum ProductEnd { kStore = 0, kLoss = 1, kLogitsGrad = 2 };
 
-enum : uint32_t { kOut32 = 1, kBase32 = 2, kOutVec = 4 /* out and base: 16-byte accesses */, kIds64 = 8, kOutCopy = 16 /* set by product_launch */ };
+enum : uint32_t { kOut32 = 1, kBase32 = 2, kOutVec = 4 /* out and base: 16-byte accesses */, kIds64 = 8 };
 
 struct ProductArgs {
     const void *a, *b;          // bf16

@@ -402,6 +402,10 @@ __device__ __forceinline__ float exp2_of(float x) {
     return y;
 }
 
+__device__ __forceinline__ void store16(void *p, uint4 u) {
+    asm volatile("st.global.v4.u32 [%0], {%1,%2,%3,%4};" ::"l"(p), "r"(u.x), "r"(u.y), "r"(u.z), "r"(u.w) : "memory");
+}
+
 // Where 32 rows of a warp go, in elements: of the first row and the matrix's first column, and the rows' distance.
 struct Target {
     int64_t at, ldo;
@@ -421,15 +425,15 @@ __device__ __forceinline__ void put_64(const ProductArgs &A, char *buffer, const
                                                                                              pack_bf16(y[4] * scale, y[5] * scale), pack_bf16(y[6] * scale, y[7] * scale));
     }
     __syncwarp();
+    uint4 y[8];  // (all read before the first is stored: for the compiler a store might write what the next read reads)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = *reinterpret_cast<const uint4 *>(buffer + (i * 4 + lane / 8) * 128 + (unit ^ ((i * 4 + lane / 8) & 7)) * 16);
+    __syncwarp();
     char *out = static_cast<char *>(A.out) + (to.at + column + lane / 8 * to.ldo) * 2 + unit * 16;
     const int64_t next = to.ldo * 8;
 #pragma unroll
-    for (int i = 0; i < 8; ++i, out += next) {
-        const int r = i * 4 + lane / 8;
-        const uint4 u = *reinterpret_cast<const uint4 *>(buffer + r * 128 + (unit ^ (r & 7)) * 16);
-        if (r < to.rows) *reinterpret_cast<uint4 *>(out) = u;
-    }
-    __syncwarp();
+    for (int i = 0; i < 8; ++i, out += next)
+        if (i * 4 + lane / 8 < to.rows) store16(out, y[i]);
 }
 
 // 32 columns, from `column` on, of which `n` are there: base + scale * x, in any type.
@@ -443,23 +447,29 @@ __device__ __forceinline__ void put_32(const ProductArgs &A, char *buffer, const
     if (A.flags & kOutVec && n >= 32) {  // eight lanes to a row, four columns to a lane
         const int unit = lane % 8;
         const int64_t at = to.at + column + unit * 4;
-#pragma unroll 4
+        float4 y[8], b[8];
+#pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int r = i * 4 + lane / 8;
-            if (r >= to.rows) break;
-            const float4 y = *reinterpret_cast<const float4 *>(buffer + r * 128 + (unit ^ (r & 7)) * 16);
-            const int64_t e = at + r * to.ldo;
-            float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (A.base && b32) {
-                b = *reinterpret_cast<const float4 *>(elem_ptr<true>(A.base, e));
-            } else if (A.base) {
-                const uint2 u = *reinterpret_cast<const uint2 *>(elem_ptr<false>(A.base, e));
-                b = make_float4(bf16_low(u.x), bf16_high(u.x), bf16_low(u.y), bf16_high(u.y));
+            y[i] = *reinterpret_cast<const float4 *>(buffer + r * 128 + (unit ^ (r & 7)) * 16);
+            b[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (!A.base || r >= to.rows) continue;
+            if (b32) {
+                b[i] = *reinterpret_cast<const float4 *>(elem_ptr<true>(A.base, at + r * to.ldo));
+            } else {
+                const uint2 u = *reinterpret_cast<const uint2 *>(elem_ptr<false>(A.base, at + r * to.ldo));
+                b[i] = make_float4(bf16_low(u.x), bf16_high(u.x), bf16_low(u.y), bf16_high(u.y));
             }
-            b = A.base ? make_float4(fmaf(y.x, scale, b.x), fmaf(y.y, scale, b.y), fmaf(y.z, scale, b.z), fmaf(y.w, scale, b.w))
-                       : make_float4(y.x * scale, y.y * scale, y.z * scale, y.w * scale);
-            if (o32) *reinterpret_cast<float4 *>(static_cast<float *>(A.out) + e) = b;
-            else *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(A.out) + e) = make_uint2(pack_bf16(b.x, b.y), pack_bf16(b.z, b.w));
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = i * 4 + lane / 8;
+            const int64_t e = at + r * to.ldo;
+            const float4 z = A.base ? make_float4(fmaf(y[i].x, scale, b[i].x), fmaf(y[i].y, scale, b[i].y), fmaf(y[i].z, scale, b[i].z), fmaf(y[i].w, scale, b[i].w))
+                                    : make_float4(y[i].x * scale, y[i].y * scale, y[i].z * scale, y[i].w * scale);
+            if (r >= to.rows) continue;
+            if (o32) store16(static_cast<float *>(A.out) + e, make_uint4(__float_as_uint(z.x), __float_as_uint(z.y), __float_as_uint(z.z), __float_as_uint(z.w)));
+            else *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(A.out) + e) = make_uint2(pack_bf16(z.x, z.y), pack_bf16(z.z, z.w));
         }
     } else {  // a row at a time, a column to a lane
         const int64_t at = to.at + column + lane;

@@ -32,16 +32,16 @@ int check_ptr(const char *what, const void *p, uintptr_t es, bool needed) {
 // The two products by rows: of `inner` columns each, times one matrix a group, to `cols` columns.
 int by_rows(ProductKind kind, const skew_experts_config_t *c, const void *x, int64_t ld, const void *w, const int32_t *offsets, int64_t rows, void *y, cudaStream_t s) {
     const bool wide = c->flags & SKEW_EXPERTS_ROWS_FP32;
-    const int32_t inner = kind == kByRows ? c->n : c->m, cols = kind == kByRows ? c->m : c->n;
+    const int32_t inner = kind == kGroupRows ? c->n : c->m, cols = kind == kGroupRows ? c->m : c->n;
     int rc;
     if ((rc = check_rows("rows", x, rows, inner, ld)) || (rc = check_ptr("w", w, 2, true)) || (rc = check_ptr("result", y, wide ? 4 : 2, rows > 0))) return rc;
     if (!rows) return SKEW_OK;
     ProductArgs A{};
-    A.a = x;
-    A.b = w;
-    A.lda = ld;
-    A.ldb = c->m;
-    A.b_group = int64_t(c->n) * c->m;
+    A.a = w;
+    A.b = x;
+    A.lda = c->m;
+    A.ldb = ld;
+    A.a_group = int64_t(c->n) * c->m;
     A.offsets = offsets;
     A.rows = rows;
     A.groups = c->experts;
@@ -63,13 +63,13 @@ extern "C" {
 
 int skew_experts_product(const skew_experts_config_t *c, const void *x, int64_t ld_x, const void *w, const int32_t *offsets, int64_t rows, void *y, void *stream) {
     const int rc = check(c, rows, offsets);
-    return rc ? rc : by_rows(kByRows, c, x, ld_x, w, offsets, rows, y, (cudaStream_t)stream);
+    return rc ? rc : by_rows(kGroupRows, c, x, ld_x, w, offsets, rows, y, (cudaStream_t)stream);
 }
 
 int skew_experts_grad_rows(const skew_experts_config_t *c, const void *dy, int64_t ld_dy, const void *w, const int32_t *offsets, int64_t rows, void *dx,
                            void *stream) {
     const int rc = check(c, rows, offsets);
-    return rc ? rc : by_rows(kByCols, c, dy, ld_dy, w, offsets, rows, dx, (cudaStream_t)stream);
+    return rc ? rc : by_rows(kGroupCols, c, dy, ld_dy, w, offsets, rows, dx, (cudaStream_t)stream);
 }
 
 size_t skew_experts_workspace_bytes(const skew_experts_config_t *c) { return check(c, 0, (const int32_t *)4) == SKEW_OK ? (product_parts_bytes() + 255) / 256 * 256 : 0; }

@@ -76,6 +76,7 @@ struct TidyArgs {
 
 __global__ void __launch_bounds__(kTidyThreads) k_tidy(const TidyArgs A) {
     __shared__ float of_warp[kTidyThreads / 32];
+    release_launch_after();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     float peak = 0.f;
     for (int64_t t = blockIdx.x * int64_t(kTidyThreads / 32) + warp; t < A.tokens; t += int64_t(gridDim.x) * (kTidyThreads / 32)) {
@@ -192,7 +193,7 @@ int skew_head_loss(const skew_head_config_t *c, const void *h, int64_t ld_h, con
     A.inner = (int32_t)c->width;
     A.cols = (int32_t)c->rows;
     A.scale = c->scale;
-    A.flags = wide ? kIds64 : 0;
+    A.flags = (wide ? kIds64 : 0) | kRelease;
     A.targets = targets;
     A.vocab = c->rows;
     A.part = (float2 *)ws;
@@ -241,7 +242,7 @@ int skew_head_grad(const skew_head_config_t *c, const void *h, int64_t ld_h, con
             P.inner = width;
             P.cols = (int32_t)n;
             P.scale = c->scale;
-            P.flags = (wide ? kIds64 : 0) | kOutVec;
+            P.flags = (wide ? kIds64 : 0) | kOutVec | kAfter | kRelease;
             P.targets = targets;
             P.first = v0;
             P.vocab = c->rows;
@@ -265,7 +266,7 @@ int skew_head_grad(const skew_head_config_t *c, const void *h, int64_t ld_h, con
             H.base = first ? nullptr : ws + L.sums;
             H.out = last ? dh : ws + L.sums;
             H.ldo = c->width;
-            H.flags = kBase32 | (last ? 0 : kOut32) | (units(c->width, H.out) ? kOutVec : 0);
+            H.flags = kBase32 | (last ? 0 : kOut32) | (units(c->width, H.out) ? kOutVec : 0) | kAfter | kRelease;
             if ((rc = ops_cuda(product_launch(kByRows, kStore, H, s), "k_product"))) return rc;
         }
         ProductArgs W{};  // its rows of dW
@@ -283,7 +284,7 @@ int skew_head_grad(const skew_head_config_t *c, const void *h, int64_t ld_h, con
         W.base = base ? (const uint16_t *)base + v0 * c->width : nullptr;
         W.out = (uint16_t *)dtable + v0 * c->width;
         W.ldo = c->width;
-        W.flags = units(c->width, W.out) && units(c->width, base) ? kOutVec : 0;
+        W.flags = (units(c->width, W.out) && units(c->width, base) ? kOutVec : 0) | (tokens ? uint32_t(kAfter) | (last ? 0u : uint32_t(kRelease)) : 0u);
         if ((rc = ops_cuda(product_launch(kOuter, kStore, W, s), "k_product"))) return rc;
     }
     return SKEW_OK;

@@ -33,6 +33,16 @@ constexpr int kTile = 256;                     // rows and columns of a tile, wh
 constexpr int kMulWarp = 0, kMemWarp = 1, kCopyWarp = 2, kCutWarp = 3, kFirstEnd = 4;  // of the warps from 4 on, each reads lanes 32 (warp % 4) on of tensor memory
 constexpr int kEndWarps = 8, kEndCols = kTile * 4 / kEndWarps, kFirstLoad = kFirstEnd + kEndWarps, kLoadWarps = 4;
 
+// How an operand lies in its lines: along the summed index, or across it.
+template <int KIND>
+constexpr bool kMajorA = KIND != kOuter && KIND != kGroupRows;
+template <int KIND>
+constexpr bool kMajorB = KIND != kOuter && KIND != kByRows;
+// The tile's rows are the matrices' columns, and its columns the group's rows.
+template <int KIND>
+constexpr bool kTurned = KIND == kGroupRows || KIND == kGroupCols;
+constexpr int kRowBox = 32;                    // lines of a copy of a group's rows where they do not fill a tile (one of 128 is 8 % quicker where they do)
+
 // COPY: the operands (1: A, 2: B) whose stages come by tensor copies, which one thread asks for. Four more warps load the others.
 constexpr int kCopyA = 1, kCopyB = 2;
 template <int COPY>
@@ -133,6 +143,8 @@ struct Tile {
     int32_t k0, steps;            // of the summed index: the first, and how many
     int32_t unit;                 // of the tile and its share of the summed index, where that is split
     bool ends;                    // the share's last step is the group's
+    // GROUP: columns of the tile, which the products take 64 at a time
+    __device__ __forceinline__ int width() const { return min(kTile, (r1 - m0 + 63) / 64 * 64); }
 };
 
 __device__ __forceinline__ int32_t *tiles_of(const ProductArgs &A, Shared &S) { return S.begin + A.groups + 1; }
@@ -348,7 +360,7 @@ constexpr uint32_t kNext16 = (MAJOR ? 32 : 16 * 128) >> 4;
 
 template <bool A_MAJOR, bool B_MAJOR>
 constexpr uint32_t kInstruction = 1u << 4 /* sums fp32 */ | 1u << 7 | 1u << 10 /* bf16 */ | uint32_t(!A_MAJOR) << 15 | uint32_t(!B_MAJOR) << 16 |
-                                  uint32_t(kTile >> 3) << 17 | uint32_t(kTile >> 4) << 24;
+                                  uint32_t(kTile >> 4) << 24;  // and the tile's columns >> 3 at bit 17
 
 // 16 steps of a tile: each CTA of the pair holds half of A's rows and of B's columns, and gets the sums of its rows.
 __device__ __forceinline__ void multiply(uint32_t acc, uint64_t a, uint64_t b, uint32_t instruction, bool add) {
@@ -643,6 +655,66 @@ __device__ __forceinline__ bool end_tile(const ProductArgs &A, char *buffer, con
     return true;
 }
 
+// The same for a turned tile: a lane has a column of the matrices, and 32 of the tile's columns are 32 rows, so that a store of the warp is 64 or 128 bytes of a row,
+// wherever it starts. `which`: of the two warps that have these lanes; they take every other 32 rows.
+template <int KIND>
+__device__ __forceinline__ bool end_turned(const ProductArgs &A, const Tile &t, int row0, int which, Sums &sums) {
+    const int column = t.n0 + row0 + (threadIdx.x & 31), width = t.width();
+    const bool mine = column < A.cols, several = t.steps > A.chunk;
+    float run[kTile / 64][32];
+    if (several) {
+#pragma unroll
+        for (int c = 0; c < kTile / 64; ++c)
+#pragma unroll
+            for (int i = 0; i < 32; ++i) run[c][i] = 0.f;
+#pragma unroll 1
+        for (int k = 0; k < t.steps; k += A.chunk) {
+            uint32_t acc;
+            if (!sums.wait(acc)) return false;
+#pragma unroll
+            for (int c = 0; c < kTile / 64; ++c) {
+                if (c * 64 >= width) break;
+                float x[32];
+                read_sums(acc + (2 * c + which) * 32, x);
+                sums_read(x);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) run[c][i] += x[i];
+            }
+            sums.free();
+        }
+    }
+    uint32_t acc = 0;
+    if (!several && !sums.wait(acc)) return false;
+#pragma unroll 1
+    for (int c = 0; c < width; c += 64) {
+        float x[32];
+        if (!several) {
+            read_sums(acc + c + which * 32, x);
+            sums_read(x);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+#pragma unroll
+                for (int j = 0; j < kTile / 64; ++j) x[i] = c == 64 * j ? run[j][i] : x[i];
+        }
+        const int first = t.m0 + c + which * 32, rows = t.r1 - first;
+        if (!mine || rows <= 0) continue;
+        if (A.flags & kOut32) {
+            float *out = static_cast<float *>(A.out) + first * A.ldo + column;
+#pragma unroll
+            for (int i = 0; i < 32; ++i, out += A.ldo)
+                if (i < rows) *out = x[i];
+        } else {
+            uint16_t *out = static_cast<uint16_t *>(A.out) + first * A.ldo + column;
+#pragma unroll
+            for (int i = 0; i < 32; ++i, out += A.ldo)
+                if (i < rows) *out = uint16_t(pack_bf16(x[i], x[i]));
+        }
+    }
+    if (!several) sums.free();
+    return true;
+}
+
 // Rows of no group are zeros.
 __device__ __forceinline__ void clear_rows(const ProductArgs &A, const Shared &S, int warp, int lane) {
     const int64_t before = S.begin[0], behind = A.rows - S.begin[A.groups];
@@ -664,7 +736,7 @@ __device__ __forceinline__ void clear_rows(const ProductArgs &A, const Shared &S
 
 template <int KIND, int END, int COPY>
 __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                                                               const ProductArgs A, const uint32_t stages) {
+                                                               const __grid_constant__ CUtensorMap map_few, const ProductArgs A, const uint32_t stages) {
     extern __shared__ char raw[];
     constexpr bool COPY_A = COPY & kCopyA, COPY_B = COPY & kCopyB;
     char *const ring = raw + (1024 - (shared_address(raw) & 1023)) % 1024, *const out_at = ring + stages * kStageBytes;
@@ -677,12 +749,14 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kMemWarp) take_tensor_memory(&S.acc);
+    wait_launch_before();
+    if (A.flags & kRelease) release_launch_after();
     groups_of<KIND, kThreads<COPY>>(A, S);
     before_sync();
     pair_sync();
     after_sync();
     const uint32_t acc = S.acc;
-    constexpr bool A_MAJOR = KIND != kOuter, B_MAJOR = KIND == kByCols;
+    constexpr bool A_MAJOR = kMajorA<KIND>, B_MAJOR = kMajorB<KIND>, TURNED = kTurned<KIND>;
     Walk<KIND> walk(A, S);
     Tile t;
     Place p;
@@ -694,18 +768,23 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
         uint32_t n = 0;
         while (ok && walk.next(t)) {
             if (!lane) {
-                const int m0 = t.m0 + rank * kLines, n0 = t.n0 + rank * kLines;
-                // A CTA whose rows all belong to the groups behind needs none of them: its sums are not read.
-                const bool rows = COPY_A && (KIND == kOuter || m0 < t.r1);
+                const int half = TURNED ? t.width() / 2 : kLines;  // lines of B
+                const int m0 = TURNED ? t.n0 + rank * kLines : t.m0 + rank * kLines, n0 = TURNED ? t.m0 + rank * half : t.n0 + rank * kLines;
+                // A CTA that has none of the rows needs nothing of A: its sums are not read.
+                const bool rows = COPY_A && (TURNED || KIND == kOuter || m0 < t.r1);
                 for (int k = 0; k < t.steps; ++k, ++n, p.next(stages)) {
                     const int s0 = (KIND == kOuter ? t.r0 : 0) + (t.k0 + k) * kStep;
                     if (!(ok = bar_wait(&S.empty[p.s], p.phase ^ 1, S))) break;
                     // The last lines of a group that ends within a stage go to the warp that clears what is behind them.
                     const bool cut = KIND == kOuter && s0 + kStep > t.r1;
                     const uint32_t to = shared_address(ring) + p.s * kStageBytes, bar = cut ? shared_address(&S.landed[p.s]) : in_first(&S.full[p.s]);
-                    bar_expect(bar, (rows ? kOperandBytes : 0) + (COPY_B ? kOperandBytes : 0));
-                    if (rows) copy_lines<A_MAJOR>(map_a, to, bar, m0, s0, 0);
-                    if (COPY_B) copy_lines<B_MAJOR>(map_b, to + kOperandBytes, bar, n0, s0, KIND == kOuter ? 0 : t.group);
+                    bar_expect(bar, (rows ? kOperandBytes : 0) + (COPY_B ? half * 128 : 0));
+                    if (rows) copy_lines<A_MAJOR>(map_a, to, bar, m0, s0, TURNED ? t.group : 0);
+                    if (COPY_B && TURNED && half < kLines) {
+                        for (int l = 0; l < half; l += kRowBox) copy_box(map_few, to + kOperandBytes + l * 128, bar, s0, n0 + l, 0);
+                    } else if (COPY_B) {
+                        copy_lines<B_MAJOR>(map_b, to + kOperandBytes, bar, n0, s0, 0);
+                    }
                 }
             }
             ok = __shfl_sync(kFullMask, ok, 0);
@@ -737,15 +816,18 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
         const int w = warp - kFirstLoad, from = w * kShare % kLines;
         const bool second = COPY ? COPY_A : w * kShare >= kLines;
         while (ok && walk.next(t)) {
-            const uint16_t *b = static_cast<const uint16_t *>(A.b) + (KIND != kOuter ? t.group * A.b_group : 0);
+            const uint16_t *const a = static_cast<const uint16_t *>(A.a) + (TURNED ? t.group * A.a_group : 0), *const b = static_cast<const uint16_t *>(A.b);
+            const int half = TURNED ? t.width() / 2 : kLines;
+            const int64_t m0 = (TURNED ? t.n0 : t.m0) + rank * kLines, m_end = TURNED ? A.cols : KIND == kOuter ? A.inner : t.r1;
+            const int64_t n0 = TURNED ? t.m0 + rank * half : t.n0 + rank * kLines, n_end = TURNED ? t.r1 : A.cols;
             for (int k = 0; k < t.steps; ++k, p.next(stages)) {
                 if (!(ok = warp_wait(&S.empty[p.s], p.phase ^ 1, S))) break;
                 char *to = ring + p.s * kStageBytes;
                 const int64_t s0 = (KIND == kOuter ? t.r0 : 0) + int64_t(t.k0 + k) * kStep, s_end = KIND == kOuter ? t.r1 : A.inner;
                 if (!second)
-                    load_lines<A_MAJOR>(static_cast<const uint16_t *>(A.a), A.lda, t.m0 + rank * kLines, KIND == kOuter ? A.inner : t.r1, s0, s_end, to, from, kShare, lane);
+                    load_lines<A_MAJOR>(a, A.lda, m0, m_end, s0, s_end, to, from, kShare, lane);
                 else
-                    load_lines<B_MAJOR>(b, A.ldb, t.n0 + rank * kLines, A.cols, s0, s_end, to + kOperandBytes, from, kShare, lane);
+                    load_lines<B_MAJOR>(b, A.ldb, n0, n_end, s0, s_end, to + kOperandBytes, from, min(kShare, half - from), lane);
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (!lane) bar_arrive(&S.full[p.s]);
@@ -757,6 +839,7 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
         while (ok && walk.next(t)) {
             if (!lane && t.steps) {
                 uint32_t to = 0;
+                const uint32_t instruction = kInstruction<A_MAJOR, B_MAJOR> | uint32_t(TURNED ? t.width() : kTile) >> 3 << 17;
                 for (int k = 0, in = 0; k < t.steps; ++k, ++in) {
                     if (in == A.chunk) {
                         commit(&S.sums[h.s]);
@@ -773,7 +856,7 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
                     const uint64_t a = operand<A_MAJOR>(at), b = operand<B_MAJOR>(at + kOperandBytes);
 #pragma unroll
                     for (int i = 0; i < kStep / 16; ++i)
-                        multiply(to, a + i * kNext16<A_MAJOR>, b + i * kNext16<B_MAJOR>, kInstruction<A_MAJOR, B_MAJOR>, in | i);
+                        multiply(to, a + i * kNext16<A_MAJOR>, b + i * kNext16<B_MAJOR>, instruction, in | i);
                     commit(&S.empty[p.s]);
                     p.next(stages);
                     some = true;
@@ -789,13 +872,16 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(COPY == 3 ? 224 : 192));
         const int q = warp % 4, col0 = (warp - kFirstEnd) / 4 * kEndCols;
         char *const buffer = out_at + (warp - kFirstEnd) * kOutBytes;
-        Sums sums{S, {}, acc + col0 + (uint32_t(q * 32) << 16)};
+        Sums sums{S, {}, acc + (TURNED ? 0 : col0) + (uint32_t(q * 32) << 16)};
         const float peak = END == kLoss ? 1.f : peak_of(A.peaks);
         while (ok && walk.next(t)) {
             if (!t.steps && KIND == kOuter && A.base == A.out) continue;
-            ok = end_tile<KIND, END, kEndCols>(A, buffer, t, peak, rank * kLines + q * 32, col0, sums);
+            if constexpr (TURNED)
+                ok = end_turned<KIND>(A, t, rank * kLines + q * 32, col0 / kEndCols, sums);
+            else
+                ok = end_tile<KIND, END, kEndCols>(A, buffer, t, peak, rank * kLines + q * 32, col0, sums);
         }
-        if (KIND != kOuter && END == kStore && A.offsets) clear_rows(A, S, warp - kFirstEnd, lane);
+        if (TURNED) clear_rows(A, S, warp - kFirstEnd, lane);
     }
     before_sync();
     __syncwarp();
@@ -808,6 +894,7 @@ constexpr int kSumThreads = 256;
 
 __global__ void __launch_bounds__(kSumThreads) k_sum(const ProductArgs A, const int32_t splits, const int64_t height) {
     wait_launch_before();
+    if (A.flags & kRelease) release_launch_after();
     const float scale = A.scale * peak_of(A.peaks);
     const int64_t mt = (height + kTile - 1) / kTile, nt = (A.cols + kTile - 1) / kTile, fours = (A.cols + 3) / 4;
     for (int64_t i = blockIdx.x * int64_t(kSumThreads) + threadIdx.x; i < A.groups * height * fours; i += int64_t(gridDim.x) * kSumThreads) {
@@ -866,7 +953,7 @@ bool copies(const void *p, int64_t ld, int64_t group, int64_t groups) {
 }
 
 template <int KIND, int END, int COPY>
-cudaError_t launch_of(const ProductArgs &A, const CUtensorMap &a, const CUtensorMap &b, cudaStream_t s) {
+cudaError_t launch_of(const ProductArgs &A, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &few, cudaStream_t s) {
     constexpr auto k = k_product<KIND, END, COPY>;
     const cudaError_t e = ops_allow_smem<k>(int(kMaxSharedBytes));
     if (e != cudaSuccess) return e;
@@ -876,18 +963,20 @@ cudaError_t launch_of(const ProductArgs &A, const CUtensorMap &a, const CUtensor
     const int64_t most = (KIND == kOuter ? int64_t((A.inner + kTile - 1) / kTile) * A.groups : A.rows / kTile + A.groups) * nt * A.splits;
     if (most > INT32_MAX) return cudaErrorInvalidValue;
     const int64_t pairs = sms() / 2;
-    cudaLaunchAttribute at{};
-    at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = 2;
-    at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cudaLaunchAttribute at[2] = {};
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = 2;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(uint32_t(most < pairs ? most : pairs) * 2);
     cfg.blockDim = dim3(kThreads<COPY>);
     cfg.dynamicSmemBytes = shared_bytes(stages, A.groups);
     cfg.stream = s;
-    cfg.attrs = &at;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, k, a, b, A, stages);
+    cfg.attrs = at;
+    cfg.numAttrs = A.flags & kAfter ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, k, a, b, few, A, stages);
 }
 
 // Steps between two additions outside of the tensor cores: 512 products (an error of 5e-7 of the result); 1024 (9e-7) for logits, of which an epilogue makes more
@@ -910,20 +999,20 @@ int shares_of(int64_t tiles, int64_t steps, int64_t pairs) {
 }
 
 template <int KIND, int END, int COPY>
-cudaError_t launch_split(ProductArgs A, const CUtensorMap &a, const CUtensorMap &b, cudaStream_t s) {
+cudaError_t launch_split(ProductArgs A, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &few, cudaStream_t s) {
     const int64_t height = KIND == kOuter ? A.inner : A.rows, mt = (height + kTile - 1) / kTile, nt = (A.cols + kTile - 1) / kTile, tiles = mt * nt * A.groups;
     const int64_t steps = KIND == kOuter ? (A.rows + int64_t(kStep) * A.groups - 1) / (int64_t(kStep) * A.groups) : (A.inner + kStep - 1) / kStep;
-    const int shares = END == kStore && A.parts && (KIND == kOuter || !A.offsets) ? shares_of(tiles, steps, sms() / 2) : 1;
-    if (shares == 1) return launch_of<KIND, END, COPY>(A, a, b, s);
+    const int shares = END == kStore && A.parts ? shares_of(tiles, steps, sms() / 2) : 1;
+    if (shares == 1) return launch_of<KIND, END, COPY>(A, a, b, few, s);
     ProductArgs P = A;
     P.splits = shares;
     P.out = A.parts;
     P.base = nullptr;
     P.peaks = nullptr;
     P.scale = 1.f;
-    P.flags = kOut32 | kOutVec;
+    P.flags = kOut32 | kOutVec | kRelease | (A.flags & kAfter);
     P.chunk = kChunk32;
-    const cudaError_t e = launch_of<KIND, END, COPY>(P, a, b, s);
+    const cudaError_t e = launch_of<KIND, END, COPY>(P, a, b, few, s);
     if (e != cudaSuccess) return e;
     const int64_t blocks = (A.groups * height * ((A.cols + 3) / 4) + kSumThreads - 1) / kSumThreads;
     return ops_launch(true, k_sum, uint32_t(blocks < sms() * 8 ? blocks : sms() * 8), kSumThreads, 0, s, A, shares, height);
@@ -931,19 +1020,20 @@ cudaError_t launch_split(ProductArgs A, const CUtensorMap &a, const CUtensorMap 
 
 template <int KIND, int END>
 cudaError_t launch(ProductArgs A, cudaStream_t s) {
-    CUtensorMap a{}, b{};
+    CUtensorMap a{}, b{}, few{};
     A.splits = 1;
     A.chunk = END == kLoss ? kChunkLoss : END == kStore && A.flags & kOut32 ? kChunk32 : kChunk16;
-    constexpr bool A_MAJOR = KIND != kOuter, B_MAJOR = KIND == kByCols;
-    const bool outer = KIND == kOuter;
-    const int64_t groups = outer ? 1 : A.groups;
-    const bool copy_a = A.rows && copies(A.a, A.lda, 0, 1) && map_of(&a, A.a, A.inner, A.lda, A.rows, 0, 1, A_MAJOR ? kLines : kStep);
-    const bool copy_b = A.rows && copies(A.b, A.ldb, A.b_group, groups) &&
-                        map_of(&b, A.b, B_MAJOR ? A.inner : A.cols, A.ldb, B_MAJOR ? A.cols : outer ? A.rows : A.inner, A.b_group, groups, B_MAJOR ? kLines : kStep);
-    if (copy_a && copy_b) return launch_split<KIND, END, 3>(A, a, b, s);
-    if (copy_a) return launch_split<KIND, END, kCopyA>(A, a, b, s);
-    if (copy_b) return launch_split<KIND, END, kCopyB>(A, a, b, s);
-    return launch_split<KIND, END, 0>(A, a, b, s);
+    constexpr bool A_MAJOR = kMajorA<KIND>, B_MAJOR = kMajorB<KIND>, TURNED = kTurned<KIND>, OUTER = KIND == kOuter;
+    // lines of an operand: how long, how many, in how many groups, and in a copy
+    const int64_t long_a = TURNED && !A_MAJOR ? A.cols : A.inner, lines_a = TURNED ? (A_MAJOR ? A.cols : A.inner) : A.rows, groups_a = TURNED ? A.groups : 1;
+    const int64_t long_b = B_MAJOR ? A.inner : A.cols, lines_b = TURNED || OUTER ? A.rows : B_MAJOR ? A.cols : A.inner;
+    const bool copy_a = A.rows && copies(A.a, A.lda, A.a_group, groups_a) && map_of(&a, A.a, long_a, A.lda, lines_a, A.a_group, groups_a, A_MAJOR ? kLines : kStep);
+    const bool copy_b = A.rows && copies(A.b, A.ldb, 0, 1) && map_of(&b, A.b, long_b, A.ldb, lines_b, 0, 1, B_MAJOR ? kLines : kStep) &&
+                        (!TURNED || map_of(&few, A.b, long_b, A.ldb, lines_b, 0, 1, kRowBox));
+    if (copy_a && copy_b) return launch_split<KIND, END, 3>(A, a, b, few, s);
+    if (copy_a) return launch_split<KIND, END, kCopyA>(A, a, b, few, s);
+    if (copy_b) return launch_split<KIND, END, kCopyB>(A, a, b, few, s);
+    return launch_split<KIND, END, 0>(A, a, b, few, s);
 }
 
 }  // namespace
@@ -955,7 +1045,12 @@ size_t product_parts_bytes() { return size_t(kMostWaves) * (sms() / 2) * kTile *
 cudaError_t product_launch(ProductKind kind, ProductEnd end, const ProductArgs &A, cudaStream_t s) {
     if (end == kLoss) return launch<kByCols, kLoss>(A, s);
     if (end == kLogitsGrad) return launch<kByCols, kLogitsGrad>(A, s);
-    return kind == kByRows ? launch<kByRows, kStore>(A, s) : kind == kByCols ? launch<kByCols, kStore>(A, s) : launch<kOuter, kStore>(A, s);
+    switch (kind) {
+        case kByRows: return launch<kByRows, kStore>(A, s);
+        case kGroupRows: return launch<kGroupRows, kStore>(A, s);
+        case kGroupCols: return launch<kGroupCols, kStore>(A, s);
+        default: return launch<kOuter, kStore>(A, s);
+    }
 }
 
 int product_status(cudaStream_t s) {

@@ -8,10 +8,13 @@
 namespace skew {
 
 // What is multiplied. A "line" is a run of memory: 64 contiguous elements of it, at a time, come to shared memory.
-//   BY_ROWS : C[r, j] = sum_k A[r, k] B_e[k, j]     A: lines of k, one for each row r; B: lines of j
-//   BY_COLS : C[r, j] = sum_k A[r, k] B_e[j, k]     A as above;                        B: lines of k
-//   OUTER   : C_e[i, j] = sum_r A[r, i] B[r, j]     A: lines of i, B: lines of j, one for each row r of the group e
-enum ProductKind { kByRows = 0, kByCols = 1, kOuter = 2 };
+//   BY_ROWS    : C[r, j] = sum_k A[r, k] B[k, j]     A: lines of k, one for each row r; B: lines of j    (STORE)
+//   BY_COLS    : C[r, j] = sum_k A[r, k] B[j, k]     A: as above;                       B: lines of k    (LOSS, LOGITS_GRAD)
+//   OUTER      : C_e[i, j] = sum_r A[r, i] B[r, j]   A: lines of i, B: lines of j, one for each row r of the group e
+//   GROUP_ROWS : C[r, j] = sum_k B[r, k] A_e[k, j]   A: lines of j, B: lines of k, one for each row r, of the group e
+//   GROUP_COLS : C[r, j] = sum_k B[r, k] A_e[j, k]   A: lines of k, B: as above
+// The GROUP kinds turn the tile: its 256 rows are columns of the matrix, of which there are always enough, and its columns the group's rows, as few as 64.
+enum ProductKind { kByRows, kByCols, kOuter, kGroupRows, kGroupCols };
 
 // What becomes of a tile of sums.
 //   STORE  : out = base + scale * peak * C
@@ -19,12 +22,14 @@ enum ProductKind { kByRows = 0, kByCols = 1, kOuter = 2 };
 //   LOGITS_GRAD : out = (exp(x - lse) - [j is the target]) * dloss / peak, bf16
 enum ProductEnd { kStore = 0, kLoss = 1, kLogitsGrad = 2 };
 
-enum : uint32_t { kOut32 = 1, kBase32 = 2, kOutVec = 4 /* out and base: 16-byte accesses */, kIds64 = 8 };
+enum : uint32_t { kOut32 = 1, kBase32 = 2, kOutVec = 4 /* out and base: 16-byte accesses */, kIds64 = 8,
+                // a launch of the call goes on after this one, and may start up meanwhile; this one is such a launch
+                kRelease = 16, kAfter = 32 };
 
 struct ProductArgs {
     const void *a, *b;          // bf16
-    int64_t lda, ldb, b_group;  // elements between lines, and between B's groups
-    const int32_t *offsets;     // groups + 1 row numbers on the device; NULL: one group of all rows
+    int64_t lda, ldb, a_group;  // elements between lines, and between A's groups (GROUP)
+    const int32_t *offsets;     // groups + 1 row numbers on the device (GROUP, OUTER); NULL: one group of all rows
     int64_t rows;               // r in [0, rows)
     int32_t groups, cols;       // j in [0, cols)
     int32_t inner;              // k, or OUTER's i, in [0, inner)

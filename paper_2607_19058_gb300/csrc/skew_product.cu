@@ -31,7 +31,7 @@ constexpr int kBandRows = 2048;                // rows of tiles that are walked 
 constexpr int kTile = 256;                     // rows and columns of a tile, which a pair of CTAs shares
 
 constexpr int kMulWarp = 0, kMemWarp = 1, kCopyWarp = 2, kCutWarp = 3, kFirstEnd = 4;  // of the warps from 4 on, each reads lanes 32 (warp % 4) on of tensor memory
-constexpr int kEndWarps = 8, kEndCols = kTile * 4 / kEndWarps, kFirstLoad = kFirstEnd + kEndWarps, kLoadWarps = 4;
+constexpr int kEndWarps = 8, kEndCols = kTile * 4 / kEndWarps, kFirstLoad = kFirstEnd + kEndWarps, kLoadWarps = 8;
 
 // How an operand lies in its lines: along the summed index, or across it.
 template <int KIND>
@@ -43,7 +43,7 @@ template <int KIND>
 constexpr bool kTurned = KIND == kGroupRows || KIND == kGroupCols;
 constexpr int kRowBox = 32;                    // lines of a copy of a group's rows where they do not fill a tile (one of 128 is 8 % quicker where they do)
 
-// COPY: the operands (1: A, 2: B) whose stages come by tensor copies, which one thread asks for. Four more warps load the others.
+// COPY: the operands (1: A, 2: B) whose stages come by tensor copies, which one thread asks for. Eight more warps load the others.
 constexpr int kCopyA = 1, kCopyB = 2;
 template <int COPY>
 constexpr int kThreads = 32 * (kFirstLoad + (COPY == 3 ? 0 : kLoadWarps));
@@ -58,11 +58,20 @@ struct Shared {
 };
 
 constexpr int kOutBytes = 32 * 128;            // 32 rows of 128 bytes, of each warp that writes out
+constexpr int kRawLine = 144;                  // a line of 64 elements that starts anywhere, by 16-byte units
 constexpr size_t kMaxSharedBytes = 232448;
-constexpr size_t shared_bytes(int stages, int groups) {
-    return 1024 + size_t(stages) * kStageBytes + size_t(kEndWarps) * kOutBytes + sizeof(Shared) + size_t(groups + 1) * 8;
+constexpr size_t shared_bytes(int stages, size_t raw, int groups) {
+    return 1024 + size_t(stages) * kStageBytes + raw + size_t(kEndWarps) * kOutBytes + sizeof(Shared) + size_t(groups + 1) * 8;
 }
-static_assert(shared_bytes(kStages - 1, kMaxGroups) <= kMaxSharedBytes, "shared memory of a CTA");
+// Stages that loaded lines are on their way for, and the stages of the ring beside them.
+template <int COPY>
+constexpr int kRawStages = COPY ? 4 : 3;
+template <int COPY>
+constexpr int kRing = COPY == 3 ? kStages : COPY ? 3 : 2;
+template <int COPY>
+constexpr size_t kRawBytes = COPY == 3 ? 0 : size_t(kRawStages<COPY>) * (COPY ? 1 : 2) * kLines * kRawLine;
+static_assert(shared_bytes(kStages - 1, 0, kMaxGroups) <= kMaxSharedBytes && shared_bytes(kRing<1>, kRawBytes<1>, kMaxGroups) <= kMaxSharedBytes &&
+              shared_bytes(kRing<0>, kRawBytes<0>, kMaxGroups) <= kMaxSharedBytes, "shared memory of a CTA");
 
 // A place in the ring of stages, and how often it was there before (odd or even).
 struct Place {
@@ -262,70 +271,84 @@ struct Walk {
 // ---------------------------------------------------------------------------
 // Loads
 // ---------------------------------------------------------------------------
-// Eight elements from `p` on, of which `n` are there, wherever they start: by the one or two 16-byte units that hold them. (A unit is read only where it holds an
-// element that is there, so that no access leaves the units of the matrix itself.)
-struct Eight {
-    uint4 a, b;
-    __device__ __forceinline__ void ask(const uint16_t *p, int n) {
-        const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(p)) & 15;
-        const uint4 *q = reinterpret_cast<const uint4 *>(reinterpret_cast<uintptr_t>(p) - off);
-        a = b = make_uint4(0, 0, 0, 0);
-        if (n > 0) a = __ldg(q);
-        if (n > int(16 - off) / 2) b = __ldg(q + 1);
+// Lines that start off a 16-byte boundary, or lie an odd number of elements apart, come as the 16-byte units that hold them, by asynchronous copies, to memory of the
+// warp's own (144 bytes a line), a few stages ahead; from there each unit of a stage is cut out of two of those. (A unit is read only where it holds an element
+// that is there, so that no access leaves the units of the matrix itself.)
+constexpr int kLooseLines = (2 * kLines) / kLoadWarps;  // of a warp, of one operand, where both are loaded; half of that of each operand's lines where one is
+
+// A warp's `N` of an operand's 128 lines of a tile's stages, from line `from` on, eight lanes to a line. MAJOR: lines along the summed index, numbered l0 on, of which
+// those before l_end are there; a stage is 64 elements, from s0 on, before s_end. Else two blocks of 64 lines, one for each step of the summed index (s0 on, before
+// s_end), of elements from l0 (and l0 + 64), before l_end; a stage is 64 lines.
+template <bool MAJOR, int N>
+struct Loose {
+    const char *at;         // the lane's first line, in this stage
+    int64_t four, stage;    // bytes from a line to the lane's next, and to the next stage
+    int lines, n;           // that are there from the lane's first line on, and elements of a line
+    int left;               // of the summed index
+
+    __device__ __forceinline__ Loose(const uint16_t *p, int64_t ld, int64_t l0, int64_t l_end, int64_t s0, int64_t s_end, int from, int lane) {
+        const int64_t mine = from % (MAJOR ? kLines : 64) + lane / 8, elem = MAJOR ? s0 : l0 + from / 64 * 64;
+        at = reinterpret_cast<const char *>(p + ((MAJOR ? l0 : s0) + mine) * ld + elem);
+        four = ld * 8;
+        stage = MAJOR ? 128 : ld * 128;
+        left = int(min(max(s_end - s0, int64_t(0)), int64_t(1 << 30)));
+        if (MAJOR) {
+            lines = int(min(max(l_end - l0 - mine, int64_t(0)), int64_t(N)));
+            n = min(left, 64);
+        } else {
+            lines = left - int(mine);
+            n = int(min(max(l_end - elem, int64_t(0)), int64_t(64)));
+        }
     }
-    __device__ __forceinline__ uint4 get(const uint16_t *p, int n) const {
-        const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(p)) & 15;
-        uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-        if (off & 8) {
+
+    __device__ __forceinline__ void next() {
+        at += stage;
+        left -= 64;
+        if (MAJOR) n = max(min(left, 64), 0); else lines -= 64;
+    }
+
+    __device__ __forceinline__ void ask(uint32_t raw, const void *any, int lane) const {
+        const uint32_t to = raw + lane / 8 * kRawLine + lane % 8 * 16;
+        const char *p = at;
 #pragma unroll
-            for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+        for (int i = 0; i < N / 4; ++i, p += four) {
+            const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(p)) & 15;
+            const int have = i * 4 < lines ? int(off) + n * 2 : 0;  // bytes, from the line's first unit on
+            const bool there = lane % 8 * 16 < have && n > 0;
+            copy_unit(to + i * 4 * kRawLine, there ? p - off + lane % 8 * 16 : any, there);
+            if (lane % 8 == 7) copy_unit(to + i * 4 * kRawLine + 16, have > 128 ? p - off + 128 : any, have > 128);
         }
-        if (off & 4) {
+    }
+
+    static __device__ __forceinline__ void copy_unit(uint32_t to, const void *from, bool there) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
+    }
+
+    // To lines `from` on of the stage.
+    __device__ __forceinline__ void cut(const char *raw, char *to, int from, int lane) const {
+        const int c = lane % 8, have = n - c * 8;
+        raw += lane / 8 * kRawLine + c * 16;
+        uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(at)) & 15;
 #pragma unroll
-            for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
-        }
-        if (off & 2) {
+        for (int i = 0; i < N / 4; ++i, off = (off + uint32_t(four)) & 15) {
+            const int L = from + i * 4 + lane / 8;
+            const uint4 a = *reinterpret_cast<const uint4 *>(raw + i * 4 * kRawLine), b = *reinterpret_cast<const uint4 *>(raw + i * 4 * kRawLine + 16);
+            uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
-        }
-        if (n < 8) {
+            for (int k = 0; k < 6; ++k) w[k] = off & 8 ? w[k + 2] : w[k];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = n >= 2 * i + 2 ? w[i] : n == 2 * i + 1 ? w[i] & 0xFFFFu : 0u;
+            for (int k = 0; k < 5; ++k) w[k] = off & 4 ? w[k + 1] : w[k];
+            const uint32_t turn = off & 2 ? 0x5432u : 0x3210u;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = __byte_perm(w[k], w[k + 1], turn);
+            if (have < 8) {  // (what the units hold behind the line is not zeros)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[k] = have >= 2 * k + 2 ? w[k] : have == 2 * k + 1 ? w[k] & 0xFFFFu : 0u;
+            }
+            *reinterpret_cast<uint4 *>(to + L * 128 + (c ^ (L & 7)) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
         }
-        return make_uint4(w[0], w[1], w[2], w[3]);
     }
 };
-
-// `count` of one operand's 128 lines of a stage, from line `from` on, by a warp. MAJOR: lines along the summed index, numbered l0 on, of which those before l_end are
-// there; elements from s0, before s_end. Else two blocks of 64 lines, one for each step of the summed index (s0 on, before s_end), of elements from l0 (and l0 + 64),
-// before l_end.
-template <bool MAJOR>
-__device__ __forceinline__ void load_lines(const uint16_t *p, int64_t ld, int64_t l0, int64_t l_end, int64_t s0, int64_t s_end, char *to, int from, int count, int lane) {
-    constexpr int kDeep = 4;  // four lines a round, eight lanes each
-    const int c = lane % 8 * 8;
-    auto place = [&](int L, const uint16_t *&q, int &n) {
-        const int64_t line = MAJOR ? l0 + L : s0 + L % 64, elem = MAJOR ? s0 + c : l0 + L / 64 * 64 + c, left = (MAJOR ? s_end : l_end) - elem;
-        q = p + line * ld + elem;
-        n = line < (MAJOR ? l_end : s_end) ? int(left < 8 ? left : 8) : 0;
-    };
-#pragma unroll 1
-    for (int i = from; i < from + count; i += 4 * kDeep) {
-        Eight u[kDeep];
-        const uint16_t *q;
-        int n;
-#pragma unroll
-        for (int j = 0; j < kDeep; ++j) {
-            place(i + j * 4 + lane / 8, q, n);
-            u[j].ask(q, n);
-        }
-#pragma unroll
-        for (int j = 0; j < kDeep; ++j) {
-            const int L = i + j * 4 + lane / 8;
-            place(L, q, n);
-            *reinterpret_cast<uint4 *>(to + L * 128 + ((lane % 8) ^ (L & 7)) * 16) = u[j].get(q, n);
-        }
-    }
-}
 
 // A box of a tensor map, from column x, line y of group z, to shared memory at `to`; its bytes count at the barrier of this address.
 __device__ __forceinline__ void copy_box(const CUtensorMap &map, uint32_t to, uint32_t bar, int x, int y, int z) {
@@ -734,12 +757,73 @@ __device__ __forceinline__ void clear_rows(const ProductArgs &A, const Shared &S
     }
 }
 
+// The stages of one operand, as one of the warps has them that load it.
+template <int KIND, int COPY, bool MAJOR, int N>
+__device__ __forceinline__ bool load_stages(const ProductArgs &A, Shared &S, Walk<KIND> &walk, char *raw, char *ring, uint32_t stages, int from, int rank, bool second) {
+    constexpr bool TURNED = kTurned<KIND>;
+    constexpr int kDeep = kRawStages<COPY>;
+    const int lane = threadIdx.x & 31;
+    const void *const any = reinterpret_cast<const void *>(reinterpret_cast<uintptr_t>(second ? A.b : A.a) & ~uintptr_t(15));
+    auto lines_of = [&](const Tile &t) {
+        const int64_t s0 = (KIND == kOuter ? t.r0 : 0) + int64_t(t.k0) * kStep, s_end = KIND == kOuter ? t.r1 : A.inner;
+        if (!second) {
+            const int64_t l0 = (TURNED ? t.n0 : t.m0) + rank * kLines;
+            return Loose<MAJOR, N>(static_cast<const uint16_t *>(A.a) + (TURNED ? t.group * A.a_group : 0), A.lda, l0, TURNED ? A.cols : KIND == kOuter ? A.inner : t.r1, s0,
+                                   s_end, from, lane);
+        }
+        const int half = TURNED ? t.width() / 2 : kLines;
+        const int64_t l0 = TURNED ? t.m0 + rank * half : t.n0 + rank * kLines;
+        return Loose<MAJOR, N>(static_cast<const uint16_t *>(A.b), A.ldb, l0, TURNED ? min(int64_t(t.r1), l0 + half) : A.cols, s0, s_end, from, lane);
+    };
+    Walk<KIND> walk_ahead = walk;
+    Tile t, ta;
+    ta.steps = 0;
+    int ka = 0;
+    uint32_t asked = 0, slot = 0;
+    Loose<MAJOR, N> ahead(nullptr, 0, 0, 0, 0, 0, 0, 0);
+    auto ask = [&] {  // for the next stage, if there is one
+        bool more = true;
+        if (ka == ta.steps) {
+            do more = walk_ahead.next(ta); while (more && !ta.steps);
+            ka = 0;
+            if (more) ahead = lines_of(ta); else ta.steps = 0;
+        }
+        if (more) {
+            ahead.ask(shared_address(raw + asked * N * kRawLine), any, lane);
+            ahead.next();
+            ++ka;
+            asked = asked + 1 == kDeep ? 0 : asked + 1;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    for (int i = 1; i < kDeep; ++i) ask();
+    Place p;
+    bool ok = true;
+    while (ok && walk.next(t)) {
+        if (!t.steps) continue;
+        Loose<MAJOR, N> lines = lines_of(t);
+        for (int k = 0; k < t.steps; ++k, p.next(stages), lines.next()) {
+            ask();
+            asm volatile("cp.async.wait_group %0;" ::"n"(kDeep - 1) : "memory");
+            if (!(ok = warp_wait(&S.empty[p.s], p.phase ^ 1, S))) break;
+            __syncwarp();
+            lines.cut(raw + slot * N * kRawLine, ring + p.s * kStageBytes, from, lane);
+            slot = slot + 1 == kDeep ? 0 : slot + 1;
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (!lane) bar_arrive(&S.full[p.s]);
+        }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    return ok;
+}
+
 template <int KIND, int END, int COPY>
 __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                                                                const __grid_constant__ CUtensorMap map_few, const ProductArgs A, const uint32_t stages) {
     extern __shared__ char raw[];
     constexpr bool COPY_A = COPY & kCopyA, COPY_B = COPY & kCopyB;
-    char *const ring = raw + (1024 - (shared_address(raw) & 1023)) % 1024, *const out_at = ring + stages * kStageBytes;
+    char *const ring = raw + (1024 - (shared_address(raw) & 1023)) % 1024, *const out_at = ring + stages * kStageBytes + kRawBytes<COPY>;
     Shared &S = *reinterpret_cast<Shared *>(out_at + kEndWarps * kOutBytes);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = blockIdx.x & 1;
     if (threadIdx.x == 0) {
@@ -762,7 +846,7 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
     Place p;
     bool ok = true;
 
-    // Registers, of the 168 (128) that a thread starts with: a warp that writes out holds 128 columns of sums, and what becomes of them.
+    // Registers, of the 168 (96) that a thread starts with: a warp that writes out holds 128 columns of sums, and what becomes of them.
     if (warp < kFirstEnd) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(COPY == 3 ? 56 : 40));
     if (COPY && warp == kCopyWarp) {  // one lane, as where the products are issued: 32 that wait for a barrier slow down what runs beside them by 3 %
         uint32_t n = 0;
@@ -811,28 +895,15 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
             __syncwarp();
         }
     } else if (COPY != 3 && warp >= kFirstLoad) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-        constexpr int kShare = (COPY ? 1 : 2) * kLines / kLoadWarps;  // lines of a warp, of one operand or of both
-        const int w = warp - kFirstLoad, from = w * kShare % kLines;
-        const bool second = COPY ? COPY_A : w * kShare >= kLines;
-        while (ok && walk.next(t)) {
-            const uint16_t *const a = static_cast<const uint16_t *>(A.a) + (TURNED ? t.group * A.a_group : 0), *const b = static_cast<const uint16_t *>(A.b);
-            const int half = TURNED ? t.width() / 2 : kLines;
-            const int64_t m0 = (TURNED ? t.n0 : t.m0) + rank * kLines, m_end = TURNED ? A.cols : KIND == kOuter ? A.inner : t.r1;
-            const int64_t n0 = TURNED ? t.m0 + rank * half : t.n0 + rank * kLines, n_end = TURNED ? t.r1 : A.cols;
-            for (int k = 0; k < t.steps; ++k, p.next(stages)) {
-                if (!(ok = warp_wait(&S.empty[p.s], p.phase ^ 1, S))) break;
-                char *to = ring + p.s * kStageBytes;
-                const int64_t s0 = (KIND == kOuter ? t.r0 : 0) + int64_t(t.k0 + k) * kStep, s_end = KIND == kOuter ? t.r1 : A.inner;
-                if (!second)
-                    load_lines<A_MAJOR>(a, A.lda, m0, m_end, s0, s_end, to, from, kShare, lane);
-                else
-                    load_lines<B_MAJOR>(b, A.ldb, n0, n_end, s0, s_end, to + kOperandBytes, from, min(kShare, half - from), lane);
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (!lane) bar_arrive(&S.full[p.s]);
-            }
-        }
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        // A warp has 16 lines of the operand that is not copied, or 32 of one of both.
+        constexpr int N = COPY ? kLooseLines / 2 : kLooseLines;
+        const int w = warp - kFirstLoad, from = w * N % kLines;
+        char *const raw = ring + stages * kStageBytes + size_t(w) * kRawStages<COPY> * N * kRawLine;
+        if (COPY ? COPY_A : w * N >= kLines)
+            ok = load_stages<KIND, COPY, B_MAJOR, N>(A, S, walk, raw, ring + kOperandBytes, stages, from, rank, true);
+        else
+            ok = load_stages<KIND, COPY, A_MAJOR, N>(A, S, walk, raw, ring, stages, from, rank, false);
     } else if (warp == kMulWarp && !rank) {
         Place h;  // of the two halves of tensor memory
         bool some = false;
@@ -869,7 +940,7 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
         // what was issued ends before the tensor memory is given back
         if (!ok && some) drain(&S.empty[p.s ? p.s - 1 : stages - 1], p.s ? p.phase : p.phase ^ 1);
     } else if (warp >= kFirstEnd && warp < kFirstLoad) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(COPY == 3 ? 224 : 192));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(COPY == 3 ? 224 : 152));
         const int q = warp % 4, col0 = (warp - kFirstEnd) / 4 * kEndCols;
         char *const buffer = out_at + (warp - kFirstEnd) * kOutBytes;
         Sums sums{S, {}, acc + (TURNED ? 0 : col0) + (uint32_t(q * 32) << 16)};
@@ -957,8 +1028,8 @@ cudaError_t launch_of(const ProductArgs &A, const CUtensorMap &a, const CUtensor
     constexpr auto k = k_product<KIND, END, COPY>;
     const cudaError_t e = ops_allow_smem<k>(int(kMaxSharedBytes));
     if (e != cudaSuccess) return e;
-    uint32_t stages = kStages;
-    while (shared_bytes(stages, A.groups) > kMaxSharedBytes) --stages;
+    uint32_t stages = kRing<COPY>;
+    while (shared_bytes(stages, kRawBytes<COPY>, A.groups) > kMaxSharedBytes) --stages;
     const int64_t nt = (A.cols + kTile - 1) / kTile;
     const int64_t most = (KIND == kOuter ? int64_t((A.inner + kTile - 1) / kTile) * A.groups : A.rows / kTile + A.groups) * nt * A.splits;
     if (most > INT32_MAX) return cudaErrorInvalidValue;
@@ -972,7 +1043,7 @@ cudaError_t launch_of(const ProductArgs &A, const CUtensorMap &a, const CUtensor
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(uint32_t(most < pairs ? most : pairs) * 2);
     cfg.blockDim = dim3(kThreads<COPY>);
-    cfg.dynamicSmemBytes = shared_bytes(stages, A.groups);
+    cfg.dynamicSmemBytes = shared_bytes(stages, kRawBytes<COPY>, A.groups);
     cfg.stream = s;
     cfg.attrs = at;
     cfg.numAttrs = A.flags & kAfter ? 2 : 1;

@@ -174,27 +174,28 @@ struct RowsArgs {
     int32_t lanes;                      // to a row (a power of two), the others take the next rows
 };
 
-// Eight elements, or fewer at the end of a row where accesses are one element wide.
+// Eight elements of a row: side by side, as one or two 16-byte accesses; or one access each, `stride` apart, so that the lanes of a row access
+// neighbours (`n`: elements from the first to the row's end).
 template <bool F32, bool VEC>
 struct Piece {
     float x[8];
-    __device__ __forceinline__ void read(const void *p, int64_t i, int n) {
+    __device__ __forceinline__ void read(const void *p, int64_t i, int n, int stride) {
         if constexpr (VEC) {
             const Vec8<F32> v = load8_cached<F32>(p, i);
 #pragma unroll
             for (int k = 0; k < 8; ++k) x[k] = v.at(k);
         } else {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) x[k] = k < n ? load1<F32>(p, i + k) : 0.f;
+            for (int k = 0; k < 8; ++k) x[k] = k * stride < n ? load1<F32>(p, i + k * stride) : 0.f;
         }
     }
-    __device__ __forceinline__ void write(void *p, int64_t i, int n) const {
+    __device__ __forceinline__ void write(void *p, int64_t i, int n, int stride) const {
         if constexpr (VEC) {
             store8<F32>(p, i, x);
         } else {
 #pragma unroll
             for (int k = 0; k < 8; ++k)
-                if (k < n) store1<F32>(p, i + k, x[k]);
+                if (k * stride < n) store1<F32>(p, i + k * stride, x[k]);
         }
     }
 };
@@ -213,12 +214,12 @@ __global__ void __launch_bounds__(kThreads) k_spread(const RowsArgs A) {
     if (!there) return;
     const int64_t used = A.offsets[A.experts];
     constexpr int kDeep = 4;
-    for (int64_t c0 = in * 8; c0 < A.width; c0 += int64_t(A.lanes) * 8 * kDeep) {
+    for (int64_t c0 = in * (VEC ? 8 : 1); c0 < A.width; c0 += int64_t(A.lanes) * 8 * kDeep) {
         Piece<TF32, VEC> x[kDeep];
 #pragma unroll
         for (int q = 0; q < kDeep; ++q) {
             const int64_t c = c0 + int64_t(q) * A.lanes * 8;
-            if (c < A.width) x[q].read(A.tokens, i * A.ld + c, int(A.width - c));
+            if (c < A.width) x[q].read(A.tokens, i * A.ld + c, int(A.width - c), A.lanes);
         }
         for (int j = 0; j < A.top_k; ++j) {
             const int64_t entry = i * A.top_k + j, place = A.places[entry];
@@ -227,8 +228,8 @@ __global__ void __launch_bounds__(kThreads) k_spread(const RowsArgs A) {
             for (int q = 0; q < kDeep; ++q) {
                 const int64_t c = c0 + int64_t(q) * A.lanes * 8;
                 if (c >= A.width) break;
-                if (put) reinterpret_cast<const Piece<RF32, VEC> &>(x[q]).write(A.out, place * A.width + c, int(A.width - c));
-                if (clear) Piece<RF32, VEC>{}.write(A.out, entry * A.width + c, int(A.width - c));
+                if (put) reinterpret_cast<const Piece<RF32, VEC> &>(x[q]).write(A.out, place * A.width + c, int(A.width - c), A.lanes);
+                if (clear) Piece<RF32, VEC>{}.write(A.out, entry * A.width + c, int(A.width - c), A.lanes);
             }
         }
     }
@@ -240,7 +241,7 @@ __global__ void __launch_bounds__(kThreads) k_combine(const RowsArgs A) {
     SKEW_ROW_OF_LANES(A.n_tokens)
     if (!there) return;
     constexpr int kDeep = 4;
-    for (int64_t c0 = in * 8; c0 < A.width; c0 += int64_t(A.lanes) * 8) {
+    for (int64_t c0 = in * (VEC ? 8 : 1); c0 < A.width; c0 += int64_t(A.lanes) * 8) {
         Piece<TF32, VEC> y{};
         const int n = int(A.width - c0);
         for (int j0 = 0; j0 < A.top_k; j0 += kDeep) {
@@ -253,14 +254,14 @@ __global__ void __launch_bounds__(kThreads) k_combine(const RowsArgs A) {
                 const bool put = place >= 0 && place < A.n_rows;
                 w[q] = put ? (A.weights ? A.weights[entry] : 1.f) : 0.f;
                 x[q] = {};
-                if (put) x[q].read(A.rows, place * A.width + c0, n);
+                if (put) x[q].read(A.rows, place * A.width + c0, n, A.lanes);
             }
 #pragma unroll
             for (int q = 0; q < kDeep; ++q)
 #pragma unroll
                 for (int k = 0; k < 8; ++k) y.x[k] = fmaf(w[q], x[q].x[k], y.x[k]);
         }
-        y.write(A.out, i * A.ld + c0, n);
+        y.write(A.out, i * A.ld + c0, n, A.lanes);
     }
 }
 
@@ -275,28 +276,28 @@ __global__ void __launch_bounds__(kThreads) k_combine_grad(const RowsArgs A) {
     float dot = 0.f;
     if (put || clear) {
         constexpr int kDeep = 2;
-        for (int64_t c0 = in * 8; c0 < A.width; c0 += int64_t(A.lanes) * 8 * kDeep) {
+        for (int64_t c0 = in * (VEC ? 8 : 1); c0 < A.width; c0 += int64_t(A.lanes) * 8 * kDeep) {
             Piece<TF32, VEC> g[kDeep];
             Piece<RF32, VEC> x[kDeep];
 #pragma unroll
             for (int q = 0; q < kDeep; ++q) {
                 const int64_t c = c0 + int64_t(q) * A.lanes * 8;
                 if (!put || c >= A.width) break;
-                g[q].read(A.tokens, from + c, int(A.width - c));
-                x[q].read(A.rows, place * A.width + c, int(A.width - c));
+                g[q].read(A.tokens, from + c, int(A.width - c), A.lanes);
+                x[q].read(A.rows, place * A.width + c, int(A.width - c), A.lanes);
             }
 #pragma unroll
             for (int q = 0; q < kDeep; ++q) {
                 const int64_t c = c0 + int64_t(q) * A.lanes * 8;
                 if (c >= A.width) break;
-                if (clear) Piece<RF32, VEC>{}.write(A.out, i * A.width + c, int(A.width - c));
+                if (clear) Piece<RF32, VEC>{}.write(A.out, i * A.width + c, int(A.width - c), A.lanes);
                 if (!put) continue;
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     dot = fmaf(g[q].x[k], x[q].x[k], dot);
                     x[q].x[k] = w * g[q].x[k];
                 }
-                x[q].write(A.out, place * A.width + c, int(A.width - c));
+                x[q].write(A.out, place * A.width + c, int(A.width - c), A.lanes);
             }
         }
     }

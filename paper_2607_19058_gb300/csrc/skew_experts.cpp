@@ -29,6 +29,12 @@ int check_ptr(const char *what, const void *p, uintptr_t es, bool needed) {
     return SKEW_OK;
 }
 
+// Rows of an expert, on average, from which on `product` takes the rows as a tile's rows, 256 at a time, instead of its columns, 64 at a time. (The matrices, whose lines
+// lie across the summed index, are the slower operand of a tile's rows; but half a tile is wasted, and a tile of few rows takes longer to write out. 128 experts of 4096 x
+// 4096, uneven loads, us for 64, 128, 256, 384 and 512 rows each: 740, 788, 1077, 1413, 1765 straight, 669, 723, 1047, 1438, 1834 turned. grad_rows, whose lines lie
+// along it, is turned always: 1774 straight, 1795 turned at 512, and 46 against 23 for 17 rows of 164 experts of 1648 x 128.)
+constexpr int64_t kStraightRows = 384;
+
 // The two products by rows: of `inner` columns each, times one matrix a group, to `cols` columns.
 int by_rows(ProductKind kind, const skew_experts_config_t *c, const void *x, int64_t ld, const void *w, const int32_t *offsets, int64_t rows, void *y, cudaStream_t s) {
     const bool wide = c->flags & SKEW_EXPERTS_ROWS_FP32;
@@ -37,11 +43,12 @@ int by_rows(ProductKind kind, const skew_experts_config_t *c, const void *x, int
     if ((rc = check_rows("rows", x, rows, inner, ld)) || (rc = check_ptr("w", w, 2, true)) || (rc = check_ptr("result", y, wide ? 4 : 2, rows > 0))) return rc;
     if (!rows) return SKEW_OK;
     ProductArgs A{};
-    A.a = w;
-    A.b = x;
-    A.lda = c->m;
-    A.ldb = ld;
-    A.a_group = int64_t(c->n) * c->m;
+    const bool straight = kind == kGroupRows && rows >= kStraightRows * c->experts;
+    A.a = straight ? x : w;
+    A.b = straight ? w : x;
+    A.lda = straight ? ld : c->m;
+    A.ldb = straight ? c->m : ld;
+    A.a_group = A.b_group = int64_t(c->n) * c->m;
     A.offsets = offsets;
     A.rows = rows;
     A.groups = c->experts;
@@ -51,7 +58,7 @@ int by_rows(ProductKind kind, const skew_experts_config_t *c, const void *x, int
     A.ldo = cols;
     A.scale = 1.f;
     A.flags = (wide ? kOut32 : 0) | (cols % 8 == 0 && ((uintptr_t)y & 15) == 0 ? kOutVec : 0);
-    return ops_cuda(product_launch(kind, kStore, A, s), "k_product");
+    return ops_cuda(product_launch(straight ? kByRows : kind, kStore, A, s), "k_product");
 }
 
 }  // namespace

@@ -773,7 +773,7 @@ __device__ __forceinline__ bool load_stages(const ProductArgs &A, Shared &S, Wal
         }
         const int half = TURNED ? t.width() / 2 : kLines;
         const int64_t l0 = TURNED ? t.m0 + rank * half : t.n0 + rank * kLines;
-        return Loose<MAJOR, N>(static_cast<const uint16_t *>(A.b), A.ldb, l0, TURNED ? min(int64_t(t.r1), l0 + half) : A.cols, s0, s_end, from, lane);
+        return Loose<MAJOR, N>(static_cast<const uint16_t *>(A.b) + (KIND == kByRows ? t.group * A.b_group : 0), A.ldb, l0, TURNED ? min(int64_t(t.r1), l0 + half) : A.cols, s0, s_end, from, lane);
     };
     Walk<KIND> walk_ahead = walk;
     Tile t, ta;
@@ -867,7 +867,7 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
                     if (COPY_B && TURNED && half < kLines) {
                         for (int l = 0; l < half; l += kRowBox) copy_box(map_few, to + kOperandBytes + l * 128, bar, s0, n0 + l, 0);
                     } else if (COPY_B) {
-                        copy_lines<B_MAJOR>(map_b, to + kOperandBytes, bar, n0, s0, 0);
+                        copy_lines<B_MAJOR>(map_b, to + kOperandBytes, bar, n0, s0, KIND == kByRows ? t.group : 0);
                     }
                 }
             }
@@ -952,7 +952,7 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
             else
                 ok = end_tile<KIND, END, kEndCols>(A, buffer, t, peak, rank * kLines + q * 32, col0, sums);
         }
-        if (TURNED) clear_rows(A, S, warp - kFirstEnd, lane);
+        if (TURNED || (KIND == kByRows && A.offsets)) clear_rows(A, S, warp - kFirstEnd, lane);
     }
     before_sync();
     __syncwarp();
@@ -1097,9 +1097,9 @@ cudaError_t launch(ProductArgs A, cudaStream_t s) {
     constexpr bool A_MAJOR = kMajorA<KIND>, B_MAJOR = kMajorB<KIND>, TURNED = kTurned<KIND>, OUTER = KIND == kOuter;
     // lines of an operand: how long, how many, in how many groups, and in a copy
     const int64_t long_a = TURNED && !A_MAJOR ? A.cols : A.inner, lines_a = TURNED ? (A_MAJOR ? A.cols : A.inner) : A.rows, groups_a = TURNED ? A.groups : 1;
-    const int64_t long_b = B_MAJOR ? A.inner : A.cols, lines_b = TURNED || OUTER ? A.rows : B_MAJOR ? A.cols : A.inner;
+    const int64_t groups_b = KIND == kByRows ? A.groups : 1, long_b = B_MAJOR ? A.inner : A.cols, lines_b = TURNED || OUTER ? A.rows : B_MAJOR ? A.cols : A.inner;
     const bool copy_a = A.rows && copies(A.a, A.lda, A.a_group, groups_a) && map_of(&a, A.a, long_a, A.lda, lines_a, A.a_group, groups_a, A_MAJOR ? kLines : kStep);
-    const bool copy_b = A.rows && copies(A.b, A.ldb, 0, 1) && map_of(&b, A.b, long_b, A.ldb, lines_b, 0, 1, B_MAJOR ? kLines : kStep) &&
+    const bool copy_b = A.rows && copies(A.b, A.ldb, A.b_group, groups_b) && map_of(&b, A.b, long_b, A.ldb, lines_b, A.b_group, groups_b, B_MAJOR ? kLines : kStep) &&
                         (!TURNED || map_of(&few, A.b, long_b, A.ldb, lines_b, 0, 1, kRowBox));
     if (copy_a && copy_b) return launch_split<KIND, END, 3>(A, a, b, few, s);
     if (copy_a) return launch_split<KIND, END, kCopyA>(A, a, b, few, s);

@@ -8,7 +8,7 @@
 namespace skew {
 
 // What is multiplied. A "line" is a run of memory: 64 contiguous elements of it, at a time, come to shared memory.
-//   BY_ROWS    : C[r, j] = sum_k A[r, k] B[k, j]     A: lines of k, one for each row r; B: lines of j    (STORE)
+//   BY_ROWS    : C[r, j] = sum_k A[r, k] B_e[k, j]   A: lines of k, one for each row r of the group e; B: lines of j  (STORE)
 //   BY_COLS    : C[r, j] = sum_k A[r, k] B[j, k]     A: as above;                       B: lines of k    (LOSS, LOGITS_GRAD)
 //   OUTER      : C_e[i, j] = sum_r A[r, i] B[r, j]   A: lines of i, B: lines of j, one for each row r of the group e
 //   GROUP_ROWS : C[r, j] = sum_k B[r, k] A_e[k, j]   A: lines of j, B: lines of k, one for each row r, of the group e
@@ -28,8 +28,8 @@ enum : uint32_t { kOut32 = 1, kBase32 = 2, kOutVec = 4 /* out and base: 16-byte 
 
 struct ProductArgs {
     const void *a, *b;          // bf16
-    int64_t lda, ldb, a_group;  // elements between lines, and between A's groups (GROUP)
-    const int32_t *offsets;     // groups + 1 row numbers on the device (GROUP, OUTER); NULL: one group of all rows
+    int64_t lda, ldb, a_group, b_group;  // elements between lines, and between A's groups (GROUP) or B's (BY_ROWS)
+    const int32_t *offsets;     // groups + 1 row numbers on the device; NULL: one group of all rows
     int64_t rows;               // r in [0, rows)
     int32_t groups, cols;       // j in [0, cols)
     int32_t inner;              // k, or OUTER's i, in [0, inner)

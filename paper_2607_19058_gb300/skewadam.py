@@ -915,7 +915,7 @@ class Dispatch:
         self._workspace, self._sizes = _Workspace(), {}
 
     def _there(self, t, dtype, shape, dev, what: str) -> int:
-        if not (t.dtype == dtype and t.shape == shape and t.is_contiguous() and t.is_cuda and (dev is None or t.device == dev)):
+        if not (t.dtype is dtype and t.shape == shape and t.is_contiguous() and (t.is_cuda if dev is None else t.device == dev)):
             raise ValueError(f"{what} must be a contiguous {tuple(shape)} {dtype} CUDA tensor, on the device of the others")
         return t.data_ptr()
 

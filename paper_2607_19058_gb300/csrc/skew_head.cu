@@ -242,7 +242,7 @@ int skew_head_grad(const skew_head_config_t *c, const void *h, int64_t ld_h, con
             P.inner = width;
             P.cols = (int32_t)n;
             P.scale = c->scale;
-            P.flags = (wide ? kIds64 : 0) | kOutVec | kAfter | kRelease;
+            P.flags = (wide ? kIds64 : 0) | kOutVec | kRelease;
             P.targets = targets;
             P.first = v0;
             P.vocab = c->rows;
@@ -266,7 +266,7 @@ int skew_head_grad(const skew_head_config_t *c, const void *h, int64_t ld_h, con
             H.base = first ? nullptr : ws + L.sums;
             H.out = last ? dh : ws + L.sums;
             H.ldo = c->width;
-            H.flags = kBase32 | (last ? 0 : kOut32) | (units(c->width, H.out) ? kOutVec : 0) | kAfter | kRelease;
+            H.flags = kBase32 | (last ? 0 : kOut32) | (units(c->width, H.out) ? kOutVec : 0) | kRelease;
             if ((rc = ops_cuda(product_launch(kByRows, kStore, H, s), "k_product"))) return rc;
         }
         ProductArgs W{};  // its rows of dW
@@ -284,7 +284,7 @@ int skew_head_grad(const skew_head_config_t *c, const void *h, int64_t ld_h, con
         W.base = base ? (const uint16_t *)base + v0 * c->width : nullptr;
         W.out = (uint16_t *)dtable + v0 * c->width;
         W.ldo = c->width;
-        W.flags = (units(c->width, W.out) && units(c->width, base) ? kOutVec : 0) | (tokens ? uint32_t(kAfter) | (last ? 0u : uint32_t(kRelease)) : 0u);
+        W.flags = (units(c->width, W.out) && units(c->width, base) ? kOutVec : 0) | (last ? 0u : uint32_t(kRelease));
         if ((rc = ops_cuda(product_launch(kOuter, kStore, W, s), "k_product"))) return rc;
     }
     return SKEW_OK;

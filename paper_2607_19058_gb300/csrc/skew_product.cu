@@ -163,6 +163,16 @@ template <int KIND, int THREADS>
 __device__ __forceinline__ void groups_of(const ProductArgs &A, Shared &S) {
     const int G = A.groups, per = (G + THREADS) / THREADS, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int rows = int(A.rows);
+    if (!A.offsets) {
+        if (threadIdx.x == 0) {
+            int32_t *const tile = tiles_of(A, S);
+            S.begin[0] = tile[0] = 0;
+            S.begin[1] = rows;
+            tile[1] = (rows + kTile - 1) / kTile;
+        }
+        __syncthreads();
+        return;
+    }
     const int i0 = threadIdx.x * per, i1 = min(i0 + per, G + 1);
     auto scan = [&](int v, auto join) {  // what the threads before this one have together; -1 for none
         int x = v;
@@ -180,7 +190,7 @@ __device__ __forceinline__ void groups_of(const ProductArgs &A, Shared &S) {
     };
     auto most = [](int a, int b) { return max(a, b); };
     auto both = [](int a, int b) { return a + b; };
-    auto at = [&](int i) { return A.offsets ? min(max(A.offsets[i], 0), rows) : i ? rows : 0; };
+    auto at = [&](int i) { return min(max(A.offsets[i], 0), rows); };
     int m = 0;
     for (int i = i0; i < i1; ++i) m = max(m, at(i));
     m = scan(m, most);
@@ -832,13 +842,17 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
         S.gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (COPY && threadIdx.x == 32 * kCopyWarp) {
+        if (COPY_A) asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a) : "memory");
+        if (COPY_B) asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b) : "memory");
+    }
     if (warp == kMemWarp) take_tensor_memory(&S.acc);
-    wait_launch_before();
-    if (A.flags & kRelease) release_launch_after();
-    groups_of<KIND, kThreads<COPY>>(A, S);
     before_sync();
     pair_sync();
     after_sync();
+    wait_launch_before();  // (what is above reads nothing that the launch before wrote, and goes on beside its end)
+    if (A.flags & kRelease) release_launch_after();
+    groups_of<KIND, kThreads<COPY>>(A, S);
     const uint32_t acc = S.acc;
     constexpr bool A_MAJOR = kMajorA<KIND>, B_MAJOR = kMajorB<KIND>, TURNED = kTurned<KIND>;
     Walk<KIND> walk(A, S);
@@ -989,6 +1003,14 @@ __global__ void __launch_bounds__(kSumThreads) k_sum(const ProductArgs A, const 
     }
 }
 
+// One wait as the kernel's, for what nothing completes.
+__global__ void k_wait_in_vain() {
+    __shared__ Shared S;
+    bar_init(&S.full[0], 1);
+    S.gave_up = 0;
+    bar_wait(&S.full[0], 0, S);
+}
+
 // ---------------------------------------------------------------------------
 // Host
 // ---------------------------------------------------------------------------
@@ -1046,7 +1068,7 @@ cudaError_t launch_of(const ProductArgs &A, const CUtensorMap &a, const CUtensor
     cfg.dynamicSmemBytes = shared_bytes(stages, kRawBytes<COPY>, A.groups);
     cfg.stream = s;
     cfg.attrs = at;
-    cfg.numAttrs = A.flags & kAfter ? 2 : 1;
+    cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, k, a, b, few, A, stages);
 }
 
@@ -1081,7 +1103,7 @@ cudaError_t launch_split(ProductArgs A, const CUtensorMap &a, const CUtensorMap 
     P.base = nullptr;
     P.peaks = nullptr;
     P.scale = 1.f;
-    P.flags = kOut32 | kOutVec | kRelease | (A.flags & kAfter);
+    P.flags = kOut32 | kOutVec | kRelease;
     P.chunk = kChunk32;
     const cudaError_t e = launch_of<KIND, END, COPY>(P, a, b, few, s);
     if (e != cudaSuccess) return e;
@@ -1137,3 +1159,7 @@ int product_status(cudaStream_t s) {
 }  // namespace skew
 
 extern "C" int skew_ops_sync_status(void *stream) { return skew::product_status((cudaStream_t)stream); }
+
+extern "C" int skew_ops_selftest_wait_timeout(void *stream) {
+    return skew::ops_cuda(skew::ops_launch(false, skew::k_wait_in_vain, 1, 1, 0, (cudaStream_t)stream), "k_wait_in_vain");
+}

@@ -23,8 +23,7 @@ enum ProductKind { kByRows, kByCols, kOuter, kGroupRows, kGroupCols };
 enum ProductEnd { kStore = 0, kLoss = 1, kLogitsGrad = 2 };
 
 enum : uint32_t { kOut32 = 1, kBase32 = 2, kOutVec = 4 /* out and base: 16-byte accesses */, kIds64 = 8,
-                // a launch of the call goes on after this one, and may start up meanwhile; this one is such a launch
-                kRelease = 16, kAfter = 32 };
+                kRelease = 16 /* a launch of the same call follows, which may start up while this one ends */ };
 
 struct ProductArgs {
     const void *a, *b;          // bf16

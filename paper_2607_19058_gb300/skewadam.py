@@ -45,7 +45,8 @@ EXPORTS = ["skew_create", "skew_destroy", "skew_state_bytes", "skew_workspace_by
            "skew_embed_lookup", "skew_embed_workspace_bytes", "skew_embed_grad",
            "skew_dispatch_workspace_bytes", "skew_dispatch_order", "skew_dispatch_spread", "skew_dispatch_combine", "skew_dispatch_combine_grad",
            "skew_experts_product", "skew_experts_grad_rows", "skew_experts_grad", "skew_experts_workspace_bytes",
-           "skew_head_loss_workspace_bytes", "skew_head_grad_workspace_bytes", "skew_head_loss", "skew_head_grad", "skew_ops_sync_status"]
+           "skew_head_loss_workspace_bytes", "skew_head_grad_workspace_bytes", "skew_head_loss", "skew_head_grad", "skew_ops_sync_status",
+           "skew_ops_selftest_wait_timeout"]
 
 
 class SkewError(RuntimeError):
@@ -199,8 +200,10 @@ def load(path: Optional[str] = None) -> C.CDLL:
         L.skew_head_loss.argtypes = [C.POINTER(HeadConfig), vp, i64, vp, vp, i64, vp, vp, vp, sz, vp]
         L.skew_head_grad.argtypes = [C.POINTER(HeadConfig), vp, i64, vp, vp, i64, vp, vp, vp, vp, vp, vp, sz, vp]
         L.skew_ops_sync_status.argtypes = [vp]
+        L.skew_ops_selftest_wait_timeout.argtypes = [vp]
         for f in (L.skew_dispatch_order, L.skew_dispatch_spread, L.skew_dispatch_combine, L.skew_dispatch_combine_grad, L.skew_experts_product,
-                  L.skew_experts_grad_rows, L.skew_experts_grad, L.skew_head_loss, L.skew_head_grad, L.skew_ops_sync_status):
+                  L.skew_experts_grad_rows, L.skew_experts_grad, L.skew_head_loss, L.skew_head_grad, L.skew_ops_sync_status,
+                  L.skew_ops_selftest_wait_timeout):
             f.restype = C.c_int
         if path is None:
             _lib = L
@@ -478,6 +481,11 @@ def skew_head_grad(c: HeadConfig, h_ptr: int, ld_h: int, table_ptr: int, targets
 def skew_ops_sync_status(stream: int) -> None:
     """Synchronises `stream`; raises SkewError(SKEW_ETIMEOUT) once if a bounded device wait of Experts or HeadLoss gave up since the last read."""
     _check_op(load().skew_ops_sync_status(stream))
+
+
+def skew_ops_selftest_wait_timeout(stream: int) -> None:
+    """Makes one bounded device wait run out, for ``skew_ops_sync_status`` to report."""
+    _check_op(load().skew_ops_selftest_wait_timeout(stream))
 
 
 def hparams(beta1=0.9, beta2=0.999, eps=1e-8, clip_d=1.0, weight_decay=0.05, policy=POLICY_TIERED) -> HParams:

@@ -76,7 +76,7 @@ def _check(loads, n, m, row=BF16, grad=BF16, first=0, behind=0, lay=None, base=F
     op.sync_status()
 
 
-LOADS = [[1], [0, 1, 0], [127, 128, 129], [64, 0, 0, 300, 5], [1] * 40, [255, 256, 257, 1, 0], [700]]
+LOADS = [[1], [0, 1, 0], [900, 3, 0, 700], [127, 128, 129], [64, 0, 0, 300, 5], [1] * 40, [255, 256, 257, 1, 0], [700]]
 
 
 @pytest.mark.parametrize("loads", LOADS, ids=lambda v: "-".join(map(str, v[:5])))
@@ -192,6 +192,19 @@ def test_matrices_past_2_31_elements():
 def test_a_long_sum():
     """One expert of many rows: the matrices' gradient sums over all of them."""
     _check([70001], 72, 136)
+
+
+def test_a_wait_that_gives_up_is_reported_once():
+    op = S.Experts(2, 64, 64)
+    x, w, o = _randn((100, 64), 1), _randn((2, 64, 64), 2), _offsets([40, 60])
+    y = op.product(x, w, o)
+    op.sync_status()
+    S.skew_ops_selftest_wait_timeout(torch.cuda.current_stream().cuda_stream)
+    with pytest.raises(S.SkewError) as e:
+        op.sync_status()
+    assert e.value.code == S.SKEW_ETIMEOUT
+    op.sync_status()
+    assert torch.equal(op.product(x, w, o), y)
 
 
 def test_gradients_are_the_products_by_differences():

@@ -582,26 +582,54 @@ __device__ __forceinline__ bool end_tile(const ProductArgs &A, char *buffer, con
     // LOSS, LOGITS_GRAD: in powers of two, exp(x) = 2^(x log2 e)
     const float scale = A.scale * peak, scale2 = A.scale * kLog2e;
     const int64_t target = END != kStore && mine ? target_of(A, row) : -1;
-    const float g = END == kLogitsGrad && target >= 0 ? A.dloss[row] / peak : 0.f, lse2 = END == kLogitsGrad && target >= 0 ? A.lse[row] * kLog2e : 0.f;
+    const float g = END == kLogitsGrad && target >= 0 ? A.dloss[row] / peak : 0.f;
+    const float lse2 = END == kLogitsGrad && target >= 0 ? A.lse[row] * kLog2e : INFINITY;  // (padding: no probability)
     float top = -INFINITY, sum = 0.f;
 
-    const int picked = target >= A.first && target < A.first + A.cols ? int(target - A.first) : -1;
-    auto turned = [&](int column, float &x, int i) {  // LOGITS_GRAD: a logit to its gradient
-        const float p = exp2_of(fmaf(x, scale2, -lse2)) - (picked == column + i ? 1.f : 0.f);
-        x = target >= 0 ? p * g : 0.f;
+    // The target's column, here; where no column is meant, one that no tile has.
+    const int picked = target >= A.first && target < A.first + A.cols ? int(target - A.first) : -kTile;
+    auto turn = [&](int column, auto &x) {  // LOGITS_GRAD: logits to their gradients
+        constexpr int N = sizeof(x) / 4;
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = exp2_of(fmaf(x[i], scale2, -lse2));
+        if (picked >= column && picked < column + N) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i] -= picked == column + i ? 1.f : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] *= g;
+    };
+    auto pick = [&](int column, const auto &x) {  // LOSS: the target's logit
+        constexpr int N = sizeof(x) / 4;
+        if (picked < column || picked >= column + N) return;
+        float p = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) p = picked == column + i ? x[i] : p;
+        A.picked[row] = p * A.scale;
+    };
+    auto sum_up = [&](const float (&x)[64]) {  // LOSS: 64 logits, all there
+        float far[4] = {x[0], x[1], x[2], x[3]}, part[4] = {};
+        if (scale2 >= 0.f) {
+#pragma unroll
+            for (int i = 4; i < 64; ++i) far[i % 4] = fmaxf(far[i % 4], x[i]);
+            far[0] = fmaxf(fmaxf(far[0], far[1]), fmaxf(far[2], far[3]));
+        } else {
+#pragma unroll
+            for (int i = 4; i < 64; ++i) far[i % 4] = fminf(far[i % 4], x[i]);
+            far[0] = fminf(fminf(far[0], far[1]), fminf(far[2], far[3]));
+        }
+        const float most = fmaxf(top, far[0] * scale2), from = most == -INFINITY ? 0.f : most;
+#pragma unroll
+        for (int i = 0; i < 64; ++i) part[i % 4] += exp2_of(fmaf(x[i], scale2, -from));
+        sum = fmaf(sum, exp2_of(top - from), (part[0] + part[1]) + (part[2] + part[3]));
+        top = most;
     };
     auto chunk = [&](int column, float (&x)[32]) {  // 32 columns
         const int n = stop - column;
         if constexpr (END == kStore) {
             put_32(A, buffer, to, column, n, scale, x);
         } else if constexpr (END == kLoss) {
-            const int64_t here = target - column;
-            if (here >= 0 && here < 32 && target >= 0) {
-                float p = 0.f;
-#pragma unroll
-                for (int i = 0; i < 32; ++i) p = here == i ? x[i] : p;
-                A.picked[row] = p * A.scale;
-            }
+            pick(column, x);
             float high[4] = {top, -INFINITY, -INFINITY, -INFINITY}, part[4] = {};
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
@@ -614,8 +642,7 @@ __device__ __forceinline__ bool end_tile(const ProductArgs &A, char *buffer, con
             sum = fmaf(sum, exp2_of(top - from), (part[0] + part[1]) + (part[2] + part[3]));
             top = most;
         } else {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) turned(column, x[i], i);
+            turn(column, x);
             put_32(A, buffer, to, column, n, 1.f, x);
         }
     };
@@ -648,7 +675,7 @@ __device__ __forceinline__ bool end_tile(const ProductArgs &A, char *buffer, con
     if (here && !sums.wait(acc)) return false;
     if (any) {
         int c = 0;
-        if (END != kLoss && here && A.flags & kOutVec && !(A.flags & kOut32) && !A.base) {
+        if (here && (END == kLoss || (A.flags & kOutVec && !(A.flags & kOut32) && !A.base))) {
 #pragma unroll 1
             for (; c < COLS && start + c + 64 <= stop; c += 64) {
                 float x[64];
@@ -656,11 +683,13 @@ __device__ __forceinline__ bool end_tile(const ProductArgs &A, char *buffer, con
                 read_sums(acc + c + 32, *reinterpret_cast<float (*)[32]>(x + 32));
                 sums_read(*reinterpret_cast<float (*)[32]>(x));
                 sums_read(*reinterpret_cast<float (*)[32]>(x + 32));
-                if constexpr (END == kLogitsGrad) {
-#pragma unroll
-                    for (int i = 0; i < 64; ++i) turned(start + c, x[i], i);
+                if constexpr (END == kLoss) {
+                    pick(start + c, x);
+                    sum_up(x);
+                } else {
+                    if (END == kLogitsGrad) turn(start + c, x);
+                    put_64(A, buffer, to, start + c, END == kLogitsGrad ? 1.f : scale, x);
                 }
-                put_64(A, buffer, to, start + c, END == kLogitsGrad ? 1.f : scale, x);
             }
         }
 #pragma unroll(END == kLoss ? COLS / 32 : 1)

@@ -172,39 +172,43 @@ struct RowsArgs {
     int64_t n_tokens, n_rows, width, ld;  // ld: of the tokens' rows
     int32_t top_k, experts;
     int32_t lanes;                      // to a row (a power of two), the others take the next rows
+    bool wide;                          // a CTA to a row instead: its warps share the columns
 };
 
-// Eight elements of a row: side by side, as one or two 16-byte accesses; or one access each, `stride` apart, so that the lanes of a row access
+// Eight elements of a row: side by side, as one or two 16-byte accesses; or one access each, 32 apart, so that the lanes of a warp access
 // neighbours (`n`: elements from the first to the row's end).
 template <bool F32, bool VEC>
 struct Piece {
     float x[8];
-    __device__ __forceinline__ void read(const void *p, int64_t i, int n, int stride) {
+    __device__ __forceinline__ void read(const void *p, int64_t i, int n) {
         if constexpr (VEC) {
             const Vec8<F32> v = load8_cached<F32>(p, i);
 #pragma unroll
             for (int k = 0; k < 8; ++k) x[k] = v.at(k);
         } else {
+            p = elem_ptr<F32>(p, i);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) x[k] = k * stride < n ? load1<F32>(p, i + k * stride) : 0.f;
+            for (int k = 0; k < 8; ++k) x[k] = k * 32 < n ? load1<F32>(p, k * 32) : 0.f;
         }
     }
-    __device__ __forceinline__ void write(void *p, int64_t i, int n, int stride) const {
+    __device__ __forceinline__ void write(void *p, int64_t i, int n) const {
         if constexpr (VEC) {
             store8<F32>(p, i, x);
         } else {
+            p = const_cast<char *>(elem_ptr<F32>(p, i));
 #pragma unroll
             for (int k = 0; k < 8; ++k)
-                if (k * stride < n) store1<F32>(p, i + k * stride, x[k]);
+                if (k * 32 < n) store1<F32>(p, k * 32, x[k]);
         }
     }
 };
 
-// A warp's first row and its share: `lanes` lanes to a row.
-#define SKEW_ROW_OF_LANES(total)                                                             \
-    const int lane = threadIdx.x & 31, in = lane & (A.lanes - 1);                            \
-    const int64_t per = 32 / A.lanes;                                                        \
-    const int64_t i = (blockIdx.x * int64_t(kWarps) + threadIdx.x / 32) * per + lane / A.lanes; \
+// A lane's row, of `total`; the first column of its first piece, and the columns from a piece to its next.
+#define SKEW_ROW_OF_LANES(total)                                                                                      \
+    const int lane = threadIdx.x & 31, in = A.wide ? int(threadIdx.x) : lane & (A.lanes - 1);                         \
+    const int64_t first = VEC ? in * 8 : (A.wide ? threadIdx.x / 32 * 256 : 0) + lane, step = (A.wide ? kThreads : A.lanes) * 8; \
+    const int64_t per = 32 / A.lanes;                                                                                 \
+    const int64_t i = A.wide ? blockIdx.x : (blockIdx.x * int64_t(kWarps) + threadIdx.x / 32) * per + lane / A.lanes; \
     const bool there = i < (total);
 
 // rows[place(t, j)] = x[t]; rows behind the last place: zeros.
@@ -214,22 +218,22 @@ __global__ void __launch_bounds__(kThreads) k_spread(const RowsArgs A) {
     if (!there) return;
     const int64_t used = A.offsets[A.experts];
     constexpr int kDeep = 4;
-    for (int64_t c0 = in * (VEC ? 8 : 1); c0 < A.width; c0 += int64_t(A.lanes) * 8 * kDeep) {
+    for (int64_t c0 = first; c0 < A.width; c0 += step * kDeep) {
         Piece<TF32, VEC> x[kDeep];
 #pragma unroll
         for (int q = 0; q < kDeep; ++q) {
-            const int64_t c = c0 + int64_t(q) * A.lanes * 8;
-            if (c < A.width) x[q].read(A.tokens, i * A.ld + c, int(A.width - c), A.lanes);
+            const int64_t c = c0 + q * step;
+            if (c < A.width) x[q].read(A.tokens, i * A.ld + c, int(A.width - c));
         }
         for (int j = 0; j < A.top_k; ++j) {
             const int64_t entry = i * A.top_k + j, place = A.places[entry];
             const bool put = place >= 0 && place < A.n_rows, clear = entry >= used;
 #pragma unroll
             for (int q = 0; q < kDeep; ++q) {
-                const int64_t c = c0 + int64_t(q) * A.lanes * 8;
+                const int64_t c = c0 + q * step;
                 if (c >= A.width) break;
-                if (put) reinterpret_cast<const Piece<RF32, VEC> &>(x[q]).write(A.out, place * A.width + c, int(A.width - c), A.lanes);
-                if (clear) Piece<RF32, VEC>{}.write(A.out, entry * A.width + c, int(A.width - c), A.lanes);
+                if (put) reinterpret_cast<const Piece<RF32, VEC> &>(x[q]).write(A.out, place * A.width + c, int(A.width - c));
+                if (clear) Piece<RF32, VEC>{}.write(A.out, entry * A.width + c, int(A.width - c));
             }
         }
     }
@@ -241,7 +245,7 @@ __global__ void __launch_bounds__(kThreads) k_combine(const RowsArgs A) {
     SKEW_ROW_OF_LANES(A.n_tokens)
     if (!there) return;
     constexpr int kDeep = 4;
-    for (int64_t c0 = in * (VEC ? 8 : 1); c0 < A.width; c0 += int64_t(A.lanes) * 8) {
+    for (int64_t c0 = first; c0 < A.width; c0 += step) {
         Piece<TF32, VEC> y{};
         const int n = int(A.width - c0);
         for (int j0 = 0; j0 < A.top_k; j0 += kDeep) {
@@ -254,14 +258,14 @@ __global__ void __launch_bounds__(kThreads) k_combine(const RowsArgs A) {
                 const bool put = place >= 0 && place < A.n_rows;
                 w[q] = put ? (A.weights ? A.weights[entry] : 1.f) : 0.f;
                 x[q] = {};
-                if (put) x[q].read(A.rows, place * A.width + c0, n, A.lanes);
+                if (put) x[q].read(A.rows, place * A.width + c0, n);
             }
 #pragma unroll
             for (int q = 0; q < kDeep; ++q)
 #pragma unroll
                 for (int k = 0; k < 8; ++k) y.x[k] = fmaf(w[q], x[q].x[k], y.x[k]);
         }
-        y.write(A.out, i * A.ld + c0, n, A.lanes);
+        y.write(A.out, i * A.ld + c0, n);
     }
 }
 
@@ -276,32 +280,39 @@ __global__ void __launch_bounds__(kThreads) k_combine_grad(const RowsArgs A) {
     float dot = 0.f;
     if (put || clear) {
         constexpr int kDeep = 2;
-        for (int64_t c0 = in * (VEC ? 8 : 1); c0 < A.width; c0 += int64_t(A.lanes) * 8 * kDeep) {
+        for (int64_t c0 = first; c0 < A.width; c0 += step * kDeep) {
             Piece<TF32, VEC> g[kDeep];
             Piece<RF32, VEC> x[kDeep];
 #pragma unroll
             for (int q = 0; q < kDeep; ++q) {
-                const int64_t c = c0 + int64_t(q) * A.lanes * 8;
+                const int64_t c = c0 + q * step;
                 if (!put || c >= A.width) break;
-                g[q].read(A.tokens, from + c, int(A.width - c), A.lanes);
-                x[q].read(A.rows, place * A.width + c, int(A.width - c), A.lanes);
+                g[q].read(A.tokens, from + c, int(A.width - c));
+                x[q].read(A.rows, place * A.width + c, int(A.width - c));
             }
 #pragma unroll
             for (int q = 0; q < kDeep; ++q) {
-                const int64_t c = c0 + int64_t(q) * A.lanes * 8;
+                const int64_t c = c0 + q * step;
                 if (c >= A.width) break;
-                if (clear) Piece<RF32, VEC>{}.write(A.out, i * A.width + c, int(A.width - c), A.lanes);
+                if (clear) Piece<RF32, VEC>{}.write(A.out, i * A.width + c, int(A.width - c));
                 if (!put) continue;
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     dot = fmaf(g[q].x[k], x[q].x[k], dot);
                     x[q].x[k] = w * g[q].x[k];
                 }
-                x[q].write(A.out, place * A.width + c, int(A.width - c), A.lanes);
+                x[q].write(A.out, place * A.width + c, int(A.width - c));
             }
         }
     }
     for (int d = A.lanes / 2; d; d >>= 1) dot += __shfl_xor_sync(kFullMask, dot, d);
+    if (A.wide) {
+        __shared__ float of_warp[kWarps];
+        if (!lane) of_warp[threadIdx.x / 32] = dot;
+        __syncthreads();
+        dot = 0.f;
+        for (int w = 0; w < kWarps; ++w) dot += of_warp[w];
+    }
     if (there && !in) A.dweights[i] = dot;
 }
 
@@ -341,9 +352,11 @@ Runs runs_of(int64_t n) {
 template <template <bool, bool, bool> class K>
 cudaError_t launch_rows(const skew_dispatch_config_t *c, RowsArgs &A, int64_t items, bool vec, cudaStream_t s) {
     A.lanes = 32;
-    while (A.lanes > 1 && int64_t(A.lanes) * 4 >= A.width) A.lanes >>= 1;
+    while (vec && A.lanes > 1 && int64_t(A.lanes) * 4 >= A.width) A.lanes >>= 1;
     const int64_t warps = (items + 32 / A.lanes - 1) / (32 / A.lanes);
-    const uint32_t grid = uint32_t((warps + kWarps - 1) / kWarps);
+    // few rows, of some width: a CTA to each (2 tokens of 10 rows of 5197 columns, combined: 72 us by a warp each)
+    A.wide = A.lanes == 32 && A.width > 512 && items <= int64_t(ops_sm_count()) * 4;
+    const uint32_t grid = uint32_t(A.wide ? items : (warps + kWarps - 1) / kWarps);
     auto run = [&](auto k) { return ops_launch(false, k, grid, kThreads, 0, s, A); };
     const bool t = c->flags & SKEW_DISPATCH_TOKENS_FP32, r = c->flags & SKEW_DISPATCH_ROWS_FP32;
     if (vec) return t ? (r ? run(K<true, true, true>::k) : run(K<true, false, true>::k)) : (r ? run(K<false, true, true>::k) : run(K<false, false, true>::k));
@@ -396,7 +409,7 @@ int skew_dispatch_spread(const skew_dispatch_config_t *c, const void *x, int64_t
         (rc = check_ptr("places", places, 4, tokens > 0)) || (rc = check_ptr("rows", rows, rf, tokens > 0)))
         return rc;
     if (!tokens) return SKEW_OK;
-    RowsArgs A{x, nullptr, rows, nullptr, nullptr, offsets, places, tokens, tokens * c->top_k, width, ld_x, c->top_k, c->experts, 0};
+    RowsArgs A{x, nullptr, rows, nullptr, nullptr, offsets, places, tokens, tokens * c->top_k, width, ld_x, c->top_k, c->experts, 0, false};
     return ops_cuda(launch_rows<Spread>(c, A, tokens, whole_units(c, width, ld_x, x, rows, nullptr), (cudaStream_t)stream), "k_spread");
 }
 
@@ -408,7 +421,7 @@ int skew_dispatch_combine(const skew_dispatch_config_t *c, const void *rows, con
         (rc = check_ptr("places", places, 4, tokens > 0)) || (rc = check_ptr("out", out, tf, tokens > 0)))
         return rc;
     if (!tokens) return SKEW_OK;
-    RowsArgs A{nullptr, rows, out, weights, nullptr, nullptr, places, tokens, tokens * c->top_k, width, ld_out, c->top_k, c->experts, 0};
+    RowsArgs A{nullptr, rows, out, weights, nullptr, nullptr, places, tokens, tokens * c->top_k, width, ld_out, c->top_k, c->experts, 0, false};
     return ops_cuda(launch_rows<Combine>(c, A, tokens, whole_units(c, width, ld_out, out, rows, nullptr), (cudaStream_t)stream), "k_combine");
 }
 
@@ -421,7 +434,7 @@ int skew_dispatch_combine_grad(const skew_dispatch_config_t *c, const void *dout
         (rc = check_ptr("drows", drows, rf, tokens > 0)) || (rc = check_ptr("dweights", dweights, 4, tokens > 0)))
         return rc;
     if (!tokens) return SKEW_OK;
-    RowsArgs A{dout, rows, drows, weights, dweights, offsets, places, tokens, tokens * c->top_k, width, ld_dout, c->top_k, c->experts, 0};
+    RowsArgs A{dout, rows, drows, weights, dweights, offsets, places, tokens, tokens * c->top_k, width, ld_dout, c->top_k, c->experts, 0, false};
     return ops_cuda(launch_rows<CombineGrad>(c, A, tokens * c->top_k, whole_units(c, width, ld_dout, dout, rows, drows), (cudaStream_t)stream), "k_combine_grad");
 }
 

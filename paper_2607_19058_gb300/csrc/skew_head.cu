@@ -65,10 +65,10 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_join(const JoinArgs A) {
         add(p);
     }
     constexpr float kLn2 = 0.693147180559945309417f;
-    const float lse = (top + log2f(sum)) * kLn2;
+    const float rest = log2f(sum);
     const int64_t v = A.wide ? static_cast<const int64_t *>(A.targets)[t] : static_cast<const int32_t *>(A.targets)[t];
-    A.lse[t] = lse;
-    A.loss[t] = v < 0 || v >= A.vocab ? 0.f : lse - A.picked[t];
+    A.lse[t] = (top + rest) * kLn2;
+    A.loss[t] = v < 0 || v >= A.vocab ? 0.f : (top - A.picked[t] + rest) * kLn2;  // (the difference first: nothing is lost where the target is the largest)
 }
 
 // What the gradients read of the activations: rows of padded tokens as zeros (whatever they hold then enters no gradient), on 16-byte boundaries;

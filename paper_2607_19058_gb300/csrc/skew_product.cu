@@ -323,11 +323,15 @@ struct Loose {
 #pragma unroll
         for (int i = 0; i < N / 4; ++i, p += four) {
             const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(p)) & 15;
-            const int have = i * 4 < lines ? int(off) + n * 2 : 0;  // bytes, from the line's first unit on
-            const bool there = lane % 8 * 16 < have && n > 0;
+            const bool there = i * 4 < lines && n > 0 && lane % 8 * 16 < int(off) + n * 2;
             copy_unit(to + i * 4 * kRawLine, there ? p - off + lane % 8 * 16 : any, there);
-            if (lane % 8 == 7) copy_unit(to + i * 4 * kRawLine + 16, have > 128 ? p - off + 128 : any, have > 128);
         }
+        // the ninth units, a line to a lane
+        const int line = lane % N;
+        const char *q = at + (four >> 2) * (line - lane / 8);
+        const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(q)) & 15;
+        const bool there = line - lane / 8 < lines && int(off) + n * 2 > 128;
+        copy_unit(raw + line * kRawLine + 128, there ? q - off + 128 : any, there);
     }
 
     static __device__ __forceinline__ void copy_unit(uint32_t to, const void *from, bool there) {
@@ -339,23 +343,32 @@ struct Loose {
         const int c = lane % 8, have = n - c * 8;
         raw += lane / 8 * kRawLine + c * 16;
         uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(at)) & 15;
+        constexpr int kDeep = 4;
 #pragma unroll
-        for (int i = 0; i < N / 4; ++i, off = (off + uint32_t(four)) & 15) {
-            const int L = from + i * 4 + lane / 8;
-            const uint4 a = *reinterpret_cast<const uint4 *>(raw + i * 4 * kRawLine), b = *reinterpret_cast<const uint4 *>(raw + i * 4 * kRawLine + 16);
-            uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        for (int i0 = 0; i0 < N / 4; i0 += kDeep) {
+            uint4 a[kDeep], b[kDeep];  // (all read before the first is stored: for the compiler a store might write what the next read reads)
 #pragma unroll
-            for (int k = 0; k < 6; ++k) w[k] = off & 8 ? w[k + 2] : w[k];
-#pragma unroll
-            for (int k = 0; k < 5; ++k) w[k] = off & 4 ? w[k + 1] : w[k];
-            const uint32_t turn = off & 2 ? 0x5432u : 0x3210u;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) w[k] = __byte_perm(w[k], w[k + 1], turn);
-            if (have < 8) {  // (what the units hold behind the line is not zeros)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) w[k] = have >= 2 * k + 2 ? w[k] : have == 2 * k + 1 ? w[k] & 0xFFFFu : 0u;
+            for (int i = 0; i < kDeep; ++i) {
+                a[i] = *reinterpret_cast<const uint4 *>(raw + (i0 + i) * 4 * kRawLine);
+                b[i] = *reinterpret_cast<const uint4 *>(raw + (i0 + i) * 4 * kRawLine + 16);
             }
-            *reinterpret_cast<uint4 *>(to + L * 128 + (c ^ (L & 7)) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+#pragma unroll
+            for (int i = 0; i < kDeep; ++i, off = (off + uint32_t(four)) & 15) {
+                const int L = from + (i0 + i) * 4 + lane / 8;
+                uint32_t w[8] = {a[i].x, a[i].y, a[i].z, a[i].w, b[i].x, b[i].y, b[i].z, b[i].w};
+#pragma unroll
+                for (int k = 0; k < 6; ++k) w[k] = off & 8 ? w[k + 2] : w[k];
+#pragma unroll
+                for (int k = 0; k < 5; ++k) w[k] = off & 4 ? w[k + 1] : w[k];
+                const uint32_t turn = off & 2 ? 0x5432u : 0x3210u;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[k] = __byte_perm(w[k], w[k + 1], turn);
+                if (have < 8) {  // (what the units hold behind the line is not zeros)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) w[k] = have >= 2 * k + 2 ? w[k] : have == 2 * k + 1 ? w[k] & 0xFFFFu : 0u;
+                }
+                *reinterpret_cast<uint4 *>(to + L * 128 + (c ^ (L & 7)) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
         }
     }
 };
@@ -605,7 +618,7 @@ __device__ __forceinline__ bool end_tile(const ProductArgs &A, char *buffer, con
         float p = 0.f;
 #pragma unroll
         for (int i = 0; i < N; ++i) p = picked == column + i ? x[i] : p;
-        A.picked[row] = p * A.scale;
+        A.picked[row] = p * scale2;
     };
     auto sum_up = [&](const float (&x)[64]) {  // LOSS: 64 logits, all there
         float far[4] = {x[0], x[1], x[2], x[3]}, part[4] = {};
@@ -1003,17 +1016,18 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
     if (warp == kMemWarp) give_tensor_memory(acc);
 }
 
-// out = base + scale * (the sum, in order, of a tile's shares), four columns to a thread.
+// out = base + scale * (the sum, in order, of a tile's shares), four columns to a thread. (Tiles that are cut are few: their elements' numbers fit 32 bits.)
 constexpr int kSumThreads = 256;
 
-__global__ void __launch_bounds__(kSumThreads) k_sum(const ProductArgs A, const int32_t splits, const int64_t height) {
+__global__ void __launch_bounds__(kSumThreads) k_sum(const ProductArgs A, const int32_t splits, const uint32_t height) {
     wait_launch_before();
     if (A.flags & kRelease) release_launch_after();
     const float scale = A.scale * peak_of(A.peaks);
-    const int64_t mt = (height + kTile - 1) / kTile, nt = (A.cols + kTile - 1) / kTile, fours = (A.cols + 3) / 4;
-    for (int64_t i = blockIdx.x * int64_t(kSumThreads) + threadIdx.x; i < A.groups * height * fours; i += int64_t(gridDim.x) * kSumThreads) {
-        const int64_t c = i % fours * 4, r = i / fours % height, g = i / fours / height;
-        const float4 *p = reinterpret_cast<const float4 *>(A.parts + ((g * mt + r / kTile) * nt + c / kTile) * splits * (kTile * kTile) + r % kTile * kTile + c % kTile);
+    const uint32_t mt = (height + kTile - 1) / kTile, nt = (uint32_t(A.cols) + kTile - 1) / kTile, fours = (uint32_t(A.cols) + 3) / 4, all = A.groups * height * fours;
+    for (uint32_t i = blockIdx.x * kSumThreads + threadIdx.x; i < all; i += gridDim.x * kSumThreads) {
+        const uint32_t q = i / fours, c = (i - q * fours) * 4, g = q / height, r = q - g * height;
+        const uint32_t unit = ((g * mt + r / kTile) * nt + c / kTile) * splits;
+        const float4 *p = reinterpret_cast<const float4 *>(A.parts + int64_t(unit) * (kTile * kTile) + r % kTile * kTile + c % kTile);
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
         for (int s = 0; s < splits; ++s) {
@@ -1024,7 +1038,7 @@ __global__ void __launch_bounds__(kSumThreads) k_sum(const ProductArgs A, const 
         const float v[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            if (c + k >= A.cols || (A.base == A.out && v[k] == 0.f)) continue;  // (in place: a matrix without rows is not touched)
+            if (c + k >= uint32_t(A.cols) || (A.base == A.out && v[k] == 0.f)) continue;  // (in place: a matrix without rows is not touched)
             const float b = !A.base ? 0.f : A.flags & kBase32 ? load1<true>(A.base, at + k) : load1<false>(A.base, at + k);
             const float y = A.base ? fmaf(v[k], scale, b) : v[k] * scale;
             if (A.flags & kOut32) store1<true>(A.out, at + k, y); else store1<false>(A.out, at + k, y);
@@ -1137,7 +1151,7 @@ cudaError_t launch_split(ProductArgs A, const CUtensorMap &a, const CUtensorMap 
     const cudaError_t e = launch_of<KIND, END, COPY>(P, a, b, few, s);
     if (e != cudaSuccess) return e;
     const int64_t blocks = (A.groups * height * ((A.cols + 3) / 4) + kSumThreads - 1) / kSumThreads;
-    return ops_launch(true, k_sum, uint32_t(blocks < sms() * 8 ? blocks : sms() * 8), kSumThreads, 0, s, A, shares, height);
+    return ops_launch(true, k_sum, uint32_t(blocks < sms() * 8 ? blocks : sms() * 8), kSumThreads, 0, s, A, shares, uint32_t(height));
 }
 
 template <int KIND, int END>

@@ -45,7 +45,7 @@ struct ProductArgs {
     int64_t first, vocab;       // the column j is the vocabulary's `first` + j
     const float *lse, *dloss;
     float2 *part;               // [part of a row][rows]: (largest, sum) in powers of two
-    float *picked;              // [rows]: the target's x
+    float *picked;              // [rows]: the target's x, in powers of two (x log2 e)
 };
 
 constexpr int kPeaks = 512;

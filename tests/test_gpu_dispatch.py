@@ -115,7 +115,7 @@ def _check(T, k, E, d, tok, row, kind, lay=None):
 
 
 @pytest.mark.parametrize("T,k,E,d", [(1, 1, 1, 1), (1, 2, 8, 64), (7, 3, 5, 5), (1000, 2, 8, 64), (129, 4, 127, 1001), (300, 8, 256, 512), (64, 64, 100, 24),
-                                     (50, 2, 128, 4096), (9, 5, 3, 8200), (5000, 1, 16, 9), (3000, 2, 4, 8)])
+                                     (50, 2, 128, 4096), (9, 5, 3, 8200), (5000, 1, 16, 9), (3000, 2, 4, 8), (2, 10, 16, 5197), (400, 2, 9, 1000)])
 @pytest.mark.parametrize("tok,row", [(BF16, BF16), (F32, BF16), (BF16, F32), (F32, F32)])
 def test_rows(T, k, E, d, tok, row):
     _check(T, k, E, d, tok, row, "even")

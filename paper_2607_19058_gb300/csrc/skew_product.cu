@@ -1,14 +1,20 @@
-// Matrix products on the fifth-generation tensor cores (skew_product.h): a persistent kernel whose warps load
-// (8 warps), multiply (one thread) and write out (4 warps) at the same time.
+// Matrix products on the fifth-generation tensor cores (skew_product.h): a persistent kernel whose warps bring operands, multiply (one thread)
+// and write out at the same time. A pair of CTAs shares a tile of 256 x 256: each holds half of either operand and gets the sums of its rows.
 //
 // A CTA brings 128 lines of A and 128 of B, 64 elements of each at a time (a stage of 32 KiB, in a ring of six), to shared
 // memory in 128-byte rows whose 16-byte units are permuted by the row's number (unit u of row L lies at u ^ (L & 7)), which is the layout that
 // tcgen05.mma reads without bank conflicts. The same layout serves both orders of an operand: lines along the summed index
-// ("K-major"), or 64 steps of the summed index, each a line along the tile ("MN-major"), 64 columns to a block of 8 KiB.
+// ("K-major"), or 64 steps of the summed index, each a line along the tile ("MN-major"), 64 columns to a block of 8 KiB. Lines on 16-byte boundaries come by tensor
+// copies that one thread asks for, others by eight warps (Loose), an operand at a time.
 // Sums stay in tensor memory in fp32, in two halves: the next tile is multiplied into one while the other is written out.
 //
-// Rows of the group behind this one, which a tile's last lines may hold, cost nothing: a row of C has its own row of A. Where the
-// rows are summed over (OUTER) they are zeros in shared memory, so that nothing of another group, NaN included, enters.
+// Rows of the group behind this one, which a tile's last lines may hold, cost nothing: a row of C has its own row of A (or, in a turned tile, column of its
+// own). Where the rows are summed over (OUTER) they are zeros in shared memory, so that nothing of another group, NaN included, enters.
+//
+// What bounds it. At the tensor cores' rate a CTA takes 64 bytes a clock from L2, as many as it can, and reads as many from shared memory, so that this is busy
+// throughout: 8192 x 4096 times 4096 x 16384 runs at 1.80 PFLOP/s in bursts (574 us without the logits' sums, 611 with; the library's product 2.05) and at what the power
+// limit leaves in a row (1.66). Tiles of few steps are bound by what becomes of their sums, some 3000 to 5500 clocks a tile; a tile of 512 rows to an expert
+// takes 4096 to multiply (the gradient of 128 matrices of 4096 x 4096 from 65,536 rows: 1.49 ms in bursts, 1.19 without writing out).
 #include "skew_product.h"
 
 #include <cuda.h>
@@ -531,16 +537,80 @@ __device__ __forceinline__ void put_32(const ProductArgs &A, char *buffer, const
         }
     } else {  // a row at a time, a column to a lane
         const int64_t at = to.at + column + lane;
-#pragma unroll 4
-        for (int r = 0; r < to.rows; ++r) {
-            const float y = *reinterpret_cast<const float *>(buffer + r * 128 + ((lane / 4) ^ (r & 7)) * 16 + lane % 4 * 4);
-            const int64_t e = at + r * to.ldo;
-            if (lane >= n) continue;
-            const float b = !A.base ? 0.f : b32 ? load1<true>(A.base, e) : load1<false>(A.base, e), z = A.base ? fmaf(y, scale, b) : y * scale;
-            if (o32) store1<true>(A.out, e, z); else store1<false>(A.out, e, z);
+        constexpr int kDeep = 16;
+        for (int r0 = 0; r0 < to.rows; r0 += kDeep) {
+            float b[kDeep];
+#pragma unroll
+            for (int i = 0; i < kDeep; ++i) {
+                b[i] = 0.f;
+                if (!A.base || lane >= n || r0 + i >= to.rows) continue;
+                b[i] = b32 ? load1<true>(A.base, at + (r0 + i) * to.ldo) : load1<false>(A.base, at + (r0 + i) * to.ldo);
+            }
+#pragma unroll
+            for (int i = 0; i < kDeep; ++i) {
+                const int r = r0 + i;
+                if (lane >= n || r >= to.rows) continue;
+                const float y = *reinterpret_cast<const float *>(buffer + r * 128 + ((lane / 4) ^ (r & 7)) * 16 + lane % 4 * 4), z = A.base ? fmaf(y, scale, b[i]) : y * scale;
+                if (o32) store1<true>(A.out, at + r * to.ldo, z); else store1<false>(A.out, at + r * to.ldo, z);
+            }
         }
     }
     __syncwarp();
+}
+
+// A tile of a group without rows: `width` (at most 128) columns of the base, which has the result's type T, as they are. By 16-byte units where both
+// tensors' rows lie alike in those, and the elements before the first and behind the last.
+template <typename T>
+__device__ __forceinline__ void copy_base(const ProductArgs &A, const Target &to, int column, int width) {
+    const int lane = threadIdx.x & 31;
+    const T *const base = static_cast<const T *>(A.base) + to.at + column;
+    T *const out = static_cast<T *>(A.out) + to.at + column;
+    constexpr int kUnit = 16 / sizeof(T);
+    if (A.flags & kOutVec && width % kUnit == 0) {
+        constexpr int kDeep = 8;
+        const int row = width / kUnit, all = to.rows * row;
+        for (int i0 = lane; i0 < all; i0 += 32 * kDeep) {
+            uint4 x[kDeep];
+#pragma unroll
+            for (int k = 0; k < kDeep; ++k) {
+                const int i = i0 + 32 * k, r = i / row;
+                if (i < all) x[k] = *reinterpret_cast<const uint4 *>(base + r * to.ldo + (i - r * row) * kUnit);
+            }
+#pragma unroll
+            for (int k = 0; k < kDeep; ++k) {
+                const int i = i0 + 32 * k, r = i / row;
+                if (i < all) store16(out + r * to.ldo + (i - r * row) * kUnit, x[k]);
+            }
+        }
+        return;
+    }
+    const bool alike = ((reinterpret_cast<uintptr_t>(base) ^ reinterpret_cast<uintptr_t>(out)) & 15) == 0;
+    constexpr int kDeep = 4;
+    for (int r0 = 0; r0 < to.rows; r0 += kDeep) {
+        uint4 x[kDeep];
+        T e[kDeep][4];
+#pragma unroll
+        for (int half = 0; half < 2; ++half)  // reads, then writes
+#pragma unroll
+            for (int k = 0; k < kDeep; ++k) {
+                if (r0 + k >= to.rows) continue;
+                const T *p = base + (r0 + k) * to.ldo;
+                T *q = out + (r0 + k) * to.ldo;
+                const int before = alike ? min(int((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / int(sizeof(T)), width) : width;
+                const int units = (width - before) / kUnit, behind = before + units * kUnit;
+                if (lane < units) {
+                    if (!half) x[k] = *reinterpret_cast<const uint4 *>(p + before + lane * kUnit); else store16(q + before + lane * kUnit, x[k]);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int c = lane + 32 * j, i = c < before ? c : behind + c - before;
+                    if (j && alike) break;
+                    if (i < width) {
+                        if (!half) e[k][j] = p[i]; else q[i] = e[k][j];
+                    }
+                }
+            }
+    }
 }
 
 __device__ __forceinline__ int64_t target_of(const ProductArgs &A, int64_t row) {  // -1: none
@@ -686,7 +756,9 @@ __device__ __forceinline__ bool end_tile(const ProductArgs &A, char *buffer, con
     const bool here = t.steps && !several;
     uint32_t acc = 0;
     if (here && !sums.wait(acc)) return false;
-    if (any) {
+    if (KIND == kOuter && END == kStore && !t.steps && A.base) {  // (through shared memory, 32 columns at a time, this took up to seven times a copy's time)
+        if (any && A.flags & kOut32) copy_base<uint32_t>(A, to, start, stop - start); else if (any) copy_base<uint16_t>(A, to, start, stop - start);
+    } else if (any) {
         int c = 0;
         if (here && (END == kLoss || (A.flags & kOutVec && !(A.flags & kOut32) && !A.base))) {
 #pragma unroll 1

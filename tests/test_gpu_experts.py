@@ -139,6 +139,26 @@ def test_matrices_off_16_bytes():
     assert torch.equal(op.grad(x, dy, o, base=off(w), out=off(torch.zeros_like(w))), dw)
 
 
+@pytest.mark.parametrize("grad", [BF16, F32])
+@pytest.mark.parametrize("m", [384, 392, 391, 130, 3])
+def test_the_base_of_experts_without_rows_stays_as_it_is(grad, m):
+    """Bit for bit, NaN and signed zeros among it, into another tensor, wherever the two start."""
+    E, n = 5, 300
+    loads = [0, 40, 0, 0, 7]
+    op, x, dy, o = S.Experts(E, n, m, grad_dtype=grad), _randn((47, n), 1), _randn((47, m), 2), _offsets(loads)
+    for skew in (0, 1):
+        store = torch.zeros(E * n * m + 1, dtype=grad, device="cuda")
+        base = store[skew:skew + E * n * m].view(E, n, m)
+        base.copy_(_randn((E, n, m), 3, grad))
+        base[0, ::7], base[2, 5], base[3, 299, m - 1] = -0.0, float("nan"), float("inf")
+        dw = op.grad(x, dy, o, base=base)
+        bits = torch.int16 if grad == BF16 else torch.int32
+        for e in (0, 2, 3):
+            assert torch.equal(dw[e].view(bits), base[e].view(bits))
+        want = base[1].double() + x[:40].double().t() @ dy[:40].double()
+        assert (dw[1].double() - want).norm() <= 2.0 ** -8 * want.norm()
+
+
 def test_infinities_and_nan_stay_in_their_rows():
     E, n, m = 2, 128, 96
     x, w, o = _randn((200, n), 1), _randn((E, n, m), 2), _offsets([90, 110])

@@ -79,7 +79,11 @@ int skew_experts_grad_rows(const skew_experts_config_t *c, const void *dy, int64
     return rc ? rc : by_rows(kGroupCols, c, dy, ld_dy, w, offsets, rows, dx, (cudaStream_t)stream);
 }
 
-size_t skew_experts_workspace_bytes(const skew_experts_config_t *c) { return check(c, 0, (const int32_t *)4) == SKEW_OK ? (product_parts_bytes() + 255) / 256 * 256 : 0; }
+size_t skew_experts_workspace_bytes(const skew_experts_config_t *c) {
+    if (check(c, 0, (const int32_t *)4) != SKEW_OK) return 0;
+    const size_t parts = product_parts_bytes(c->experts, c->n, c->m);
+    return parts ? parts : 256;
+}
 
 int skew_experts_grad(const skew_experts_config_t *c, const void *x, int64_t ld_x, const void *dy, int64_t ld_dy, const int32_t *offsets, int64_t rows,
                       const void *base, void *dw, void *workspace, size_t workspace_bytes, void *stream) {
@@ -93,7 +97,7 @@ int skew_experts_grad(const skew_experts_config_t *c, const void *x, int64_t ld_
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)
         return ops_fail(SKEW_EINVAL, "workspace must be 256-byte aligned and at least %zu bytes", need);
     ProductArgs A{};
-    A.parts = (float *)workspace;
+    A.parts = product_parts_bytes(c->experts, c->n, c->m) ? (float *)workspace : nullptr;
     A.a = x;
     A.b = dy;
     A.lda = ld_x;

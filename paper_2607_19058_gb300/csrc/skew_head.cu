@@ -152,7 +152,7 @@ struct Layout {
     int64_t parts, piece, pieces;
     size_t picked, loss_bytes;     // parts, then the picked logits
     int64_t ld;                    // of the activations' copy
-    size_t sums, tidy, peaks, shares, grad_bytes;  // a piece, dh's sums over the pieces, the copy, peaks, shares of tiles
+    size_t sums, tidy, peaks, shares, dh_parts, grad_bytes;  // a piece, dh's sums over the pieces, the copy, peaks, shares of tiles
 };
 
 Layout layout(const skew_head_config_t *c, int64_t tokens) {
@@ -171,7 +171,13 @@ Layout layout(const skew_head_config_t *c, int64_t tokens) {
     L.tidy = L.sums + (L.pieces > 1 ? whole(size_t(T) * c->width * 4) : 0);
     L.peaks = L.tidy + whole(size_t(T) * L.ld * 2);
     L.shares = L.peaks + whole(kPeaks * 4);
-    L.grad_bytes = L.shares + whole(product_parts_bytes());
+    // the parts of dh, and of dW's rows of a piece (the last may be shorter)
+    L.dh_parts = product_parts_bytes(1, T, c->width);
+    const int64_t rest = c->rows - (L.pieces - 1) * L.piece;
+    size_t parts = L.dh_parts;
+    for (const int64_t n : {L.piece, rest})
+        if (const size_t b = product_parts_bytes(1, n, c->width); b > parts) parts = b;
+    L.grad_bytes = L.shares + whole(parts);
     return L;
 }
 
@@ -280,7 +286,7 @@ int skew_head_grad(const skew_head_config_t *c, const void *h, int64_t ld_h, con
             H.cols = width;
             H.scale = c->scale;
             H.peaks = peaks;
-            H.parts = (float *)(ws + L.shares);
+            H.parts = L.dh_parts ? (float *)(ws + L.shares) : nullptr;
             H.base = first ? nullptr : ws + L.sums;
             H.out = last ? dh : ws + L.sums;
             H.ldo = c->width;
@@ -293,7 +299,7 @@ int skew_head_grad(const skew_head_config_t *c, const void *h, int64_t ld_h, con
         W.lda = L.piece;
         W.ldb = L.ld;
         W.peaks = tokens ? peaks : nullptr;
-        W.parts = (float *)(ws + L.shares);
+        W.parts = product_parts_bytes(1, n, c->width) ? (float *)(ws + L.shares) : nullptr;
         W.rows = tokens;
         W.groups = 1;
         W.inner = (int32_t)n;

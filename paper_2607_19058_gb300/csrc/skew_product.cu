@@ -1248,7 +1248,10 @@ cudaError_t launch(ProductArgs A, cudaStream_t s) {
 
 int32_t product_loss_columns() { return kPart; }
 
-size_t product_parts_bytes() { return size_t(kMostWaves) * (sms() / 2) * kTile * kTile * 4; }
+size_t product_parts_bytes(int64_t groups, int64_t height, int64_t cols) {
+    const int64_t tiles = groups * ((height + kTile - 1) / kTile) * ((cols + kTile - 1) / kTile), units = kMostWaves * (sms() / 2);
+    return tiles > 0 && 2 * tiles <= units ? size_t(units / tiles * tiles) * kTile * kTile * 4 : 0;
+}
 
 cudaError_t product_launch(ProductKind kind, ProductEnd end, const ProductArgs &A, cudaStream_t s) {
     if (end == kLoss) return launch<kByCols, kLoss>(A, s);

@@ -37,7 +37,7 @@ struct ProductArgs {
     const void *base;           // strides as out; may be out
     int64_t ldo, o_group;
     float scale;
-    float *parts;               // product_parts_bytes() for the sums of tiles that are cut along the summed index (OUTER, or one group); NULL: none is
+    float *parts;               // product_parts_bytes() for the sums of tiles that are cut along the summed index (STORE of OUTER or BY_ROWS); NULL: none is
     const float *peaks;         // kPeaks numbers that are not negative, or NULL. LOGITS_GRAD divides by the largest, STORE multiplies by it
     int32_t splits, chunk;      // set by product_launch: shares of the summed index; its steps between two additions outside of the tensor cores
     // LOSS, LOGITS_GRAD
@@ -50,7 +50,8 @@ struct ProductArgs {
 
 constexpr int kPeaks = 512;
 
-size_t product_parts_bytes();
+// Bytes for the parts of a result of `groups` matrices of height x cols (BY_ROWS: one, of rows x cols); 0 where its tiles are too many to be cut.
+size_t product_parts_bytes(int64_t groups, int64_t height, int64_t cols);
 // Columns of a LOSS part.
 int32_t product_loss_columns();
 // Runs the product on `stream`; every pointer, size and stride has been checked.

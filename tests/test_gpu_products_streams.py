@@ -74,6 +74,34 @@ def test_graphs_that_share_workspaces():
             assert all(torch.equal(x, y) for x, y in zip(got[k], want[k])) and len(junk) == 8
 
 
+def test_captured_behind_other_things_than_kernels():
+    """A product right behind a copy, a zero-fill, and what comes from another stream: in a graph as without."""
+    a = Set()
+    chosen, x, w, weights, table, targets, dloss = a.inputs(700)
+    order = a.d.order(chosen)
+    rows = a.d.spread(x, order)
+    want = a.e.product(rows, w, order[0]), a.h.loss(x, table, targets)[1]
+    into, side = torch.empty_like(rows), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        main = torch.cuda.current_stream()
+        into.copy_(rows)
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            h = x * 1
+            lse = a.h.loss(h, table, targets)[1]
+        y = a.e.product(into, w, order[0])
+        z = torch.zeros((1000, 1000), device="cuda")
+        main.wait_stream(side)
+        y2 = a.e.product(into, w, order[0])
+        z += 1
+    for _ in range(2):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want[0]) and torch.equal(y2, want[0]) and torch.equal(lse, want[1]) and (z == 1).all()
+
+
 def test_rows_behind_a_view_are_left_as_they_were():
     """Results go where they belong: out= tensors that lie inside a larger one."""
     a = Set()

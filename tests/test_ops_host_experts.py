@@ -170,3 +170,62 @@ def test_wrappers_refuse():
     head = S.HeadLoss(10, 8)
     with pytest.raises(ValueError):
         head.loss(x, torch.zeros((10, 8), dtype=BF16), torch.zeros(4, dtype=torch.int64))
+
+
+def test_workspaces_are_what_the_tiles_need():
+    """Matrices of many tiles are not cut along the rows, and keep nothing for it."""
+    assert S.skew_experts_workspace_bytes(S.ExpertsConfig(128, 4096, 4096, 0)) == 256
+    small = S.skew_experts_workspace_bytes(S.ExpertsConfig(1, 64, 64, 0))
+    assert 256 * 256 * 4 < small <= 100 << 20
+    assert S.skew_head_grad_workspace_bytes(S.HeadConfig(50304, 4096, 1.0, 0), 8192) < (512 << 20) + 8192 * 4096 * 6 + 8192
+
+
+def _fakes(monkeypatch):
+    from test_ops_host_streams import FakeTensor as F
+    launched, current = [], [0]
+    launch = lambda *a: launched.append(a) or 0  # noqa: E731
+    monkeypatch.setattr(torch.cuda, "device_count", lambda: 2)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    monkeypatch.setattr(S, "_raw_stream", lambda: lambda index: 100 + index)
+    monkeypatch.setattr(torch, "empty", lambda n, dtype=None, device=None: F((n,), dtype, torch.device(device).index))
+    d, e, h = S.Dispatch(8, 2), S.Experts(8, 16, 24), S.HeadLoss(50, 16)
+    for o in (d, e, h):
+        o._new = lambda shape, strides, dtype, device: F(shape, dtype, device.index)
+    d._order = d._spread = d._combine = d._combine_grad = e._product = e._grad_rows = e._grad = h._loss = h._grad = launch
+
+    def calls(i):
+        f = lambda shape, dtype=BF16: F(shape, dtype, i)  # noqa: E731
+        I, W = torch.int32, torch.float32
+        order, x, rows, w = (f((9,), I), f((5, 2), I)), f((5, 16)), f((10, 16)), f((5, 2), W)
+        dy, m, t, l = f((10, 24)), f((8, 16, 24)), f((5,), torch.int64), f((5,), W)
+        return [lambda: d.order(f((5, 2), I)), lambda: d.spread(x, order), lambda: d.combine(rows, w, order), lambda: d.combine_grad(x, rows, w, order),
+                lambda: e.product(rows, m, order[0]), lambda: e.grad_rows(dy, m, order[0]), lambda: e.grad(rows, dy, order[0]),
+                lambda: h.loss(x, f((50, 16)), t), lambda: h.grad(x, f((50, 16)), t, l, l)]
+    return launched, current, calls
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    launched, current, calls = _fakes(monkeypatch)
+    for k, call in enumerate(calls(0)):
+        call()
+        assert len(launched) == k + 1
+    launched.clear()
+    for call in calls(1):
+        with pytest.raises(ValueError, match="current device"):
+            call()
+    assert not launched
+    current[0] = 1
+    for call in calls(1):
+        call()
+    assert len(launched) == 9 and all(a[-1] == 101 for a in launched)
+
+
+def test_a_workspace_for_each_device(monkeypatch):
+    launched, current, calls = _fakes(monkeypatch)
+    at = {0: set(), 1: set()}
+    for k in range(6):
+        current[0] = i = k % 2
+        for call in (calls(i)[0], calls(i)[6], calls(i)[8]):
+            call()
+            at[i].add(launched[-1][-3])
+    assert len(at[0]) == len(at[1]) == 3 and not at[0] & at[1]

@@ -239,34 +239,51 @@ __global__ void __launch_bounds__(kThreads) k_spread(const RowsArgs A) {
     }
 }
 
-// out[t] = sum over j of weights[t, j] * rows[place(t, j)]
-template <bool TF32, bool RF32, bool VEC>
-__global__ void __launch_bounds__(kThreads) k_combine(const RowsArgs A) {
-    SKEW_ROW_OF_LANES(A.n_tokens)
-    if (!there) return;
-    constexpr int kDeep = 4;
-    for (int64_t c0 = first; c0 < A.width; c0 += step) {
-        Piece<TF32, VEC> y{};
-        const int n = int(A.width - c0);
-        for (int j0 = 0; j0 < A.top_k; j0 += kDeep) {
-            Piece<RF32, VEC> x[kDeep];
-            float w[kDeep];
+// out[t] = sum over j of weights[t, j] * rows[place(t, j)]: kRows rows at a time, of kPieces pieces of columns.
+template <bool TF32, bool RF32, bool VEC, int kRows, int kPieces>
+__device__ __forceinline__ void combine(const RowsArgs &A, int64_t i, int64_t first, int64_t step) {
+    for (int64_t c0 = first; c0 < A.width; c0 += step * kPieces) {
+        Piece<TF32, VEC> y[kPieces] = {};
+        for (int j0 = 0; j0 < A.top_k; j0 += kRows) {
+            Piece<RF32, VEC> x[kRows][kPieces];
+            float w[kRows];
 #pragma unroll
-            for (int q = 0; q < kDeep; ++q) {
+            for (int q = 0; q < kRows; ++q) {
                 const int64_t entry = i * A.top_k + j0 + q;
                 const int64_t place = j0 + q < A.top_k ? A.places[entry] : -1;
                 const bool put = place >= 0 && place < A.n_rows;
                 w[q] = put ? (A.weights ? A.weights[entry] : 1.f) : 0.f;
-                x[q] = {};
-                if (put) x[q].read(A.rows, place * A.width + c0, n);
+#pragma unroll
+                for (int p = 0; p < kPieces; ++p) {
+                    const int64_t c = c0 + p * step;
+                    x[q][p] = {};
+                    if (put && c < A.width) x[q][p].read(A.rows, place * A.width + c, int(A.width - c));
+                }
             }
 #pragma unroll
-            for (int q = 0; q < kDeep; ++q)
+            for (int q = 0; q < kRows; ++q)
 #pragma unroll
-                for (int k = 0; k < 8; ++k) y.x[k] = fmaf(w[q], x[q].x[k], y.x[k]);
+                for (int p = 0; p < kPieces; ++p)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) y[p].x[k] = fmaf(w[q], x[q][p].x[k], y[p].x[k]);
         }
-        y.write(A.out, i * A.ld + c0, n);
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) {
+            const int64_t c = c0 + p * step;
+            if (c < A.width) y[p].write(A.out, i * A.ld + c, int(A.width - c));
+        }
     }
+}
+
+template <bool TF32, bool RF32, bool VEC>
+__global__ void __launch_bounds__(kThreads) k_combine(const RowsArgs A) {
+    SKEW_ROW_OF_LANES(A.n_tokens)
+    if (!there) return;
+    // Four rows' loads under way, or two rows' of two pieces: with one or two experts a token, half of them would be none.
+    if (A.top_k <= 2)
+        combine<TF32, RF32, VEC, 2, 2>(A, i, first, step);
+    else
+        combine<TF32, RF32, VEC, 4, 1>(A, i, first, step);
 }
 
 // drows[place] = weights[t, j] * dout[t], dweights[t, j] = <dout[t], rows[place]>; an entry (t, j) to `lanes` lanes.

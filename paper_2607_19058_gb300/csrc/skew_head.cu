@@ -84,6 +84,7 @@ struct TidyArgs {
     float *peaks;
     int64_t tokens, vocab, width, ld, ld_out;
     bool wide, vec;
+    bool as_is;  // the loss: only the boundaries
 };
 
 __global__ void __launch_bounds__(kTidyThreads) k_tidy(const TidyArgs A) {
@@ -94,9 +95,9 @@ __global__ void __launch_bounds__(kTidyThreads) k_tidy(const TidyArgs A) {
     const int64_t shares = (A.ld_out + kTidyCols - 1) / kTidyCols;
     for (int64_t i = blockIdx.x * int64_t(kTidyThreads / 32) + warp; i < A.tokens * shares; i += int64_t(gridDim.x) * (kTidyThreads / 32)) {
         const int64_t t = i / shares, c0 = i % shares * kTidyCols + lane * 8;
-        const int64_t v = A.wide ? static_cast<const int64_t *>(A.targets)[t] : static_cast<const int32_t *>(A.targets)[t];
+        const int64_t v = A.as_is ? 0 : A.wide ? static_cast<const int64_t *>(A.targets)[t] : static_cast<const int32_t *>(A.targets)[t];
         const bool there = v >= 0 && v < A.vocab;
-        if (there && c0 == 0) peak = fmaxf(peak, fabsf(A.dloss[t]));
+        if (there && c0 == 0 && !A.as_is) peak = fmaxf(peak, fabsf(A.dloss[t]));
         const uint16_t *from = A.h + t * A.ld;
         uint4 u[kTidyCols / 256];
 #pragma unroll
@@ -117,6 +118,7 @@ __global__ void __launch_bounds__(kTidyThreads) k_tidy(const TidyArgs A) {
         for (int j = 0; j < kTidyCols / 256; ++j)
             if (c0 + j * 256 < A.ld_out) *reinterpret_cast<uint4 *>(A.out + t * A.ld_out + c0 + j * 256) = u[j];
     }
+    if (A.as_is) return;
     if (!lane) of_warp[warp] = peak;
     __syncthreads();
     if (threadIdx.x) return;
@@ -150,7 +152,7 @@ size_t whole(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
 struct Layout {
     int64_t parts, piece, pieces;
-    size_t picked, loss_bytes;     // parts, then the picked logits
+    size_t picked, copy, loss_bytes;  // parts, then the picked logits, and the activations' copy
     int64_t ld;                    // of the activations' copy
     size_t sums, tidy, peaks, shares, dh_parts, grad_bytes;  // a piece, dh's sums over the pieces, the copy, peaks, shares of tiles
 };
@@ -160,14 +162,15 @@ Layout layout(const skew_head_config_t *c, int64_t tokens) {
     const int64_t T = tokens ? tokens : 1, wide = product_loss_columns();
     L.parts = (c->rows + wide - 1) / wide;
     L.picked = whole(size_t(T) * L.parts * 8);
-    L.loss_bytes = L.picked + whole(size_t(T) * 4);
+    L.ld = (c->width + 7) / 8 * 8;
+    L.copy = L.picked + whole(size_t(T) * 4);
+    L.loss_bytes = L.copy + whole(size_t(T) * L.ld * 2);
     int64_t most = kPieceBytes / (2 * T) / kPieceCols * kPieceCols;
     if (most < kPieceCols) most = kPieceCols;
     L.pieces = (c->rows + most - 1) / most;
     L.piece = ((c->rows + L.pieces - 1) / L.pieces + kPieceCols - 1) / kPieceCols * kPieceCols;
     L.pieces = (c->rows + L.piece - 1) / L.piece;
     L.sums = whole(size_t(T) * L.piece * 2);
-    L.ld = (c->width + 7) / 8 * 8;
     L.tidy = L.sums + (L.pieces > 1 ? whole(size_t(T) * c->width * 4) : 0);
     L.peaks = L.tidy + whole(size_t(T) * L.ld * 2);
     L.shares = L.peaks + whole(kPeaks * 4);
@@ -179,6 +182,11 @@ Layout layout(const skew_head_config_t *c, int64_t tokens) {
         if (const size_t b = product_parts_bytes(1, n, c->width); b > parts) parts = b;
     L.grad_bytes = L.shares + whole(parts);
     return L;
+}
+
+cudaError_t launch_tidy(const TidyArgs &A, cudaStream_t s) {
+    const int64_t blocks = (A.tokens * ((A.ld_out + kTidyCols - 1) / kTidyCols) + kTidyThreads / 32 - 1) / (kTidyThreads / 32);
+    return ops_launch(false, k_tidy, uint32_t(blocks < kPeaks ? blocks : kPeaks), kTidyThreads, 0, s, A);
 }
 
 bool units(int64_t width, const void *p) { return width % 8 == 0 && ((uintptr_t)p & 15) == 0; }
@@ -207,10 +215,15 @@ int skew_head_loss(const skew_head_config_t *c, const void *h, int64_t ld_h, con
     if (!tokens) return SKEW_OK;
     char *ws = (char *)workspace;
     cudaStream_t s = (cudaStream_t)stream;
+    // Activations off 16-byte boundaries come from a copy: the table alone is then cut out of its lines (2314 tokens, 311 x 3149: 103 us without).
+    const bool copy = !units(c->width, h) || ld_h % 8;
+    if (copy && (rc = ops_cuda(launch_tidy({(const uint16_t *)h, (uint16_t *)(ws + L.copy), targets, nullptr, nullptr, tokens, c->rows, c->width, ld_h, L.ld, wide, false, true}, s),
+                               "k_tidy")))
+        return rc;
     ProductArgs A{};
-    A.a = h;
+    A.a = copy ? (const void *)(ws + L.copy) : h;
     A.b = table;
-    A.lda = ld_h;
+    A.lda = copy ? L.ld : ld_h;
     A.ldb = c->width;
     A.rows = tokens;
     A.groups = 1;
@@ -246,9 +259,8 @@ int skew_head_grad(const skew_head_config_t *c, const void *h, int64_t ld_h, con
     const uint16_t *const tidy = (const uint16_t *)(ws + L.tidy);
     if (tokens) {
         const TidyArgs A{(const uint16_t *)h, (uint16_t *)(ws + L.tidy), targets, dloss, peaks, tokens, c->rows, c->width, ld_h, L.ld, wide,
-                         units(c->width, h) && ld_h % 8 == 0};
-        const int64_t blocks = (tokens * ((L.ld + kTidyCols - 1) / kTidyCols) + kTidyThreads / 32 - 1) / (kTidyThreads / 32);
-        if ((rc = ops_cuda(ops_launch(false, k_tidy, uint32_t(blocks < kPeaks ? blocks : kPeaks), kTidyThreads, 0, s, A), "k_tidy"))) return rc;
+                         units(c->width, h) && ld_h % 8 == 0, false};
+        if ((rc = ops_cuda(launch_tidy(A, s), "k_tidy"))) return rc;
     }
     for (int64_t v0 = 0; v0 < c->rows; v0 += L.piece) {
         const int64_t n = c->rows - v0 < L.piece ? c->rows - v0 : L.piece;

@@ -175,3 +175,24 @@ def test_rows_past_2_31_elements():
             assert torch.equal(rows[int(order[1][t, j])], x[t])
     y = op.combine(rows, None, order)
     assert torch.equal(y, (2 * x.float()).to(BF16))
+
+
+def test_gradients_by_differences():
+    """spread and combine are linear in each argument, so that a difference along a direction is the result for the direction: what it
+    makes of dy is what the gradient makes of the direction, within the roundings of 2^-24 that either takes of the terms' magnitudes (fewer than 100)."""
+    T, k, E, d = 90, 3, 7, 50
+    op = S.Dispatch(E, k, token_dtype=F32, row_dtype=F32)
+    order = op.order(_chosen("outside", T, k, E))
+    x, u, dy = (_randn((T, d), F32, s) for s in (1, 2, 3))
+    rows, r, drows = (_randn((T * k, d), F32, s) for s in (4, 5, 6))
+    w, v = (torch.rand((T, k), device="cuda", generator=_gen(s)) for s in (7, 8))
+    kept = int(order[0][-1])
+    for t in (r, drows):
+        t[kept:] = 0
+    dr, dw = op.combine_grad(dy, rows, w, order)
+    dot = lambda a, b: (a.double() * b.double()).sum()  # noqa: E731
+    size = lambda a, b: (a.double() * b.double()).abs().sum()  # noqa: E731
+    there = order[1] >= 0
+    for a, b in (((op.spread(u, order), drows), (u, op.combine(drows, None, order))), ((op.combine(r, w, order), dy), (dr, r)),
+                 ((op.combine(rows, v, order), dy), (dw, torch.where(there, v, 0.0)))):
+        assert abs(float(dot(*a) - dot(*b))) <= 100 * 2.0 ** -24 * float(size(*a) + size(*b)) * k

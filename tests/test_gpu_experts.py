@@ -214,6 +214,17 @@ def test_a_long_sum():
     _check([70001], 72, 136)
 
 
+@pytest.mark.parametrize("loads,n,m", [([70001], 73, 137), ([9000, 0, 20001], 264, 520), ([300, 0, 7], 3001, 40), ([500], 41, 5000), ([3], 9000, 24)])
+def test_long_sums_in_fp32(loads, n, m):
+    """Sums that are taken out of the tensor cores several times, of lines on 16-byte boundaries and off them: as near as fp32 is, however long."""
+    _check(loads, n, m, F32, F32, base=True, behind=1)
+    x, w, o = _randn((sum(loads), n), 1).abs(), _randn((len(loads), n, m), 2).abs(), _offsets(loads)
+    y = S.Experts(len(loads), n, m, row_dtype=F32).product(x, w, o)
+    want = torch.cat([x[o[e]:o[e + 1]].double() @ w[e].double() for e in range(len(loads))])
+    # 32 additions of 16 products each, rounded down by at most 2^-23 of a sum that grows to its size, so by half of that on average; then n / 512 of 2^-24
+    assert float((y.double() - want).norm()) <= (32 * 2.0 ** -24 + n / 512 * 2.0 ** -24) * float(want.norm())
+
+
 def test_a_wait_that_gives_up_is_reported_once():
     op = S.Experts(2, 64, 64)
     x, w, o = _randn((100, 64), 1), _randn((2, 64, 64), 2), _offsets([40, 60])

@@ -206,7 +206,7 @@ struct Piece {
 // A lane's row, of `total`; the first column of its first piece, and the columns from a piece to its next.
 #define SKEW_ROW_OF_LANES(total)                                                                                      \
     const int lane = threadIdx.x & 31, in = A.wide ? int(threadIdx.x) : lane & (A.lanes - 1);                         \
-    const int64_t first = VEC ? in * 8 : (A.wide ? threadIdx.x / 32 * 256 : 0) + lane, step = (A.wide ? kThreads : A.lanes) * 8; \
+    const int64_t first = VEC ? in * 8 : A.wide ? threadIdx.x / 32 * 256 + lane : in, step = (A.wide ? kThreads : A.lanes) * 8; \
     const int64_t per = 32 / A.lanes;                                                                                 \
     const int64_t i = A.wide ? blockIdx.x : (blockIdx.x * int64_t(kWarps) + threadIdx.x / 32) * per + lane / A.lanes; \
     const bool there = i < (total);
@@ -361,7 +361,7 @@ Runs runs_of(int64_t n) {
 template <template <bool, bool, bool> class K>
 cudaError_t launch_rows(const skew_dispatch_config_t *c, RowsArgs &A, int64_t items, bool vec, cudaStream_t s) {
     A.lanes = 32;
-    while (vec && A.lanes > 1 && int64_t(A.lanes) * 4 >= A.width) A.lanes >>= 1;
+    while (A.lanes > 1 && (vec ? int64_t(A.lanes) * 4 >= A.width : A.lanes / 2 >= A.width)) A.lanes >>= 1;  // (one access each: a piece's first element alone is there)
     const int64_t warps = (items + 32 / A.lanes - 1) / (32 / A.lanes);
     // few rows, of some width: a CTA to each (2 tokens of 10 rows of 5197 columns, combined: 72 us by a warp each)
     A.wide = A.lanes == 32 && A.width > 512 && items <= int64_t(ops_sm_count()) * 4;

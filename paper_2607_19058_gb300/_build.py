@@ -15,7 +15,8 @@ INCLUDE = os.path.join(ROOT, "include")
 
 SOURCES = ["skew_host.cpp", "skew_kernels.cu", "skew_noalloc.cu", "skew_ops.cpp", "skew_clip.cu", "skew_gate.cu",
            "skew_embed.cu", "skew_dispatch.cu", "skew_product.cu", "skew_experts.cpp", "skew_head.cu"]
-HEADERS = [os.path.join(CSRC, "skew_plan.h"), os.path.join(CSRC, "skew_ops.h"), os.path.join(CSRC, "skew_product.h"), os.path.join(INCLUDE, "skewadam.h")]
+HEADERS = [os.path.join(CSRC, "skew_plan.h"), os.path.join(CSRC, "skew_ops.h"), os.path.join(CSRC, "skew_product.h"), os.path.join(CSRC, "skew_lines.h"),
+           os.path.join(INCLUDE, "skewadam.h")]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall",
               "-I", INCLUDE, "-I", CSRC] + ARCH

@@ -21,12 +21,13 @@
 
 #include <atomic>
 
+#include "skew_lines.h"
 #include "skew_ops.h"
 
 namespace skew {
 namespace {
 
-constexpr int kLines = 128;                    // of each operand, in a CTA's stage
+constexpr int kLines = kOperandLines;
 constexpr int kStep = 64;                      // elements of the summed index in a stage
 constexpr uint32_t kOperandBytes = kLines * kStep * 2;
 constexpr uint32_t kStageBytes = 2 * kOperandBytes;
@@ -64,7 +65,6 @@ struct Shared {
 };
 
 constexpr int kOutBytes = 32 * 128;            // 32 rows of 128 bytes, of each warp that writes out
-constexpr int kRawLine = 144;                  // a line of 64 elements that starts anywhere, by 16-byte units
 constexpr size_t kMaxSharedBytes = 232448;
 constexpr size_t shared_bytes(int stages, size_t raw, int groups) {
     return 1024 + size_t(stages) * kStageBytes + raw + size_t(kEndWarps) * kOutBytes + sizeof(Shared) + size_t(groups + 1) * 8;
@@ -292,52 +292,13 @@ struct Walk {
 // that is there, so that no access leaves the units of the matrix itself.)
 constexpr int kLooseLines = (2 * kLines) / kLoadWarps;  // of a warp, of one operand, where both are loaded; half of that of each operand's lines where one is
 
-// A warp's `N` of an operand's 128 lines of a tile's stages, from line `from` on, eight lanes to a line. MAJOR: lines along the summed index, numbered l0 on, of which
-// those before l_end are there; a stage is 64 elements, from s0 on, before s_end. Else two blocks of 64 lines, one for each step of the summed index (s0 on, before
-// s_end), of elements from l0 (and l0 + 64), before l_end; a stage is 64 lines.
+// Those lines (skew_lines.h), to the warp's own memory and from there to a stage.
 template <bool MAJOR, int N>
-struct Loose {
-    const char *at;         // the lane's first line, in this stage
-    int64_t four, stage;    // bytes from a line to the lane's next, and to the next stage
-    int lines, n;           // that are there from the lane's first line on, and elements of a line
-    int left;               // of the summed index
-
-    __device__ __forceinline__ Loose(const uint16_t *p, int64_t ld, int64_t l0, int64_t l_end, int64_t s0, int64_t s_end, int from, int lane) {
-        const int64_t mine = from % (MAJOR ? kLines : 64) + lane / 8, elem = MAJOR ? s0 : l0 + from / 64 * 64;
-        at = reinterpret_cast<const char *>(p + ((MAJOR ? l0 : s0) + mine) * ld + elem);
-        four = ld * 8;
-        stage = MAJOR ? 128 : ld * 128;
-        left = int(min(max(s_end - s0, int64_t(0)), int64_t(1 << 30)));
-        if (MAJOR) {
-            lines = int(min(max(l_end - l0 - mine, int64_t(0)), int64_t(N)));
-            n = min(left, 64);
-        } else {
-            lines = left - int(mine);
-            n = int(min(max(l_end - elem, int64_t(0)), int64_t(64)));
-        }
-    }
-
-    __device__ __forceinline__ void next() {
-        at += stage;
-        left -= 64;
-        if (MAJOR) n = max(min(left, 64), 0); else lines -= 64;
-    }
+struct Loose : Lines<MAJOR, N> {
+    using Lines<MAJOR, N>::Lines;
 
     __device__ __forceinline__ void ask(uint32_t raw, const void *any, int lane) const {
-        const uint32_t to = raw + lane / 8 * kRawLine + lane % 8 * 16;
-        const char *p = at;
-#pragma unroll
-        for (int i = 0; i < N / 4; ++i, p += four) {
-            const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(p)) & 15;
-            const bool there = i * 4 < lines && n > 0 && lane % 8 * 16 < int(off) + n * 2;
-            copy_unit(to + i * 4 * kRawLine, there ? p - off + lane % 8 * 16 : any, there);
-        }
-        // the ninth units, a line to a lane
-        const int line = lane % N;
-        const char *q = at + (four >> 2) * (line - lane / 8);
-        const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(q)) & 15;
-        const bool there = line - lane / 8 < lines && int(off) + n * 2 > 128;
-        copy_unit(raw + line * kRawLine + 128, there ? q - off + 128 : any, there);
+        this->units(lane, [&](uint32_t to, const char *from, bool there) { copy_unit(raw + to, there ? from : any, there); });
     }
 
     static __device__ __forceinline__ void copy_unit(uint32_t to, const void *from, bool there) {
@@ -346,9 +307,9 @@ struct Loose {
 
     // To lines `from` on of the stage.
     __device__ __forceinline__ void cut(const char *raw, char *to, int from, int lane) const {
-        const int c = lane % 8, have = n - c * 8;
+        const int c = lane % 8, have = this->n - c * 8;
         raw += lane / 8 * kRawLine + c * 16;
-        uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(at)) & 15;
+        uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(this->at)) & 15;
         constexpr int kDeep = 4;
 #pragma unroll
         for (int i0 = 0; i0 < N / 4; i0 += kDeep) {
@@ -359,7 +320,7 @@ struct Loose {
                 b[i] = *reinterpret_cast<const uint4 *>(raw + (i0 + i) * 4 * kRawLine + 16);
             }
 #pragma unroll
-            for (int i = 0; i < kDeep; ++i, off = (off + uint32_t(four)) & 15) {
+            for (int i = 0; i < kDeep; ++i, off = (off + uint32_t(this->four)) & 15) {
                 const int L = from + (i0 + i) * 4 + lane / 8;
                 uint32_t w[8] = {a[i].x, a[i].y, a[i].z, a[i].w, b[i].x, b[i].y, b[i].z, b[i].w};
 #pragma unroll

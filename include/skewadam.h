@@ -610,7 +610,8 @@ int skew_experts_grad(const skew_experts_config_t *c, const void *x, int64_t ld_
  *   p[t, v] = dloss[t] * (exp(l[t, v] - lse[t]) - [v = target_t])
  * A target outside [0, rows) is padding: its loss is zero, its dloss is not read, and neither it nor its h, NaN included, enters a gradient. h, W, dh, base and dW
  * are bf16. l is summed in fp32 and never stored; the gradients take the vocabulary in pieces and make a piece's p from l anew, rounded to bf16 (for the
- * tensor cores: an error of up to 2^-8 of each term, about that of rounding the result), with sums in fp32. Results do not depend on timing.
+ * tensor cores: an error of up to 2^-8 of each term, about that of rounding the result), with sums in fp32. Both sum l alike, so that at a target that is nearly
+ * certain exp(l - lse) - 1 is off by fp32's rounding of lse alone besides (some 2^-22 of its size). Results do not depend on timing.
  */
 #define SKEW_HEAD_IDS_64 1u /* targets are int64 (else int32) */
 

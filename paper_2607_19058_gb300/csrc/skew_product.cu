@@ -1149,7 +1149,9 @@ cudaError_t launch_of(const ProductArgs &A, const CUtensorMap &a, const CUtensor
 }
 
 // Steps between two additions outside of the tensor cores: 512 products (an error of 5e-7 of the result); 1024 (9e-7) for logits, of which an epilogue makes more
-// (at 4096 columns 597 us for 8192 x 16384 of them, 619 with 512, 574 with all); 8192 (8e-6) where bf16 is made of it.
+// (at 4096 columns 597 us for 8192 x 16384 of them, 619 with 512, 574 with all); 8192 (8e-6) where bf16 is made of it. The logits that the gradient makes anew
+// are summed as the loss's are, though bf16 is made of them too: their bits are then the same, and an error that lse and a logit share leaves exp(l - lse), which
+// is subtracted from 1 at a certain target (l = 60, 8192 columns: 4e-4 of dloss with 8192 products, where nothing should be left).
 constexpr int kChunk32 = 512 / kStep, kChunkLoss = 1024 / kStep, kChunk16 = 8192 / kStep;
 
 constexpr int kMostWaves = 4;  // of shares: what their sums' memory is sized for
@@ -1191,7 +1193,7 @@ template <int KIND, int END>
 cudaError_t launch(ProductArgs A, cudaStream_t s) {
     CUtensorMap a{}, b{}, few{};
     A.splits = 1;
-    A.chunk = END == kLoss ? kChunkLoss : END == kStore && A.flags & kOut32 ? kChunk32 : kChunk16;
+    A.chunk = END != kStore ? kChunkLoss : A.flags & kOut32 ? kChunk32 : kChunk16;
     constexpr bool A_MAJOR = kMajorA<KIND>, B_MAJOR = kMajorB<KIND>, TURNED = kTurned<KIND>, OUTER = KIND == kOuter;
     // lines of an operand: how long, how many, in how many groups, and in a copy
     const int64_t long_a = TURNED && !A_MAJOR ? A.cols : A.inner, lines_a = TURNED ? (A_MAJOR ? A.cols : A.inner) : A.rows, groups_a = TURNED ? A.groups : 1;

@@ -42,7 +42,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_join(const JoinArgs A) {
         float high = top;
 #pragma unroll
         for (int j = 0; j < kDeep; ++j) high = fmaxf(high, p[j].x);
-        const float from = high == -INFINITY ? 0.f : high;
+        const float from = fabsf(high) < INFINITY ? high : 0.f;  // (as the parts)
         sum *= exp2f(top - from);
 #pragma unroll
         for (int j = 0; j < kDeep; ++j) sum = fmaf(p[j].y, exp2f(p[j].x - from), sum);

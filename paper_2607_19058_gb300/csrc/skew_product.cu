@@ -427,6 +427,9 @@ __device__ __forceinline__ float exp2_of(float x) {
     return y;
 }
 
+// What a row's logits are taken off before their exponentials: an infinite one would make NaN of itself.
+__device__ __forceinline__ float finite_or_0(float x) { return fabsf(x) < INFINITY ? x : 0.f; }
+
 __device__ __forceinline__ void store16(void *p, uint4 u) {
     asm volatile("st.global.v4.u32 [%0], {%1,%2,%3,%4};" ::"l"(p), "r"(u.x), "r"(u.y), "r"(u.z), "r"(u.w) : "memory");
 }
@@ -662,7 +665,7 @@ __device__ __forceinline__ bool end_tile(const ProductArgs &A, char *buffer, con
             for (int i = 4; i < 64; ++i) far[i % 4] = fminf(far[i % 4], x[i]);
             far[0] = fminf(fminf(far[0], far[1]), fminf(far[2], far[3]));
         }
-        const float most = fmaxf(top, far[0] * scale2), from = most == -INFINITY ? 0.f : most;
+        const float most = fmaxf(top, far[0] * scale2), from = finite_or_0(most);
 #pragma unroll
         for (int i = 0; i < 64; ++i) part[i % 4] += exp2_of(fmaf(x[i], scale2, -from));
         sum = fmaf(sum, exp2_of(top - from), (part[0] + part[1]) + (part[2] + part[3]));
@@ -680,7 +683,7 @@ __device__ __forceinline__ bool end_tile(const ProductArgs &A, char *buffer, con
                 x[i] = i < n ? x[i] * scale2 : -INFINITY;
                 high[i % 4] = fmaxf(high[i % 4], x[i]);
             }
-            const float most = fmaxf(fmaxf(high[0], high[1]), fmaxf(high[2], high[3])), from = most == -INFINITY ? 0.f : most;
+            const float most = fmaxf(fmaxf(high[0], high[1]), fmaxf(high[2], high[3])), from = finite_or_0(most);
 #pragma unroll
             for (int i = 0; i < 32; ++i) part[i % 4] += exp2_of(x[i] - from);
             sum = fmaf(sum, exp2_of(top - from), (part[0] + part[1]) + (part[2] + part[3]));

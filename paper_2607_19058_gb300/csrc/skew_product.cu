@@ -645,6 +645,10 @@ __device__ __forceinline__ bool end_tile(const ProductArgs &A, char *buffer, con
         }
 #pragma unroll
         for (int i = 0; i < N; ++i) x[i] *= g;
+        if (target < 0) {  // (padding: its zeros times an infinity of the table are NaN)
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i] = 0.f;
+        }
     };
     auto pick = [&](int column, const auto &x) {  // LOSS: the target's logit
         constexpr int N = sizeof(x) / 4;

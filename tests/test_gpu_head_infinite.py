@@ -59,3 +59,25 @@ def test_infinities_of_both_signs():
     assert (lse == INF).all() and (loss == INF).all()
     loss, lse = S.HeadLoss(V, d).loss(h, w, torch.full_like(targets, 2))   # a target without probability
     assert (lse == INF).all() and (loss == INF).all()
+
+
+@pytest.mark.parametrize("T,V,d", [(50, 600, 32), (70, 337, 65), (300, 700, 2048)])
+def test_padding_enters_no_gradient_of_a_table_with_infinities(T, V, d):
+    """Rows of the table that no token's target may be (-Inf times what is positive): none has a probability, and padded tokens add nothing to the table's gradient,
+    whatever they hold."""
+    h, w, targets = _inputs(T, V, d)
+    w[V // 2:, 0] = -INF
+    targets %= V // 2
+    targets[::3] = -1
+    h[::6] = float("nan")
+    there = targets >= 0
+    op = S.HeadLoss(V, d)
+    _, lse = op.loss(h, w, targets)
+    dloss = torch.rand(T, device="cuda", generator=torch.Generator(device="cuda").manual_seed(2)) + 0.5
+    dloss[~there] = float("nan")
+    dw = op.grad(h, w, targets, lse, dloss)[1]
+    assert dw.isfinite().all() and (dw[V // 2:] == 0).all()
+    kept = op.grad(h[there], w, targets[there], lse[there].contiguous(), dloss[there])[1]
+    # the same terms, added up in another order: sums of up to T, each rounded to bf16
+    size = (torch.softmax(h[there].double() @ w[: V // 2].double().t(), 1) + torch.nn.functional.one_hot(targets[there], V // 2)).t() @ (h[there].double() * 1.5)
+    assert ((dw[: V // 2].double() - kept[: V // 2].double()).abs() <= 2.0 ** -7 * kept[: V // 2].double().abs() + T * 2.0 ** -22 * size).all()

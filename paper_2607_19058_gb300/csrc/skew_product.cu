@@ -1079,6 +1079,11 @@ __global__ void __launch_bounds__(kSumThreads) k_sum(const ProductArgs A, const 
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             if (c + k >= uint32_t(A.cols) || (A.base == A.out && v[k] == 0.f)) continue;  // (in place: a matrix without rows is not touched)
+            if (A.base && v[k] == 0.f && bool(A.flags & kOut32) == bool(A.flags & kBase32)) {  // (nor are its bits changed on the way to another tensor)
+                if (A.flags & kOut32) static_cast<uint32_t *>(A.out)[at + k] = static_cast<const uint32_t *>(A.base)[at + k];
+                else static_cast<uint16_t *>(A.out)[at + k] = static_cast<const uint16_t *>(A.base)[at + k];
+                continue;
+            }
             const float b = !A.base ? 0.f : A.flags & kBase32 ? load1<true>(A.base, at + k) : load1<false>(A.base, at + k);
             const float y = A.base ? fmaf(v[k], scale, b) : v[k] * scale;
             if (A.flags & kOut32) store1<true>(A.out, at + k, y); else store1<false>(A.out, at + k, y);

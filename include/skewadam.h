@@ -644,7 +644,7 @@ int skew_head_grad(const skew_head_config_t *c, const void *h, int64_t ld_h, con
  * given up since the last such call (SKEW_ETIMEOUT; what that call wrote is then not to be used). Errors: also SKEW_ECUDA.
  */
 int skew_ops_sync_status(void *stream);
-/* Self-test of that: enqueues one such wait, for what nothing completes; it gives up after some two seconds. Errors: SKEW_ECUDA. */
+/* Self-test of that: enqueues one such wait, for what nothing completes; it gives up after some four seconds. Errors: SKEW_ECUDA. */
 int skew_ops_selftest_wait_timeout(void *stream);
 
 #ifdef __cplusplus

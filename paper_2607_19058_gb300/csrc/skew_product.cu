@@ -59,6 +59,7 @@ struct Shared {
     uint64_t full[kStages], empty[kStages], landed[kStages], sums[2], freed[2];
     uint32_t acc;                     // where the sums are in tensor memory
     uint32_t gave_up;
+    uint32_t asked;                   // OUTER: stages that copies were asked for
     int32_t total[32];
     int32_t begin[1];                 // [groups + 1]: first row of each group, and the end of the last; then
                                       // [groups + 1]: tiles of rows before it (BY_ROWS, BY_COLS)
@@ -121,13 +122,18 @@ __device__ __forceinline__ bool bar_poll(uint64_t *b, uint32_t parity) {
     return ok != 0;
 }
 
-// False once this or another of the CTA's waits has given up, after some two seconds: the kernel then ends as it stands and
-// leaves its mark for skew_ops_sync_status.
-__device__ __forceinline__ bool bar_wait(uint64_t *b, uint32_t parity, Shared &S) {
+// False once this or another of the CTA's waits has given up, after some four seconds: the kernel then ends as it stands and
+// leaves its mark for skew_ops_sync_status. A wait that may be for much later, at any step of the work before it, is given a count of those steps: its four
+// seconds start anew with each.
+__device__ __forceinline__ bool bar_wait(uint64_t *b, uint32_t parity, Shared &S, const uint32_t *progress = nullptr) {
     if (bar_poll(b, parity)) return true;
+    uint32_t seen = 0;
     for (uint32_t i = 0; i < 1u << 20; ++i) {
         if (bar_poll(b, parity)) return true;
         if (*reinterpret_cast<volatile uint32_t *>(&S.gave_up)) return false;
+        if (!progress) continue;
+        const uint32_t now = *reinterpret_cast<const volatile uint32_t *>(progress);
+        if (now != seen) seen = now, i = 0;
     }
     *reinterpret_cast<volatile uint32_t *>(&S.gave_up) = 1;
     atomicOr(&g_status, 1u);
@@ -135,9 +141,9 @@ __device__ __forceinline__ bool bar_wait(uint64_t *b, uint32_t parity, Shared &S
 }
 
 // One lane waits for its warp.
-__device__ __forceinline__ bool warp_wait(uint64_t *b, uint32_t parity, Shared &S) {
+__device__ __forceinline__ bool warp_wait(uint64_t *b, uint32_t parity, Shared &S, const uint32_t *progress = nullptr) {
     bool ok = true;
-    if ((threadIdx.x & 31) == 0) ok = bar_wait(b, parity, S);
+    if ((threadIdx.x & 31) == 0) ok = bar_wait(b, parity, S, progress);
     return __shfl_sync(kFullMask, ok, 0);
 }
 
@@ -921,7 +927,7 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) bar_init(&S.full[i], 2 * ((COPY ? 1 : 0) + (COPY == 3 ? 0 : kLoadWarps))), bar_init(&S.empty[i], 1), bar_init(&S.landed[i], 1);
         for (int i = 0; i < 2; ++i) bar_init(&S.sums[i], 1), bar_init(&S.freed[i], 2 * kEndWarps);
-        S.gave_up = 0;
+        S.gave_up = S.asked = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (COPY && threadIdx.x == 32 * kCopyWarp) {
@@ -958,6 +964,7 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
                     // The last lines of a group that ends within a stage go to the warp that clears what is behind them.
                     const bool cut = KIND == kOuter && s0 + kStep > t.r1;
                     const uint32_t to = shared_address(ring) + p.s * kStageBytes, bar = cut ? shared_address(&S.landed[p.s]) : in_first(&S.full[p.s]);
+                    if (KIND == kOuter) *reinterpret_cast<volatile uint32_t *>(&S.asked) = n + 1;
                     bar_expect(bar, (rows ? kOperandBytes : 0) + (COPY_B ? half * 128 : 0));
                     if (rows) copy_lines<A_MAJOR>(map_a, to, bar, m0, s0, TURNED ? t.group : 0);
                     if (COPY_B && TURNED && half < kLines) {
@@ -979,7 +986,8 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
             n = (n + t.steps) % stages;
             if (!left) continue;
             const uint32_t s = n ? n - 1 : stages - 1;
-            if (!(ok = warp_wait(&S.landed[s], phases >> s & 1, S))) break;
+            // (all groups before this one may have whole stages, for as long as they take)
+            if (!(ok = warp_wait(&S.landed[s], phases >> s & 1, S, &S.asked))) break;
             phases ^= 1u << s;
             char *const at = ring + s * kStageBytes;
             for (int i = left * 8 + lane; i < kStep * 8; i += 32)  // 16-byte units of a block's lines

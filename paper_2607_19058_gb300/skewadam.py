@@ -863,10 +863,22 @@ class Router:
 class _Workspace:
     """Device memory that an object's calls share, one block for each device: it grows, and what a graph or another stream may still use is kept."""
 
-    __slots__ = ("blocks", "kept")
+    __slots__ = ("blocks", "kept", "sizes")
 
     def __init__(self):
-        self.blocks, self.kept = {}, []
+        self.blocks, self.kept, self.sizes = {}, [], {}
+
+    def size(self, dev, call, ask):
+        """What ``ask()`` says that a call needs on a device (how many SMs that has enters), remembered for a thousand calls; none is refused."""
+        need = self.sizes.get((dev.index, call))
+        if need is None:
+            need = ask()
+            if not need:
+                raise SkewError(SKEW_EINVAL, skew_ops_last_error())
+            if len(self.sizes) >= 1024:
+                self.sizes.clear()
+            self.sizes[dev.index, call] = need
+        return need
 
     def get(self, dev, need: int, handle: int) -> int:
         ws = self.blocks.get(dev.index)
@@ -920,7 +932,7 @@ class Dispatch:
         L = load()
         self._order, self._spread, self._combine, self._combine_grad = L.skew_dispatch_order, L.skew_dispatch_spread, L.skew_dispatch_combine, L.skew_dispatch_combine_grad
         self._stream, self._elsewhere = _raw_stream(), _device_check()
-        self._workspace, self._sizes = _Workspace(), {}
+        self._workspace = _Workspace()
 
     def _there(self, t, dtype, shape, dev, what: str) -> int:
         if not (t.dtype is dtype and t.shape == shape and t.is_contiguous() and (t.is_cuda if dev is None else t.device == dev)):
@@ -960,12 +972,7 @@ class Dispatch:
         p = self._there(chosen, self._i32, (T, self.top_k), None, "chosen")
         if self._elsewhere:
             self._elsewhere(dev)
-        need = self._sizes.get(T)
-        if need is None:
-            need = self._sizes[T] = skew_dispatch_workspace_bytes(self.config, T)
-            if not need:
-                del self._sizes[T]
-                raise SkewError(SKEW_EINVAL, skew_ops_last_error())
+        need = self._workspace.size(dev, T, lambda: skew_dispatch_workspace_bytes(self.config, T))
         handle = self._stream(dev.index)
         ws = self._workspace.get(dev, need, handle)
         offsets = self._new((self.experts + 1,), (1,), self._i32, dev)
@@ -1043,8 +1050,7 @@ class Experts:
         self.config = ExpertsConfig(experts, n, m, (EXPERTS_ROWS_FP32 if self.row_dtype == torch.float32 else 0) |
                                     (EXPERTS_GRAD_FP32 if self.grad_dtype == torch.float32 else 0))
         self._ref, self._new = C.byref(self.config), _allocator()
-        self._ws_bytes = skew_experts_workspace_bytes(self.config)
-        if not self._ws_bytes:
+        if not skew_experts_workspace_bytes(self.config):
             raise SkewError(SKEW_EINVAL, skew_ops_last_error())
         self._shape = (experts, n, m)
         self._bf16, self._i32 = torch.bfloat16, torch.int32
@@ -1111,8 +1117,8 @@ class Experts:
             p = out.data_ptr()
         else:
             p = self._matrices(out, self.grad_dtype, dev, "out")
-        handle = self._stream(dev.index)
-        rc = self._grad(self._ref, x.data_ptr(), ld, dy.data_ptr(), ldd, o, x.shape[0], b, p, self._workspace.get(dev, self._ws_bytes, handle), self._ws_bytes, handle)
+        need, handle = self._workspace.size(dev, None, lambda: skew_experts_workspace_bytes(self.config)), self._stream(dev.index)
+        rc = self._grad(self._ref, x.data_ptr(), ld, dy.data_ptr(), ldd, o, x.shape[0], b, p, self._workspace.get(dev, need, handle), need, handle)
         if rc:
             _check_op(rc)
         return out
@@ -1142,10 +1148,10 @@ class HeadLoss:
         if not skew_head_loss_workspace_bytes(self.config[torch.int32], 0):
             raise SkewError(SKEW_EINVAL, skew_ops_last_error())
         self._ref = {dt: C.byref(c) for dt, c in self.config.items()}
-        self._shape, self._bf16, self._f32 = (rows, width), torch.bfloat16, torch.float32
+        self._shape, self._bf16, self._f32, self._i32 = (rows, width), torch.bfloat16, torch.float32, torch.int32
         self._new, self._loss, self._grad = _allocator(), load().skew_head_loss, load().skew_head_grad
         self._stream, self._elsewhere = _raw_stream(), _device_check()
-        self._workspace, self._sizes = _Workspace(), {}
+        self._workspace = _Workspace()
 
     def _table(self, t, dev, what: str) -> int:
         if not (t.dtype == self._bf16 and t.shape == self._shape and t.is_contiguous() and t.device == dev):
@@ -1172,14 +1178,9 @@ class HeadLoss:
 
     def _space(self, T, dev, handle: int, which: int):
         """The workspace, of what the loss (0) or its gradients (1) need."""
-        need = self._sizes.get(T)
-        if need is None:
-            c = next(iter(self.config.values()))
-            need = skew_head_loss_workspace_bytes(c, T), skew_head_grad_workspace_bytes(c, T)
-            if not need[0]:
-                raise SkewError(SKEW_EINVAL, skew_ops_last_error())
-            self._sizes[T] = need
-        return self._workspace.get(dev, need[which], handle), need[which]
+        of = skew_head_grad_workspace_bytes if which else skew_head_loss_workspace_bytes
+        need = self._workspace.size(dev, (T, which), lambda: of(self.config[self._i32], T))
+        return self._workspace.get(dev, need, handle), need
 
     def loss(self, h, table, targets, stream=None):
         """(loss, lse), fp32 (T,): each token's loss, and the logarithm of its sum of exponentials, which ``grad`` takes.

@@ -528,61 +528,6 @@ __device__ __forceinline__ void put_32(const ProductArgs &A, char *buffer, const
     __syncwarp();
 }
 
-// A tile of a group without rows: `width` (at most 128) columns of the base, which has the result's type T, as they are. By 16-byte units where both
-// tensors' rows lie alike in those, and the elements before the first and behind the last.
-template <typename T>
-__device__ __forceinline__ void copy_base(const ProductArgs &A, const Target &to, int column, int width) {
-    const int lane = threadIdx.x & 31;
-    const T *const base = static_cast<const T *>(A.base) + to.at + column;
-    T *const out = static_cast<T *>(A.out) + to.at + column;
-    constexpr int kUnit = 16 / sizeof(T);
-    if (A.flags & kOutVec && width % kUnit == 0) {
-        constexpr int kDeep = 8;
-        const int row = width / kUnit, all = to.rows * row;
-        for (int i0 = lane; i0 < all; i0 += 32 * kDeep) {
-            uint4 x[kDeep];
-#pragma unroll
-            for (int k = 0; k < kDeep; ++k) {
-                const int i = i0 + 32 * k, r = i / row;
-                if (i < all) x[k] = *reinterpret_cast<const uint4 *>(base + r * to.ldo + (i - r * row) * kUnit);
-            }
-#pragma unroll
-            for (int k = 0; k < kDeep; ++k) {
-                const int i = i0 + 32 * k, r = i / row;
-                if (i < all) store16(out + r * to.ldo + (i - r * row) * kUnit, x[k]);
-            }
-        }
-        return;
-    }
-    const bool alike = ((reinterpret_cast<uintptr_t>(base) ^ reinterpret_cast<uintptr_t>(out)) & 15) == 0;
-    constexpr int kDeep = 4;
-    for (int r0 = 0; r0 < to.rows; r0 += kDeep) {
-        uint4 x[kDeep];
-        T e[kDeep][4];
-#pragma unroll
-        for (int half = 0; half < 2; ++half)  // reads, then writes
-#pragma unroll
-            for (int k = 0; k < kDeep; ++k) {
-                if (r0 + k >= to.rows) continue;
-                const T *p = base + (r0 + k) * to.ldo;
-                T *q = out + (r0 + k) * to.ldo;
-                const int before = alike ? min(int((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / int(sizeof(T)), width) : width;
-                const int units = (width - before) / kUnit, behind = before + units * kUnit;
-                if (lane < units) {
-                    if (!half) x[k] = *reinterpret_cast<const uint4 *>(p + before + lane * kUnit); else store16(q + before + lane * kUnit, x[k]);
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int c = lane + 32 * j, i = c < before ? c : behind + c - before;
-                    if (j && alike) break;
-                    if (i < width) {
-                        if (!half) e[k][j] = p[i]; else q[i] = e[k][j];
-                    }
-                }
-            }
-    }
-}
-
 __device__ __forceinline__ int64_t target_of(const ProductArgs &A, int64_t row) {  // -1: none
     const int64_t v = A.flags & kIds64 ? static_cast<const int64_t *>(A.targets)[row] : static_cast<const int32_t *>(A.targets)[row];
     return v < 0 || v >= A.vocab ? -1 : v;
@@ -730,9 +675,7 @@ __device__ __forceinline__ bool end_tile(const ProductArgs &A, char *buffer, con
     const bool here = t.steps && !several;
     uint32_t acc = 0;
     if (here && !sums.wait(acc)) return false;
-    if (KIND == kOuter && END == kStore && !t.steps && A.base) {  // (through shared memory, 32 columns at a time, this took up to seven times a copy's time)
-        if (any && A.flags & kOut32) copy_base<uint32_t>(A, to, start, stop - start); else if (any) copy_base<uint16_t>(A, to, start, stop - start);
-    } else if (any) {
+    if (any) {
         int c = 0;
         if (here && (END == kLoss || (A.flags & kOutVec && !(A.flags & kOut32) && !A.base))) {
 #pragma unroll 1
@@ -1050,7 +993,7 @@ __global__ void __launch_bounds__(kThreads<COPY>, 1) k_product(const __grid_cons
         Sums sums{S, {}, acc + (TURNED ? 0 : col0) + (uint32_t(q * 32) << 16)};
         const float peak = END == kLoss ? 1.f : peak_of(A.peaks);
         while (ok && walk.next(t)) {
-            if (!t.steps && KIND == kOuter && A.base == A.out) continue;
+            if (!t.steps && KIND == kOuter && A.base) continue;  // (there already, or k_keep's)
             if constexpr (TURNED)
                 ok = end_turned<KIND>(A, t, rank * kLines + q * 32, col0 / kEndCols, sums);
             else
@@ -1095,6 +1038,64 @@ __global__ void __launch_bounds__(kSumThreads) k_sum(const ProductArgs A, const 
             const float b = !A.base ? 0.f : A.flags & kBase32 ? load1<true>(A.base, at + k) : load1<false>(A.base, at + k);
             const float y = A.base ? fmaf(v[k], scale, b) : v[k] * scale;
             if (A.flags & kOut32) store1<true>(A.out, at + k, y); else store1<false>(A.out, at + k, y);
+        }
+    }
+}
+
+// The matrices of groups without rows stay as the base has them, bit for bit, in another tensor of its type: each one run of memory in both, copied in 16-byte
+// units where both lie alike in those, and the elements before the first and behind the last. (By the warps that write out tiles this was slower for every call: the
+// registers that it needed went to and from memory in each tile. The gradient of 65,536 rows took 143 us, 104 now, by one expert of 1024 x 1024, and 1942, 1878 now, by 128 of
+// 4096 x 4096; that of 20 rows by 60 experts onto an fp32 base 270, 245 now, of 1304 x 1304, and 915, 376 now, of 1300 x 1301. A call whose experts all have rows pays 2 us.)
+constexpr int kKeepThreads = 256, kKeepDeep = 8, kKeepBytes = kKeepThreads * kKeepDeep * 16;  // of a CTA at a time
+
+template <typename T>
+__global__ void __launch_bounds__(kKeepThreads) k_keep(const ProductArgs A, const int64_t size /* elements of a matrix */) {
+    __shared__ __align__(16) char memory[sizeof(Shared) + (kMaxGroups + 1) * 8];
+    Shared &S = *reinterpret_cast<Shared *>(memory);
+    wait_launch_before();
+    release_launch_after();
+    groups_of<kOuter, kKeepThreads>(A, S);
+    const int64_t shares = (size * int64_t(sizeof(T)) + kKeepBytes - 1) / kKeepBytes, all = shares * A.groups;
+    for (int64_t u = blockIdx.x; u < all;) {
+        const int64_t g = u / shares, first = (u - g * shares) * kKeepBytes / int64_t(sizeof(T));
+        if (S.begin[g] != S.begin[g + 1]) {  // on to the next group
+            u += ((g + 1) * shares - u + gridDim.x - 1) / gridDim.x * gridDim.x;
+            continue;
+        }
+        u += gridDim.x;
+        const T *const p = static_cast<const T *>(A.base) + g * A.o_group;
+        T *const q = static_cast<T *>(A.out) + g * A.o_group;
+        constexpr int kUnit = 16 / sizeof(T);
+        if (((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(q)) & 15) == 0) {
+            const int64_t before = min(int64_t(-(reinterpret_cast<uintptr_t>(p) / sizeof(T)) & (kUnit - 1)), size), units = (size - before) / kUnit;
+            uint4 x[kKeepDeep];
+#pragma unroll
+            for (int k = 0; k < kKeepDeep; ++k) {
+                const int64_t i = first / kUnit + k * kKeepThreads + threadIdx.x;
+                if (i < units) x[k] = ld_stream(p + before + i * kUnit);
+            }
+#pragma unroll
+            for (int k = 0; k < kKeepDeep; ++k) {
+                const int64_t i = first / kUnit + k * kKeepThreads + threadIdx.x;
+                if (i < units) st_stream(q + before + i * kUnit, x[k]);
+            }
+            const int64_t rest = threadIdx.x, i = rest < before ? rest : units * kUnit + rest;
+            if (!first && i < size && rest < 2 * kUnit) q[i] = p[i];
+        } else {
+#pragma unroll 1
+            for (int64_t i0 = first; i0 < first + kKeepBytes / int(sizeof(T)) && i0 < size; i0 += kKeepThreads * kKeepDeep) {
+                T x[kKeepDeep];
+#pragma unroll
+                for (int k = 0; k < kKeepDeep; ++k) {
+                    const int64_t i = i0 + k * kKeepThreads + threadIdx.x;
+                    if (i < size) x[k] = p[i];
+                }
+#pragma unroll
+                for (int k = 0; k < kKeepDeep; ++k) {
+                    const int64_t i = i0 + k * kKeepThreads + threadIdx.x;
+                    if (i < size) q[i] = x[k];
+                }
+            }
         }
     }
 }
@@ -1194,7 +1195,14 @@ cudaError_t launch_split(ProductArgs A, const CUtensorMap &a, const CUtensorMap 
     const int64_t height = KIND == kOuter ? A.inner : A.rows, mt = (height + kTile - 1) / kTile, nt = (A.cols + kTile - 1) / kTile, tiles = mt * nt * A.groups;
     const int64_t steps = KIND == kOuter ? (A.rows + int64_t(kStep) * A.groups - 1) / (int64_t(kStep) * A.groups) : (A.inner + kStep - 1) / kStep;
     const int shares = END == kStore && A.parts ? shares_of(tiles, steps, sms() / 2) : 1;
-    if (shares == 1) return launch_of<KIND, END, COPY>(A, a, b, few, s);
+    if (shares == 1) {
+        if (KIND == kOuter && A.base && A.base != A.out && (A.offsets || !A.rows)) {
+            const int64_t size = A.inner * A.ldo, ctas = (size * (A.flags & kOut32 ? 4 : 2) + kKeepBytes - 1) / kKeepBytes * A.groups, most = sms() * 8;
+            const cudaError_t e = ops_launch(true, A.flags & kOut32 ? k_keep<uint32_t> : k_keep<uint16_t>, uint32_t(ctas < most ? ctas : most), kKeepThreads, 0, s, A, size);
+            if (e != cudaSuccess) return e;
+        }
+        return launch_of<KIND, END, COPY>(A, a, b, few, s);
+    }
     ProductArgs P = A;
     P.splits = shares;
     P.out = A.parts;

@@ -593,7 +593,7 @@ typedef struct {
 int skew_experts_product(const skew_experts_config_t *c, const void *x, int64_t ld_x, const void *w, const int32_t *offsets, int64_t rows, void *y, void *stream);
 int skew_experts_grad_rows(const skew_experts_config_t *c, const void *dy, int64_t ld_dy, const void *w, const int32_t *offsets, int64_t rows, void *dx,
                            void *stream);
-/* Bytes of device workspace that skew_experts_grad needs, for any number of rows (0 for an invalid config). */
+/* Bytes of device workspace that skew_experts_grad needs, for any number of rows (0 for an invalid config); how many SMs the current device has enters. */
 size_t skew_experts_workspace_bytes(const skew_experts_config_t *c);
 /*
  * base: NULL, a tensor like dW that overlaps nothing else, or dW itself, to which the gradient is then added; matrices of experts without rows are
@@ -622,7 +622,10 @@ typedef struct {
     uint32_t flags; /* SKEW_HEAD_* */
 } skew_head_config_t;
 
-/* Bytes of device workspace that the loss, or its gradients, of `tokens` tokens (0 to 2^24) need (0 for an invalid config). */
+/*
+ * Bytes of device workspace that the loss, or its gradients, of `tokens` tokens (0 to 2^24) need (0 for an invalid config). Room for a copy of h is among them: the loss
+ * makes it of rows off 16-byte boundaries alone. How many SMs the current device has enters the gradients'.
+ */
 size_t skew_head_loss_workspace_bytes(const skew_head_config_t *c, int64_t tokens);
 size_t skew_head_grad_workspace_bytes(const skew_head_config_t *c, int64_t tokens);
 /*

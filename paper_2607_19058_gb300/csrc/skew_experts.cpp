@@ -29,10 +29,12 @@ int check_ptr(const char *what, const void *p, uintptr_t es, bool needed) {
     return SKEW_OK;
 }
 
-// Rows of an expert, on average, from which on `product` takes the rows as a tile's rows, 256 at a time, instead of its columns, 64 at a time. (The matrices, whose lines
-// lie across the summed index, are the slower operand of a tile's rows; but half a tile is wasted, and a tile of few rows takes longer to write out. 128 experts of 4096 x
-// 4096, uneven loads, us for 64, 128, 256, 384 and 512 rows each: 740, 788, 1077, 1413, 1765 straight, 669, 723, 1047, 1438, 1834 turned. grad_rows, whose lines lie
-// along it, is turned always: 1774 straight, 1795 turned at 512, and 46 against 23 for 17 rows of 164 experts of 1648 x 128.)
+// Rows of an expert, on average over all experts (those without rows too: what each has is known on the device alone), from which on `product` takes the rows as a
+// tile's rows, 256 at a time, instead of its columns, 64 at a time. (The matrices, whose lines lie across the summed index, are the slower operand of a tile's rows; but half a
+// tile is wasted, and a tile of few rows takes longer to write out. us straight / turned for 64, 128, 256, 384 and 512 rows each, uneven loads: 128 experts of 4096 x 4096
+// 689 / 650, 729 / 691, 970 / 946, 1269 / 1358, 1592 / 1757; 256 of 2048 x 512 107 / 102, 124 / 122, 150 / 144, 195 / 189, 236 / 230; 64 of 4096 x 1024 105 / 107, 108 / 108,
+// 130 / 130, 172 / 170, 214 / 216. Even loads of 384 differ the most: 1264 / 1539 at 4096 x 4096, 171 / 182 at 4096 x 1024, 195 / 190 at 2048 x 512. grad_rows, whose lines
+// lie along the summed index, is turned always: 1774 straight, 1795 turned at 512 rows, and 46 against 23 for 17 rows of 164 experts of 1648 x 128.)
 constexpr int64_t kStraightRows = 384;
 
 // The two products by rows: of `inner` columns each, times one matrix a group, to `cols` columns.

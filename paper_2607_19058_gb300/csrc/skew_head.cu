@@ -12,8 +12,8 @@ namespace skew {
 namespace {
 
 constexpr int64_t kMaxTokens = int64_t(1) << 24, kMaxRows = int64_t(1) << 24;
-constexpr int64_t kPieceBytes = int64_t(512) << 20;  // of the logits' gradient
-constexpr int64_t kPieceCols = 256;                  // at least, and a multiple
+constexpr int64_t kPieceBytes = int64_t(512) << 20;  // of the logits' gradient, at most
+constexpr int64_t kPieceCols = 256;                  // but this many columns at least (more bytes then, from 2^20 tokens on: 8 GiB for 2^24), and a multiple
 
 constexpr int kJoinWarps = 16;
 

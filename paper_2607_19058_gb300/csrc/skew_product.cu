@@ -352,7 +352,7 @@ __device__ __forceinline__ void copy_box(const CUtensorMap &map, uint32_t to, ui
                  ::"r"(to), "l"(&map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
 }
 
-// One operand's 128 lines, as load_lines brings them. Beyond the matrix the boxes hold zeros.
+// One operand's 128 lines, where Loose would put them. Beyond the matrix the boxes hold zeros.
 template <bool MAJOR>
 __device__ __forceinline__ void copy_lines(const CUtensorMap &map, uint32_t to, uint32_t bar, int l0, int s0, int group) {
     if constexpr (MAJOR) {
@@ -1178,7 +1178,10 @@ constexpr int kChunk32 = 512 / kStep, kChunkLoss = 1024 / kStep, kChunk16 = 8192
 constexpr int kMostWaves = 4;  // of shares: what their sums' memory is sized for
 
 // How many shares the summed index is cut into, so that few tiles keep the SMs busy: the fewest steps (of 64 products, about 0.3 us) that a pair of CTAs does in
-// turn, a share's start and end counted as 6, and the launch that adds the shares as 10 and 0.4 for each.
+// turn, a share's start and end counted as 6, and the launch that adds the shares as 10 and 0.4 for each: an estimate, which reckons with even loads and lines on 16-byte
+// boundaries. us by the rule, with the best of 1 to 32 shares, and uncut: the gradient of 65,536 rows by one expert of 1024 x 1024 103, 103, 300; of 30,000 by 3 of
+// 256 x 256 27, 24, 92; of 8192 by one of 4096 x 4096 176, 170, 170; of 5000 by 9 of 1000 x 511 46, 46, 46; the head's gradients of 44 tokens over 20879 x 520 78, 77, 152;
+// of 512 over 50304 x 4096 489, 486, 577; of 4096 over 50257 x 768 667, 662, 691.
 int shares_of(int64_t tiles, int64_t steps, int64_t pairs) {
     int best = 1;
     double least = 0;

@@ -14,7 +14,7 @@
 // What bounds it. At the tensor cores' rate a CTA takes 64 bytes a clock from L2, as many as it can, and reads as many from shared memory, so that this is busy
 // throughout: 8192 x 4096 times 4096 x 16384 runs at 1.80 PFLOP/s in bursts (574 us without the logits' sums, 611 with; the library's product 2.05) and at what the power
 // limit leaves in a row (1.66). Tiles of few steps are bound by what becomes of their sums, some 3000 to 5500 clocks a tile; a tile of 512 rows to an expert
-// takes 4096 to multiply (the gradient of 128 matrices of 4096 x 4096 from 65,536 rows: 1.49 ms in bursts, 1.19 without writing out).
+// takes 4096 to multiply (the gradient of 128 matrices of 4096 x 4096 from 512 rows each: 1.52 ms in bursts, 1.19 without writing out).
 #include "skew_product.h"
 
 #include <cuda.h>

@@ -572,7 +572,8 @@ int skew_dispatch_combine_grad(const skew_dispatch_config_t *c, const void *dout
  *   product    y[r]  = x[r] W_e                       x (rows, n), y (rows, m)
  *   grad_rows  dx[r] = dy[r] W_e^T
  *   grad       dW_e  = base_e + sum over its rows r of x[r]^T dy[r]
- * x, dy and W are bf16; sums are fp32 on the tensor cores, each result is rounded once. Rows of no expert (before offsets[0] and from
+ * x, dy and W are bf16; sums are fp32 on the tensor cores, whose additions round towards zero (fp32 results are off by some 5e-7 of a sum of products of one sign, bf16
+ * ones by up to 8e-6 before they are rounded, once). Rows of no expert (before offsets[0] and from
  * offsets[E] on) give zeros, and enter no dW, whatever they hold. Offsets are read on the device and taken as they come: one
  * below the one before counts as that one, one beyond `rows` as `rows`. Results do not depend on timing.
  */
@@ -611,7 +612,7 @@ int skew_experts_grad(const skew_experts_config_t *c, const void *x, int64_t ld_
  * A target outside [0, rows) is padding: its loss is zero, its dloss is not read, and neither it nor its h, NaN included, enters a gradient. h, W, dh, base and dW
  * are bf16. l is summed in fp32 and never stored; the gradients take the vocabulary in pieces and make a piece's p from l anew, rounded to bf16 (for the
  * tensor cores: an error of up to 2^-8 of each term, about that of rounding the result), with sums in fp32. Both sum l alike, so that at a target that is nearly
- * certain exp(l - lse) - 1 is off by fp32's rounding of lse alone besides (some 2^-22 of its size). Results do not depend on timing.
+ * certain exp(l - lse) - 1 is off by fp32's rounding of lse alone besides (some 2^-21 of its size). Results do not depend on timing.
  */
 #define SKEW_HEAD_IDS_64 1u /* targets are int64 (else int32) */
 
